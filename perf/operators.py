@@ -165,15 +165,15 @@ def _prepare_adamw(case, seed):
             st[name + "_scale"] = (top / E4M3_MAX).reshape(-1)
             st[name] = (x.view(-1, QBLOCK) * (E4M3_MAX / top)).clamp_(-E4M3_MAX, E4M3_MAX).to(torch.float8_e4m3fn).reshape(-1)
     if own:
-        # the optimiser object that a program makes once beside its weights: the list of its tensors
+        # the optimiser object that a program makes once beside its weights: the list of its tensors and gradient buffers
         from paper_2203_10991_b200 import optim
 
         def parts(x, unit=1):
             return None if x is None else [x[a // unit:a // unit + (-(-n // unit))] for a, n in zip(starts, sizes)]
 
         st["plan"] = optim.AdamWPlan(parts(st["param"]), parts(st["m"]), parts(st["v"]), masters=parts(st["master"]),
-                                     exp_avg_scales=parts(st["m_scale"], QBLOCK), exp_avg_sq_scales=parts(st["v_scale"], QBLOCK))
-        st["grads"] = parts(st["grad"])
+                                     exp_avg_scales=parts(st["m_scale"], QBLOCK), exp_avg_sq_scales=parts(st["v_scale"], QBLOCK),
+                                     grads=parts(st["grad"]))
     return st
 
 
@@ -278,14 +278,15 @@ def _adamw(st):
     weight = st["param"].float() if st["master"] is None else st["master"]
     weight = weight * (1 - st["lr"] * st["decay"]) - m / den * (st["lr"] / (1 - b1 ** t))
     units = torch.arange(g.numel() // 8, device=g.device)
+    random = None if wide and st["case"]["param"] != "bf16" else _random16(units, 2, st["seed"] + t)
     if wide:
         st["m"], st["v"] = m, v
     else:
-        random = _random16(units, 2, st["seed"] + t)
-        st["m"], st["m_scale"] = _to_e4m3(m, random, False)
-        st["v"], st["v_scale"] = _to_e4m3(root, random, True)
+        swapped = (random & 0xFF) << 8 | random >> 8
+        st["m"], st["m_scale"] = _to_e4m3(m, swapped, False)
+        st["v"], st["v_scale"] = _to_e4m3(root, swapped, True)
     if st["case"]["param"] == "bf16":
-        bits = (weight.view(torch.int32) + _random16(units, 3, st["seed"] + t).int()) & -65536
+        bits = (weight.view(torch.int32) + random.int()) & -65536
         st["param"] = bits.view(torch.float32).to(torch.bfloat16)
     else:
         st["param"] = weight.to(st["param"].dtype)
@@ -319,7 +320,7 @@ def run(state):
         return binding.mvue_embedding(st["ids"], st["weight"], scale=st["scale"])
     if op == "embed_grad":
         return binding.mvue_embedding_grad(st["ids"], st["dy"], st["v"], scale=st["scale"], padding_idx=st["padding"])
-    st["plan"].step(st["grads"], step=st["step"], lr=st["lr"], beta1=st["beta1"], beta2=st["beta2"], eps=st["eps"], weight_decay=st["decay"],
+    st["plan"].step(step=st["step"], lr=st["lr"], beta1=st["beta1"], beta2=st["beta2"], eps=st["eps"], weight_decay=st["decay"],
                     seed=st["seed"] + st["step"], stochastic_rounding=True)
     st["step"] += 1
     return _adamw_answer(st)
