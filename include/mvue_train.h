@@ -1,0 +1,92 @@
+/*
+ * mvue_train.h -- what a training step needs around the pruned products of mvue.h:
+ * the AdamW step over many tensors that takes the dW the update products leave, group
+ * normalisation with an activation on channels-last maps (its backward pass hands the
+ * neural gradient to mvue_prune), and embedding lookup with its gradient (which takes the
+ * dh of the last backward product).
+ *
+ * The general rules of mvue.h hold (device pointers, caller-owned buffers, work enqueued on `stream`, argument
+ * errors found on the host before anything is launched), with these differences: empty extents are accepted where a
+ * call says so, and tensors need no more than the alignment of their element type -- 32-byte aligned buffers and
+ * leading dimensions take the wide loads, others are slower.
+ */
+#ifndef MVUE_TRAIN_H_
+#define MVUE_TRAIN_H_
+
+#include "mvue.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * AdamW over many tensors
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* Elements that share one scale of the 8-bit states. */
+#define MVUE_ADAMW_BLOCK 256
+
+/* One tensor of the step: numel elements, contiguous (any order of dimensions that is the same in all its buffers).
+ *  param      MVUE_F32 or MVUE_BF16 (param_dtype), updated in place.
+ *  master     optional float copy of a bf16 param: the step reads and updates the copy, and param receives it rounded
+ *             to the nearest bf16 (param itself is not read).  NULL otherwise; an MVUE_F32 param takes none.
+ *  grad       MVUE_F32 or MVUE_BF16 (grad_dtype), read only.
+ *  exp_avg, exp_avg_sq   state_bits = 32: float m and v.
+ *             state_bits = 8: one byte per element, 8-bit floats of four exponent and three mantissa bits (e4m3) of m
+ *             and of sqrt(v), in units of exp_avg_scale / exp_avg_sq_scale: one float for each MVUE_ADAMW_BLOCK
+ *             consecutive elements (the last block of a tensor may be short).  All zero bytes and scales = zero state.
+ * Buffers of one call must not overlap. */
+typedef struct {
+    void* param;
+    void* master;
+    const void* grad;
+    void* exp_avg;
+    void* exp_avg_sq;
+    void* exp_avg_scale;
+    void* exp_avg_sq_scale;
+    int64_t numel;
+    int32_t param_dtype;
+    int32_t grad_dtype;
+} mvue_adamw_tensor;
+
+/* The step (step = t >= 1), in binary32, each operation rounded on its own; constants are formed in double on the host:
+ *   g' = g * grad_scale (* *dev_grad_scale)
+ *   m' = beta1 m + (1 - beta1) g'
+ *   v' = beta2 v + ((1 - beta2) g') g'
+ *   param' = param (1 - lr weight_decay) - (lr / (1 - beta1^t)) * (m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
+ * (the square root of the 32-bit states' update and the quotient are within 2 units in the last place).
+ * grad_scale: HOST value, 1 for none; dev_grad_scale: optional DEVICE float (a clipping factor or a loss scale's
+ * inverse that the host does not know), read when the step runs.
+ * state_bits: 32 or 8.  With 8 bits the new m and sqrt(v) of a block are divided by the block's new scale
+ * top / 448 (top the largest magnitude; the new scale is top * fl(1/448), the factor 448 * fl(1/top), a magnitude
+ * is capped at 448) and rounded to a neighbouring code at random so that the code's expectation is the value: an
+ * average that moves by a thousandth per step, less than a hundredth of the distance of two codes, would otherwise never move.
+ * A non-zero v keeps a code of at least the smallest.  Blocks whose largest |m| is below 2^-110 store zeros; a
+ * non-finite value makes its block's scale NaN.
+ * options: MVUE_OPT_STOCHASTIC_ROUNDING: a bf16 param without master is rounded to bf16 stochastically (as the
+ * survivors of mvue_prune_opts) instead of to the nearest -- updates below half a unit in the last place then count in
+ * the mean.  Other bits: MVUE_ERR_OPTION.
+ * The random bits: the tensors of a call, each padded to a multiple of MVUE_ADAMW_BLOCK elements, are numbered through
+ * in order; elements 8u .. 8u + 7 take the eight halves (low first) of the words of Philox4x32-10 with counter
+ * (lo32(u), hi32(u), 2, 0) under the key `seed` (pass another one each step).  The param takes the 16 bits as they are, the two
+ * states the same bits with their bytes exchanged.  Equal inputs and seed give equal bits. */
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+    double grad_scale;
+    const float* dev_grad_scale;
+    uint64_t seed;
+    int32_t state_bits;
+    uint32_t options;
+} mvue_adamw_config;
+
+/* tensors: HOST array of `count` entries (count = 0 and numel = 0 are accepted and do nothing); it may be freed on
+ * return.  Errors: MVUE_ERR_NULL, MVUE_ERR_DTYPE (a dtype, a master beside an MVUE_F32 param, state_bits),
+ * MVUE_ERR_SHAPE (negative count or numel, step < 1, more than 2^31 - 1 tiles of 2048 elements), MVUE_ERR_ALIGN
+ * (a pointer not aligned to its element), MVUE_ERR_OPTION (an unknown bit; a beta outside [0, 1)). */
+MVUE_API int mvue_adamw_step(const mvue_adamw_tensor* tensors, int64_t count, const mvue_adamw_config* config, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MVUE_TRAIN_H_ */

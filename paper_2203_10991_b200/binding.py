@@ -24,7 +24,22 @@ EXPORTS = ("mvue_version", "mvue_status_string", "mvue_last_cuda_error", "mvue_p
            "mvue_prune", "mvue_prune_joint", "mvue_prune_opts", "mvue_prune_4of8", "mvue_unpack", "mvue_sparse_update_gemm", "mvue_sparse_backward_gemm",
            "mvue_sparse_backward_gemm_pruned",
            "mvue_gemm_workspace_bytes", "mvue_sparse_update_gemm_noalloc", "mvue_fused_update_gemm", "mvue_fused_update_gemm_joint",
-           "mvue_probe_sparse_mma", "mvue_selftest_wait_timeout")
+           "mvue_probe_sparse_mma", "mvue_selftest_wait_timeout",
+           "mvue_adamw_step")
+
+
+class AdamWTensor(ctypes.Structure):
+    """mvue_adamw_tensor"""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("param", "master", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale",
+                                                     "exp_avg_sq_scale")] + \
+               [("numel", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
+class AdamWConfig(ctypes.Structure):
+    """mvue_adamw_config"""
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
+               [("step", ctypes.c_int64), ("grad_scale", ctypes.c_double), ("dev_grad_scale", ctypes.c_void_p),
+                ("seed", ctypes.c_uint64), ("state_bits", ctypes.c_int32), ("options", ctypes.c_uint32)]
 
 
 class MvueError(RuntimeError):
@@ -70,6 +85,7 @@ def lib() -> ctypes.CDLL:
         L.mvue_sparse_update_gemm_noalloc.argtypes = [vp, vp, ci, i64, i64, vp, i64, i64, vp, ci, i64, ci, vp, vp]
         L.mvue_probe_sparse_mma.argtypes = [ci, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_double), vp, vp]
         L.mvue_selftest_wait_timeout.argtypes = [ci, vp, vp]
+        L.mvue_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, ctypes.POINTER(AdamWConfig), vp]
         _lib = L
     return _lib
 
@@ -287,3 +303,8 @@ def mvue_selftest_wait_timeout(polls: int, dev_status: torch.Tensor) -> None:
     """One launch whose only wait nobody answers: it expires after `polls` polls and the blocks leave through the
     ordinary exit, writing MVUE_ERR_DEVICE_TIMEOUT (-10) to dev_status (int32 CUDA tensor)."""
     _check(lib().mvue_selftest_wait_timeout(polls, dev_status.data_ptr(), _stream_ptr()), "mvue_selftest_wait_timeout")
+
+
+def mvue_adamw_step(tensors: ctypes.Array, count: int, config: AdamWConfig) -> None:
+    """One AdamW step over `count` entries of a ctypes array of AdamWTensor (optim.AdamWPlan fills and keeps one)."""
+    _check(lib().mvue_adamw_step(tensors, count, config, _stream_ptr()), "mvue_adamw_step")

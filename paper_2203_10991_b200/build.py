@@ -15,7 +15,7 @@ from pathlib import Path
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libmvue_b200.so"
-SOURCES = ["mvue_api.cu", "mvue_prune.cu", "mvue_gemm.cu"]
+SOURCES = ["mvue_api.cu", "mvue_prune.cu", "mvue_gemm.cu", "mvue_adamw.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--cudart", "static", "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 
@@ -31,7 +31,7 @@ def up_to_date() -> bool:
     if not LIB.exists():
         return False
     t = LIB.stat().st_mtime
-    deps = list(CSRC.glob("*")) + [HERE.parent / "include" / "mvue.h", Path(__file__)]
+    deps = list(CSRC.glob("*")) + list((HERE.parent / "include").glob("*.h")) + [Path(__file__)]
     return all(d.stat().st_mtime <= t for d in deps)
 
 
