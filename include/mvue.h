@@ -51,7 +51,9 @@ typedef enum {
     MVUE_ERR_CUDA = -9,           /* a CUDA runtime/driver call failed; text in mvue_last_cuda_error() */
     MVUE_ERR_DEVICE_TIMEOUT = -10,/* only ever written to a device status word: a bounded wait expired */
     MVUE_ERR_JOINT = -11,         /* unknown mvue_joint */
-    MVUE_ERR_OPTION = -12         /* unknown bit in the options of mvue_prune_opts */
+    MVUE_ERR_OPTION = -12,        /* unknown bit in the options of a call (mvue_adamw_step: or a beta outside [0, 1)) */
+    MVUE_ERR_INDEX = -13,         /* only ever written to a device status word: a token id outside the vocabulary */
+    MVUE_ERR_ACT = -14            /* unknown mvue_act (mvue_train.h) */
 } mvue_status;
 
 typedef enum { MVUE_F32 = 0, MVUE_BF16 = 1 } mvue_dtype;

@@ -86,6 +86,32 @@ typedef struct {
  * (a pointer not aligned to its element), MVUE_ERR_OPTION (an unknown bit; a beta outside [0, 1)). */
 MVUE_API int mvue_adamw_step(const mvue_adamw_tensor* tensors, int64_t count, const mvue_adamw_config* config, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Embedding
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* out[t] = scale * W[ids[t]] for t < tokens (tokens = 0: nothing).
+ *  ids      device integers of id_bits = 32 or 64 bits.  An id outside [0, vocab) gives a row of zeros and writes
+ *           MVUE_ERR_INDEX to *dev_status (optional device int, otherwise left untouched).
+ *  W        [vocab x cols], MVUE_F32 or MVUE_BF16, ldW >= cols;  out [tokens x cols], MVUE_F32 or MVUE_BF16, ldout >= cols.
+ * The product is formed in binary32 and rounded once.  Rows whose base, cols and leading dimension are multiples of eight
+ * elements (16 bytes of bf16, 32 of fp32) are moved in pieces of eight, others element by element. */
+MVUE_API int mvue_embedding(const void* ids, int id_bits, int64_t tokens, const void* W, int w_dtype, int64_t vocab, int64_t cols,
+                            int64_t ldW, float scale, void* out, int out_dtype, int64_t ldout, int* dev_status, void* stream);
+
+/* The lookup's gradient: dW[v] (+)= scale * sum of dy[t] over the tokens with ids[t] = v, for all v < vocab; rows that no
+ * token names are zero (accumulate != 0: dW is added to, MVUE_F32 only, and rows that no token names are not touched).
+ *  dy       [tokens x cols], MVUE_F32 or MVUE_BF16;  dW [vocab x cols], MVUE_F32 or MVUE_BF16.
+ *  padding_idx   tokens with this id add nothing (a negative one: none does so).  Ids outside [0, vocab) add nothing and
+ *           write MVUE_ERR_INDEX to *dev_status (optional).
+ *  workspace     mvue_embedding_grad_workspace_bytes(tokens, cols) bytes, 32-byte aligned; contents scratch.
+ * Sums are formed in binary32, within each run of 32 tokens of the list sorted by id in token order, the runs in order:
+ * equal inputs give equal bits.  tokens = 0 gives zeros. */
+MVUE_API int mvue_embedding_grad(const void* ids, int id_bits, int64_t tokens, const void* dy, int dy_dtype, int64_t cols, int64_t lddy,
+                                 float scale, int64_t padding_idx, void* dW, int dW_dtype, int64_t vocab, int64_t lddW, int accumulate,
+                                 void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
+MVUE_API int mvue_embedding_grad_workspace_bytes(int64_t tokens, int64_t cols, size_t* bytes);   /* bytes: HOST */
+
 #ifdef __cplusplus
 }
 #endif

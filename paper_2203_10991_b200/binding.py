@@ -25,7 +25,7 @@ EXPORTS = ("mvue_version", "mvue_status_string", "mvue_last_cuda_error", "mvue_p
            "mvue_sparse_backward_gemm_pruned",
            "mvue_gemm_workspace_bytes", "mvue_sparse_update_gemm_noalloc", "mvue_fused_update_gemm", "mvue_fused_update_gemm_joint",
            "mvue_probe_sparse_mma", "mvue_selftest_wait_timeout",
-           "mvue_adamw_step")
+           "mvue_adamw_step", "mvue_embedding", "mvue_embedding_grad", "mvue_embedding_grad_workspace_bytes")
 
 
 class AdamWTensor(ctypes.Structure):
@@ -85,6 +85,10 @@ def lib() -> ctypes.CDLL:
         L.mvue_sparse_update_gemm_noalloc.argtypes = [vp, vp, ci, i64, i64, vp, i64, i64, vp, ci, i64, ci, vp, vp]
         L.mvue_probe_sparse_mma.argtypes = [ci, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_double), vp, vp]
         L.mvue_selftest_wait_timeout.argtypes = [ci, vp, vp]
+        cf, csz = ctypes.c_float, ctypes.c_size_t
+        L.mvue_embedding.argtypes = [vp, ci, i64, vp, ci, i64, i64, i64, cf, vp, ci, i64, vp, vp]
+        L.mvue_embedding_grad.argtypes = [vp, ci, i64, vp, ci, i64, i64, cf, i64, vp, ci, i64, i64, ci, vp, csz, vp, vp]
+        L.mvue_embedding_grad_workspace_bytes.argtypes = [i64, i64, szp]
         L.mvue_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, ctypes.POINTER(AdamWConfig), vp]
         _lib = L
     return _lib
@@ -308,3 +312,64 @@ def mvue_selftest_wait_timeout(polls: int, dev_status: torch.Tensor) -> None:
 def mvue_adamw_step(tensors: ctypes.Array, count: int, config: AdamWConfig) -> None:
     """One AdamW step over `count` entries of a ctypes array of AdamWTensor (optim.AdamWPlan fills and keeps one)."""
     _check(lib().mvue_adamw_step(tensors, count, config, _stream_ptr()), "mvue_adamw_step")
+
+
+def _id_list(ids: torch.Tensor) -> tuple[torch.Tensor, int]:
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"unsupported id dtype {ids.dtype}")
+    return ids.reshape(-1), 8 * ids.element_size()
+
+
+def mvue_embedding(ids: torch.Tensor, W: torch.Tensor, *, scale: float = 1.0, out: torch.Tensor | None = None, out_dtype=None,
+                   dev_status: torch.Tensor | None = None) -> torch.Tensor:
+    """scale * W[ids]: ids int32 or int64 of any shape, W [vocab, cols] fp32 or bf16 (unit column stride).  Ids outside the
+    vocabulary give rows of zeros and write MVUE_ERR_INDEX (-13) to dev_status (int32 CUDA tensor).  Returns
+    [*ids.shape, cols] of out_dtype (W's own unless given); out: [tokens, cols] with unit column stride instead."""
+    flat, id_bits = _id_list(ids)
+    assert ids.is_cuda and W.dim() == 2 and W.stride(1) == 1
+    vocab, cols = W.shape
+    tokens = flat.numel()
+    if out is None:
+        res = rows = torch.empty((*ids.shape, cols), dtype=out_dtype or W.dtype, device=W.device)
+        ldout = cols
+    else:
+        res = rows = out
+        assert out.shape == (tokens, cols) and out.stride(1) == 1
+        ldout = out.stride(0) if tokens > 1 else cols
+    _check(lib().mvue_embedding(flat.data_ptr(), id_bits, tokens, W.data_ptr(), _dtype_code(W), vocab, cols,
+                                W.stride(0) if vocab > 1 else cols, scale, rows.data_ptr(), _dtype_code(rows), ldout,
+                                None if dev_status is None else dev_status.data_ptr(), _stream_ptr()), "mvue_embedding")
+    return res
+
+
+def mvue_embedding_grad_workspace_bytes(tokens: int, cols: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().mvue_embedding_grad_workspace_bytes(tokens, cols, ctypes.byref(b)), "mvue_embedding_grad_workspace_bytes")
+    return b.value
+
+
+def mvue_embedding_grad(ids: torch.Tensor, dy: torch.Tensor, vocab: int, *, scale: float = 1.0, padding_idx: int = -1,
+                        out: torch.Tensor | None = None, out_dtype=torch.float32, accumulate: bool = False,
+                        workspace: torch.Tensor | None = None, dev_status: torch.Tensor | None = None) -> torch.Tensor:
+    """dW[v] (+)= scale * sum of dy[t] over ids[t] = v: dy [*ids.shape, cols] fp32 or bf16, or [tokens, cols] with a row
+    stride.  Rows that no token names are zero (accumulate: out, fp32, is added to).  Returns dW [vocab, cols]."""
+    flat, id_bits = _id_list(ids)
+    cols = dy.shape[-1]
+    tokens = flat.numel()
+    if dy.dim() != 2:
+        dy = dy.reshape(tokens, cols)
+    assert ids.is_cuda and dy.shape[0] == tokens and dy.stride(1) == 1
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate adds to a given out")
+        out = torch.empty((vocab, cols), dtype=out_dtype, device=dy.device)
+    assert out.shape == (vocab, cols) and out.stride(1) == 1
+    need = mvue_embedding_grad_workspace_bytes(tokens, cols)
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+    _check(lib().mvue_embedding_grad(flat.data_ptr(), id_bits, tokens, dy.data_ptr(), _dtype_code(dy), cols,
+                                     dy.stride(0) if tokens > 1 else cols, scale, padding_idx, out.data_ptr(), _dtype_code(out), vocab,
+                                     out.stride(0) if vocab > 1 else cols, int(accumulate), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(),
+                                     None if dev_status is None else dev_status.data_ptr(), _stream_ptr()), "mvue_embedding_grad")
+    return out

@@ -100,7 +100,9 @@ const char* mvue_status_string(int status) {
         case MVUE_ERR_CUDA: return "CUDA call failed (see mvue_last_cuda_error)";
         case MVUE_ERR_DEVICE_TIMEOUT: return "a bounded device-side wait expired";
         case MVUE_ERR_JOINT: return "unknown 2:4 estimator (App. A.2 table, systematic sampling or approx-MVUE)";
-        case MVUE_ERR_OPTION: return "unknown prune option bit";
+        case MVUE_ERR_OPTION: return "unknown option bit, or an option's value out of range";
+        case MVUE_ERR_INDEX: return "a token id outside the vocabulary";
+        case MVUE_ERR_ACT: return "unknown activation";
         default: return "unknown status";
     }
 }
