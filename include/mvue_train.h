@@ -112,6 +112,38 @@ MVUE_API int mvue_embedding_grad(const void* ids, int id_bits, int64_t tokens, c
                                  void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
 MVUE_API int mvue_embedding_grad_workspace_bytes(int64_t tokens, int64_t cols, size_t* bytes);   /* bytes: HOST */
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Group normalisation with an activation, channels last
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* GELU: z times the normal distribution function of z (not its tanh approximation). */
+typedef enum { MVUE_ACT_NONE = 0, MVUE_ACT_RELU = 1, MVUE_ACT_SILU = 2, MVUE_ACT_GELU = 3 } mvue_act;
+
+/* x [n, s, c] (s positions of c channels; c a multiple of groups, cg = c / groups), over each group of cg neighbouring
+ * channels of a sample:
+ *   mean = sum x / (s cg);  rstd = 1 / sqrt(sum (x - mean)^2 / (s cg) + eps)
+ *   z = (x - mean) rstd gamma_c + beta_c;  y = act(z)
+ *  x, y       MVUE_F32 or MVUE_BF16 (the same); ldx, ldy >= c: elements between positions; a sample has s of them.
+ *             y may be x.
+ *  gamma, beta   [c], MVUE_F32 or MVUE_BF16 (affine_dtype), either may be NULL (ones, zeros).
+ *  mean, rstd [n, groups] float outputs for the backward pass, either may be NULL.
+ *  workspace  mvue_group_norm_workspace_bytes(n, s, c, groups) bytes, 16-byte aligned; contents scratch.
+ * Arithmetic in binary32; the output is rounded once.  n = 0: nothing.  s >= 1. */
+MVUE_API int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t c, int64_t ldx, int groups, const void* gamma,
+                                 const void* beta, int affine_dtype, float eps, int act, void* y, int64_t ldy, float* mean, float* rstd,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its backward pass, z formed again from x and the forward pass's mean and rstd:
+ *   dz = dy act'(z);  dbeta_c = sum dz;  dgamma_c = sum dz xh, xh = (x - mean) rstd   (over n and s)
+ *   dx = rstd (gamma_c dz - mean over the group of gamma dz - xh * mean over the group of gamma dz xh)
+ * (the derivative of ReLU at 0 is 0).  dgamma, dbeta: [c] float, either may be NULL; n = 0 sets them to zero.  dx is what
+ * mvue_prune takes as the neural gradient of the layer below.  dx may be dy.  Equal inputs give equal bits. */
+MVUE_API int mvue_group_norm_act_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int dtype, int64_t n, int64_t s,
+                                          int64_t c, int groups, const float* mean, const float* rstd, const void* gamma,
+                                          const void* beta, int affine_dtype, int act, void* dx, int64_t lddx, float* dgamma,
+                                          float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+MVUE_API int mvue_group_norm_workspace_bytes(int64_t n, int64_t s, int64_t c, int groups, size_t* bytes);   /* bytes: HOST */
+
 #ifdef __cplusplus
 }
 #endif

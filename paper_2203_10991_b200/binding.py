@@ -19,13 +19,15 @@ MVUE_LAYOUT_CANONICAL = 0
 MVUE_LAYOUT_TC = 1
 MVUE_JOINT_TABLE, MVUE_JOINT_SYSTEMATIC, MVUE_JOINT_APPROX = 0, 1, 2
 MVUE_OPT_NONE, MVUE_OPT_STOCHASTIC_ROUNDING, MVUE_OPT_EPS16 = 0, 1, 2
+MVUE_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 EXPORTS = ("mvue_version", "mvue_status_string", "mvue_last_cuda_error", "mvue_packed_sizes",
            "mvue_prune", "mvue_prune_joint", "mvue_prune_opts", "mvue_prune_4of8", "mvue_unpack", "mvue_sparse_update_gemm", "mvue_sparse_backward_gemm",
            "mvue_sparse_backward_gemm_pruned",
            "mvue_gemm_workspace_bytes", "mvue_sparse_update_gemm_noalloc", "mvue_fused_update_gemm", "mvue_fused_update_gemm_joint",
            "mvue_probe_sparse_mma", "mvue_selftest_wait_timeout",
-           "mvue_adamw_step", "mvue_embedding", "mvue_embedding_grad", "mvue_embedding_grad_workspace_bytes")
+           "mvue_adamw_step", "mvue_embedding", "mvue_embedding_grad", "mvue_embedding_grad_workspace_bytes",
+           "mvue_group_norm_act", "mvue_group_norm_act_backward", "mvue_group_norm_workspace_bytes")
 
 
 class AdamWTensor(ctypes.Structure):
@@ -89,6 +91,10 @@ def lib() -> ctypes.CDLL:
         L.mvue_embedding.argtypes = [vp, ci, i64, vp, ci, i64, i64, i64, cf, vp, ci, i64, vp, vp]
         L.mvue_embedding_grad.argtypes = [vp, ci, i64, vp, ci, i64, i64, cf, i64, vp, ci, i64, i64, ci, vp, csz, vp, vp]
         L.mvue_embedding_grad_workspace_bytes.argtypes = [i64, i64, szp]
+        L.mvue_group_norm_act.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, vp, ci, cf, ci, vp, i64, vp, vp, vp, csz, vp]
+        L.mvue_group_norm_act_backward.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, ci, vp, vp, vp, vp, ci, ci, vp, i64, vp, vp,
+                                                   vp, csz, vp]
+        L.mvue_group_norm_workspace_bytes.argtypes = [i64, i64, i64, ci, szp]
         L.mvue_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, ctypes.POINTER(AdamWConfig), vp]
         _lib = L
     return _lib
@@ -344,7 +350,8 @@ def mvue_embedding(ids: torch.Tensor, W: torch.Tensor, *, scale: float = 1.0, ou
 
 def mvue_embedding_grad_workspace_bytes(tokens: int, cols: int) -> int:
     b = ctypes.c_size_t()
-    _check(lib().mvue_embedding_grad_workspace_bytes(tokens, cols, ctypes.byref(b)), "mvue_embedding_grad_workspace_bytes")
+    _check(lib().mvue_embedding_grad_workspace_bytes(tokens, cols, ctypes.byref(b)), "mvue_embedding_grad_workspace_bytes",
+           "mvue_group_norm_act", "mvue_group_norm_act_backward", "mvue_group_norm_workspace_bytes")
     return b.value
 
 
@@ -373,3 +380,90 @@ def mvue_embedding_grad(ids: torch.Tensor, dy: torch.Tensor, vocab: int, *, scal
                                      workspace.numel() * workspace.element_size(),
                                      None if dev_status is None else dev_status.data_ptr(), _stream_ptr()), "mvue_embedding_grad")
     return out
+
+
+def _ptr(t: torch.Tensor | None):
+    return None if t is None else t.data_ptr()
+
+
+def _positions(t: torch.Tensor):
+    """(n, s, c, ld) of a channels-last tensor [n, ..., c] whose positions lie one row stride apart."""
+    if t.dim() < 2 or t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError("wants [n, ..., channels] with unit channel stride")
+    c = t.shape[-1]
+    rows = t.numel() // c if c else 0
+    s = rows // t.shape[0] if t.shape[0] else 1
+    for d in t.shape[1:-1]:
+        if t.shape[0] == 0:
+            s *= d
+    ld, step = None, None
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):       # innermost position first
+        if size != 1:
+            if ld is None:
+                ld = stride
+            elif stride != step:
+                raise ValueError("positions are not one row stride apart")
+            step = stride * size
+    return t.shape[0], s, c, c if ld is None or t.numel() == 0 else ld
+
+
+def _affine(weight, bias, c: int) -> int:
+    for t in (weight, bias):
+        if t is not None and (t.shape != (c,) or not t.is_contiguous() or not t.is_cuda):
+            raise ValueError("weight and bias are contiguous CUDA tensors of one element per channel")
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError("weight and bias have one dtype")
+    return MVUE_F32 if weight is None and bias is None else _dtype_code(bias if weight is None else weight)
+
+
+def mvue_group_norm_workspace_bytes(n: int, s: int, c: int, groups: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().mvue_group_norm_workspace_bytes(n, s, c, groups, ctypes.byref(b)), "mvue_group_norm_workspace_bytes")
+    return b.value
+
+
+def _norm_workspace(n, s, c, groups, device, workspace):
+    need = mvue_group_norm_workspace_bytes(n, s, c, groups)
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, *,
+                        eps: float = 1e-5, act: str = "none", out: torch.Tensor | None = None,
+                        workspace: torch.Tensor | None = None):
+    """act(group_norm(x) * weight + bias) on a channels-last CUDA tensor x [n, ..., c], fp32 or bf16 (act: none, relu, silu,
+    gelu).  Returns (y, mean, rstd); mean and rstd [n, groups] fp32 are what the backward pass takes."""
+    n, s, c, ldx = _positions(x)
+    assert x.is_cuda
+    code = _affine(weight, bias, c)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    assert out.shape == x.shape and out.dtype == x.dtype
+    stats = torch.empty((2, n, groups), dtype=torch.float32, device=x.device)
+    ws, ws_bytes = _norm_workspace(n, s, c, groups, x.device, workspace)
+    _check(lib().mvue_group_norm_act(x.data_ptr(), _dtype_code(x), n, s, c, ldx, groups, _ptr(weight), _ptr(bias), code, eps,
+                                     MVUE_ACTS[act], out.data_ptr(), _positions(out)[3], stats[0].data_ptr(), stats[1].data_ptr(),
+                                     ws.data_ptr(), ws_bytes, _stream_ptr()), "mvue_group_norm_act")
+    return out, stats[0], stats[1]
+
+
+def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, groups: int,
+                                 weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, *, act: str = "none",
+                                 out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Backward pass of mvue_group_norm_act.  Returns (dx, dweight, dbias); the last two [c] fp32."""
+    n, s, c, ldx = _positions(x)
+    assert x.is_cuda and dy.shape == x.shape and dy.dtype == x.dtype
+    for t in (mean, rstd):
+        assert t.shape == (n, groups) and t.dtype == torch.float32 and t.is_contiguous()
+    code = _affine(weight, bias, c)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    assert out.shape == x.shape and out.dtype == x.dtype
+    grads = torch.empty((2, c), dtype=torch.float32, device=x.device)
+    ws, ws_bytes = _norm_workspace(n, s, c, groups, x.device, workspace)
+    _check(lib().mvue_group_norm_act_backward(dy.data_ptr(), _positions(dy)[3], x.data_ptr(), ldx, _dtype_code(x), n, s, c, groups,
+                                              mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(bias), code, MVUE_ACTS[act],
+                                              out.data_ptr(), _positions(out)[3], grads[0].data_ptr(), grads[1].data_ptr(),
+                                              ws.data_ptr(), ws_bytes, _stream_ptr()), "mvue_group_norm_act_backward")
+    return out, grads[0], grads[1]

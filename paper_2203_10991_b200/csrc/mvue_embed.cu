@@ -38,47 +38,6 @@ struct Ids {
     }
 };
 
-// Eight elements of a row per thread: consecutive ones where the rows allow wide accesses, else one of every
-// `stride` (the team's threads), so that a warp's accesses stay together.
-template <bool kWide>
-struct Cols {
-    int64_t first;
-    int step, count;
-    __device__ __forceinline__ Cols(int64_t slab0, int64_t cols, int lane, int team) {
-        first = slab0 + (kWide ? (int64_t)lane * 8 : lane);
-        step = kWide ? 1 : team;
-        const int64_t left = cols - first;
-        count = left <= 0 ? 0 : (int)min((int64_t)8, kWide ? left : (left + team - 1) / team);
-    }
-    template <typename T> __device__ __forceinline__ void load(const T* row, float (&x)[8]) const {
-        if (kWide) {
-            load8(row + first, true, 8, x);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = j < count ? (float)row[first + (int64_t)j * step] : 0.0f;
-        }
-    }
-    __device__ __forceinline__ void store(float* row, const float (&x)[8]) const {
-        if (kWide) {
-            store8(row + first, true, 8, x);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < count) row[first + (int64_t)j * step] = x[j];
-        }
-    }
-    __device__ __forceinline__ void store(__nv_bfloat16* row, const float (&x)[8]) const {
-        if (kWide) {
-            const uint32_t w[4] = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-            store8_words(row + first, true, 8, w);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < count) row[first + (int64_t)j * step] = __float2bfloat16_rn(x[j]);
-        }
-    }
-};
-
 // ---- lookup ----------------------------------------------------------------------------------------------------------
 template <typename TW, typename TO, bool kWide>
 __global__ void __launch_bounds__(256) embed_kernel(Ids ids, int64_t tokens, const TW* __restrict__ w, int64_t vocab, int64_t cols,
