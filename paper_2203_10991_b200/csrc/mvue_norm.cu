@@ -7,10 +7,12 @@
 // (no atomics).  Variances: means first, squares of distances from them afterwards, and parts joined by
 //   M2 = sum of M2_i + n_i (mean_i - mean)^2,
 // so a mean that is large against the deviation costs no digits.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <numeric>
 
 #include "../../include/mvue_train.h"
 #include "mvue_device.cuh"
@@ -19,6 +21,8 @@
 
 namespace mvue {
 namespace {
+
+namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256;
 constexpr int kMaxPieces = 32;       // pieces of eight channels that a block is wide: 256 channels
@@ -364,6 +368,327 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
     }
 }
 
+// ---- resident: a cluster of blocks keeps its part of one sample in shared memory ---------------------------------------
+// The route through memory reads x twice (three passes over HBM in all, five in the backward pass).  Here a cluster of up
+// to eight blocks takes one slab of whole groups of one sample, every block a run of its rows: the rows are copied to shared
+// memory once, a thread reads back only what it copied itself (no barrier between the copy and its use), the blocks
+// exchange their groups' sums through distributed shared memory, and the output is formed from the same copy.  One read
+// and one write of HBM.
+struct ResidentArgs {
+    NormArgs norm;
+    int cluster, iters;              // blocks of a cluster; rows of a thread at most
+    int64_t rows;                    // rows of a block
+};
+
+constexpr int kPartPitch = kThreads + 1;
+
+__device__ __forceinline__ void copy16(void* smem, const void* global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
+}
+template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+// A thread's rows of one tensor in shared memory: 16-byte slots, consecutive threads side by side.
+template <typename T>
+struct Slots {
+    static constexpr int kHalves = sizeof(T) * 8 / 16;
+    char* base;
+    __device__ __forceinline__ Slots(char* area) : base(area + threadIdx.x * 16) {}
+    __device__ __forceinline__ void fetch(int i, const T* from) const {
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) copy16(base + (i * kHalves + h) * (kThreads * 16), reinterpret_cast<const char*>(from) + 16 * h);
+    }
+    __device__ __forceinline__ void read(int i, float (&x)[8]) const {
+        uint4 w[kHalves];
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) w[h] = *reinterpret_cast<const uint4*>(base + (i * kHalves + h) * (kThreads * 16));
+        if (kHalves == 1) {
+            x[0] = bf16_lo(w[0].x); x[1] = bf16_hi(w[0].x); x[2] = bf16_lo(w[0].y); x[3] = bf16_hi(w[0].y);
+            x[4] = bf16_lo(w[0].z); x[5] = bf16_hi(w[0].z); x[6] = bf16_lo(w[0].w); x[7] = bf16_hi(w[0].w);
+        } else {
+            const uint4 v = w[kHalves - 1];
+            x[0] = __uint_as_float(w[0].x); x[1] = __uint_as_float(w[0].y); x[2] = __uint_as_float(w[0].z); x[3] = __uint_as_float(w[0].w);
+            x[4] = __uint_as_float(v.x); x[5] = __uint_as_float(v.y); x[6] = __uint_as_float(v.z); x[7] = __uint_as_float(v.w);
+        }
+    }
+};
+
+// Where a block of the cluster stands, and its shared memory.
+template <typename T, int kTensors>
+struct Resident {
+    int pieces, ty, threads_down, group_size, groups_here, channels_here, rank, cluster;
+    int64_t n, c0, r0;
+    int rows_here, iters;            // of the block; of this thread (0: it has no channels)
+    char* area[2];
+    float *part, *channel, *group_a, *group_b, *all;
+
+    __device__ __forceinline__ Resident(const ResidentArgs& a, char* smem) {
+        const NormArgs& q = a.norm;
+        pieces = q.pieces;
+        cluster = a.cluster;
+        rank = blockIdx.x % cluster;
+        const int64_t unit = blockIdx.x / cluster;
+        n = unit / q.slabs;
+        c0 = (unit % q.slabs) * pieces * 8;
+        channels_here = (int)min((int64_t)pieces * 8, q.c - c0);
+        group_size = q.group_size;
+        groups_here = channels_here / group_size;
+        threads_down = kThreads / pieces;
+        ty = threadIdx.x / pieces;
+        r0 = min(q.s, rank * a.rows);
+        rows_here = (int)(min(q.s, r0 + a.rows) - r0);
+        const bool mine = ty < threads_down && (int)(threadIdx.x % pieces) * 8 < channels_here;
+        iters = mine && ty < rows_here ? (rows_here - ty + threads_down - 1) / threads_down : 0;
+        const size_t slots = (size_t)a.iters * Slots<T>::kHalves * kThreads * 16;
+        area[0] = smem;
+        area[1] = smem + (kTensors - 1) * slots;
+        part = reinterpret_cast<float*>(smem + kTensors * slots);
+        channel = part + 8 * kPartPitch;
+        const int width = pieces * 8, most = width / group_size;
+        group_a = channel + 2 * width;
+        group_b = group_a + most;
+        all = group_b + most;        // [cluster][groups][2]
+    }
+    __device__ __forceinline__ int64_t first_channel() const { return c0 + (threadIdx.x % pieces) * 8; }
+    __device__ __forceinline__ int64_t row(int i) const { return r0 + ty + (int64_t)i * threads_down; }
+
+    // sums over the block's rows of every thread's eight values -> channel[0 .. channels_here)
+    __device__ __forceinline__ void channel_sums(const float (&x)[8], float* into) const {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[j * kPartPitch + threadIdx.x] = x[j];
+        __syncthreads();
+        for (int k = threadIdx.x; k < channels_here; k += kThreads) {
+            const float* p = part + (k & 7) * kPartPitch + (k >> 3);
+            float s0 = 0.0f, s1 = 0.0f;
+            int t = 0;
+            for (; t + 1 < threads_down; t += 2) {
+                s0 += p[t * pieces];
+                s1 += p[(t + 1) * pieces];
+            }
+            if (t < threads_down) s0 += p[t * pieces];
+            into[k] = s0 + s1;
+        }
+        __syncthreads();
+    }
+    // a warp adds f(channel) over each group and hands the sum to `put(group, sum)` on every lane
+    template <typename F, typename P> __device__ __forceinline__ void group_sums(F f, P put) const {
+        const int lane = threadIdx.x & 31;
+        for (int g = threadIdx.x >> 5; g < groups_here; g += kThreads / 32) {
+            float s = 0.0f;
+            for (int c = lane; c < group_size; c += 32) s += f(g * group_size + c);
+            put(g, warp_sum(s));
+        }
+    }
+    // block `to`'s copy of p (the same place in its shared memory)
+    __device__ __forceinline__ float* remote(float* p, int to) const { return cg::this_cluster().map_shared_rank(p, to); }
+};
+
+template <typename T, int kAct>
+__global__ void __launch_bounds__(kThreads) norm_resident_kernel(const __grid_constant__ ResidentArgs a) {
+    grid_dependency_wait();
+    extern __shared__ __align__(16) char smem[];
+    const Resident<T, 1> r(a, smem);
+    const NormArgs& q = a.norm;
+    const int64_t c = r.first_channel();
+    const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row(0)) * q.ldx + c;
+    const Slots<T> xs(r.area[0]);
+    const int64_t step = (int64_t)r.threads_down * q.ldx;
+    const int quarter = (a.iters + 3) / 4;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) xs.fetch(i, x + i * step);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    if (r.cluster > 1) cg::this_cluster().sync();              // every block of the cluster runs: its memory may be written
+    float sum[8] = {};
+    const auto add = [&](int k) {
+        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) {
+            float v[8];
+            xs.read(i, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += v[j];
+        }
+    };
+    copies_wait<3>(); add(0);
+    copies_wait<2>(); add(1);
+    copies_wait<1>(); add(2);
+    copies_wait<0>(); add(3);
+    r.channel_sums(sum, r.channel);
+    const float mine = (float)r.rows_here * r.group_size, inv = mine > 0.0f ? 1.0f / mine : 0.0f;
+    r.group_sums([&](int k) { return r.channel[k]; }, [&](int g, float s) { r.group_a[g] = s * inv; });
+    __syncthreads();
+    // squares about the block's own means, from shared memory
+    float mean[8];
+    const int first = (int)(c - r.c0);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        mean[j] = r.iters ? r.group_a[(first + j) / r.group_size] : 0.0f;
+        sum[j] = 0.0f;
+    }
+    for (int i = 0; i < r.iters; ++i) {
+        float v[8];
+        xs.read(i, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = v[j] - mean[j];
+            sum[j] = fmaf(d, d, sum[j]);
+        }
+    }
+    r.channel_sums(sum, r.channel);
+    r.group_sums([&](int k) { return r.channel[k]; }, [&](int g, float s) {
+        const int lane = threadIdx.x & 31;
+        if (lane < r.cluster) {
+            float* to = r.cluster > 1 ? r.remote(r.all, lane) : r.all;
+            to[(r.rank * r.groups_here + g) * 2] = r.group_a[g];
+            to[(r.rank * r.groups_here + g) * 2 + 1] = s;
+        }
+    });
+    if (r.cluster > 1) cg::this_cluster().sync(); else __syncthreads();
+    for (int g = threadIdx.x; g < r.groups_here; g += kThreads) {
+        const auto rows_of = [&](int b) { return (float)max((int64_t)0, min(a.rows, q.s - b * a.rows)); };
+        const float per_row = 1.0f / (float)q.s;
+        float m = 0.0f, dev = 0.0f;
+        for (int b = 0; b < r.cluster; ++b) m = fmaf(rows_of(b), r.all[(b * r.groups_here + g) * 2], m);
+        m *= per_row;
+        for (int b = 0; b < r.cluster; ++b) {
+            const float d = r.all[(b * r.groups_here + g) * 2] - m;
+            dev += fmaf(rows_of(b) * r.group_size * d, d, r.all[(b * r.groups_here + g) * 2 + 1]);
+        }
+        const float rstd = 1.0f / sqrtf(dev / ((float)q.s * r.group_size) + q.eps);
+        r.group_a[g] = m;
+        r.group_b[g] = rstd;
+        if (r.rank == 0) {
+            const int64_t at = r.n * q.groups + r.c0 / r.group_size + g;
+            q.mean[at] = m;
+            q.rstd[at] = rstd;
+        }
+    }
+    __syncthreads();
+    if (r.iters == 0) return;
+    float slope[8], shift[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int g = (first + j) / r.group_size;
+        mean[j] = r.group_a[g];
+        slope[j] = r.group_b[g] * affine(q.gamma, q.affine_bf16, c + j, 1.0f);
+        shift[j] = affine(q.beta, q.affine_bf16, c + j, 0.0f);
+    }
+    T* y = static_cast<T*>(q.out) + (r.n * q.s + r.row(0)) * q.ldo;
+    const Cols<true> cols(c, q.c, 0, 1);
+    for (int i = 0; i < r.iters; ++i) {
+        float v[8];
+        xs.read(i, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = act<kAct>(fmaf(v[j] - mean[j], slope[j], shift[j]));
+        cols.store(y + (int64_t)i * r.threads_down * q.ldo, v);
+    }
+}
+
+// Backward: x and dy resident; the block's sums per channel go to `partial` for the gradients of gamma and beta
+// (norm_grad_join_kernel), the groups' means through the cluster.
+template <typename T, int kAct>
+__global__ void __launch_bounds__(kThreads) norm_resident_grad_kernel(const __grid_constant__ ResidentArgs a) {
+    grid_dependency_wait();
+    extern __shared__ __align__(16) char smem[];
+    const Resident<T, 2> r(a, smem);
+    const NormArgs& q = a.norm;
+    const int64_t c = r.first_channel();
+    const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row(0)) * q.ldx + c;
+    const T* dy = static_cast<const T*>(q.dy) + (r.n * q.s + r.row(0)) * q.lddy + c;
+    const Slots<T> xs(r.area[0]), ds(r.area[1]);
+    const int quarter = (a.iters + 3) / 4;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) {
+            xs.fetch(i, x + (int64_t)i * r.threads_down * q.ldx);
+            ds.fetch(i, dy + (int64_t)i * r.threads_down * q.lddy);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    if (r.cluster > 1) cg::this_cluster().sync();
+    float mean[8], slope[8], shift[8], sum[8] = {}, along[8] = {};
+    const int64_t g0 = r.n * q.groups;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int64_t g = g0 + (c + j) / r.group_size;
+        mean[j] = r.iters ? q.mean[g] : 0.0f;
+        slope[j] = r.iters ? q.rstd[g] * affine(q.gamma, q.affine_bf16, c + j, 1.0f) : 0.0f;
+        shift[j] = r.iters ? affine(q.beta, q.affine_bf16, c + j, 0.0f) : 0.0f;
+    }
+    const auto add = [&](int k) {
+        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) {
+            float v[8], d[8];
+            xs.read(i, v);
+            ds.read(i, d);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xc = v[j] - mean[j];
+                const float dz = d[j] * act_grad<kAct>(fmaf(xc, slope[j], shift[j]));
+                sum[j] += dz;
+                along[j] = fmaf(dz, xc, along[j]);
+            }
+        }
+    };
+    copies_wait<3>(); add(0);
+    copies_wait<2>(); add(1);
+    copies_wait<1>(); add(2);
+    copies_wait<0>(); add(3);
+    float* channel_b = r.channel + r.pieces * 8;
+    r.channel_sums(sum, r.channel);
+    r.channel_sums(along, channel_b);
+    for (int k = threadIdx.x; k < r.channels_here; k += kThreads) {
+        const float2 s = make_float2(r.channel[k], channel_b[k] * q.rstd[g0 + (r.c0 + k) / r.group_size]);
+        const float gamma = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
+        q.partial[((r.n * r.cluster) + r.rank) * q.c + r.c0 + k] = s;
+        r.channel[k] = gamma * s.x;
+        channel_b[k] = gamma * s.y;
+    }
+    __syncthreads();
+    const auto send = [&](int which) {
+        return [&r, which](int g, float s) {
+            const int lane = threadIdx.x & 31;
+            if (lane < r.cluster) (r.cluster > 1 ? r.remote(r.all, lane) : r.all)[(r.rank * r.groups_here + g) * 2 + which] = s;
+        };
+    };
+    r.group_sums([&](int k) { return r.channel[k]; }, send(0));
+    r.group_sums([&](int k) { return channel_b[k]; }, send(1));
+    if (r.cluster > 1) cg::this_cluster().sync(); else __syncthreads();
+    const float inv = (float)(1.0 / ((double)q.s * r.group_size));
+    for (int g = threadIdx.x; g < r.groups_here; g += kThreads) {
+        float sa = 0.0f, sb = 0.0f;
+        for (int b = 0; b < r.cluster; ++b) {
+            sa += r.all[(b * r.groups_here + g) * 2];
+            sb += r.all[(b * r.groups_here + g) * 2 + 1];
+        }
+        const float rstd = q.rstd[g0 + r.c0 / r.group_size + g];
+        r.group_a[g] = rstd * (sa * inv);
+        r.group_b[g] = rstd * rstd * (sb * inv);
+    }
+    __syncthreads();
+    if (r.iters == 0) return;
+    float level[8], tilt[8];          // dx = slope dz - level - tilt (x - mean)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int g = (int)(c - r.c0 + j) / r.group_size;
+        level[j] = r.group_a[g];
+        tilt[j] = r.group_b[g];
+    }
+    T* dx = static_cast<T*>(q.out) + (r.n * q.s + r.row(0)) * q.ldo;
+    const Cols<true> cols(c, q.c, 0, 1);
+    for (int i = 0; i < r.iters; ++i) {
+        float v[8], d[8];
+        xs.read(i, v);
+        ds.read(i, d);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float xc = v[j] - mean[j];
+            const float dz = d[j] * act_grad<kAct>(fmaf(xc, slope[j], shift[j]));
+            v[j] = fmaf(slope[j], dz, fmaf(xc, -tilt[j], -level[j]));
+        }
+        cols.store(dx + (int64_t)i * r.threads_down * q.ldo, v);
+    }
+}
+
 // ---- host ------------------------------------------------------------------------------------------------------------
 int64_t size_of(int dtype) { return dtype == MVUE_BF16 ? 2 : 4; }
 bool off(const void* p, int64_t size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) != 0; }
@@ -388,6 +713,71 @@ Split split_of(int64_t n, int64_t s, int64_t c) {
     return p;
 }
 
+constexpr int kMaxCluster = 8;
+constexpr size_t kBlockBytes[3] = {56 << 10, 113 << 10, 226 << 10};     // shared memory of four, two and one blocks on an SM
+
+struct Keep {
+    int pieces = 0, slabs, cluster, iters;      // pieces = 0: the slab of one sample does not fit a cluster
+    int64_t rows;
+    size_t smem;
+};
+// A slab is the fewest whole groups that are whole pieces of eight channels and 128 bytes of a row (or all channels); small
+// maps take more, as long as two blocks are left for every SM.  Then the fewest blocks that hold a slab in the
+// smallest of the three shares of shared memory that does, and more where the grid would leave SMs idle.
+Keep keep_of(int64_t n, int64_t s, int64_t c, int groups, int64_t esz, int tensors) {
+    Keep k;
+    const int64_t cg = c / groups, least = std::lcm(cg, (int64_t)8);
+    if (c % 8 != 0 || least > kThreads * 8) return k;
+    int64_t width = std::min(c, (128 / esz + least - 1) / least * least);
+    while (width * 2 <= std::min<int64_t>(c, kThreads * 8) && s * width * esz < (8 << 10) && n * ((c + 2 * width - 1) / (2 * width)) >= 2 * 148)
+        width *= 2;
+    const int pieces = (int)(width / 8), down = kThreads / pieces;
+    const int64_t slabs = (c + width - 1) / width, most = width / cg;
+    const auto try_cluster = [&](int cluster, size_t limit) {
+        const int64_t rows = (s + cluster - 1) / cluster, iters = (rows + down - 1) / down;
+        if (iters > (1 << 16)) return false;
+        const size_t smem = (size_t)tensors * iters * esz * 8 * kThreads + 4 * (8 * kPartPitch + 2 * width + 2 * most + 2 * most * cluster);
+        if (smem > limit) return false;
+        k.rows = rows;
+        k.iters = (int)iters;
+        k.cluster = cluster;
+        k.smem = smem;
+        return true;
+    };
+    bool found = false;
+    for (int level = 0; level < 3 && !found; ++level)
+        for (int cluster = 1; cluster <= kMaxCluster && !found; cluster *= 2) found = try_cluster(cluster, kBlockBytes[level]);
+    if (!found) return k;
+    while (k.cluster < kMaxCluster && n * slabs * k.cluster * 2 <= 2 * 148 && s >= (int64_t)k.cluster * 2 * down)
+        if (!try_cluster(k.cluster * 2, kBlockBytes[2])) break;
+    if (n * slabs > 0x7FFFFFFF / kMaxCluster) return k;
+    k.pieces = pieces;
+    k.slabs = (int)slabs;
+    return k;
+}
+
+template <typename K>
+cudaError_t launch_resident(K kernel, PerDeviceOnce& once, const ResidentArgs& a, const Keep& k, cudaStream_t st) {
+    cudaError_t e = once_per_device(once, [&](int) {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockBytes[2]);
+    });
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.norm.n * k.slabs * k.cluster));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = k.smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)k.cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 struct Layout {
     size_t partial, coef, mean, rstd, bytes;
 };
@@ -395,7 +785,7 @@ Layout layout_of(int64_t n, int64_t s, int64_t c, int groups) {
     Layout l;
     size_t at = 0;
     const auto take = [&](size_t b) { const size_t here = at; at += (b + 255) / 256 * 256; return here; };
-    l.partial = take((size_t)n * (size_t)split_of(n, s, c).chunks * (size_t)c * sizeof(float2));
+    l.partial = take((size_t)n * (size_t)std::max<int64_t>(split_of(n, s, c).chunks, kMaxCluster) * (size_t)c * sizeof(float2));
     l.coef = take((size_t)n * groups * sizeof(float2));
     l.mean = take((size_t)n * groups * 4);
     l.rstd = take((size_t)n * groups * 4);
@@ -422,6 +812,21 @@ cudaError_t backward(const NormArgs& a, dim3 grid, cudaStream_t st) {
 }
 template <typename T, bool kWide, int kAct>
 cudaError_t either(const NormArgs& a, dim3 grid, cudaStream_t st) {
+    if constexpr (kWide) {
+        const Keep k = keep_of(a.n, a.s, a.c, a.groups, sizeof(T), a.dy ? 2 : 1);
+        if (k.pieces) {
+            ResidentArgs r{a, k.cluster, k.iters, k.rows};
+            r.norm.pieces = k.pieces;
+            r.norm.slabs = k.slabs;
+            r.norm.chunks = k.cluster;
+            static PerDeviceOnce once[2];
+            if (!a.dy) return launch_resident(&norm_resident_kernel<T, kAct>, once[0], r, k, st);
+            cudaError_t e = launch_resident(&norm_resident_grad_kernel<T, kAct>, once[1], r, k, st);
+            if (e == cudaSuccess && (a.dgamma || a.dbeta))
+                e = launch_dependent(&norm_grad_join_kernel, dim3((unsigned)((a.c + 31) / 32)), dim3(kThreads), 0, st, r.norm, (int64_t)0);
+            return e;
+        }
+    }
     return a.dy ? backward<T, kWide, kAct>(a, grid, st) : forward<T, kWide, kAct>(a, grid, st);
 }
 template <typename T, bool kWide>
