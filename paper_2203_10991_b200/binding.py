@@ -350,8 +350,7 @@ def mvue_embedding(ids: torch.Tensor, W: torch.Tensor, *, scale: float = 1.0, ou
 
 def mvue_embedding_grad_workspace_bytes(tokens: int, cols: int) -> int:
     b = ctypes.c_size_t()
-    _check(lib().mvue_embedding_grad_workspace_bytes(tokens, cols, ctypes.byref(b)), "mvue_embedding_grad_workspace_bytes",
-           "mvue_group_norm_act", "mvue_group_norm_act_backward", "mvue_group_norm_workspace_bytes")
+    _check(lib().mvue_embedding_grad_workspace_bytes(tokens, cols, ctypes.byref(b)), "mvue_embedding_grad_workspace_bytes")
     return b.value
 
 
