@@ -127,7 +127,9 @@ typedef enum { MVUE_ACT_NONE = 0, MVUE_ACT_RELU = 1, MVUE_ACT_SILU = 2, MVUE_ACT
  *             y may be x.
  *  gamma, beta   [c], MVUE_F32 or MVUE_BF16 (affine_dtype), either may be NULL (ones, zeros).
  *  mean, rstd [n, groups] float outputs for the backward pass, either may be NULL.
- *  workspace  mvue_group_norm_workspace_bytes(n, s, c, groups) bytes, 16-byte aligned; contents scratch.
+ *  workspace  mvue_group_norm_workspace_bytes(n, s, c, groups) bytes, 16-byte aligned; contents scratch.  A call that
+ *             gives mean and rstd and whose samples stay in shared memory (x and y aligned for wide accesses, whole groups
+ *             that fit eight thread blocks) uses none and accepts NULL; others return MVUE_ERR_WORKSPACE without it.
  * Arithmetic in binary32; the output is rounded once.  n = 0: nothing.  s >= 1. */
 MVUE_API int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t c, int64_t ldx, int groups, const void* gamma,
                                  const void* beta, int affine_dtype, float eps, int act, void* y, int64_t ldy, float* mean, float* rstd,

@@ -19,6 +19,7 @@ MVUE_LAYOUT_CANONICAL = 0
 MVUE_LAYOUT_TC = 1
 MVUE_JOINT_TABLE, MVUE_JOINT_SYSTEMATIC, MVUE_JOINT_APPROX = 0, 1, 2
 MVUE_OPT_NONE, MVUE_OPT_STOCHASTIC_ROUNDING, MVUE_OPT_EPS16 = 0, 1, 2
+MVUE_ERR_WORKSPACE = -7
 MVUE_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 EXPORTS = ("mvue_version", "mvue_status_string", "mvue_last_cuda_error", "mvue_packed_sizes",
@@ -106,7 +107,8 @@ def _check(status: int, what: str):
 
 
 def _stream_ptr() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the current stream's handle without a Stream object around it (0.5 us instead of 5 us)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -321,9 +323,11 @@ def mvue_adamw_step(tensors: ctypes.Array, count: int, config: AdamWConfig) -> N
 
 
 def _id_list(ids: torch.Tensor) -> tuple[torch.Tensor, int]:
-    if ids.dtype not in (torch.int32, torch.int64):
-        raise TypeError(f"unsupported id dtype {ids.dtype}")
-    return ids.reshape(-1), 8 * ids.element_size()
+    if ids.dtype is torch.int64:
+        return ids.contiguous(), 64
+    if ids.dtype is torch.int32:
+        return ids.contiguous(), 32
+    raise TypeError(f"unsupported id dtype {ids.dtype}")
 
 
 def mvue_embedding(ids: torch.Tensor, W: torch.Tensor, *, scale: float = 1.0, out: torch.Tensor | None = None, out_dtype=None,
@@ -336,16 +340,15 @@ def mvue_embedding(ids: torch.Tensor, W: torch.Tensor, *, scale: float = 1.0, ou
     vocab, cols = W.shape
     tokens = flat.numel()
     if out is None:
-        res = rows = torch.empty((*ids.shape, cols), dtype=out_dtype or W.dtype, device=W.device)
+        out = W.new_empty((*ids.shape, cols), dtype=out_dtype)
         ldout = cols
     else:
-        res = rows = out
         assert out.shape == (tokens, cols) and out.stride(1) == 1
         ldout = out.stride(0) if tokens > 1 else cols
     _check(lib().mvue_embedding(flat.data_ptr(), id_bits, tokens, W.data_ptr(), _dtype_code(W), vocab, cols,
-                                W.stride(0) if vocab > 1 else cols, scale, rows.data_ptr(), _dtype_code(rows), ldout,
+                                W.stride(0) if vocab > 1 else cols, scale, out.data_ptr(), _dtype_code(out), ldout,
                                 None if dev_status is None else dev_status.data_ptr(), _stream_ptr()), "mvue_embedding")
-    return res
+    return out
 
 
 def mvue_embedding_grad_workspace_bytes(tokens: int, cols: int) -> int:
@@ -368,11 +371,11 @@ def mvue_embedding_grad(ids: torch.Tensor, dy: torch.Tensor, vocab: int, *, scal
     if out is None:
         if accumulate:
             raise ValueError("accumulate adds to a given out")
-        out = torch.empty((vocab, cols), dtype=out_dtype, device=dy.device)
+        out = dy.new_empty((vocab, cols), dtype=out_dtype)
     assert out.shape == (vocab, cols) and out.stride(1) == 1
     need = mvue_embedding_grad_workspace_bytes(tokens, cols)
     if workspace is None or workspace.numel() * workspace.element_size() < need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        workspace = dy.new_empty(need, dtype=torch.uint8)
     _check(lib().mvue_embedding_grad(flat.data_ptr(), id_bits, tokens, dy.data_ptr(), _dtype_code(dy), cols,
                                      dy.stride(0) if tokens > 1 else cols, scale, padding_idx, out.data_ptr(), _dtype_code(out), vocab,
                                      out.stride(0) if vocab > 1 else cols, int(accumulate), workspace.data_ptr(),
@@ -387,6 +390,9 @@ def _ptr(t: torch.Tensor | None):
 
 def _positions(t: torch.Tensor):
     """(n, s, c, ld) of a channels-last tensor [n, ..., c] whose positions lie one row stride apart."""
+    if t.dim() >= 2 and t.numel() and t.is_contiguous():
+        n, c = t.shape[0], t.shape[-1]
+        return n, t.numel() // (n * c), c, c
     if t.dim() < 2 or t.stride(-1) != 1 and t.shape[-1] != 1:
         raise ValueError("wants [n, ..., channels] with unit channel stride")
     c = t.shape[-1]
@@ -421,13 +427,6 @@ def mvue_group_norm_workspace_bytes(n: int, s: int, c: int, groups: int) -> int:
     return b.value
 
 
-def _norm_workspace(n, s, c, groups, device, workspace):
-    need = mvue_group_norm_workspace_bytes(n, s, c, groups)
-    if workspace is None or workspace.numel() * workspace.element_size() < need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    return workspace, workspace.numel() * workspace.element_size()
-
-
 def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, *,
                         eps: float = 1e-5, act: str = "none", out: torch.Tensor | None = None,
                         workspace: torch.Tensor | None = None):
@@ -437,14 +436,23 @@ def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | Non
     assert x.is_cuda
     code = _affine(weight, bias, c)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    assert out.shape == x.shape and out.dtype == x.dtype
-    stats = torch.empty((2, n, groups), dtype=torch.float32, device=x.device)
-    ws, ws_bytes = _norm_workspace(n, s, c, groups, x.device, workspace)
-    _check(lib().mvue_group_norm_act(x.data_ptr(), _dtype_code(x), n, s, c, ldx, groups, _ptr(weight), _ptr(bias), code, eps,
-                                     MVUE_ACTS[act], out.data_ptr(), _positions(out)[3], stats[0].data_ptr(), stats[1].data_ptr(),
-                                     ws.data_ptr(), ws_bytes, _stream_ptr()), "mvue_group_norm_act")
-    return out, stats[0], stats[1]
+        out = x.new_empty(x.shape)
+        ldy = c
+    else:
+        assert out.shape == x.shape and out.dtype == x.dtype
+        ldy = _positions(out)[3]
+    mean, rstd = x.new_empty((n, groups), dtype=torch.float32), x.new_empty((n, groups), dtype=torch.float32)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    while True:
+        status = lib().mvue_group_norm_act(x.data_ptr(), _dtype_code(x), n, s, c, ldx, groups, _ptr(weight), _ptr(bias), code, eps,
+                                           MVUE_ACTS[act], out.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(), _ptr(workspace),
+                                           ws_bytes, _stream_ptr())
+        need = 0 if status != MVUE_ERR_WORKSPACE else mvue_group_norm_workspace_bytes(n, s, c, groups)
+        if need <= ws_bytes:
+            break
+        workspace, ws_bytes = x.new_empty(need, dtype=torch.uint8), need       # only maps that no cluster holds need it
+    _check(status, "mvue_group_norm_act")
+    return out, mean, rstd
 
 
 def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, groups: int,
@@ -457,12 +465,18 @@ def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.
         assert t.shape == (n, groups) and t.dtype == torch.float32 and t.is_contiguous()
     code = _affine(weight, bias, c)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    assert out.shape == x.shape and out.dtype == x.dtype
-    grads = torch.empty((2, c), dtype=torch.float32, device=x.device)
-    ws, ws_bytes = _norm_workspace(n, s, c, groups, x.device, workspace)
+        out = x.new_empty(x.shape)
+        lddx = c
+    else:
+        assert out.shape == x.shape and out.dtype == x.dtype
+        lddx = _positions(out)[3]
+    dweight, dbias = x.new_empty(c, dtype=torch.float32), x.new_empty(c, dtype=torch.float32)
+    need = mvue_group_norm_workspace_bytes(n, s, c, groups)
+    if workspace is None or workspace.numel() * workspace.element_size() < need:
+        workspace = x.new_empty(need, dtype=torch.uint8)
     _check(lib().mvue_group_norm_act_backward(dy.data_ptr(), _positions(dy)[3], x.data_ptr(), ldx, _dtype_code(x), n, s, c, groups,
                                               mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(bias), code, MVUE_ACTS[act],
-                                              out.data_ptr(), _positions(out)[3], grads[0].data_ptr(), grads[1].data_ptr(),
-                                              ws.data_ptr(), ws_bytes, _stream_ptr()), "mvue_group_norm_act_backward")
-    return out, grads[0], grads[1]
+                                              out.data_ptr(), lddx, dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(),
+                                              workspace.numel() * workspace.element_size(), _stream_ptr()),
+           "mvue_group_norm_act_backward")
+    return out, dweight, dbias

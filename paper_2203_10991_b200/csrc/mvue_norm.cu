@@ -50,22 +50,55 @@ __device__ __forceinline__ float affine(const void* p, int is_bf16, int64_t i, f
     return is_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// 1 / (1 + exp(-z))
+__device__ __forceinline__ f2 sigmoid(f2 z) {
+    float a, b;
+    unpair(mul2(z, pair(-1.4426950408889634f)), a, b);
+    unpair(add2(pair(fast_exp2(a), fast_exp2(b)), pair(1.0f)), a, b);
+    return pair(fast_reciprocal(a), fast_reciprocal(b));
+}
 
 template <int kAct>
-__device__ __forceinline__ float act(float z) {
-    if (kAct == MVUE_ACT_RELU) return z < 0.0f ? 0.0f : z;                       // NaN stays
-    if (kAct == MVUE_ACT_SILU) return z * sigmoid(z);
-    if (kAct == MVUE_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    return z;
+__device__ __forceinline__ f2 act(f2 z) {
+    if (kAct == MVUE_ACT_NONE) return z;
+    if (kAct == MVUE_ACT_SILU) return mul2(z, sigmoid(z));
+    float a, b;
+    unpair(z, a, b);
+    if (kAct == MVUE_ACT_RELU) {                                                            // NaN stays
+        asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(a));
+        asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(b));
+        return pair(a, b);
+    }
+    const f2 e = pair(erff(a * 0.70710678118654752f), erff(b * 0.70710678118654752f));
+    return mul2(mul2(z, pair(0.5f)), add2(e, pair(1.0f)));
 }
+// d act'(z)
 template <int kAct>
-__device__ __forceinline__ float act_grad(float z) {
-    if (kAct == MVUE_ACT_RELU) return z <= 0.0f ? 0.0f : 1.0f;
-    if (kAct == MVUE_ACT_SILU) { const float s = sigmoid(z); return fmaf(z * s, 1.0f - s, s); }
-    if (kAct == MVUE_ACT_GELU)
-        return fmaf(z * 0.39894228040143268f, __expf(-0.5f * z * z), fmaf(0.5f, erff(z * 0.70710678118654752f), 0.5f));
-    return 1.0f;
+__device__ __forceinline__ f2 act_grad(f2 z, f2 d) {
+    if (kAct == MVUE_ACT_NONE) return d;
+    if (kAct == MVUE_ACT_SILU) {                       // s + z s (1 - s)
+        const f2 s = sigmoid(z);
+        return mul2(d, fma2(mul2(z, s), fma2(s, pair(-1.0f), pair(1.0f)), s));
+    }
+    float a, b, da, db;
+    unpair(z, a, b);
+    if (kAct == MVUE_ACT_RELU) {
+        unpair(d, da, db);
+        return pair(a <= 0.0f ? 0.0f : da, b <= 0.0f ? 0.0f : db);
+    }
+    const f2 e = pair(erff(a * 0.70710678118654752f), erff(b * 0.70710678118654752f));
+    unpair(mul2(mul2(z, z), pair(-0.72134752044448170f)), a, b);                            // -z^2 / 2 in powers of two
+    const f2 density = mul2(pair(fast_exp2(a), fast_exp2(b)), pair(0.39894228040143268f));
+    return mul2(d, fma2(z, density, fma2(e, pair(0.5f), pair(0.5f))));
+}
+
+__device__ __forceinline__ void pairs(const float (&x)[8], f2 (&p)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = pair(x[2 * j], x[2 * j + 1]);
+}
+__device__ __forceinline__ void unpairs(const f2 (&p)[4], float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unpair(p[j], x[2 * j], x[2 * j + 1]);
 }
 
 // A thread's place: its channels, and its rows first, first + stride, ... below end.
@@ -187,21 +220,48 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const __grid_consta
     }
 }
 
-// mean, rstd gamma and beta of the thread's channels in sample n
-template <bool kWide>
-struct Constants {
-    float mean[8], slope[8], shift[8];
-    __device__ __forceinline__ Constants(const NormArgs& a, const Place<kWide>& p, int64_t n) {
+// What the elements of eight channels need: z = (x - mean) slope + shift, slope = rstd gamma, shift = beta; backward
+// dx = slope dz - level - tilt (x - mean).
+struct Channels {
+    f2 neg_mean[4], slope[4], shift[4];
+
+    // stat(j): (mean, rstd) of channel j's group; channel(j) its number, for j < count
+    template <typename S, typename C> __device__ __forceinline__ void set(const NormArgs& a, int count, S stat, C channel) {
+        float m[8], k[8], b[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const bool in = j < p.cols.count;
-            const int64_t c = in ? p.channel(j) : 0, g = n * a.groups + c / a.group_size;
-            mean[j] = in ? a.mean[g] : 0.0f;
-            slope[j] = in ? a.rstd[g] * affine(a.gamma, a.affine_bf16, c, 1.0f) : 0.0f;
-            shift[j] = in ? affine(a.beta, a.affine_bf16, c, 0.0f) : 0.0f;
+            m[j] = k[j] = b[j] = 0.0f;
+            if (j < count) {
+                const float2 q = stat(j);
+                m[j] = -q.x;
+                k[j] = q.y * affine(a.gamma, a.affine_bf16, channel(j), 1.0f);
+                b[j] = affine(a.beta, a.affine_bf16, channel(j), 0.0f);
+            }
+        }
+        pairs(m, neg_mean);
+        pairs(k, slope);
+        pairs(b, shift);
+    }
+    template <int kAct> __device__ __forceinline__ void output(f2 (&x)[4]) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = act<kAct>(fma2(add2(x[j], neg_mean[j]), slope[j], shift[j]));
+    }
+    // x becomes x - mean, d becomes dz = d act'(z)
+    template <int kAct> __device__ __forceinline__ void gradient(f2 (&x)[4], f2 (&d)[4]) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[j] = add2(x[j], neg_mean[j]);
+            d[j] = act_grad<kAct>(fma2(x[j], slope[j], shift[j]), d[j]);
         }
     }
 };
+
+template <bool kWide>
+__device__ __forceinline__ void set_channels(Channels& k, const NormArgs& a, const Place<kWide>& p) {
+    k.set(a, p.cols.count,
+          [&](int j) { const int64_t g = p.n * a.groups + p.channel(j) / a.group_size; return make_float2(a.mean[g], a.rstd[g]); },
+          [&](int j) { return p.channel(j); });
+}
 
 template <typename T, bool kWide, int kAct>
 __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_constant__ NormArgs a) {
@@ -211,7 +271,8 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_const
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     T* y = static_cast<T*>(a.out) + n * a.s * a.ldo;
-    const Constants<kWide> k(a, p, n);
+    Channels k;
+    set_channels(k, a, p);
     for (; p.row < p.end; p.row += (int64_t)p.stride * kRowsAhead) {
         float v[kRowsAhead][8];
 #pragma unroll
@@ -220,8 +281,10 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_const
 #pragma unroll
         for (int u = 0; u < kRowsAhead; ++u)
             if (p.row + (int64_t)u * p.stride < p.end) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[u][j] = act<kAct>(fmaf(v[u][j] - k.mean[j], k.slope[j], k.shift[j]));
+                f2 z[4];
+                pairs(v[u], z);
+                k.output<kAct>(z);
+                unpairs(z, v[u]);
                 p.cols.store(y + (p.row + (int64_t)u * p.stride) * a.ldo, v[u]);
             }
     }
@@ -237,9 +300,10 @@ __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_c
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + n * a.s * a.lddy;
-    float sum[8] = {}, along[8] = {};
+    f2 sums[4] = {}, alongs[4] = {};
     if (p.row < p.end) {
-        const Constants<kWide> k(a, p, n);
+        Channels k;
+        set_channels(k, a, p);
         for (; p.row < p.end; p.row += (int64_t)p.stride * 2) {
             float v[2][8], d[2][8];
 #pragma unroll
@@ -250,16 +314,22 @@ __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_c
                 }
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-                if (p.row + (int64_t)u * p.stride < p.end)
+                if (p.row + (int64_t)u * p.stride < p.end) {
+                    f2 xc[4], dz[4];
+                    pairs(v[u], xc);
+                    pairs(d[u], dz);
+                    k.gradient<kAct>(xc, dz);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float xc = v[u][j] - k.mean[j];
-                        const float dz = d[u][j] * act_grad<kAct>(fmaf(xc, k.slope[j], k.shift[j]));
-                        sum[j] += dz;
-                        along[j] = fmaf(dz, xc, along[j]);
+                    for (int j = 0; j < 4; ++j) {
+                        sums[j] = add2(sums[j], dz[j]);
+                        alongs[j] = fma2(dz[j], xc[j], alongs[j]);
                     }
+                }
         }
     }
+    float sum[8], along[8];
+    unpairs(sums, sum);
+    unpairs(alongs, along);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         s_a[j * kThreads + threadIdx.x] = sum[j];
@@ -336,16 +406,20 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + n * a.s * a.lddy;
     T* dx = static_cast<T*>(a.out) + n * a.s * a.ldo;
-    const Constants<kWide> k(a, p, n);
-    float level[8], tilt[8];          // dx = slope dz - level - tilt (x - mean)
+    Channels k;
+    set_channels(k, a, p);
+    float low[8], off[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int64_t g = n * a.groups + (j < p.cols.count ? p.channel(j) : 0) / a.group_size;
         const float r = a.rstd[g];
         const float2 q = a.coef[g];
-        level[j] = r * q.x;
-        tilt[j] = r * r * q.y;
+        low[j] = -r * q.x;
+        off[j] = -r * r * q.y;
     }
+    f2 level[4], tilt[4];
+    pairs(low, level);
+    pairs(off, tilt);
     for (; p.row < p.end; p.row += (int64_t)p.stride * 2) {
         float v[2][8], d[2][8];
 #pragma unroll
@@ -357,12 +431,13 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
 #pragma unroll
         for (int u = 0; u < 2; ++u)
             if (p.row + (int64_t)u * p.stride < p.end) {
+                f2 xc[4], dz[4];
+                pairs(v[u], xc);
+                pairs(d[u], dz);
+                k.gradient<kAct>(xc, dz);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float xc = v[u][j] - k.mean[j];
-                    const float dz = d[u][j] * act_grad<kAct>(fmaf(xc, k.slope[j], k.shift[j]));
-                    v[u][j] = fmaf(k.slope[j], dz, fmaf(xc, -tilt[j], -level[j]));
-                }
+                for (int j = 0; j < 4; ++j) xc[j] = fma2(k.slope[j], dz[j], fma2(xc[j], tilt[j], level[j]));
+                unpairs(xc, v[u]);
                 p.cols.store(dx + (p.row + (int64_t)u * p.stride) * a.ldo, v[u]);
             }
     }
@@ -376,111 +451,163 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
 // and one write of HBM.
 struct ResidentArgs {
     NormArgs norm;
-    int cluster, iters;              // blocks of a cluster; rows of a thread at most
-    int64_t rows;                    // rows of a block
+    int cluster, rows, iters;        // blocks of a cluster; rows of a block and of a thread at most
+    int fold;                        // a warp holds whole rows of the slab (a power of two of at most 16 pieces)
 };
 
-constexpr int kPartPitch = kThreads + 1;
-
-__device__ __forceinline__ void copy16(void* smem, const void* global) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(global) : "memory");
+__device__ __forceinline__ void copy16(uint32_t smem, const void* global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory");
 }
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
 // A thread's rows of one tensor in shared memory: 16-byte slots, consecutive threads side by side.
 template <typename T>
 struct Slots {
-    static constexpr int kHalves = sizeof(T) * 8 / 16;
-    char* base;
-    __device__ __forceinline__ Slots(char* area) : base(area + threadIdx.x * 16) {}
-    __device__ __forceinline__ void fetch(int i, const T* from) const {
+    static constexpr int kHalves = sizeof(T) * 8 / 16, kRowBytes = kHalves * kThreads * 16;
+    static __device__ __forceinline__ void fetch(const char* slot, const T* from) {
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) copy16(base + (i * kHalves + h) * (kThreads * 16), reinterpret_cast<const char*>(from) + 16 * h);
+        for (int h = 0; h < kHalves; ++h) copy16(to + h * (kThreads * 16), reinterpret_cast<const char*>(from) + 16 * h);
     }
-    __device__ __forceinline__ void read(int i, float (&x)[8]) const {
+    static __device__ __forceinline__ void read(const char* slot, f2 (&x)[4]) {
         uint4 w[kHalves];
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) w[h] = *reinterpret_cast<const uint4*>(base + (i * kHalves + h) * (kThreads * 16));
+        for (int h = 0; h < kHalves; ++h) w[h] = *reinterpret_cast<const uint4*>(slot + h * (kThreads * 16));
         if (kHalves == 1) {
-            x[0] = bf16_lo(w[0].x); x[1] = bf16_hi(w[0].x); x[2] = bf16_lo(w[0].y); x[3] = bf16_hi(w[0].y);
-            x[4] = bf16_lo(w[0].z); x[5] = bf16_hi(w[0].z); x[6] = bf16_lo(w[0].w); x[7] = bf16_hi(w[0].w);
+            x[0] = pair(bf16_lo(w[0].x), bf16_hi(w[0].x));
+            x[1] = pair(bf16_lo(w[0].y), bf16_hi(w[0].y));
+            x[2] = pair(bf16_lo(w[0].z), bf16_hi(w[0].z));
+            x[3] = pair(bf16_lo(w[0].w), bf16_hi(w[0].w));
         } else {
             const uint4 v = w[kHalves - 1];
-            x[0] = __uint_as_float(w[0].x); x[1] = __uint_as_float(w[0].y); x[2] = __uint_as_float(w[0].z); x[3] = __uint_as_float(w[0].w);
-            x[4] = __uint_as_float(v.x); x[5] = __uint_as_float(v.y); x[6] = __uint_as_float(v.z); x[7] = __uint_as_float(v.w);
+            x[0] = pair(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
+            x[1] = pair(__uint_as_float(w[0].z), __uint_as_float(w[0].w));
+            x[2] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
+            x[3] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
         }
     }
 };
+__device__ __forceinline__ void store_row(float* to, const f2 (&x)[4]) {
+    float v[8];
+    unpairs(x, v);
+    store8(to, true, 8, v);
+}
+__device__ __forceinline__ void store_row(__nv_bfloat16* to, const f2 (&x)[4]) {
+    float v[8];
+    unpairs(x, v);
+    const uint32_t w[4] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    store8_words(to, true, 8, w);
+}
+__device__ __forceinline__ void read8(const float* p, f2 (&x)[4]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = pair(a.x, a.y);
+    x[1] = pair(a.z, a.w);
+    x[2] = pair(b.x, b.y);
+    x[3] = pair(b.z, b.w);
+}
 
-// Where a block of the cluster stands, and its shared memory.
+// Where a block of the cluster stands, and its shared memory.  Values per channel are worked out once per block, by the
+// thread that has the channel's number, and read back eight at a time.
 template <typename T, int kTensors>
 struct Resident {
-    int pieces, ty, threads_down, group_size, groups_here, channels_here, rank, cluster;
-    int64_t n, c0, r0;
-    int rows_here, iters;            // of the block; of this thread (0: it has no channels)
-    char* area[2];
-    float *part, *channel, *group_a, *group_b, *all;
+    const ResidentArgs& a;
+    int piece, ty, threads_down, width, channels, groups, rank, rows_here, iters;   // iters: rows of this thread
+    int64_t n, c0, row0;             // row0: the thread's first row of the sample
+    char* slots[2];
+    float *part, *one, *two, *slope, *shift, *group;     // group: two values for each group and block of the cluster
 
-    __device__ __forceinline__ Resident(const ResidentArgs& a, char* smem) {
+    __device__ __forceinline__ Resident(const ResidentArgs& args, char* smem) : a(args) {
         const NormArgs& q = a.norm;
-        pieces = q.pieces;
-        cluster = a.cluster;
-        rank = blockIdx.x % cluster;
-        const int64_t unit = blockIdx.x / cluster;
-        n = unit / q.slabs;
-        c0 = (unit % q.slabs) * pieces * 8;
-        channels_here = (int)min((int64_t)pieces * 8, q.c - c0);
-        group_size = q.group_size;
-        groups_here = channels_here / group_size;
-        threads_down = kThreads / pieces;
-        ty = threadIdx.x / pieces;
-        r0 = min(q.s, rank * a.rows);
-        rows_here = (int)(min(q.s, r0 + a.rows) - r0);
-        const bool mine = ty < threads_down && (int)(threadIdx.x % pieces) * 8 < channels_here;
-        iters = mine && ty < rows_here ? (rows_here - ty + threads_down - 1) / threads_down : 0;
-        const size_t slots = (size_t)a.iters * Slots<T>::kHalves * kThreads * 16;
-        area[0] = smem;
-        area[1] = smem + (kTensors - 1) * slots;
-        part = reinterpret_cast<float*>(smem + kTensors * slots);
-        channel = part + 8 * kPartPitch;
-        const int width = pieces * 8, most = width / group_size;
-        group_a = channel + 2 * width;
-        group_b = group_a + most;
-        all = group_b + most;        // [cluster][groups][2]
+        const unsigned unit = blockIdx.x / (unsigned)a.cluster;
+        rank = (int)(blockIdx.x - unit * a.cluster);
+        const unsigned sample = unit / (unsigned)q.slabs;
+        n = sample;
+        width = q.pieces * 8;
+        c0 = (int64_t)(unit - sample * q.slabs) * width;
+        channels = (int)min((int64_t)width, q.c - c0);
+        groups = channels / q.group_size;
+        threads_down = kThreads / q.pieces;
+        ty = threadIdx.x / (unsigned)q.pieces;
+        piece = threadIdx.x - ty * q.pieces;
+        const int r0 = min((int)q.s, rank * a.rows);
+        rows_here = min((int)q.s, r0 + a.rows) - r0;
+        row0 = r0 + ty;
+        const bool mine = ty < threads_down && piece * 8 < channels && ty < rows_here;
+        iters = mine ? (rows_here - ty + threads_down - 1) / threads_down : 0;
+        const size_t bytes = (size_t)a.iters * Slots<T>::kRowBytes;
+        slots[0] = smem + threadIdx.x * 16;
+        slots[kTensors - 1] = slots[0] + (kTensors - 1) * bytes;
+        float* f = reinterpret_cast<float*>(smem + kTensors * bytes);
+        one = f;
+        two = one + width;
+        slope = two + width;
+        shift = slope + width;
+        part = shift + width;
+        group = part + (a.fold ? kThreads / 32 : threads_down) * width;
     }
-    __device__ __forceinline__ int64_t first_channel() const { return c0 + (threadIdx.x % pieces) * 8; }
-    __device__ __forceinline__ int64_t row(int i) const { return r0 + ty + (int64_t)i * threads_down; }
-
-    // sums over the block's rows of every thread's eight values -> channel[0 .. channels_here)
-    __device__ __forceinline__ void channel_sums(const float (&x)[8], float* into) const {
-        __syncthreads();
+    // rows [k / 4, (k + 1) / 4) of the thread
+    __device__ __forceinline__ void quarter(int k, int& begin, int& end) const {
+        const int q = (a.iters + 3) >> 2;
+        begin = k * q;
+        end = min(begin + q, iters);
+    }
+    // sums over the block's rows of every thread's eight values -> into[0 .. channels)
+    __device__ __forceinline__ void channel_sums(const f2 (&x)[4], float* into) const {
+        f2 v[4] = {x[0], x[1], x[2], x[3]};
+        bool writes = ty < threads_down;
+        int at = ty;
+        if (a.fold) {
+            for (int o = a.norm.pieces; o < 32; o <<= 1)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) part[j * kPartPitch + threadIdx.x] = x[j];
+                for (int j = 0; j < 4; ++j) v[j] = add2(v[j], f2{__shfl_xor_sync(0xFFFFFFFFu, v[j].v, o)});
+            writes = (threadIdx.x & 31) < (unsigned)a.norm.pieces;
+            at = threadIdx.x >> 5;
+        }
+        if (writes) {
+            float w[8];
+            unpairs(v, w);
+            float4* p = reinterpret_cast<float4*>(part + at * width + piece * 8);
+            p[0] = make_float4(w[0], w[1], w[2], w[3]);
+            p[1] = make_float4(w[4], w[5], w[6], w[7]);
+        }
         __syncthreads();
-        for (int k = threadIdx.x; k < channels_here; k += kThreads) {
-            const float* p = part + (k & 7) * kPartPitch + (k >> 3);
-            float s0 = 0.0f, s1 = 0.0f;
+        const int down = a.fold ? kThreads / 32 : threads_down;
+        for (int k = threadIdx.x; k < channels; k += kThreads) {
+            const float* p = part + k;
+            float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
             int t = 0;
-            for (; t + 1 < threads_down; t += 2) {
-                s0 += p[t * pieces];
-                s1 += p[(t + 1) * pieces];
+            for (; t + 3 < down; t += 4, p += 4 * width) {
+                s0 += p[0];
+                s1 += p[width];
+                s2 += p[2 * width];
+                s3 += p[3 * width];
             }
-            if (t < threads_down) s0 += p[t * pieces];
-            into[k] = s0 + s1;
+            for (; t < down; ++t, p += width) s0 += p[0];
+            into[k] = (s0 + s1) + (s2 + s3);
         }
         __syncthreads();
     }
-    // a warp adds f(channel) over each group and hands the sum to `put(group, sum)` on every lane
-    template <typename F, typename P> __device__ __forceinline__ void group_sums(F f, P put) const {
-        const int lane = threadIdx.x & 31;
-        for (int g = threadIdx.x >> 5; g < groups_here; g += kThreads / 32) {
+    // a warp adds p over the channels of a group; put(group, sum) on every lane
+    template <typename P> __device__ __forceinline__ void group_sums(const float* p, P put) const {
+        const int lane = threadIdx.x & 31, size = a.norm.group_size;
+        for (int g = threadIdx.x >> 5; g < groups; g += kThreads / 32) {
             float s = 0.0f;
-            for (int c = lane; c < group_size; c += 32) s += f(g * group_size + c);
+            for (int c = lane; c < size; c += 32) s += p[g * size + c];
             put(g, warp_sum(s));
         }
     }
-    // block `to`'s copy of p (the same place in its shared memory)
-    __device__ __forceinline__ float* remote(float* p, int to) const { return cg::this_cluster().map_shared_rank(p, to); }
+    // this block's two values of a group to all blocks of the cluster, a lane for each
+    __device__ __forceinline__ void send(int g, float x, float y) const {
+        const int lane = threadIdx.x & 31;
+        if (lane >= a.cluster) return;
+        float* to = a.cluster > 1 ? cg::this_cluster().map_shared_rank(group, lane) : group;
+        *reinterpret_cast<float2*>(to + (rank * groups + g) * 2) = make_float2(x, y);
+    }
+    __device__ __forceinline__ float2 sent(int block, int g) const { return *reinterpret_cast<const float2*>(group + (block * groups + g) * 2); }
+    __device__ __forceinline__ void meet() const {
+        if (a.cluster > 1) cg::this_cluster().sync(); else __syncthreads();
+    }
 };
 
 template <typename T, int kAct>
@@ -489,143 +616,155 @@ __global__ void __launch_bounds__(kThreads) norm_resident_kernel(const __grid_co
     extern __shared__ __align__(16) char smem[];
     const Resident<T, 1> r(a, smem);
     const NormArgs& q = a.norm;
-    const int64_t c = r.first_channel();
-    const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row(0)) * q.ldx + c;
-    const Slots<T> xs(r.area[0]);
-    const int64_t step = (int64_t)r.threads_down * q.ldx;
-    const int quarter = (a.iters + 3) / 4;
+    using S = Slots<T>;
+    {
+        const int64_t step = (int64_t)r.threads_down * q.ldx;
+        const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row0) * q.ldx + r.c0 + r.piece * 8;
+        char* slot = r.slots[0];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) xs.fetch(i, x + i * step);
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        for (int k = 0; k < 4; ++k) {
+            int i, end;
+            for (r.quarter(k, i, end); i < end; ++i, x += step, slot += S::kRowBytes) S::fetch(slot, x);
+            copies_end();
+        }
     }
-    if (r.cluster > 1) cg::this_cluster().sync();              // every block of the cluster runs: its memory may be written
-    float sum[8] = {};
+    for (int k = threadIdx.x; k < r.channels; k += kThreads) {
+        r.slope[k] = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
+        r.shift[k] = affine(q.beta, q.affine_bf16, r.c0 + k, 0.0f);
+    }
+    if (a.cluster > 1) cg::this_cluster().sync();              // every block of the cluster runs: its memory may be written
+    f2 sum[4] = {};
     const auto add = [&](int k) {
-        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) {
-            float v[8];
-            xs.read(i, v);
+        int i, end;
+        r.quarter(k, i, end);
+        const char* slot = r.slots[0] + i * S::kRowBytes;
+#pragma unroll 4
+        for (; i < end; ++i, slot += S::kRowBytes) {
+            f2 v[4];
+            S::read(slot, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += v[j];
+            for (int j = 0; j < 4; ++j) sum[j] = add2(sum[j], v[j]);
         }
     };
     copies_wait<3>(); add(0);
     copies_wait<2>(); add(1);
     copies_wait<1>(); add(2);
     copies_wait<0>(); add(3);
-    r.channel_sums(sum, r.channel);
-    const float mine = (float)r.rows_here * r.group_size, inv = mine > 0.0f ? 1.0f / mine : 0.0f;
-    r.group_sums([&](int k) { return r.channel[k]; }, [&](int g, float s) { r.group_a[g] = s * inv; });
+    r.channel_sums(sum, r.one);
+    const float own = (float)r.rows_here * q.group_size, inv = own > 0.0f ? 1.0f / own : 0.0f;
+    const int lane = threadIdx.x & 31;
+    r.group_sums(r.one, [&](int g, float s) {
+        __syncwarp();
+        for (int c = lane; c < q.group_size; c += 32) r.one[g * q.group_size + c] = -s * inv;     // the block's own mean, per channel
+    });
     __syncthreads();
     // squares about the block's own means, from shared memory
-    float mean[8];
-    const int first = (int)(c - r.c0);
+    f2 neg_mean[4] = {};
+    if (r.iters) read8(r.one + r.piece * 8, neg_mean);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        mean[j] = r.iters ? r.group_a[(first + j) / r.group_size] : 0.0f;
-        sum[j] = 0.0f;
-    }
-    for (int i = 0; i < r.iters; ++i) {
-        float v[8];
-        xs.read(i, v);
+    for (int j = 0; j < 4; ++j) sum[j] = pair(0.0f);
+    const char* slot = r.slots[0];
+#pragma unroll 4
+    for (int i = 0; i < r.iters; ++i, slot += S::kRowBytes) {
+        f2 v[4];
+        S::read(slot, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = v[j] - mean[j];
-            sum[j] = fmaf(d, d, sum[j]);
+        for (int j = 0; j < 4; ++j) {
+            const f2 d = add2(v[j], neg_mean[j]);
+            sum[j] = fma2(d, d, sum[j]);
         }
     }
-    r.channel_sums(sum, r.channel);
-    r.group_sums([&](int k) { return r.channel[k]; }, [&](int g, float s) {
-        const int lane = threadIdx.x & 31;
-        if (lane < r.cluster) {
-            float* to = r.cluster > 1 ? r.remote(r.all, lane) : r.all;
-            to[(r.rank * r.groups_here + g) * 2] = r.group_a[g];
-            to[(r.rank * r.groups_here + g) * 2 + 1] = s;
+    r.channel_sums(sum, r.two);
+    r.group_sums(r.two, [&](int g, float s) { r.send(g, -r.one[g * q.group_size], s); });
+    r.meet();
+    for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
+        // a warp per group, a lane per block of the cluster
+        const float2 p = lane < a.cluster ? r.sent(lane, g) : make_float2(0.0f, 0.0f);
+        const float rows = lane < a.cluster ? (float)max(0, min(a.rows, (int)q.s - lane * a.rows)) : 0.0f;
+        const float mean = warp_sum(rows * p.x) / (float)q.s;
+        const float d = p.x - mean;
+        const float dev = warp_sum(fmaf(rows * q.group_size * d, d, p.y));
+        const float rstd = 1.0f / sqrtf(dev / ((float)q.s * q.group_size) + q.eps);
+        for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
+            r.one[c] = -mean;
+            r.slope[c] *= rstd;
         }
-    });
-    if (r.cluster > 1) cg::this_cluster().sync(); else __syncthreads();
-    for (int g = threadIdx.x; g < r.groups_here; g += kThreads) {
-        const auto rows_of = [&](int b) { return (float)max((int64_t)0, min(a.rows, q.s - b * a.rows)); };
-        const float per_row = 1.0f / (float)q.s;
-        float m = 0.0f, dev = 0.0f;
-        for (int b = 0; b < r.cluster; ++b) m = fmaf(rows_of(b), r.all[(b * r.groups_here + g) * 2], m);
-        m *= per_row;
-        for (int b = 0; b < r.cluster; ++b) {
-            const float d = r.all[(b * r.groups_here + g) * 2] - m;
-            dev += fmaf(rows_of(b) * r.group_size * d, d, r.all[(b * r.groups_here + g) * 2 + 1]);
-        }
-        const float rstd = 1.0f / sqrtf(dev / ((float)q.s * r.group_size) + q.eps);
-        r.group_a[g] = m;
-        r.group_b[g] = rstd;
-        if (r.rank == 0) {
-            const int64_t at = r.n * q.groups + r.c0 / r.group_size + g;
-            q.mean[at] = m;
+        if (r.rank == 0 && lane == 0) {
+            const int64_t at = r.n * q.groups + (int)r.c0 / q.group_size + g;
+            q.mean[at] = mean;
             q.rstd[at] = rstd;
         }
     }
     __syncthreads();
     if (r.iters == 0) return;
-    float slope[8], shift[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int g = (first + j) / r.group_size;
-        mean[j] = r.group_a[g];
-        slope[j] = r.group_b[g] * affine(q.gamma, q.affine_bf16, c + j, 1.0f);
-        shift[j] = affine(q.beta, q.affine_bf16, c + j, 0.0f);
-    }
-    T* y = static_cast<T*>(q.out) + (r.n * q.s + r.row(0)) * q.ldo;
-    const Cols<true> cols(c, q.c, 0, 1);
-    for (int i = 0; i < r.iters; ++i) {
-        float v[8];
-        xs.read(i, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = act<kAct>(fmaf(v[j] - mean[j], slope[j], shift[j]));
-        cols.store(y + (int64_t)i * r.threads_down * q.ldo, v);
+    Channels k8;
+    read8(r.one + r.piece * 8, k8.neg_mean);
+    read8(r.slope + r.piece * 8, k8.slope);
+    read8(r.shift + r.piece * 8, k8.shift);
+    T* y = static_cast<T*>(q.out) + (r.n * q.s + r.row0) * q.ldo + r.c0 + r.piece * 8;
+    const int64_t down = (int64_t)r.threads_down * q.ldo;
+    slot = r.slots[0];
+#pragma unroll 2
+    for (int i = 0; i < r.iters; ++i, y += down, slot += S::kRowBytes) {
+        f2 v[4];
+        S::read(slot, v);
+        k8.output<kAct>(v);
+        store_row(y, v);
     }
 }
 
 // Backward: x and dy resident; the block's sums per channel go to `partial` for the gradients of gamma and beta
 // (norm_grad_join_kernel), the groups' means through the cluster.
 template <typename T, int kAct>
-__global__ void __launch_bounds__(kThreads) norm_resident_grad_kernel(const __grid_constant__ ResidentArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const __grid_constant__ ResidentArgs a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) char smem[];
     const Resident<T, 2> r(a, smem);
     const NormArgs& q = a.norm;
-    const int64_t c = r.first_channel();
-    const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row(0)) * q.ldx + c;
-    const T* dy = static_cast<const T*>(q.dy) + (r.n * q.s + r.row(0)) * q.lddy + c;
-    const Slots<T> xs(r.area[0]), ds(r.area[1]);
-    const int quarter = (a.iters + 3) / 4;
+    using S = Slots<T>;
+    {
+        const int64_t step = (int64_t)r.threads_down * q.ldx, dstep = (int64_t)r.threads_down * q.lddy;
+        const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row0) * q.ldx + r.c0 + r.piece * 8;
+        const T* dy = static_cast<const T*>(q.dy) + (r.n * q.s + r.row0) * q.lddy + r.c0 + r.piece * 8;
+        char *slot = r.slots[0], *dslot = r.slots[1];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) {
-            xs.fetch(i, x + (int64_t)i * r.threads_down * q.ldx);
-            ds.fetch(i, dy + (int64_t)i * r.threads_down * q.lddy);
+        for (int k = 0; k < 4; ++k) {
+            int i, end;
+            for (r.quarter(k, i, end); i < end; ++i, x += step, dy += dstep, slot += S::kRowBytes, dslot += S::kRowBytes) {
+                S::fetch(slot, x);
+                S::fetch(dslot, dy);
+            }
+            copies_end();
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    if (r.cluster > 1) cg::this_cluster().sync();
-    float mean[8], slope[8], shift[8], sum[8] = {}, along[8] = {};
-    const int64_t g0 = r.n * q.groups;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int64_t g = g0 + (c + j) / r.group_size;
-        mean[j] = r.iters ? q.mean[g] : 0.0f;
-        slope[j] = r.iters ? q.rstd[g] * affine(q.gamma, q.affine_bf16, c + j, 1.0f) : 0.0f;
-        shift[j] = r.iters ? affine(q.beta, q.affine_bf16, c + j, 0.0f) : 0.0f;
+    const int64_t g0 = r.n * q.groups + (int)r.c0 / q.group_size;
+    for (int k = threadIdx.x; k < r.channels; k += kThreads) {
+        const int64_t g = g0 + k / q.group_size;
+        r.one[k] = -q.mean[g];
+        r.slope[k] = q.rstd[g] * affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
+        r.shift[k] = affine(q.beta, q.affine_bf16, r.c0 + k, 0.0f);
     }
+    r.meet();                        // also: every block of the cluster runs, its memory may be written
+    Channels k8 = {};
+    if (r.iters) {
+        read8(r.one + r.piece * 8, k8.neg_mean);
+        read8(r.slope + r.piece * 8, k8.slope);
+        read8(r.shift + r.piece * 8, k8.shift);
+    }
+    f2 sum[4] = {}, along[4] = {};
     const auto add = [&](int k) {
-        for (int i = k * quarter; i < min((k + 1) * quarter, r.iters); ++i) {
-            float v[8], d[8];
-            xs.read(i, v);
-            ds.read(i, d);
+        int i, end;
+        r.quarter(k, i, end);
+        const char *slot = r.slots[0] + i * S::kRowBytes, *dslot = r.slots[1] + i * S::kRowBytes;
+        for (; i < end; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
+            f2 v[4], d[4];
+            S::read(slot, v);
+            S::read(dslot, d);
+            k8.gradient<kAct>(v, d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float xc = v[j] - mean[j];
-                const float dz = d[j] * act_grad<kAct>(fmaf(xc, slope[j], shift[j]));
-                sum[j] += dz;
-                along[j] = fmaf(dz, xc, along[j]);
+            for (int j = 0; j < 4; ++j) {
+                sum[j] = add2(sum[j], d[j]);
+                along[j] = fma2(d[j], v[j], along[j]);
             }
         }
     };
@@ -633,59 +772,50 @@ __global__ void __launch_bounds__(kThreads) norm_resident_grad_kernel(const __gr
     copies_wait<2>(); add(1);
     copies_wait<1>(); add(2);
     copies_wait<0>(); add(3);
-    float* channel_b = r.channel + r.pieces * 8;
-    r.channel_sums(sum, r.channel);
-    r.channel_sums(along, channel_b);
-    for (int k = threadIdx.x; k < r.channels_here; k += kThreads) {
-        const float2 s = make_float2(r.channel[k], channel_b[k] * q.rstd[g0 + (r.c0 + k) / r.group_size]);
-        const float gamma = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
-        q.partial[((r.n * r.cluster) + r.rank) * q.c + r.c0 + k] = s;
-        r.channel[k] = gamma * s.x;
-        channel_b[k] = gamma * s.y;
+    __syncthreads();                 // all have read r.one
+    r.channel_sums(sum, r.one);
+    r.channel_sums(along, r.two);
+    for (int k = threadIdx.x; k < r.channels; k += kThreads) {
+        const float rstd = q.rstd[g0 + k / q.group_size], gamma = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
+        const float2 s = make_float2(r.one[k], r.two[k] * rstd);
+        q.partial[(r.n * a.cluster + r.rank) * q.c + r.c0 + k] = s;
+        r.one[k] = gamma * s.x;
+        r.two[k] = gamma * s.y;
     }
     __syncthreads();
-    const auto send = [&](int which) {
-        return [&r, which](int g, float s) {
-            const int lane = threadIdx.x & 31;
-            if (lane < r.cluster) (r.cluster > 1 ? r.remote(r.all, lane) : r.all)[(r.rank * r.groups_here + g) * 2 + which] = s;
-        };
-    };
-    r.group_sums([&](int k) { return r.channel[k]; }, send(0));
-    r.group_sums([&](int k) { return channel_b[k]; }, send(1));
-    if (r.cluster > 1) cg::this_cluster().sync(); else __syncthreads();
-    const float inv = (float)(1.0 / ((double)q.s * r.group_size));
-    for (int g = threadIdx.x; g < r.groups_here; g += kThreads) {
-        float sa = 0.0f, sb = 0.0f;
-        for (int b = 0; b < r.cluster; ++b) {
-            sa += r.all[(b * r.groups_here + g) * 2];
-            sb += r.all[(b * r.groups_here + g) * 2 + 1];
+    const int lane = threadIdx.x & 31;
+    r.group_sums(r.one, [&](int g, float s) {
+        float t = 0.0f;
+        for (int c = lane; c < q.group_size; c += 32) t += r.two[g * q.group_size + c];
+        r.send(g, s, warp_sum(t));
+    });
+    r.meet();
+    const float inv = 1.0f / ((float)q.s * q.group_size);
+    for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
+        const float2 p = lane < a.cluster ? r.sent(lane, g) : make_float2(0.0f, 0.0f);
+        const float rstd = q.rstd[g0 + g];
+        const float level = -rstd * (warp_sum(p.x) * inv), tilt = -rstd * rstd * (warp_sum(p.y) * inv);
+        for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
+            r.one[c] = level;
+            r.two[c] = tilt;
         }
-        const float rstd = q.rstd[g0 + r.c0 / r.group_size + g];
-        r.group_a[g] = rstd * (sa * inv);
-        r.group_b[g] = rstd * rstd * (sb * inv);
     }
     __syncthreads();
     if (r.iters == 0) return;
-    float level[8], tilt[8];          // dx = slope dz - level - tilt (x - mean)
+    f2 level[4], tilt[4];            // dx = slope dz + level + tilt (x - mean)
+    read8(r.one + r.piece * 8, level);
+    read8(r.two + r.piece * 8, tilt);
+    T* dx = static_cast<T*>(q.out) + (r.n * q.s + r.row0) * q.ldo + r.c0 + r.piece * 8;
+    const int64_t down = (int64_t)r.threads_down * q.ldo;
+    const char *slot = r.slots[0], *dslot = r.slots[1];
+    for (int i = 0; i < r.iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
+        f2 v[4], d[4];
+        S::read(slot, v);
+        S::read(dslot, d);
+        k8.gradient<kAct>(v, d);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int g = (int)(c - r.c0 + j) / r.group_size;
-        level[j] = r.group_a[g];
-        tilt[j] = r.group_b[g];
-    }
-    T* dx = static_cast<T*>(q.out) + (r.n * q.s + r.row(0)) * q.ldo;
-    const Cols<true> cols(c, q.c, 0, 1);
-    for (int i = 0; i < r.iters; ++i) {
-        float v[8], d[8];
-        xs.read(i, v);
-        ds.read(i, d);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float xc = v[j] - mean[j];
-            const float dz = d[j] * act_grad<kAct>(fmaf(xc, slope[j], shift[j]));
-            v[j] = fmaf(slope[j], dz, fmaf(xc, -tilt[j], -level[j]));
-        }
-        cols.store(dx + (int64_t)i * r.threads_down * q.ldo, v);
+        for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt[j], level[j]));
+        store_row(dx, v);
     }
 }
 
@@ -714,16 +844,15 @@ Split split_of(int64_t n, int64_t s, int64_t c) {
 }
 
 constexpr int kMaxCluster = 8;
-constexpr size_t kBlockBytes[3] = {56 << 10, 113 << 10, 226 << 10};     // shared memory of four, two and one blocks on an SM
+constexpr size_t kBlockBytes[4] = {56 << 10, 75 << 10, 113 << 10, 226 << 10};     // shared memory of four, three, two and one blocks on an SM
 
 struct Keep {
-    int pieces = 0, slabs, cluster, iters;      // pieces = 0: the slab of one sample does not fit a cluster
-    int64_t rows;
+    int pieces = 0, slabs, cluster, rows, iters, fold;      // pieces = 0: the slab of one sample does not fit a cluster
     size_t smem;
 };
 // A slab is the fewest whole groups that are whole pieces of eight channels and 128 bytes of a row (or all channels); small
 // maps take more, as long as two blocks are left for every SM.  Then the fewest blocks that hold a slab in the
-// smallest of the three shares of shared memory that does, and more where the grid would leave SMs idle.
+// smallest of the four shares of shared memory that does, and more where the grid would leave SMs idle.
 Keep keep_of(int64_t n, int64_t s, int64_t c, int groups, int64_t esz, int tensors) {
     Keep k;
     const int64_t cg = c / groups, least = std::lcm(cg, (int64_t)8);
@@ -733,23 +862,24 @@ Keep keep_of(int64_t n, int64_t s, int64_t c, int groups, int64_t esz, int tenso
         width *= 2;
     const int pieces = (int)(width / 8), down = kThreads / pieces;
     const int64_t slabs = (c + width - 1) / width, most = width / cg;
+    k.fold = pieces <= 16 && (pieces & (pieces - 1)) == 0;
     const auto try_cluster = [&](int cluster, size_t limit) {
         const int64_t rows = (s + cluster - 1) / cluster, iters = (rows + down - 1) / down;
         if (iters > (1 << 16)) return false;
-        const size_t smem = (size_t)tensors * iters * esz * 8 * kThreads + 4 * (8 * kPartPitch + 2 * width + 2 * most + 2 * most * cluster);
+        const size_t smem = (size_t)tensors * iters * esz * 8 * kThreads + 4 * ((4 + (k.fold ? kThreads / 32 : down)) * width + 2 * most * cluster);
         if (smem > limit) return false;
-        k.rows = rows;
+        k.rows = (int)rows;
         k.iters = (int)iters;
         k.cluster = cluster;
         k.smem = smem;
         return true;
     };
     bool found = false;
-    for (int level = 0; level < 3 && !found; ++level)
+    for (int level = 0; level < 4 && !found; ++level)
         for (int cluster = 1; cluster <= kMaxCluster && !found; cluster *= 2) found = try_cluster(cluster, kBlockBytes[level]);
     if (!found) return k;
     while (k.cluster < kMaxCluster && n * slabs * k.cluster * 2 <= 2 * 148 && s >= (int64_t)k.cluster * 2 * down)
-        if (!try_cluster(k.cluster * 2, kBlockBytes[2])) break;
+        if (!try_cluster(k.cluster * 2, kBlockBytes[3])) break;
     if (n * slabs > 0x7FFFFFFF / kMaxCluster) return k;
     k.pieces = pieces;
     k.slabs = (int)slabs;
@@ -759,7 +889,7 @@ Keep keep_of(int64_t n, int64_t s, int64_t c, int groups, int64_t esz, int tenso
 template <typename K>
 cudaError_t launch_resident(K kernel, PerDeviceOnce& once, const ResidentArgs& a, const Keep& k, cudaStream_t st) {
     cudaError_t e = once_per_device(once, [&](int) {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockBytes[2]);
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockBytes[3]);
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -815,7 +945,7 @@ cudaError_t either(const NormArgs& a, dim3 grid, cudaStream_t st) {
     if constexpr (kWide) {
         const Keep k = keep_of(a.n, a.s, a.c, a.groups, sizeof(T), a.dy ? 2 : 1);
         if (k.pieces) {
-            ResidentArgs r{a, k.cluster, k.iters, k.rows};
+            ResidentArgs r{a, k.cluster, k.rows, k.iters, k.fold};
             r.norm.pieces = k.pieces;
             r.norm.slabs = k.slabs;
             r.norm.chunks = k.cluster;
@@ -850,8 +980,10 @@ int check(int dtype, int64_t n, int64_t s, int64_t c, int groups, int affine_dty
 }
 
 int run(NormArgs& a, int dtype, int act, bool wide, void* workspace, size_t workspace_bytes, void* stream, const char* what) {
+    // a forward pass whose samples stay in shared memory leaves nothing outside when it is given room for mean and rstd
+    const bool none = wide && !a.dy && a.mean && a.rstd && keep_of(a.n, a.s, a.c, a.groups, size_of(dtype), 1).pieces;
     const Layout l = layout_of(a.n, a.s, a.c, a.groups);
-    if (!workspace || workspace_bytes < l.bytes || off(workspace, 16)) return MVUE_ERR_WORKSPACE;
+    if (!none && (!workspace || workspace_bytes < l.bytes || off(workspace, 16))) return MVUE_ERR_WORKSPACE;
     DeviceInfo dev;
     if (int e = current_device_info(&dev)) return e;
     char* ws = static_cast<char*>(workspace);
