@@ -130,10 +130,12 @@ typedef enum { MVUE_ACT_NONE = 0, MVUE_ACT_RELU = 1, MVUE_ACT_SILU = 2, MVUE_ACT
  *  workspace  mvue_group_norm_workspace_bytes(n, s, c, groups) bytes, 16-byte aligned; contents scratch.  A call that
  *             gives mean and rstd and whose samples stay in shared memory (x and y aligned for wide accesses, whole groups
  *             that fit eight thread blocks) uses none and accepts NULL; others return MVUE_ERR_WORKSPACE without it.
+ *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait between the blocks of a cluster expires
+ *             (then the outputs are unspecified); otherwise left untouched.
  * Arithmetic in binary32; the output is rounded once.  n = 0: nothing.  s >= 1. */
 MVUE_API int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t c, int64_t ldx, int groups, const void* gamma,
                                  const void* beta, int affine_dtype, float eps, int act, void* y, int64_t ldy, float* mean, float* rstd,
-                                 void* workspace, size_t workspace_bytes, void* stream);
+                                 void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
 
 /* Its backward pass, z formed again from x and the forward pass's mean and rstd:
  *   dz = dy act'(z);  dbeta_c = sum dz;  dgamma_c = sum dz xh, xh = (x - mean) rstd   (over n and s)
@@ -143,7 +145,7 @@ MVUE_API int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s,
 MVUE_API int mvue_group_norm_act_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int dtype, int64_t n, int64_t s,
                                           int64_t c, int groups, const float* mean, const float* rstd, const void* gamma,
                                           const void* beta, int affine_dtype, int act, void* dx, int64_t lddx, float* dgamma,
-                                          float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+                                          float* dbeta, void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
 MVUE_API int mvue_group_norm_workspace_bytes(int64_t n, int64_t s, int64_t c, int groups, size_t* bytes);   /* bytes: HOST */
 
 #ifdef __cplusplus

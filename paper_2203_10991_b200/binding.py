@@ -92,9 +92,9 @@ def lib() -> ctypes.CDLL:
         L.mvue_embedding.argtypes = [vp, ci, i64, vp, ci, i64, i64, i64, cf, vp, ci, i64, vp, vp]
         L.mvue_embedding_grad.argtypes = [vp, ci, i64, vp, ci, i64, i64, cf, i64, vp, ci, i64, i64, ci, vp, csz, vp, vp]
         L.mvue_embedding_grad_workspace_bytes.argtypes = [i64, i64, szp]
-        L.mvue_group_norm_act.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, vp, ci, cf, ci, vp, i64, vp, vp, vp, csz, vp]
+        L.mvue_group_norm_act.argtypes = [vp, ci, i64, i64, i64, i64, ci, vp, vp, ci, cf, ci, vp, i64, vp, vp, vp, csz, vp, vp]
         L.mvue_group_norm_act_backward.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, ci, vp, vp, vp, vp, ci, ci, vp, i64, vp, vp,
-                                                   vp, csz, vp]
+                                                   vp, csz, vp, vp]
         L.mvue_group_norm_workspace_bytes.argtypes = [i64, i64, i64, ci, szp]
         L.mvue_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, ctypes.POINTER(AdamWConfig), vp]
         _lib = L
@@ -429,7 +429,7 @@ def mvue_group_norm_workspace_bytes(n: int, s: int, c: int, groups: int) -> int:
 
 def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, *,
                         eps: float = 1e-5, act: str = "none", out: torch.Tensor | None = None,
-                        workspace: torch.Tensor | None = None):
+                        workspace: torch.Tensor | None = None, dev_status: torch.Tensor | None = None):
     """act(group_norm(x) * weight + bias) on a channels-last CUDA tensor x [n, ..., c], fp32 or bf16 (act: none, relu, silu,
     gelu).  Returns (y, mean, rstd); mean and rstd [n, groups] fp32 are what the backward pass takes."""
     n, s, c, ldx = _positions(x)
@@ -446,7 +446,7 @@ def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | Non
     while True:
         status = lib().mvue_group_norm_act(x.data_ptr(), _dtype_code(x), n, s, c, ldx, groups, _ptr(weight), _ptr(bias), code, eps,
                                            MVUE_ACTS[act], out.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(), _ptr(workspace),
-                                           ws_bytes, _stream_ptr())
+                                           ws_bytes, _ptr(dev_status), _stream_ptr())
         need = 0 if status != MVUE_ERR_WORKSPACE else mvue_group_norm_workspace_bytes(n, s, c, groups)
         if need <= ws_bytes:
             break
@@ -457,7 +457,8 @@ def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | Non
 
 def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, groups: int,
                                  weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, *, act: str = "none",
-                                 out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+                                 out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                                 dev_status: torch.Tensor | None = None):
     """Backward pass of mvue_group_norm_act.  Returns (dx, dweight, dbias); the last two [c] fp32."""
     n, s, c, ldx = _positions(x)
     assert x.is_cuda and dy.shape == x.shape and dy.dtype == x.dtype
@@ -477,6 +478,6 @@ def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.
     _check(lib().mvue_group_norm_act_backward(dy.data_ptr(), _positions(dy)[3], x.data_ptr(), ldx, _dtype_code(x), n, s, c, groups,
                                               mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(bias), code, MVUE_ACTS[act],
                                               out.data_ptr(), lddx, dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(),
-                                              workspace.numel() * workspace.element_size(), _stream_ptr()),
+                                              workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream_ptr()),
            "mvue_group_norm_act_backward")
     return out, dweight, dbias

@@ -25,6 +25,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256;
+constexpr int kResidentCols = 8;       // channels of a thread where a sample stays in shared memory
 constexpr int kMaxPieces = 32;       // pieces of eight channels that a block is wide: 256 channels
 constexpr int kRowsAhead = 4;        // rows that a thread has in flight
 
@@ -43,6 +44,7 @@ struct NormArgs {
     float2* partial;                 // [n, chunks, c]: (mean, M2), backward (sum dz, sum dz xh)
     float2* coef;                    // backward: [n, groups]: means over the group of gamma dz and of gamma dz xh
     float *dgamma, *dbeta;
+    int* dev_status;
 };
 
 __device__ __forceinline__ float affine(const void* p, int is_bf16, int64_t i, float none) {
@@ -50,12 +52,14 @@ __device__ __forceinline__ float affine(const void* p, int is_bf16, int64_t i, f
     return is_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
 }
 
-// 1 / (1 + exp(-z))
+// 1 / (1 + exp(-z)) of two numbers with one reciprocal, that of the product of the two denominators: the special-function
+// unit takes 16 values a cycle, and two each would hold up the backward pass.  The exponentials are capped at 2^60
+// (z below -41.6, where the factor stays at 2^-60), which keeps the product finite.
 __device__ __forceinline__ f2 sigmoid(f2 z) {
     float a, b;
     unpair(mul2(z, pair(-1.4426950408889634f)), a, b);
-    unpair(add2(pair(fast_exp2(a), fast_exp2(b)), pair(1.0f)), a, b);
-    return pair(fast_reciprocal(a), fast_reciprocal(b));
+    unpair(add2(pair(fast_exp2(fminf(a, 60.0f)), fast_exp2(fminf(b, 60.0f))), pair(1.0f)), a, b);
+    return mul2(pair(fast_reciprocal(a * b)), pair(b, a));
 }
 
 template <int kAct>
@@ -92,13 +96,15 @@ __device__ __forceinline__ f2 act_grad(f2 z, f2 d) {
     return mul2(d, fma2(z, density, fma2(e, pair(0.5f), pair(0.5f))));
 }
 
-__device__ __forceinline__ void pairs(const float (&x)[8], f2 (&p)[4]) {
+template <int kPairs>
+__device__ __forceinline__ void pairs(const float (&x)[2 * kPairs], f2 (&p)[kPairs]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) p[j] = pair(x[2 * j], x[2 * j + 1]);
+    for (int j = 0; j < kPairs; ++j) p[j] = pair(x[2 * j], x[2 * j + 1]);
 }
-__device__ __forceinline__ void unpairs(const f2 (&p)[4], float (&x)[8]) {
+template <int kPairs>
+__device__ __forceinline__ void unpairs(const f2 (&p)[kPairs], float (&x)[2 * kPairs]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) unpair(p[j], x[2 * j], x[2 * j + 1]);
+    for (int j = 0; j < kPairs; ++j) unpair(p[j], x[2 * j], x[2 * j + 1]);
 }
 
 // A thread's place: its channels, and its rows first, first + stride, ... below end.
@@ -220,36 +226,20 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const __grid_consta
     }
 }
 
-// What the elements of eight channels need: z = (x - mean) slope + shift, slope = rstd gamma, shift = beta; backward
-// dx = slope dz - level - tilt (x - mean).
+// What the elements of a thread's channels need: z = (x - mean) slope + shift, slope = rstd gamma, shift = beta; backward
+// dx = slope dz + level + tilt (x - mean).
+template <int kPairs>
 struct Channels {
-    f2 neg_mean[4], slope[4], shift[4];
+    f2 neg_mean[kPairs], slope[kPairs], shift[kPairs];
 
-    // stat(j): (mean, rstd) of channel j's group; channel(j) its number, for j < count
-    template <typename S, typename C> __device__ __forceinline__ void set(const NormArgs& a, int count, S stat, C channel) {
-        float m[8], k[8], b[8];
+    template <int kAct> __device__ __forceinline__ void output(f2 (&x)[kPairs]) const {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            m[j] = k[j] = b[j] = 0.0f;
-            if (j < count) {
-                const float2 q = stat(j);
-                m[j] = -q.x;
-                k[j] = q.y * affine(a.gamma, a.affine_bf16, channel(j), 1.0f);
-                b[j] = affine(a.beta, a.affine_bf16, channel(j), 0.0f);
-            }
-        }
-        pairs(m, neg_mean);
-        pairs(k, slope);
-        pairs(b, shift);
-    }
-    template <int kAct> __device__ __forceinline__ void output(f2 (&x)[4]) const {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = act<kAct>(fma2(add2(x[j], neg_mean[j]), slope[j], shift[j]));
+        for (int j = 0; j < kPairs; ++j) x[j] = act<kAct>(fma2(add2(x[j], neg_mean[j]), slope[j], shift[j]));
     }
     // x becomes x - mean, d becomes dz = d act'(z)
-    template <int kAct> __device__ __forceinline__ void gradient(f2 (&x)[4], f2 (&d)[4]) const {
+    template <int kAct> __device__ __forceinline__ void gradient(f2 (&x)[kPairs], f2 (&d)[kPairs]) const {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kPairs; ++j) {
             x[j] = add2(x[j], neg_mean[j]);
             d[j] = act_grad<kAct>(fma2(x[j], slope[j], shift[j]), d[j]);
         }
@@ -257,10 +247,21 @@ struct Channels {
 };
 
 template <bool kWide>
-__device__ __forceinline__ void set_channels(Channels& k, const NormArgs& a, const Place<kWide>& p) {
-    k.set(a, p.cols.count,
-          [&](int j) { const int64_t g = p.n * a.groups + p.channel(j) / a.group_size; return make_float2(a.mean[g], a.rstd[g]); },
-          [&](int j) { return p.channel(j); });
+__device__ __forceinline__ void set_channels(Channels<4>& k, const NormArgs& a, const Place<kWide>& p) {
+    float m[8], t[8], b[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        m[j] = t[j] = b[j] = 0.0f;
+        if (j < p.cols.count) {
+            const int64_t c = p.channel(j), g = p.n * a.groups + c / a.group_size;
+            m[j] = -a.mean[g];
+            t[j] = a.rstd[g] * affine(a.gamma, a.affine_bf16, c, 1.0f);
+            b[j] = affine(a.beta, a.affine_bf16, c, 0.0f);
+        }
+    }
+    pairs(m, k.neg_mean);
+    pairs(t, k.slope);
+    pairs(b, k.shift);
 }
 
 template <typename T, bool kWide, int kAct>
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_const
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     T* y = static_cast<T*>(a.out) + n * a.s * a.ldo;
-    Channels k;
+    Channels<4> k;
     set_channels(k, a, p);
     for (; p.row < p.end; p.row += (int64_t)p.stride * kRowsAhead) {
         float v[kRowsAhead][8];
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_c
     const T* dy = static_cast<const T*>(a.dy) + n * a.s * a.lddy;
     f2 sums[4] = {}, alongs[4] = {};
     if (p.row < p.end) {
-        Channels k;
+        Channels<4> k;
         set_channels(k, a, p);
         for (; p.row < p.end; p.row += (int64_t)p.stride * 2) {
             float v[2][8], d[2][8];
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + n * a.s * a.lddy;
     T* dx = static_cast<T*>(a.out) + n * a.s * a.ldo;
-    Channels k;
+    Channels<4> k;
     set_channels(k, a, p);
     float low[8], off[8];
 #pragma unroll
@@ -453,123 +454,156 @@ struct ResidentArgs {
     NormArgs norm;
     int cluster, rows, iters;        // blocks of a cluster; rows of a block and of a thread at most
     int fold;                        // a warp holds whole rows of the slab (a power of two of at most 16 pieces)
+    int units;                       // slabs of all samples
 };
 
-__device__ __forceinline__ void copy16(uint32_t smem, const void* global) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory");
+template <int kBytes>
+__device__ __forceinline__ void copy(uint32_t smem, const char* global) {
+    if (kBytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem), "l"(global) : "memory");
+    else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory");
 }
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// A thread's rows of one tensor in shared memory: 16-byte slots, consecutive threads side by side.
-template <typename T>
+// A thread's rows of one tensor in shared memory, kCols channels of each: slots of 8 or 16 bytes, consecutive threads side
+// by side.
+template <typename T, int kCols>
 struct Slots {
-    static constexpr int kHalves = sizeof(T) * 8 / 16, kRowBytes = kHalves * kThreads * 16;
-    static __device__ __forceinline__ void fetch(const char* slot, const T* from) {
-        const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
+    static constexpr int kBytes = sizeof(T) * kCols, kSlot = kBytes < 16 ? kBytes : 16, kParts = kBytes / kSlot, kRowBytes = kBytes * kThreads;
+    static constexpr int kPairs = kCols / 2;
+    static __device__ __forceinline__ void fetch(uint32_t to, const T* from) {
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) copy16(to + h * (kThreads * 16), reinterpret_cast<const char*>(from) + 16 * h);
+        for (int h = 0; h < kParts; ++h) copy<kSlot>(to + h * (kThreads * kSlot), reinterpret_cast<const char*>(from) + kSlot * h);
     }
-    static __device__ __forceinline__ void read(const char* slot, f2 (&x)[4]) {
-        uint4 w[kHalves];
+    static __device__ __forceinline__ void read(const char* slot, f2 (&x)[kPairs]) {
+        uint32_t w[kBytes / 4];
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) w[h] = *reinterpret_cast<const uint4*>(slot + h * (kThreads * 16));
-        if (kHalves == 1) {
-            x[0] = pair(bf16_lo(w[0].x), bf16_hi(w[0].x));
-            x[1] = pair(bf16_lo(w[0].y), bf16_hi(w[0].y));
-            x[2] = pair(bf16_lo(w[0].z), bf16_hi(w[0].z));
-            x[3] = pair(bf16_lo(w[0].w), bf16_hi(w[0].w));
+        for (int h = 0; h < kParts; ++h) {
+            if (kSlot == 16) {
+                const uint4 v = *reinterpret_cast<const uint4*>(slot + h * (kThreads * kSlot));
+                w[4 * h] = v.x; w[4 * h + 1] = v.y; w[4 * h + 2] = v.z; w[4 * h + 3] = v.w;
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2*>(slot);
+                w[0] = v.x; w[1] = v.y;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j)
+            x[j] = sizeof(T) == 2 ? pair(bf16_lo(w[j]), bf16_hi(w[j])) : pair(__uint_as_float(w[2 * j % (kBytes / 4)]), __uint_as_float(w[(2 * j + 1) % (kBytes / 4)]));
+    }
+    static __device__ __forceinline__ void store(T* to, const f2 (&x)[kPairs]) {
+        float v[kCols];
+        unpairs(x, v);
+        uint32_t w[kBytes / 4];
+#pragma unroll
+        for (int j = 0; j < kBytes / 4; ++j)
+            w[j] = sizeof(T) == 2 ? pack_bf16x2(v[2 * j % kCols], v[(2 * j + 1) % kCols]) : __float_as_uint(v[j % kCols]);
+        if constexpr (kBytes == 32) {
+            st256(to, w);
+        } else if constexpr (kBytes == 16) {
+            *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
         } else {
-            const uint4 v = w[kHalves - 1];
-            x[0] = pair(__uint_as_float(w[0].x), __uint_as_float(w[0].y));
-            x[1] = pair(__uint_as_float(w[0].z), __uint_as_float(w[0].w));
-            x[2] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
-            x[3] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
+            *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
         }
     }
 };
-__device__ __forceinline__ void store_row(float* to, const f2 (&x)[4]) {
-    float v[8];
-    unpairs(x, v);
-    store8(to, true, 8, v);
-}
-__device__ __forceinline__ void store_row(__nv_bfloat16* to, const f2 (&x)[4]) {
-    float v[8];
-    unpairs(x, v);
-    const uint32_t w[4] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-    store8_words(to, true, 8, w);
-}
-__device__ __forceinline__ void read8(const float* p, f2 (&x)[4]) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = pair(a.x, a.y);
-    x[1] = pair(a.z, a.w);
-    x[2] = pair(b.x, b.y);
-    x[3] = pair(b.z, b.w);
+template <int kPairs>
+__device__ __forceinline__ void read_values(const float* p, f2 (&x)[kPairs]) {
+#pragma unroll
+    for (int j = 0; j < kPairs; j += 2) {
+        const float4 a = *reinterpret_cast<const float4*>(p + 2 * j);
+        x[j] = pair(a.x, a.y);
+        x[j + 1] = pair(a.z, a.w);
+    }
 }
 
 // Where a block of the cluster stands, and its shared memory.  Values per channel are worked out once per block, by the
 // thread that has the channel's number, and read back eight at a time.
-template <typename T, int kTensors>
+template <typename T, int kTensors, int kCols>
 struct Resident {
+    using S = Slots<T, kCols>;
+    static constexpr int kPairs = kCols / 2;
     const ResidentArgs& a;
-    int piece, ty, threads_down, width, channels, groups, rank, rows_here, iters;   // iters: rows of this thread
-    int64_t n, c0, row0;             // row0: the thread's first row of the sample
-    char* slots[2];
-    float *part, *one, *two, *slope, *shift, *group;     // group: two values for each group and block of the cluster
+    int piece, ty, threads_down, width, rank, rows_here, iters, row0;      // iters: rows of this thread below row0, its first one
+    int channels, groups;            // of the unit at hand
+    int64_t n, c0;
+    bool mine;                       // the thread's piece exists in the unit at hand
+    char* smem;
+    size_t tensor_bytes;
+    float *part, *one, *two, *slope, *shift, *group;     // group: two values for each group and block of the cluster, two units deep
+    unsigned long long* bars;
 
-    __device__ __forceinline__ Resident(const ResidentArgs& args, char* smem) : a(args) {
+    __device__ __forceinline__ Resident(const ResidentArgs& args, char* shared) : a(args), smem(shared) {
         const NormArgs& q = a.norm;
-        const unsigned unit = blockIdx.x / (unsigned)a.cluster;
-        rank = (int)(blockIdx.x - unit * a.cluster);
-        const unsigned sample = unit / (unsigned)q.slabs;
-        n = sample;
-        width = q.pieces * 8;
-        c0 = (int64_t)(unit - sample * q.slabs) * width;
-        channels = (int)min((int64_t)width, q.c - c0);
-        groups = channels / q.group_size;
+        rank = (int)(blockIdx.x % (unsigned)a.cluster);
+        width = q.pieces * kCols;
         threads_down = kThreads / q.pieces;
         ty = threadIdx.x / (unsigned)q.pieces;
         piece = threadIdx.x - ty * q.pieces;
         const int r0 = min((int)q.s, rank * a.rows);
         rows_here = min((int)q.s, r0 + a.rows) - r0;
         row0 = r0 + ty;
-        const bool mine = ty < threads_down && piece * 8 < channels && ty < rows_here;
-        iters = mine ? (rows_here - ty + threads_down - 1) / threads_down : 0;
-        const size_t bytes = (size_t)a.iters * Slots<T>::kRowBytes;
-        slots[0] = smem + threadIdx.x * 16;
-        slots[kTensors - 1] = slots[0] + (kTensors - 1) * bytes;
-        float* f = reinterpret_cast<float*>(smem + kTensors * bytes);
-        one = f;
+        iters = ty < threads_down && ty < rows_here ? (rows_here - ty + threads_down - 1) / threads_down : 0;
+        tensor_bytes = (size_t)a.iters * S::kRowBytes;
+        bars = reinterpret_cast<unsigned long long*>(smem + kTensors * tensor_bytes);
+        one = reinterpret_cast<float*>(bars + 2);
         two = one + width;
         slope = two + width;
         shift = slope + width;
         part = shift + width;
         group = part + (a.fold ? kThreads / 32 : threads_down) * width;
     }
-    // rows [k / 4, (k + 1) / 4) of the thread
-    __device__ __forceinline__ void quarter(int k, int& begin, int& end) const {
-        const int q = (a.iters + 3) >> 2;
-        begin = k * q;
-        end = min(begin + q, iters);
+    __device__ __forceinline__ void place(unsigned unit, int64_t& sample, int64_t& first) const {
+        const unsigned i = unit / (unsigned)a.norm.slabs;
+        sample = i;
+        first = (int64_t)(unit - i * a.norm.slabs) * width;
     }
-    // sums over the block's rows of every thread's eight values -> into[0 .. channels)
-    __device__ __forceinline__ void channel_sums(const f2 (&x)[4], float* into) const {
-        f2 v[4] = {x[0], x[1], x[2], x[3]};
+    __device__ __forceinline__ void enter(unsigned unit) {
+        place(unit, n, c0);
+        channels = (int)min((int64_t)width, a.norm.c - c0);
+        groups = channels / a.norm.group_size;
+        mine = iters > 0 && exists();
+    }
+    __device__ __forceinline__ bool exists() const { return piece * kCols < channels; }
+    __device__ __forceinline__ int64_t channel() const { return c0 + piece * kCols; }      // the thread's first one
+    // the thread's first slot of a tensor
+    __device__ __forceinline__ char* slots(int tensor) const { return smem + tensor * tensor_bytes + threadIdx.x * S::kSlot; }
+    // the thread's channels of its first row of this unit
+    template <typename P> __device__ __forceinline__ P* at(P* base, int64_t ld) const { return base + (n * a.norm.s + row0) * ld + channel(); }
+    // starts the copies of a unit's rows
+    __device__ __forceinline__ void fetch(unsigned unit) const {
+        int64_t sample, first;
+        place(unit, sample, first);
+        const NormArgs& q = a.norm;
+        if (piece * kCols < q.c - first)
+#pragma unroll
+            for (int t = 0; t < kTensors; ++t) {
+                const int64_t ld = t ? q.lddy : q.ldx, step = (int64_t)threads_down * ld;
+                const T* from = static_cast<const T*>(t ? q.dy : q.x) + (sample * q.s + row0) * ld + first + piece * kCols;
+                uint32_t to = (uint32_t)__cvta_generic_to_shared(slots(t));
+#pragma unroll 2
+                for (int i = 0; i < iters; ++i, from += step, to += S::kRowBytes) S::fetch(to, from);
+            }
+    }
+    // sums over the block's rows of every thread's values -> into[0 .. channels)
+    __device__ __forceinline__ void channel_sums(const f2 (&x)[kPairs], float* into) const {
+        f2 v[kPairs];
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) v[j] = x[j];
         bool writes = ty < threads_down;
         int at = ty;
         if (a.fold) {
             for (int o = a.norm.pieces; o < 32; o <<= 1)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = add2(v[j], f2{__shfl_xor_sync(0xFFFFFFFFu, v[j].v, o)});
+                for (int j = 0; j < kPairs; ++j) v[j] = add2(v[j], f2{__shfl_xor_sync(0xFFFFFFFFu, v[j].v, o)});
             writes = (threadIdx.x & 31) < (unsigned)a.norm.pieces;
             at = threadIdx.x >> 5;
         }
         if (writes) {
-            float w[8];
+            float w[kCols];
             unpairs(v, w);
-            float4* p = reinterpret_cast<float4*>(part + at * width + piece * 8);
-            p[0] = make_float4(w[0], w[1], w[2], w[3]);
-            p[1] = make_float4(w[4], w[5], w[6], w[7]);
+#pragma unroll
+            for (int j = 0; j < kCols; j += 4)
+                *reinterpret_cast<float4*>(part + at * width + piece * kCols + j) = make_float4(w[j], w[j + 1], w[j + 2], w[j + 3]);
         }
         __syncthreads();
         const int down = a.fold ? kThreads / 32 : threads_down;
@@ -597,120 +631,163 @@ struct Resident {
             put(g, warp_sum(s));
         }
     }
-    // this block's two values of a group to all blocks of the cluster, a lane for each
-    __device__ __forceinline__ void send(int g, float x, float y) const {
-        const int lane = threadIdx.x & 31;
-        if (lane >= a.cluster) return;
-        float* to = a.cluster > 1 ? cg::this_cluster().map_shared_rank(group, lane) : group;
-        *reinterpret_cast<float2*>(to + (rank * groups + g) * 2) = make_float2(x, y);
+    // Exchange of two values per group: each block stores its own into every block's shared memory, where the stores count
+    // towards an mbarrier that the block waits on -- unlike a barrier of the cluster this does not wait for the block's
+    // earlier stores to global memory.  Units alternate between two places: a block may send those of the next unit while
+    // another still reads these, but not those of the one after, since it has to have the other's of the next one first.
+    __device__ __forceinline__ float* place_of(int turn, int block, int g) const {
+        return group + ((turn * a.cluster + block) * (width / a.norm.group_size) + g) * 2;
     }
-    __device__ __forceinline__ float2 sent(int block, int g) const { return *reinterpret_cast<const float2*>(group + (block * groups + g) * 2); }
-    __device__ __forceinline__ void meet() const {
-        if (a.cluster > 1) cg::this_cluster().sync(); else __syncthreads();
+    __device__ __forceinline__ uint32_t bar(int turn) const { return (uint32_t)__cvta_generic_to_shared(bars + turn); }
+    // once: the barriers exist and every block of the cluster runs
+    __device__ __forceinline__ void open() const {
+        if (a.cluster == 1) return;
+        if (threadIdx.x == 0) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar(0)));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar(1)));
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        cg::this_cluster().sync();
+    }
+    __device__ __forceinline__ void expect(int turn) const {
+        if (a.cluster > 1 && threadIdx.x == 0)
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(turn)), "r"(a.cluster * groups * 8) : "memory");
+    }
+    // to the block `block` of the cluster
+    __device__ __forceinline__ void send(int turn, int block, int g, float x, float y) const {
+        float* to = place_of(turn, rank, g);
+        if (a.cluster == 1) {
+            *reinterpret_cast<float2*>(to) = make_float2(x, y);
+            return;
+        }
+        uint32_t there, counter;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(to)), "r"(block));
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(counter) : "r"(bar(turn)), "r"(block));
+        asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(there), "f"(x), "f"(y),
+                     "r"(counter) : "memory");
+    }
+    __device__ __forceinline__ float2 sent(int turn, int block, int g) const { return *reinterpret_cast<const float2*>(place_of(turn, block, g)); }
+    // waits for the values of all blocks; false (and MVUE_ERR_DEVICE_TIMEOUT in dev_status) when they do not come
+    __device__ __forceinline__ bool meet(int turn, uint32_t parity) const {
+        if (a.cluster == 1) {
+            __syncthreads();
+            return true;
+        }
+        for (uint32_t spin = 0; spin < (1u << 22); ++spin) {
+            uint32_t done;
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                         : "=r"(done) : "r"(bar(turn)), "r"(parity) : "memory");
+            if (done) return true;
+            if (spin > 64) __nanosleep(spin > 4096 ? 256 : 32);
+        }
+        if (a.norm.dev_status) *a.norm.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
+        return false;
+    }
+    // before the block ends: nobody stores into its shared memory any more
+    __device__ __forceinline__ void close() const {
+        if (a.cluster > 1) cg::this_cluster().sync();
     }
 };
 
+// Clusters take units in turn: cluster i the units i, i + clusters, ...
 template <typename T, int kAct>
-__global__ void __launch_bounds__(kThreads) norm_resident_kernel(const __grid_constant__ ResidentArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(const __grid_constant__ ResidentArgs a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) char smem[];
-    const Resident<T, 1> r(a, smem);
+    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
+    Resident<T, 1, kCols> r(a, smem);
     const NormArgs& q = a.norm;
-    using S = Slots<T>;
-    {
-        const int64_t step = (int64_t)r.threads_down * q.ldx;
-        const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row0) * q.ldx + r.c0 + r.piece * 8;
-        char* slot = r.slots[0];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            int i, end;
-            for (r.quarter(k, i, end); i < end; ++i, x += step, slot += S::kRowBytes) S::fetch(slot, x);
-            copies_end();
-        }
-    }
-    for (int k = threadIdx.x; k < r.channels; k += kThreads) {
-        r.slope[k] = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
-        r.shift[k] = affine(q.beta, q.affine_bf16, r.c0 + k, 0.0f);
-    }
-    if (a.cluster > 1) cg::this_cluster().sync();              // every block of the cluster runs: its memory may be written
-    f2 sum[4] = {};
-    const auto add = [&](int k) {
-        int i, end;
-        r.quarter(k, i, end);
-        const char* slot = r.slots[0] + i * S::kRowBytes;
+    using S = Slots<T, kCols>;
+    const unsigned clusters = gridDim.x / (unsigned)a.cluster;
+    unsigned unit = blockIdx.x / (unsigned)a.cluster;
+    const int lane = threadIdx.x & 31;
+    const float own = (float)r.rows_here * q.group_size, inv = own > 0.0f ? 1.0f / own : 0.0f;
+    const float all = (float)q.s * q.group_size;
+    const float lane_rows = lane < a.cluster ? (float)max(0, min(a.rows, (int)q.s - lane * a.rows)) : 0.0f;
+    r.fetch(unit);
+    r.open();
+    int turn = 0;
+    uint32_t parity = 0;
+    for (; unit < (unsigned)a.units; unit += clusters, parity ^= turn, turn ^= 1) {
+        r.enter(unit);
+        r.expect(turn);
+        copies_wait();
+        f2 sum[kPairs] = {};
+        const int iters = r.mine ? r.iters : 0;
+        const char* const first = r.slots(0);
+        const char* slot = first;
 #pragma unroll 4
-        for (; i < end; ++i, slot += S::kRowBytes) {
-            f2 v[4];
+        for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
+            f2 v[kPairs];
             S::read(slot, v);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] = add2(sum[j], v[j]);
+            for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
         }
-    };
-    copies_wait<3>(); add(0);
-    copies_wait<2>(); add(1);
-    copies_wait<1>(); add(2);
-    copies_wait<0>(); add(3);
-    r.channel_sums(sum, r.one);
-    const float own = (float)r.rows_here * q.group_size, inv = own > 0.0f ? 1.0f / own : 0.0f;
-    const int lane = threadIdx.x & 31;
-    r.group_sums(r.one, [&](int g, float s) {
-        __syncwarp();
-        for (int c = lane; c < q.group_size; c += 32) r.one[g * q.group_size + c] = -s * inv;     // the block's own mean, per channel
-    });
-    __syncthreads();
-    // squares about the block's own means, from shared memory
-    f2 neg_mean[4] = {};
-    if (r.iters) read8(r.one + r.piece * 8, neg_mean);
+        r.channel_sums(sum, r.one);
+        for (int k = threadIdx.x; k < r.channels; k += kThreads) {
+            r.slope[k] = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
+            r.shift[k] = affine(q.beta, q.affine_bf16, r.c0 + k, 0.0f);
+        }
+        r.group_sums(r.one, [&](int g, float s) {
+            __syncwarp();
+            for (int c = lane; c < q.group_size; c += 32) r.one[g * q.group_size + c] = -s * inv;     // the block's own mean, per channel
+        });
+        __syncthreads();
+        // squares about the block's own means, from shared memory
+        f2 neg_mean[kPairs];
+        read_values(r.one + r.piece * kCols, neg_mean);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum[j] = pair(0.0f);
-    const char* slot = r.slots[0];
+        for (int j = 0; j < kPairs; ++j) sum[j] = pair(0.0f);
+        slot = first;
 #pragma unroll 4
-    for (int i = 0; i < r.iters; ++i, slot += S::kRowBytes) {
-        f2 v[4];
-        S::read(slot, v);
+        for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
+            f2 v[kPairs];
+            S::read(slot, v);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const f2 d = add2(v[j], neg_mean[j]);
-            sum[j] = fma2(d, d, sum[j]);
+            for (int j = 0; j < kPairs; ++j) {
+                const f2 d = add2(v[j], neg_mean[j]);
+                sum[j] = fma2(d, d, sum[j]);
+            }
         }
-    }
-    r.channel_sums(sum, r.two);
-    r.group_sums(r.two, [&](int g, float s) { r.send(g, -r.one[g * q.group_size], s); });
-    r.meet();
-    for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
-        // a warp per group, a lane per block of the cluster
-        const float2 p = lane < a.cluster ? r.sent(lane, g) : make_float2(0.0f, 0.0f);
-        const float rows = lane < a.cluster ? (float)max(0, min(a.rows, (int)q.s - lane * a.rows)) : 0.0f;
-        const float mean = warp_sum(rows * p.x) / (float)q.s;
-        const float d = p.x - mean;
-        const float dev = warp_sum(fmaf(rows * q.group_size * d, d, p.y));
-        const float rstd = 1.0f / sqrtf(dev / ((float)q.s * q.group_size) + q.eps);
-        for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
-            r.one[c] = -mean;
-            r.slope[c] *= rstd;
+        r.channel_sums(sum, r.two);
+        r.group_sums(r.two, [&](int g, float s) { if (lane < a.cluster) r.send(turn, lane, g, -r.one[g * q.group_size], s); });
+        if (!r.meet(turn, parity)) break;
+        for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
+            // a warp per group, a lane per block of the cluster
+            const float2 p = lane < a.cluster ? r.sent(turn, lane, g) : make_float2(0.0f, 0.0f);
+            const float mean = warp_sum(lane_rows * p.x) / (float)q.s;
+            const float d = p.x - mean;
+            const float dev = warp_sum(fmaf(lane_rows * q.group_size * d, d, p.y));
+            const float rstd = 1.0f / sqrtf(dev / all + q.eps);
+            for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
+                r.one[c] = -mean;
+                r.slope[c] *= rstd;
+            }
+            if (r.rank == 0 && lane == 0) {
+                const int64_t at = r.n * q.groups + (int)r.c0 / q.group_size + g;
+                q.mean[at] = mean;
+                q.rstd[at] = rstd;
+            }
         }
-        if (r.rank == 0 && lane == 0) {
-            const int64_t at = r.n * q.groups + (int)r.c0 / q.group_size + g;
-            q.mean[at] = mean;
-            q.rstd[at] = rstd;
-        }
-    }
-    __syncthreads();
-    if (r.iters == 0) return;
-    Channels k8;
-    read8(r.one + r.piece * 8, k8.neg_mean);
-    read8(r.slope + r.piece * 8, k8.slope);
-    read8(r.shift + r.piece * 8, k8.shift);
-    T* y = static_cast<T*>(q.out) + (r.n * q.s + r.row0) * q.ldo + r.c0 + r.piece * 8;
-    const int64_t down = (int64_t)r.threads_down * q.ldo;
-    slot = r.slots[0];
+        __syncthreads();
+        Channels<kPairs> k8;
+        read_values(r.one + r.piece * kCols, k8.neg_mean);
+        read_values(r.slope + r.piece * kCols, k8.slope);
+        read_values(r.shift + r.piece * kCols, k8.shift);
+        T* y = r.at(static_cast<T*>(q.out), q.ldo);
+        const int64_t down = (int64_t)r.threads_down * q.ldo;
+        slot = first;
 #pragma unroll 2
-    for (int i = 0; i < r.iters; ++i, y += down, slot += S::kRowBytes) {
-        f2 v[4];
-        S::read(slot, v);
-        k8.output<kAct>(v);
-        store_row(y, v);
+        for (int i = 0; i < iters; ++i, y += down, slot += S::kRowBytes) {
+            f2 v[kPairs];
+            S::read(slot, v);
+            k8.output<kAct>(v);
+            S::store(y, v);
+        }
+        if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
     }
+    copies_wait();
+    r.close();
 }
 
 // Backward: x and dy resident; the block's sums per channel go to `partial` for the gradients of gamma and beta
@@ -719,103 +796,376 @@ template <typename T, int kAct>
 __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const __grid_constant__ ResidentArgs a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) char smem[];
-    const Resident<T, 2> r(a, smem);
+    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
+    Resident<T, 2, kCols> r(a, smem);
     const NormArgs& q = a.norm;
-    using S = Slots<T>;
-    {
-        const int64_t step = (int64_t)r.threads_down * q.ldx, dstep = (int64_t)r.threads_down * q.lddy;
-        const T* x = static_cast<const T*>(q.x) + (r.n * q.s + r.row0) * q.ldx + r.c0 + r.piece * 8;
-        const T* dy = static_cast<const T*>(q.dy) + (r.n * q.s + r.row0) * q.lddy + r.c0 + r.piece * 8;
-        char *slot = r.slots[0], *dslot = r.slots[1];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            int i, end;
-            for (r.quarter(k, i, end); i < end; ++i, x += step, dy += dstep, slot += S::kRowBytes, dslot += S::kRowBytes) {
-                S::fetch(slot, x);
-                S::fetch(dslot, dy);
-            }
-            copies_end();
+    using S = Slots<T, kCols>;
+    const unsigned clusters = gridDim.x / (unsigned)a.cluster;
+    unsigned unit = blockIdx.x / (unsigned)a.cluster;
+    const int lane = threadIdx.x & 31;
+    const float inv = 1.0f / ((float)q.s * q.group_size);
+    r.fetch(unit);
+    r.open();
+    int turn = 0;
+    uint32_t parity = 0;
+    for (; unit < (unsigned)a.units; unit += clusters, parity ^= turn, turn ^= 1) {
+        r.enter(unit);
+        r.expect(turn);
+        const int64_t g0 = r.n * q.groups + (int)r.c0 / q.group_size;
+        __syncthreads();             // the last unit's values per channel have been read
+        for (int k = threadIdx.x; k < r.channels; k += kThreads) {
+            const int64_t g = g0 + k / q.group_size;
+            r.one[k] = -q.mean[g];
+            r.slope[k] = q.rstd[g] * affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
+            r.shift[k] = affine(q.beta, q.affine_bf16, r.c0 + k, 0.0f);
         }
-    }
-    const int64_t g0 = r.n * q.groups + (int)r.c0 / q.group_size;
-    for (int k = threadIdx.x; k < r.channels; k += kThreads) {
-        const int64_t g = g0 + k / q.group_size;
-        r.one[k] = -q.mean[g];
-        r.slope[k] = q.rstd[g] * affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
-        r.shift[k] = affine(q.beta, q.affine_bf16, r.c0 + k, 0.0f);
-    }
-    r.meet();                        // also: every block of the cluster runs, its memory may be written
-    Channels k8 = {};
-    if (r.iters) {
-        read8(r.one + r.piece * 8, k8.neg_mean);
-        read8(r.slope + r.piece * 8, k8.slope);
-        read8(r.shift + r.piece * 8, k8.shift);
-    }
-    f2 sum[4] = {}, along[4] = {};
-    const auto add = [&](int k) {
-        int i, end;
-        r.quarter(k, i, end);
-        const char *slot = r.slots[0] + i * S::kRowBytes, *dslot = r.slots[1] + i * S::kRowBytes;
-        for (; i < end; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[4], d[4];
+        copies_wait();
+        __syncthreads();
+        Channels<kPairs> k8;
+        read_values(r.one + r.piece * kCols, k8.neg_mean);
+        read_values(r.slope + r.piece * kCols, k8.slope);
+        read_values(r.shift + r.piece * kCols, k8.shift);
+        f2 sum[kPairs] = {}, along[kPairs] = {};
+        const int iters = r.mine ? r.iters : 0;
+        const char *slot = r.slots(0), *dslot = r.slots(1);
+        for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
+            f2 v[kPairs], d[kPairs];
             S::read(slot, v);
             S::read(dslot, d);
             k8.gradient<kAct>(v, d);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < kPairs; ++j) {
                 sum[j] = add2(sum[j], d[j]);
                 along[j] = fma2(d[j], v[j], along[j]);
             }
         }
-    };
-    copies_wait<3>(); add(0);
-    copies_wait<2>(); add(1);
-    copies_wait<1>(); add(2);
-    copies_wait<0>(); add(3);
-    __syncthreads();                 // all have read r.one
-    r.channel_sums(sum, r.one);
-    r.channel_sums(along, r.two);
-    for (int k = threadIdx.x; k < r.channels; k += kThreads) {
-        const float rstd = q.rstd[g0 + k / q.group_size], gamma = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
-        const float2 s = make_float2(r.one[k], r.two[k] * rstd);
-        q.partial[(r.n * a.cluster + r.rank) * q.c + r.c0 + k] = s;
-        r.one[k] = gamma * s.x;
-        r.two[k] = gamma * s.y;
-    }
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    r.group_sums(r.one, [&](int g, float s) {
-        float t = 0.0f;
-        for (int c = lane; c < q.group_size; c += 32) t += r.two[g * q.group_size + c];
-        r.send(g, s, warp_sum(t));
-    });
-    r.meet();
-    const float inv = 1.0f / ((float)q.s * q.group_size);
-    for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
-        const float2 p = lane < a.cluster ? r.sent(lane, g) : make_float2(0.0f, 0.0f);
-        const float rstd = q.rstd[g0 + g];
-        const float level = -rstd * (warp_sum(p.x) * inv), tilt = -rstd * rstd * (warp_sum(p.y) * inv);
-        for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
-            r.one[c] = level;
-            r.two[c] = tilt;
+        __syncthreads();             // all have read r.one
+        r.channel_sums(sum, r.one);
+        r.channel_sums(along, r.two);
+        for (int k = threadIdx.x; k < r.channels; k += kThreads) {
+            const float rstd = q.rstd[g0 + k / q.group_size], gamma = affine(q.gamma, q.affine_bf16, r.c0 + k, 1.0f);
+            const float2 s = make_float2(r.one[k], r.two[k] * rstd);
+            q.partial[(r.n * a.cluster + r.rank) * q.c + r.c0 + k] = s;
+            r.one[k] = gamma * s.x;
+            r.two[k] = gamma * s.y;
         }
+        __syncthreads();
+        r.group_sums(r.one, [&](int g, float s) {
+            float t = 0.0f;
+            for (int c = lane; c < q.group_size; c += 32) t += r.two[g * q.group_size + c];
+            t = warp_sum(t);
+            if (lane < a.cluster) r.send(turn, lane, g, s, t);
+        });
+        if (!r.meet(turn, parity)) break;
+        for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
+            const float2 p = lane < a.cluster ? r.sent(turn, lane, g) : make_float2(0.0f, 0.0f);
+            const float rstd = q.rstd[g0 + g];
+            const float level = -rstd * (warp_sum(p.x) * inv), tilt = -rstd * rstd * (warp_sum(p.y) * inv);
+            for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
+                r.one[c] = level;
+                r.two[c] = tilt;
+            }
+        }
+        __syncthreads();
+        f2 level[kPairs], tilt[kPairs];            // dx = slope dz + level + tilt (x - mean)
+        read_values(r.one + r.piece * kCols, level);
+        read_values(r.two + r.piece * kCols, tilt);
+        T* dx = r.at(static_cast<T*>(q.out), q.ldo);
+        const int64_t down = (int64_t)r.threads_down * q.ldo;
+        slot = r.slots(0);
+        dslot = r.slots(1);
+        for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
+            f2 v[kPairs], d[kPairs];
+            S::read(slot, v);
+            S::read(dslot, d);
+            k8.gradient<kAct>(v, d);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt[j], level[j]));
+            S::store(dx, v);
+        }
+        if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
+    }
+    copies_wait();
+    r.close();
+}
+
+// The common case: a warp holds whole rows of the slab and every group is whole pieces of the threads' channels.  Then a thread's
+// channels are of one group, a sum over a group is a handful of shuffles and eight values in shared memory, and
+// every thread works the group's statistics out for itself: two barriers of the block a unit (one backward), no values per
+// channel in shared memory.  64 x 3136 x 256 bf16 in 32 groups: NOTE_FWD.
+template <typename T, int kTensors, int kCols>
+struct Folded : Resident<T, kTensors, kCols> {
+    using Base = Resident<T, kTensors, kCols>;
+    int per_group, g;                // pieces of a group; the thread's group in the unit
+    float* sums;                     // [2][8 warps][pieces][2]
+
+    __device__ __forceinline__ Folded(const ResidentArgs& args, char* shared) : Base(args, shared) {
+        per_group = args.norm.group_size / kCols;
+        g = this->piece / (unsigned)per_group;
+        sums = this->one;
+        this->group = sums + 2 * (kThreads / 32) * args.norm.pieces * 2;
+    }
+    // over the warp's lanes of this thread's group
+    __device__ __forceinline__ float fold(float x) const {
+        for (int o = 1; o < per_group; o <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+        for (int o = this->a.norm.pieces; o < 32; o <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+        return x;
+    }
+    // over the block's threads of this thread's group; `half`: calls in turn use different halves, one barrier each
+    __device__ __forceinline__ float2 block_sum(float x, float y, int half) const {
+        const int pieces = this->a.norm.pieces;
+        float2* s = reinterpret_cast<float2*>(sums) + half * (kThreads / 32) * pieces;
+        x = fold(x);
+        y = fold(y);
+        if ((threadIdx.x & 31) < (unsigned)pieces) s[(threadIdx.x >> 5) * pieces + this->piece] = make_float2(x, y);
+        __syncthreads();
+        float2 t = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            const float2 v = s[w * pieces + this->piece];
+            t.x += v.x;
+            t.y += v.y;
+        }
+        return t;
+    }
+    __device__ __forceinline__ float block_sum(float x, int half) const {
+        const int pieces = this->a.norm.pieces;
+        float* s = sums + half * (kThreads / 32) * pieces * 2;
+        x = fold(x);
+        if ((threadIdx.x & 31) < (unsigned)pieces) s[(threadIdx.x >> 5) * pieces + this->piece] = x;
+        __syncthreads();
+        float t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) t += s[w * pieces + this->piece];
+        return t;
+    }
+    // one thread for each group of the unit and block of the cluster
+    __device__ __forceinline__ bool sends() const {
+        return this->ty < this->a.cluster && this->piece == g * per_group && this->exists();
+    }
+};
+
+template <int kPairs>
+__device__ __forceinline__ float total(const f2 (&x)[kPairs]) {
+    f2 s = x[0];
+#pragma unroll
+    for (int j = 1; j < kPairs; ++j) s = add2(s, x[j]);
+    float a, b;
+    unpair(s, a, b);
+    return a + b;
+}
+// a thread's values of gamma or beta from channel c on
+template <int kPairs>
+__device__ __forceinline__ void affine_values(const void* p, int is_bf16, int64_t c, float none, f2 (&x)[kPairs]) {
+    float v[2 * kPairs];
+#pragma unroll
+    for (int j = 0; j < 2 * kPairs; ++j) v[j] = affine(p, is_bf16, c + j, none);
+    pairs(v, x);
+}
+
+template <typename T, int kAct>
+__global__ void __launch_bounds__(kThreads, 4) norm_folded_kernel(const __grid_constant__ ResidentArgs a) {
+    grid_dependency_wait();
+    extern __shared__ __align__(16) char smem[];
+    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
+    Folded<T, 1, kCols> r(a, smem);
+    const NormArgs& q = a.norm;
+    using S = Slots<T, kCols>;
+    const unsigned clusters = gridDim.x / (unsigned)a.cluster;
+    unsigned unit = blockIdx.x / (unsigned)a.cluster;
+    const float own = (float)r.rows_here * q.group_size, inv = own > 0.0f ? 1.0f / own : 0.0f;
+    const float all = (float)q.s * q.group_size;
+    r.fetch(unit);
+    r.open();
+    int turn = 0;
+    uint32_t parity = 0;
+    for (; unit < (unsigned)a.units; unit += clusters, parity ^= turn, turn ^= 1) {
+        r.enter(unit);
+        r.expect(turn);
+        Channels<kPairs> k8;
+        if (r.exists()) {
+            affine_values(q.gamma, q.affine_bf16, r.channel(), 1.0f, k8.slope);
+            affine_values(q.beta, q.affine_bf16, r.channel(), 0.0f, k8.shift);
+        }
+        copies_wait();
+        f2 sum[kPairs] = {};
+        const int iters = r.mine ? r.iters : 0;
+        const char* const first = r.slots(0);
+        const char* slot = first;
+#pragma unroll 4
+        for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
+            f2 v[kPairs];
+            S::read(slot, v);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+        }
+        const float block_mean = r.block_sum(total(sum), 0) * inv;
+        // squares about the block's own mean, from shared memory
+        const f2 low = pair(-block_mean);
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) sum[j] = pair(0.0f);
+        slot = first;
+#pragma unroll 4
+        for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
+            f2 v[kPairs];
+            S::read(slot, v);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                const f2 d = add2(v[j], low);
+                sum[j] = fma2(d, d, sum[j]);
+            }
+        }
+        const float block_dev = r.block_sum(total(sum), 1);
+        if (r.sends()) r.send(turn, r.ty, r.g, block_mean, block_dev);
+        if (!r.meet(turn, parity)) break;
+        float mean = 0.0f, dev = 0.0f;
+        int left = (int)q.s;
+        for (int b = 0; b < a.cluster; ++b, left -= a.rows) mean = fmaf((float)max(0, min(a.rows, left)), r.sent(turn, b, r.g).x, mean);
+        mean /= (float)q.s;
+        left = (int)q.s;
+        for (int b = 0; b < a.cluster; ++b, left -= a.rows) {
+            const float2 p = r.sent(turn, b, r.g);
+            const float d = p.x - mean;
+            dev += fmaf((float)max(0, min(a.rows, left)) * q.group_size * d, d, p.y);
+        }
+        const float rstd = 1.0f / sqrtf(dev / all + q.eps);
+        if (r.rank == 0 && r.ty == 0 && r.sends()) {
+            const int64_t at = r.n * q.groups + (int)r.c0 / q.group_size + r.g;
+            q.mean[at] = mean;
+            q.rstd[at] = rstd;
+        }
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            k8.neg_mean[j] = pair(-mean);
+            k8.slope[j] = mul2(k8.slope[j], pair(rstd));
+        }
+        T* y = r.at(static_cast<T*>(q.out), q.ldo);
+        const int64_t down = (int64_t)r.threads_down * q.ldo;
+        slot = first;
+#pragma unroll 2
+        for (int i = 0; i < iters; ++i, y += down, slot += S::kRowBytes) {
+            f2 v[kPairs];
+            S::read(slot, v);
+            k8.output<kAct>(v);
+            S::store(y, v);
+        }
+        if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
+    }
+    copies_wait();
+    r.close();
+}
+
+// Backward.  The grid's clusters are a multiple of the slabs (or there is one for each unit), so a cluster stays with its
+// channels and the sums for the gradients of gamma and beta stay in registers until its last sample.
+template <typename T, int kAct>
+__global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __grid_constant__ ResidentArgs a) {
+    grid_dependency_wait();
+    extern __shared__ __align__(16) char smem[];
+    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
+    Folded<T, 2, kCols> r(a, smem);
+    const NormArgs& q = a.norm;
+    using S = Slots<T, kCols>;
+    const unsigned clusters = gridDim.x / (unsigned)a.cluster;
+    const unsigned mine = blockIdx.x / (unsigned)a.cluster;
+    unsigned unit = mine;
+    const float inv = 1.0f / ((float)q.s * q.group_size);
+    r.fetch(unit);
+    r.enter(unit);
+    const bool has = r.exists();
+    f2 gamma[kPairs] = {}, all_sum[kPairs] = {}, all_along[kPairs] = {};
+    Channels<kPairs> k8 = {};
+    if (has) {
+        affine_values(q.gamma, q.affine_bf16, r.channel(), 1.0f, gamma);
+        affine_values(q.beta, q.affine_bf16, r.channel(), 0.0f, k8.shift);
+    }
+    r.open();
+    int turn = 0;
+    uint32_t parity = 0;
+    bool met = true;
+    for (; unit < (unsigned)a.units; unit += clusters, parity ^= turn, turn ^= 1) {
+        r.enter(unit);
+        r.expect(turn);
+        const int64_t g = r.n * q.groups + (int)r.c0 / q.group_size + r.g;
+        const float mean = has ? q.mean[g] : 0.0f, rstd = has ? q.rstd[g] : 0.0f;
+        copies_wait();
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            k8.neg_mean[j] = pair(-mean);
+            k8.slope[j] = mul2(gamma[j], pair(rstd));
+        }
+        f2 sum[kPairs] = {}, along[kPairs] = {};
+        const int iters = r.mine ? r.iters : 0;
+        const char *slot = r.slots(0), *dslot = r.slots(1);
+        for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
+            f2 v[kPairs], d[kPairs];
+            S::read(slot, v);
+            S::read(dslot, d);
+            k8.gradient<kAct>(v, d);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                sum[j] = add2(sum[j], d[j]);
+                along[j] = fma2(d[j], v[j], along[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            all_sum[j] = add2(all_sum[j], sum[j]);
+            all_along[j] = fma2(along[j], pair(rstd), all_along[j]);
+            sum[j] = mul2(sum[j], gamma[j]);
+            along[j] = mul2(along[j], gamma[j]);
+        }
+        const float2 block = r.block_sum(total(sum), total(along), turn);
+        if (r.sends()) r.send(turn, r.ty, r.g, block.x, block.y);
+        met = r.meet(turn, parity);
+        if (!met) break;
+        float sa = 0.0f, sb = 0.0f;
+        for (int b = 0; b < a.cluster; ++b) {
+            const float2 p = r.sent(turn, b, r.g);
+            sa += p.x;
+            sb += p.y;
+        }
+        const f2 level = pair(-rstd * (sa * inv)), tilt = pair(-rstd * rstd * (rstd * sb * inv));    // dx = slope dz + level + tilt (x - mean)
+        T* dx = r.at(static_cast<T*>(q.out), q.ldo);
+        const int64_t down = (int64_t)r.threads_down * q.ldo;
+        slot = r.slots(0);
+        dslot = r.slots(1);
+        for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
+            f2 v[kPairs], d[kPairs];
+            S::read(slot, v);
+            S::read(dslot, d);
+            k8.gradient<kAct>(v, d);
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt, level));
+            S::store(dx, v);
+        }
+        if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
+    }
+    copies_wait();
+    r.close();
+    // the cluster's channels, summed over its samples: the warps' sums through the buffers, which are free now
+    __syncthreads();
+    float sum[kCols], along[kCols];
+    unpairs(all_sum, sum);
+    unpairs(all_along, along);
+    float* scratch = reinterpret_cast<float*>(smem);
+    const int pieces = q.pieces, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) {
+        for (int o = pieces; o < 32; o <<= 1) {
+            sum[j] += __shfl_xor_sync(0xFFFFFFFFu, sum[j], o);
+            along[j] += __shfl_xor_sync(0xFFFFFFFFu, along[j], o);
+        }
+        if (lane < pieces) *reinterpret_cast<float2*>(scratch + (((threadIdx.x >> 5) * pieces + lane) * kCols + j) * 2) = make_float2(sum[j], along[j]);
     }
     __syncthreads();
-    if (r.iters == 0) return;
-    f2 level[4], tilt[4];            // dx = slope dz + level + tilt (x - mean)
-    read8(r.one + r.piece * 8, level);
-    read8(r.two + r.piece * 8, tilt);
-    T* dx = static_cast<T*>(q.out) + (r.n * q.s + r.row0) * q.ldo + r.c0 + r.piece * 8;
-    const int64_t down = (int64_t)r.threads_down * q.ldo;
-    const char *slot = r.slots[0], *dslot = r.slots[1];
-    for (int i = 0; i < r.iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
-        f2 v[4], d[4];
-        S::read(slot, v);
-        S::read(dslot, d);
-        k8.gradient<kAct>(v, d);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt[j], level[j]));
-        store_row(dx, v);
+    for (int k = threadIdx.x; k < r.channels; k += kThreads) {
+        float2 t = make_float2(0.0f, 0.0f);
+        for (int w = 0; w < kThreads / 32; ++w) {
+            const float2 v = *reinterpret_cast<const float2*>(scratch + (w * pieces * kCols + k) * 2);
+            t.x += v.x;
+            t.y += v.y;
+        }
+        q.partial[((int64_t)(mine / (unsigned)q.slabs) * a.cluster + r.rank) * q.c + r.c0 + k] = t;
     }
 }
 
@@ -844,29 +1194,38 @@ Split split_of(int64_t n, int64_t s, int64_t c) {
 }
 
 constexpr int kMaxCluster = 8;
-constexpr size_t kBlockBytes[4] = {56 << 10, 75 << 10, 113 << 10, 226 << 10};     // shared memory of four, three, two and one blocks on an SM
+// shared memory of a block when four, two and one are on an SM
+constexpr size_t kShare[3] = {56 << 10, 113 << 10, 226 << 10};
 
 struct Keep {
     int pieces = 0, slabs, cluster, rows, iters, fold;      // pieces = 0: the slab of one sample does not fit a cluster
+    bool folded;                     // the folded kernels: whole rows in a warp, groups of whole pieces
     size_t smem;
 };
-// A slab is the fewest whole groups that are whole pieces of eight channels and 128 bytes of a row (or all channels); small
-// maps take more, as long as two blocks are left for every SM.  Then the fewest blocks that hold a slab in the
-// smallest of the four shares of shared memory that does, and more where the grid would leave SMs idle.
+// A slab is the fewest whole groups that are 64 bytes of a row (two sectors; 128 bytes need twice the blocks to a cluster
+// for the same share of shared memory and were no faster) and a multiple of eight channels; small maps take more, as long as two blocks are left for
+// every SM.  Then the fewest blocks that hold a slab in the smallest share of shared memory that does (four blocks
+// on an SM need 64 registers a thread: the folded forward kernel), and more where the grid would leave SMs idle.
 Keep keep_of(int64_t n, int64_t s, int64_t c, int groups, int64_t esz, int tensors) {
     Keep k;
     const int64_t cg = c / groups, least = std::lcm(cg, (int64_t)8);
     if (c % 8 != 0 || least > kThreads * 8) return k;
-    int64_t width = std::min(c, (128 / esz + least - 1) / least * least);
-    while (width * 2 <= std::min<int64_t>(c, kThreads * 8) && s * width * esz < (8 << 10) && n * ((c + 2 * width - 1) / (2 * width)) >= 2 * 148)
-        width *= 2;
-    const int pieces = (int)(width / 8), down = kThreads / pieces;
+    const int64_t row = 64 / esz;
+    int64_t width = std::min(c, (row + least - 1) / least * least);
+    const auto spare = [&](int64_t w) { return s * w * esz < (8 << 10) && n * ((c + 2 * w - 1) / (2 * w)) >= 2 * 148; };
+    while (width * 2 <= std::min<int64_t>(c, kThreads * 4) && spare(width)) width *= 2;
+    constexpr int cols = kResidentCols;
+    const int pieces = (int)(width / cols), down = kThreads / pieces;
     const int64_t slabs = (c + width - 1) / width, most = width / cg;
+    if (n * slabs > 0x7FFFFFFF / kMaxCluster) return k;
     k.fold = pieces <= 16 && (pieces & (pieces - 1)) == 0;
-    const auto try_cluster = [&](int cluster, size_t limit) {
+    k.folded = k.fold && cg % cols == 0;
+    const auto fits = [&](int cluster, size_t limit) {
         const int64_t rows = (s + cluster - 1) / cluster, iters = (rows + down - 1) / down;
         if (iters > (1 << 16)) return false;
-        const size_t smem = (size_t)tensors * iters * esz * 8 * kThreads + 4 * ((4 + (k.fold ? kThreads / 32 : down)) * width + 2 * most * cluster);
+        const int64_t sums = k.folded ? 4 * (kThreads / 32) * pieces : (4 + (k.fold ? kThreads / 32 : down)) * width;
+        const size_t smem = std::max<size_t>((size_t)tensors * iters * esz * cols * kThreads, k.folded && tensors == 2 ? 64 * width : 0) + 16 +
+                            4 * (sums + 4 * most * cluster);
         if (smem > limit) return false;
         k.rows = (int)rows;
         k.iters = (int)iters;
@@ -875,35 +1234,63 @@ Keep keep_of(int64_t n, int64_t s, int64_t c, int groups, int64_t esz, int tenso
         return true;
     };
     bool found = false;
-    for (int level = 0; level < 4 && !found; ++level)
-        for (int cluster = 1; cluster <= kMaxCluster && !found; cluster *= 2) found = try_cluster(cluster, kBlockBytes[level]);
+    for (int share = k.folded && tensors == 1 ? 0 : 1; share < 3 && !found; ++share)
+        for (int cluster = 1; cluster <= kMaxCluster && !found; cluster *= 2) found = fits(cluster, kShare[share]);
     if (!found) return k;
     while (k.cluster < kMaxCluster && n * slabs * k.cluster * 2 <= 2 * 148 && s >= (int64_t)k.cluster * 2 * down)
-        if (!try_cluster(k.cluster * 2, kBlockBytes[3])) break;
-    if (n * slabs > 0x7FFFFFFF / kMaxCluster) return k;
+        if (!fits(k.cluster * 2, kShare[2])) break;
     k.pieces = pieces;
     k.slabs = (int)slabs;
     return k;
 }
 
+// What a launch needs to know of the device: how many clusters of a size and an amount of shared memory are resident at once.
+struct ClusterFacts {
+    std::mutex mu;
+    struct { int dev, cluster, count; size_t smem; } known[16];
+    int filled = 0, next = 0;
+};
 template <typename K>
-cudaError_t launch_resident(K kernel, PerDeviceOnce& once, const ResidentArgs& a, const Keep& k, cudaStream_t st) {
+cudaError_t launch_resident(K kernel, PerDeviceOnce& once, ClusterFacts& facts, const ResidentArgs& a, const Keep& k, int multiple,
+                            int* launched, cudaStream_t st) {
     cudaError_t e = once_per_device(once, [&](int) {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockBytes[3]);
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kShare[2]);
     });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.norm.n * k.slabs * k.cluster));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = k.smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)k.cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)k.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = a.units;
+    if ((int64_t)a.units * k.cluster > 148) {
+        int dev = 0;
+        e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        std::lock_guard<std::mutex> lock(facts.mu);
+        int count = 0;
+        for (int i = 0; i < facts.filled; ++i)
+            if (facts.known[i].dev == dev && facts.known[i].cluster == k.cluster && facts.known[i].smem == k.smem) count = facts.known[i].count;
+        if (count == 0) {
+            cfg.gridDim = dim3((unsigned)k.cluster);
+            e = cudaOccupancyMaxActiveClusters(&count, kernel, &cfg);
+            if (e != cudaSuccess) return e;
+            facts.known[facts.next] = {dev, k.cluster, count, k.smem};
+            facts.next = (facts.next + 1) % 16;
+            facts.filled = std::min(16, facts.filled + 1);
+        }
+        // each cluster with one slab of the channels where that is asked for
+        if (count < clusters) clusters = std::max(multiple, count / multiple * multiple);
+    }
+    *launched = clusters;
+    cfg.gridDim = dim3((unsigned)(clusters * k.cluster));
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
@@ -945,13 +1332,22 @@ cudaError_t either(const NormArgs& a, dim3 grid, cudaStream_t st) {
     if constexpr (kWide) {
         const Keep k = keep_of(a.n, a.s, a.c, a.groups, sizeof(T), a.dy ? 2 : 1);
         if (k.pieces) {
-            ResidentArgs r{a, k.cluster, k.rows, k.iters, k.fold};
+            ResidentArgs r{a, k.cluster, k.rows, k.iters, k.fold, (int)(a.n * k.slabs)};
             r.norm.pieces = k.pieces;
             r.norm.slabs = k.slabs;
             r.norm.chunks = k.cluster;
-            static PerDeviceOnce once[2];
-            if (!a.dy) return launch_resident(&norm_resident_kernel<T, kAct>, once[0], r, k, st);
-            cudaError_t e = launch_resident(&norm_resident_grad_kernel<T, kAct>, once[1], r, k, st);
+            static PerDeviceOnce once[4];
+            static ClusterFacts facts[4];
+            const bool folded = k.folded;
+            int clusters = 0;
+            if (!a.dy)
+                return folded ? launch_resident(&norm_folded_kernel<T, kAct>, once[0], facts[0], r, k, 1, &clusters, st)
+                              : launch_resident(&norm_resident_kernel<T, kAct>, once[1], facts[1], r, k, 1, &clusters, st);
+            cudaError_t e = folded ? launch_resident(&norm_folded_grad_kernel<T, kAct>, once[2], facts[2], r, k, k.slabs, &clusters, st)
+                                   : launch_resident(&norm_resident_grad_kernel<T, kAct>, once[3], facts[3], r, k, 1, &clusters, st);
+            if (folded) {            // a row of sums per cluster and block, not per sample and block
+                r.norm.n = clusters / k.slabs;
+            }
             if (e == cudaSuccess && (a.dgamma || a.dbeta))
                 e = launch_dependent(&norm_grad_join_kernel, dim3((unsigned)((a.c + 31) / 32)), dim3(kThreads), 0, st, r.norm, (int64_t)0);
             return e;
@@ -1021,18 +1417,18 @@ int mvue_group_norm_workspace_bytes(int64_t n, int64_t s, int64_t c, int groups,
 
 int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t c, int64_t ldx, int groups, const void* gamma,
                         const void* beta, int affine_dtype, float eps, int act, void* y, int64_t ldy, float* mean, float* rstd,
-                        void* workspace, size_t workspace_bytes, void* stream) {
+                        void* workspace, size_t workspace_bytes, int* dev_status, void* stream) {
     if (int e = check(dtype, n, s, c, groups, affine_dtype, gamma, beta, act)) return e;
     if (ldx < c || ldy < c) return MVUE_ERR_SHAPE;
     if (n == 0) return MVUE_OK;
     if (!x || !y) return MVUE_ERR_NULL;
     const int64_t esz = size_of(dtype), asz = size_of(affine_dtype);
-    if (off(x, esz) || off(y, esz) || off(gamma, asz) || off(beta, asz) || off(mean, 4) || off(rstd, 4)) return MVUE_ERR_ALIGN;
+    if (off(x, esz) || off(y, esz) || off(gamma, asz) || off(beta, asz) || off(mean, 4) || off(rstd, 4) || off(dev_status, 4)) return MVUE_ERR_ALIGN;
     NormArgs a = {};
     a.x = x; a.out = y; a.n = n; a.s = s; a.c = c; a.ldx = ldx; a.ldo = ldy;
     a.groups = groups; a.group_size = (int)(c / groups);
     a.gamma = gamma; a.beta = beta; a.affine_bf16 = affine_dtype == MVUE_BF16;
-    a.eps = eps; a.mean = mean; a.rstd = rstd;
+    a.eps = eps; a.mean = mean; a.rstd = rstd; a.dev_status = dev_status;
     return run(a, dtype, act, wide_rows(x, ldx, c, dtype) && wide_rows(y, ldy, c, dtype), workspace, workspace_bytes, stream,
                "mvue_group_norm_act launch");
 }
@@ -1040,13 +1436,13 @@ int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t 
 int mvue_group_norm_act_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int dtype, int64_t n, int64_t s, int64_t c,
                                  int groups, const float* mean, const float* rstd, const void* gamma, const void* beta, int affine_dtype,
                                  int act, void* dx, int64_t lddx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
-                                 void* stream) {
+                                 int* dev_status, void* stream) {
     if (int e = check(dtype, n, s, c, groups, affine_dtype, gamma, beta, act)) return e;
     if (ldx < c || lddy < c || lddx < c) return MVUE_ERR_SHAPE;
     if (n > 0 && (!x || !dy || !dx || !mean || !rstd)) return MVUE_ERR_NULL;
     const int64_t esz = size_of(dtype), asz = size_of(affine_dtype);
     if (off(x, esz) || off(dy, esz) || off(dx, esz) || off(gamma, asz) || off(beta, asz) || off(mean, 4) || off(rstd, 4) || off(dgamma, 4) ||
-        off(dbeta, 4))
+        off(dbeta, 4) || off(dev_status, 4))
         return MVUE_ERR_ALIGN;
     if (n == 0) {
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -1060,7 +1456,7 @@ int mvue_group_norm_act_backward(const void* dy, int64_t lddy, const void* x, in
     a.groups = groups; a.group_size = (int)(c / groups);
     a.gamma = gamma; a.beta = beta; a.affine_bf16 = affine_dtype == MVUE_BF16;
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);      // only read here
-    a.dgamma = dgamma; a.dbeta = dbeta;
+    a.dgamma = dgamma; a.dbeta = dbeta; a.dev_status = dev_status;
     return run(a, dtype, act, wide_rows(x, ldx, c, dtype) && wide_rows(dy, lddy, c, dtype) && wide_rows(dx, lddx, c, dtype), workspace,
                workspace_bytes, stream, "mvue_group_norm_act_backward launch");
 }

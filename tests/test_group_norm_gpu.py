@@ -166,7 +166,7 @@ def test_refusals_before_any_launch():
     p = ctypes.c_void_p
 
     def fwd(x=4096, dtype=1, n=2, s=4, c=16, ldx=16, groups=4, w=8192, aff=0, act=1, y=16384, ldy=16, ws=32768, nws=1 << 20):
-        return L.mvue_group_norm_act(p(x), dtype, n, s, c, ldx, groups, p(w), p(w), aff, 1e-5, act, p(y), ldy, None, None, p(ws), nws, None)
+        return L.mvue_group_norm_act(p(x), dtype, n, s, c, ldx, groups, p(w), p(w), aff, 1e-5, act, p(y), ldy, None, None, p(ws), nws, None, None)
 
     assert fwd(x=None) == -1 and fwd(y=None) == -1
     assert fwd(n=-1) == -3 and fwd(s=0) == -3 and fwd(c=0) == -3 and fwd(groups=5) == -3 and fwd(groups=0) == -3
@@ -178,7 +178,7 @@ def test_refusals_before_any_launch():
 
     def bwd(dy=4096, lddy=16, x=8192, mean=1 << 14, dx=1 << 15, ld=16, act=2, dg=1 << 16, ws=1 << 17, nws=1 << 20):
         return L.mvue_group_norm_act_backward(p(dy), lddy, p(x), 16, 1, 2, 4, 16, 4, p(mean), p(mean), None, None, 0, act, p(dx), ld, p(dg), p(dg),
-                                              p(ws), nws, None)
+                                              p(ws), nws, None, None)
 
     assert bwd(dy=None) == -1 and bwd(x=None) == -1 and bwd(mean=None) == -1 and bwd(dx=None) == -1
     assert bwd(lddy=8) == -3 and bwd(ld=8) == -3 and bwd(act=9) == -14 and bwd(dg=65538) == -4 and bwd(ws=None) == -7
