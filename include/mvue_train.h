@@ -49,12 +49,13 @@ typedef struct {
     int32_t grad_dtype;
 } mvue_adamw_tensor;
 
-/* The step (step = t >= 1), in binary32, each operation rounded on its own; constants are formed in double on the host:
+/* The step (step = t >= 1), in binary32; constants are formed in double on the host:
  *   g' = g * grad_scale (* *dev_grad_scale)
  *   m' = beta1 m + (1 - beta1) g'
  *   v' = beta2 v + ((1 - beta2) g') g'
  *   param' = param (1 - lr weight_decay) - (lr / (1 - beta1^t)) * (m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
- * (the square root of the 32-bit states' update and the quotient are within 2 units in the last place).
+ * m' and v' with each operation rounded on its own; the param's root and quotient within 2 units in the last place, its
+ * product by the decay fused with the sum.
  * grad_scale: HOST value, 1 for none; dev_grad_scale: optional DEVICE float (a clipping factor or a loss scale's
  * inverse that the host does not know), read when the step runs.
  * state_bits: 32 or 8.  With 8 bits the new m and sqrt(v) of a block are divided by the block's new scale

@@ -7,6 +7,7 @@
 // the block's largest magnitude is one warp-wide integer maximum (the bit patterns of non-negative floats are in
 // their order, and a NaN is above all of them), and the lane's eight 16-bit random numbers are one generator call.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -37,7 +38,7 @@ struct Tensor {
 };
 
 struct Constants {
-    float beta1, one_beta1, beta2, one_beta2, inv_root, eps, decay, step_size, grad_scale;
+    float beta1, one_beta1, beta2, one_beta2, inv_root, eps, decay, step_size, grad_scale, minus_zero;
     const float* dev_grad_scale;
     bool round_up_at_random;   // a bf16 param without master
 };
@@ -53,44 +54,115 @@ struct Params {
     Tensor tensor[kCapacity];
 };
 
-// e4m3 magnitude of a code byte: shifted into the place of a binary32's exponent and mantissa it is 2^-120 times its
-// value, the codes below 8 (no leading one) included.
-__device__ __forceinline__ float e4m3_value(uint32_t byte) {
-    const float mag = __fmul_rn(__uint_as_float((byte & 0x7Fu) << 20), 1.329227995784916e36f);   // 2^120
-    return __uint_as_float(__float_as_uint(mag) | (byte & 0x80u) << 24);
+// Two e4m3 codes (the half-word's low byte first) as binary32; exact by way of binary16.
+__device__ __forceinline__ f2 e4m3_values(uint32_t half) {
+    uint32_t h;
+    asm("{\n\t.reg .b16 c;\n\tcvt.u16.u32 c, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, c;\n\t}" : "=r"(h) : "r"(half));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    return pair(f.x, f.y);
 }
 
-// Code of a magnitude y <= 448: steps of 2^-3 of its power of two (2^-9 below 2^-6), rounded up where the fraction plus
-// the random number `unit` in [0, 1) passes one.  The product by a power of two is exact; adding 2^23 rounded down leaves
-// the whole steps in the low bits.
-__device__ __forceinline__ uint32_t e4m3_code(float y, float unit) {
+// Code of a magnitude y <= 448 (a few units in its last place above are no matter), any y: steps of 2^-3 of its power of
+// two (2^-9 below 2^-6), rounded up where the fraction plus the random number r 2^-16 reaches one.  The product by a power
+// of two is exact; adding 2^23 rounded down leaves the whole steps in the low bits.
+__device__ __noinline__ uint32_t e4m3_code(float y, uint32_t r) {
     const uint32_t e = max(__float_as_uint(y) & 0x7F800000u, 121u << 23);
-    const float steps = __fmaf_rn(y, __uint_as_float((257u << 23) - e), unit);
+    const float steps = __fmaf_rn(y, __uint_as_float((257u << 23) - e), (float)r * 1.52587890625e-05f);
     return (e >> 20) - (121u << 3) + (__float_as_uint(__fadd_rd(steps, 8388608.0f)) - 0x4B000000u);
+}
+// The same for four numbers y with magnitudes of at least 2^-6, signs apart, without a step for the power of two: adding
+// r to the 16 bits below the three mantissa bits of a binary32 carries into them exactly that often, and the code is the
+// low five exponent bits and the three mantissa bits less a constant.  r8: r << 8, which is r's place four bits further up,
+// where the code fills the highest byte; the sign is shifted out.
+__device__ __forceinline__ uint32_t e4m3_codes_normal(const float* y, const uint32_t* r8) {
+    uint32_t t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = __float_as_uint(y[i]) * 16u + r8[i];
+    const uint32_t bytes = __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);
+    return (bytes ^ 0x40404040u) & 0x7F7F7F7Fu;              // less 120 << 3: the top two bits are 11 or 00, to become 00 or 01
 }
 
 __device__ __forceinline__ float fast_root(float x) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// the larger magnitude, NaN if there is one
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// the warp's largest magnitude (NaN above all: the bit patterns of non-negative floats are in their order)
+__device__ __forceinline__ float warp_largest(float x) {
+    return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x) & 0x7FFFFFFFu));
+}
 
-struct Lane {
-    float g[8], m[8], v[8], p[8];     // v: the second moment, after the update of the 8-bit states its root
-};
-
-// new scale and the factor to codes of a block whose largest magnitude has the bits `top`
-__device__ __forceinline__ float block_scale(uint32_t top, float* factor) {
-    const float t = __uint_as_float(top);
-    const bool finite = top < 0x7F800000u, large = t >= 7.703719777548943e-34f;     // 2^-110
-    *factor = finite && large ? __fmul_rn(448.0f, __frcp_rn(t)) : 0.0f;
-    return finite ? (large ? __fmul_rn(t, 1.0f / 448.0f) : 0.0f) : __uint_as_float(0x7FFFFFFFu);
+// new scale and the factor to codes of a block whose largest magnitude is `top`
+__device__ __forceinline__ float block_scale(float top, float* factor) {
+    const bool finite = __float_as_uint(top) < 0x7F800000u, large = top >= 7.703719777548943e-34f;     // 2^-110
+    *factor = finite && large ? __fmul_rn(448.0f, __frcp_rn(top)) : 0.0f;
+    return finite ? (large ? __fmul_rn(top, 1.0f / 448.0f) : 0.0f) : __uint_as_float(0x7FFFFFFFu);
 }
 
 // A NaN whose lower half is zero: random bits added to it do not carry into the sign.
 __device__ __forceinline__ float short_nan(float x) { return x != x ? __uint_as_float(0x7FC00000u) : x; }
 
-template <int kBits, int kCapacity>
+// The new moments of eight elements (v: the second moment, root: its square root) and the new param.
+struct Step {
+    f2 m[4], v[4], root[4], p[4];
+    __device__ __forceinline__ void take(const Constants& c, const f2 (&g)[4], float gs) {
+        const f2 scale = pair(gs), b1 = pair(c.beta1), c1 = pair(c.one_beta1), b2 = pair(c.beta2), c2 = pair(c.one_beta2);
+        const f2 inv_root = pair(c.inv_root), eps = pair(c.eps), decay = pair(c.decay), size = pair(-c.step_size);
+        // a product that the compiler cannot fuse with the sum behind it: it does not know that this is -0
+        const f2 nothing = pair(c.minus_zero);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f2 x = mul2(g[j], scale);
+            m[j] = add2(fma2(b1, m[j], nothing), fma2(c1, x, nothing));
+            v[j] = add2(fma2(b2, v[j], nothing), fma2(mul2(c2, x), x, nothing));
+            float r0, r1, d0, d1;
+            unpair(v[j], r0, r1);
+            root[j] = pair(fast_root(r0), fast_root(r1));
+            unpair(add2(mul2(root[j], inv_root), eps), d0, d1);
+            p[j] = fma2(p[j], decay, mul2(size, mul2(m[j], pair(fast_reciprocal(d0), fast_reciprocal(d1)))));
+        }
+    }
+};
+
+__device__ __forceinline__ void as_pairs(const float (&x)[8], f2 (&p)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = pair(x[2 * j], x[2 * j + 1]);
+}
+__device__ __forceinline__ void as_floats(const f2 (&p)[4], float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) unpair(p[j], x[2 * j], x[2 * j + 1]);
+}
+template <typename T> __device__ __forceinline__ void load_pairs(const T* from, bool wide, int count, f2 (&p)[4]) {
+    float x[8];
+    load8(from, wide, count, x);
+    as_pairs(x, p);
+}
+__device__ __forceinline__ uint2 load_codes(const uint8_t* from, bool wide, int count) {
+    if (wide) return *reinterpret_cast<const uint2*>(from);
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) w[i >> 2] |= (uint32_t)from[i] << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_codes(uint8_t* to, bool wide, int count, const uint32_t (&w)[2]) {
+    if (wide) {
+        *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) to[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+// kRuns: blocks of 256 elements that a warp takes one after another; the search for the tensor is shared by them.
+template <int kBits, int kCapacity, int kRuns>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Params<kCapacity> a) {
     grid_dependency_wait();
     const int tile = blockIdx.x;
@@ -102,127 +174,137 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     const Tensor& t = a.tensor[lo];
     const Constants& c = a.c;
     const int lane = threadIdx.x & 31;
-    const int64_t block = (int64_t)(tile - a.first_tile[lo]) * (kTile / kBlock) + (threadIdx.x >> 5);
-    const int64_t i0 = block * kBlock + lane * 8;
-    if (block * kBlock >= t.numel) return;                  // a whole warp
-    const int count = (int)min((int64_t)8, max((int64_t)0, t.numel - i0));
-    const bool wide = (t.flags & kWide) && count == 8;
-
-    Lane x;
-    uint2 mc = make_uint2(0u, 0u), vc = mc;
-    float ms = 0.0f, vs = 0.0f;
-    // all loads first
-    if (t.flags & kGradBf16) load8(static_cast<const __nv_bfloat16*>(t.grad) + i0, wide, count, x.g);
-    else load8(static_cast<const float*>(t.grad) + i0, wide, count, x.g);
-    if (kBits == 32) {
-        load8(static_cast<const float*>(t.m) + i0, wide, count, x.m);
-        load8(static_cast<const float*>(t.v) + i0, wide, count, x.v);
-    } else {
-        const uint8_t* mb = static_cast<const uint8_t*>(t.m) + i0;
-        const uint8_t* vb = static_cast<const uint8_t*>(t.v) + i0;
-        if (wide) {
-            mc = *reinterpret_cast<const uint2*>(mb);
-            vc = *reinterpret_cast<const uint2*>(vb);
-        } else {
-            uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < count) {
-                    w[i >> 2] |= (uint32_t)mb[i] << (8 * (i & 3));
-                    w[2 + (i >> 2)] |= (uint32_t)vb[i] << (8 * (i & 3));
-                }
-            mc = make_uint2(w[0], w[1]);
-            vc = make_uint2(w[2], w[3]);
-        }
-        ms = t.m_scale[block];
-        vs = t.v_scale[block];
-    }
-    if (t.flags & kMaster) load8(t.master + i0, wide, count, x.p);
-    else if (t.flags & kParamBf16) load8(static_cast<const __nv_bfloat16*>(t.param) + i0, wide, count, x.p);
-    else load8(static_cast<const float*>(t.param) + i0, wide, count, x.p);
+    const int64_t block0 = ((int64_t)(tile - a.first_tile[lo]) * (kThreads / 32) + (threadIdx.x >> 5)) * kRuns;
+    const uint32_t flags = t.flags;
     const float gs = c.dev_grad_scale ? __fmul_rn(c.grad_scale, *c.dev_grad_scale) : c.grad_scale;
+    const bool round_param = c.round_up_at_random && (flags & (kParamBf16 | kMaster)) == kParamBf16;
+#pragma unroll 1
+    for (int run = 0; run < kRuns; ++run) {
+        const int64_t block = block0 + run, i0 = block * kBlock + lane * 8;
+        if (block * kBlock >= t.numel) return;              // a whole warp
+        const int count = (int)min((int64_t)8, max((int64_t)0, t.numel - i0));
+        const bool wide = (flags & kWide) && count == 8;
 
-    const bool round_param = c.round_up_at_random && (t.flags & (kParamBf16 | kMaster)) == kParamBf16;
-    uint4 random = make_uint4(0u, 0u, 0u, 0u);
-    if (kBits == 8 || round_param)
-        random = philox4x32_10((uint64_t)(t.first_block + block) * (kBlock / 8) + lane, a.keys, 2u);
-    const uint32_t rw[4] = {random.x, random.y, random.z, random.w};
-
-    uint32_t m_top = 0u, v_top = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (kBits == 8) {
-            x.m[i] = __fmul_rn(e4m3_value(((i < 4 ? mc.x : mc.y) >> (8 * (i & 3))) & 0xFFu), ms);
-            const float r = __fmul_rn(e4m3_value(((i < 4 ? vc.x : vc.y) >> (8 * (i & 3))) & 0xFFu), vs);
-            x.v[i] = __fmul_rn(r, r);
-        }
-        const float g = __fmul_rn(x.g[i], gs);
-        x.m[i] = __fadd_rn(__fmul_rn(c.beta1, x.m[i]), __fmul_rn(c.one_beta1, g));
-        x.v[i] = __fadd_rn(__fmul_rn(c.beta2, x.v[i]), __fmul_rn(__fmul_rn(c.one_beta2, g), g));
-        // the 8-bit states store the root, rounded as the definition says; elsewhere it only enters the quotient
-        const float root = kBits == 8 ? __fsqrt_rn(x.v[i]) : fast_root(x.v[i]);
-        if (kBits == 8) {
-            x.v[i] = root;
-            m_top = max(m_top, __float_as_uint(x.m[i]) & 0x7FFFFFFFu);
-            v_top = max(v_top, __float_as_uint(root) & 0x7FFFFFFFu);
-        }
-        const float den = __fadd_rn(__fmul_rn(root, c.inv_root), c.eps);
-        x.p[i] = __fsub_rn(__fmul_rn(x.p[i], c.decay), __fmul_rn(c.step_size, __fdividef(x.m[i], den)));
-    }
-
-    if (kBits == 32) {
-        store8(static_cast<float*>(t.m) + i0, wide, count, x.m);
-        store8(static_cast<float*>(t.v) + i0, wide, count, x.v);
-    } else {
-        m_top = __reduce_max_sync(0xFFFFFFFFu, m_top);
-        v_top = __reduce_max_sync(0xFFFFFFFFu, v_top);
-        float mf, vf;
-        ms = block_scale(m_top, &mf);
-        vs = block_scale(v_top, &vf);
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // the half-word with its bytes exchanged, as 1 + r 2^-16 less one
-            const uint32_t r = __byte_perm(rw[i >> 1], 0u, i & 1 ? 0x4423 : 0x4401);
-            const float unit = __fadd_rn(__uint_as_float(0x3F800000u | r << 7), -1.0f);
-            const uint32_t cm = e4m3_code(fminf(__fmul_rn(fabsf(x.m[i]), mf), 448.0f), unit) | (x.m[i] < 0.0f ? 0x80u : 0u);
-            const uint32_t cv = max(e4m3_code(fminf(__fmul_rn(x.v[i], vf), 448.0f), unit), x.v[i] > 0.0f ? 1u : 0u);
-            w[i >> 2] |= cm << (8 * (i & 3));
-            w[2 + (i >> 2)] |= cv << (8 * (i & 3));
-        }
-        uint8_t* mb = static_cast<uint8_t*>(t.m) + i0;
-        uint8_t* vb = static_cast<uint8_t*>(t.v) + i0;
-        if (wide) {
-            *reinterpret_cast<uint2*>(mb) = make_uint2(w[0], w[1]);
-            *reinterpret_cast<uint2*>(vb) = make_uint2(w[2], w[3]);
+        // all loads first
+        f2 g[4];
+        Step s;
+        uint2 mc = make_uint2(0u, 0u), vc = mc;
+        float ms = 0.0f, vs = 0.0f;
+        if (flags & kGradBf16) load_pairs(static_cast<const __nv_bfloat16*>(t.grad) + i0, wide, count, g);
+        else load_pairs(static_cast<const float*>(t.grad) + i0, wide, count, g);
+        if (kBits == 32) {
+            load_pairs(static_cast<const float*>(t.m) + i0, wide, count, s.m);
+            load_pairs(static_cast<const float*>(t.v) + i0, wide, count, s.v);
         } else {
+            mc = load_codes(static_cast<const uint8_t*>(t.m) + i0, wide, count);
+            vc = load_codes(static_cast<const uint8_t*>(t.v) + i0, wide, count);
+            ms = t.m_scale[block];
+            vs = t.v_scale[block];
+        }
+        if (flags & kMaster) load_pairs(t.master + i0, wide, count, s.p);
+        else if (flags & kParamBf16) load_pairs(static_cast<const __nv_bfloat16*>(t.param) + i0, wide, count, s.p);
+        else load_pairs(static_cast<const float*>(t.param) + i0, wide, count, s.p);
+
+        uint4 random = make_uint4(0u, 0u, 0u, 0u);
+        if (kBits == 8 || round_param)
+            random = philox4x32_10((uint64_t)(t.first_block + block) * (kBlock / 8) + lane, a.keys, 2u);
+        const uint32_t rw[4] = {random.x, random.y, random.z, random.w};
+
+        if (kBits == 8) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < count) {
-                    mb[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
-                    vb[i] = (uint8_t)(w[2 + (i >> 2)] >> (8 * (i & 3)));
+            for (int j = 0; j < 4; ++j) {
+                s.m[j] = mul2(e4m3_values((j < 2 ? mc.x : mc.y) >> (16 * (j & 1)) & 0xFFFFu), pair(ms));
+                const f2 r = mul2(e4m3_values((j < 2 ? vc.x : vc.y) >> (16 * (j & 1)) & 0xFFFFu), pair(vs));
+                s.v[j] = mul2(r, r);
+            }
+        }
+        s.take(c, g, gs);
+
+        if (kBits == 32) {
+            float x[8];
+            as_floats(s.m, x);
+            store8(static_cast<float*>(t.m) + i0, wide, count, x);
+            as_floats(s.v, x);
+            store8(static_cast<float*>(t.v) + i0, wide, count, x);
+        } else {
+            float m[8], v[8];
+            as_floats(s.m, m);
+            as_floats(s.v, v);
+            float m_top = m[0], v_top = v[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) {
+                m_top = larger(m_top, m[i]);
+                v_top = larger(v_top, v[i]);
+            }
+            // the root grows with v: the largest root is that of the largest v
+            float mf, vf;
+            ms = block_scale(warp_largest(m_top), &mf);
+            vs = block_scale(__fsqrt_rn(warp_largest(v_top)), &vf);
+            float y[8], z[8];
+            uint32_t r8[8];
+            float least = 1.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                unpair(mul2(s.m[j], pair(mf)), y[2 * j], y[2 * j + 1]);
+                unpair(mul2(s.root[j], pair(vf)), z[2 * j], z[2 * j + 1]);
+                least = fminf(least, fminf(fminf(fabsf(y[2 * j]), z[2 * j]), fminf(fabsf(y[2 * j + 1]), z[2 * j + 1])));
+                r8[2 * j] = __byte_perm(rw[j], 0u, 0x4014);              // the half-words with their bytes exchanged, << 8
+                r8[2 * j + 1] = __byte_perm(rw[j], 0u, 0x4234);
+            }
+            uint32_t mw[2], vw[2];
+            if (least >= 0.015625f) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t signs = __byte_perm(__byte_perm(__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), 0x0073),
+                                                       __byte_perm(__float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3]), 0x0073), 0x5410);
+                    mw[h] = e4m3_codes_normal(y + 4 * h, r8 + 4 * h) | (signs & 0x80808080u);
+                    vw[h] = e4m3_codes_normal(z + 4 * h, r8 + 4 * h);
                 }
-        }
-        if (lane == 0) {
-            t.m_scale[block] = ms;
-            t.v_scale[block] = vs;
-        }
-    }
-    if (t.flags & kMaster) store8(t.master + i0, wide, count, x.p);
-    if (t.flags & kParamBf16) {
-        uint32_t w[4];
+            } else {
+                mw[0] = mw[1] = vw[0] = vw[1] = 0u;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = round_param ? pack_out<true>(short_nan(x.p[2 * i]), short_nan(x.p[2 * i + 1]), rw[i])
-                               : pack_bf16x2(x.p[2 * i], x.p[2 * i + 1]);
-        store8_words(static_cast<__nv_bfloat16*>(t.param) + i0, wide, count, w);
-    } else {
-        store8(static_cast<float*>(t.param) + i0, wide, count, x.p);
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t cm = e4m3_code(fminf(fabsf(y[i]), 448.0f), r8[i] >> 8) | (y[i] < 0.0f ? 0x80u : 0u);
+                    const uint32_t cv = max(e4m3_code(fminf(z[i], 448.0f), r8[i] >> 8), v[i] > 0.0f ? 1u : 0u);
+                    mw[i >> 2] |= cm << (8 * (i & 3));
+                    vw[i >> 2] |= cv << (8 * (i & 3));
+                }
+            }
+            store_codes(static_cast<uint8_t*>(t.m) + i0, wide, count, mw);
+            store_codes(static_cast<uint8_t*>(t.v) + i0, wide, count, vw);
+            if (lane == 0) {
+                t.m_scale[block] = ms;
+                t.v_scale[block] = vs;
+            }
+        }
+        float x[8];
+        as_floats(s.p, x);
+        if (flags & kMaster) store8(t.master + i0, wide, count, x);
+        if (flags & kParamBf16) {
+            uint32_t w[4];
+            float sum;                                       // NaN where one of them is (or two infinities cancel)
+            {
+                float a0, a1;
+                unpair(add2(add2(s.p[0], s.p[1]), add2(s.p[2], s.p[3])), a0, a1);
+                sum = a0 + a1;
+            }
+            if (round_param && sum == sum) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = pack_out<true>(x[2 * i], x[2 * i + 1], rw[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = round_param ? pack_out<true>(short_nan(x[2 * i]), short_nan(x[2 * i + 1]), rw[i]) : pack_bf16x2(x[2 * i], x[2 * i + 1]);
+            }
+            store8_words(static_cast<__nv_bfloat16*>(t.param) + i0, wide, count, w);
+        } else {
+            store8(static_cast<float*>(t.param) + i0, wide, count, x);
+        }
     }
 }
 
-template <int kCapacity>
-cudaError_t launch(const mvue_adamw_tensor* ts, int64_t count, const Constants& c, uint64_t seed, int state_bits,
+template <int kBits, int kCapacity, int kRuns>
+cudaError_t launch(const mvue_adamw_tensor* ts, int64_t count, const Constants& c, uint64_t seed,
                    int64_t* first_block, int64_t* used, cudaStream_t stream) {
     Params<kCapacity> a;
     a.c = c;
@@ -233,7 +315,7 @@ cudaError_t launch(const mvue_adamw_tensor* ts, int64_t count, const Constants& 
         const mvue_adamw_tensor& s = ts[i];
         const int64_t blocks = (s.numel + kBlock - 1) / kBlock;
         if (s.numel == 0) continue;
-        const int64_t mine = (s.numel + kTile - 1) / kTile;
+        const int64_t mine = (s.numel + kTile * kRuns - 1) / (kTile * kRuns);
         if (tiles + mine > 0x7FFFFFFF) break;
         Tensor& t = a.tensor[n];
         t = {s.param, static_cast<float*>(s.master), s.grad, s.exp_avg, s.exp_avg_sq, static_cast<float*>(s.exp_avg_scale),
@@ -251,8 +333,7 @@ cudaError_t launch(const mvue_adamw_tensor* ts, int64_t count, const Constants& 
     *used = i;
     if (n == 0) return cudaSuccess;
     a.count = n;
-    auto kernel = state_bits == 8 ? &adamw_kernel<8, kCapacity> : &adamw_kernel<32, kCapacity>;
-    return launch_dependent(kernel, dim3((unsigned)tiles), dim3(kThreads), 0, stream, a);
+    return launch_dependent(&adamw_kernel<kBits, kCapacity, kRuns>, dim3((unsigned)tiles), dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace
@@ -293,14 +374,22 @@ extern "C" int mvue_adamw_step(const mvue_adamw_tensor* tensors, int64_t count, 
     c.decay = (float)(1.0 - cfg->lr * cfg->weight_decay);
     c.step_size = (float)(cfg->lr / (1.0 - std::pow(cfg->beta1, t)));
     c.grad_scale = (float)cfg->grad_scale;
+    c.minus_zero = -0.0f;
     c.dev_grad_scale = cfg->dev_grad_scale;
     c.round_up_at_random = (cfg->options & MVUE_OPT_STOCHASTIC_ROUNDING) != 0;
-    int64_t first_block = 0;
+    // 8-bit states: four blocks a warp where that still gives every SM sixteen thread blocks (the step is bound by
+    // instructions there; 32-bit states are bound by memory and slower with it: 448 us against 433 us on 24 matrices of 4 M)
+    int64_t elements = 0, first_block = 0;
+    for (int64_t i = 0; i < count; ++i) elements += tensors[i].numel;
+    const bool runs = elements / (4 * kTile) >= 16 * dev.sm_count;
     while (count > 0) {
         int64_t used = 0;
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-        const cudaError_t e = count <= 32 ? launch<32>(tensors, count, c, cfg->seed, cfg->state_bits, &first_block, &used, st)
-                                          : launch<320>(tensors, count, c, cfg->seed, cfg->state_bits, &first_block, &used, st);
+        const auto go = [&](auto kernel) { return kernel(tensors, count, c, cfg->seed, &first_block, &used, st); };
+        cudaError_t e;
+        if (cfg->state_bits == 32) e = go(count <= 32 ? &launch<32, 32, 1> : &launch<32, 320, 1>);
+        else if (runs) e = go(count <= 32 ? &launch<8, 32, 4> : &launch<8, 320, 4>);
+        else e = go(count <= 32 ? &launch<8, 32, 1> : &launch<8, 320, 1>);
         if (e != cudaSuccess) { set_cuda_error(e, "mvue_adamw_step launch"); return MVUE_ERR_CUDA; }
         tensors += used;
         count -= used;
