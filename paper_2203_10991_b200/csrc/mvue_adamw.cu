@@ -163,7 +163,7 @@ __device__ __forceinline__ void store_codes(uint8_t* to, bool wide, int count, c
 
 // kRuns: blocks of 256 elements that a warp takes one after another; the search for the tensor is shared by them.
 template <int kBits, int kCapacity, int kRuns>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Params<kCapacity> a) {
+__global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constant__ Params<kCapacity> a) {
     grid_dependency_wait();
     const int tile = blockIdx.x;
     int lo = 0, hi = a.count - 1;

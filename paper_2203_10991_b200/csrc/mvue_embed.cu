@@ -1,13 +1,12 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
 //
-// Both move rows and are bound by HBM.  Lookup: a row in, a row out, a team of threads per row.  Gradient, three
-// launches: (1) one cluster of eight thread blocks sorts the tokens by id (stable radix sort, digits of up to nine bits,
-// histograms exchanged through distributed shared memory) while every other block fills the rows of dW that no token
-// names with zeros -- each marks the ids of its own rows in a bitmap by reading the whole token list, which costs two
-// microseconds of L2 reads at 32768 tokens and saves a dependent launch; (2) the sorted tokens are cut into chunks of
-// equal length, a team adds the rows of a chunk in token order and writes the sums of the ids that begin and end in it;
-// what crosses a chunk's edge goes to the workspace as a partial sum; (3) those are added in chunk order.  No atomics on
-// data: equal inputs give equal bits.
+// Both move rows and are bound by HBM.  Lookup: a row in, a row out, a team of threads per row.  Gradient: (1) one
+// cluster of eight thread blocks sorts the tokens by id (stable radix sort, digits of up to nine bits, histograms exchanged
+// through distributed shared memory); (2) beside it the other SMs fill the rows of dW that no token names with zeros -- each
+// block marks the ids of its own rows in a bitmap by reading the whole token list, which costs two microseconds of L2 reads at
+// 32768 tokens and saves a dependent launch; (3) the sorted tokens are cut into chunks of equal length, a team adds the
+// rows of a chunk in token order and writes the sums of the ids that begin and end in it; what crosses a chunk's edge goes to
+// the workspace as a partial sum; (4) those are added in chunk order.  No atomics on data: equal inputs give equal bits.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -49,14 +48,21 @@ __global__ void __launch_bounds__(256) embed_kernel(Ids ids, int64_t tokens, con
     const int64_t id = ids.at(t);
     const bool known = id >= 0 && id < vocab;
     if (!known && threadIdx.x == 0 && blockIdx.y == 0 && dev_status) *dev_status = MVUE_ERR_INDEX;
-    for (int64_t c0 = (int64_t)blockIdx.y * team * 8; c0 < cols; c0 += (int64_t)gridDim.y * team * 8) {
-        const Cols<kWide> c(c0, cols, threadIdx.x, team);
-        if (c.count == 0) continue;
-        float x[8] = {};
-        if (known) c.load(w + id * ldw, x);
+    w += known ? id * ldw : 0;
+    out += t * ldo;
+    // two pieces at a time: both loads are out before the first is used
+    for (int64_t c0 = (int64_t)blockIdx.y * team * 16; c0 < cols; c0 += (int64_t)gridDim.y * team * 16) {
+        const Cols<kWide> a(c0, cols, threadIdx.x, team), b(c0 + team * 8, cols, threadIdx.x, team);
+        float x[8] = {}, y[8] = {};
+        if (known && a.count) a.load(w, x);
+        if (known && b.count) b.load(w, y);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= scale;
-        c.store(out + t * ldo, x);
+        for (int j = 0; j < 8; ++j) {
+            x[j] *= scale;
+            y[j] *= scale;
+        }
+        if (a.count) a.store(out, x);
+        if (b.count) b.store(out, y);
     }
 }
 
@@ -66,7 +72,7 @@ struct SortArgs {
     int64_t tokens, vocab, padding;
     uint32_t *key[2], *pos[2];       // pass p reads [p & 1 ^ 1] (the first one the ids) and writes [p & 1]
     int passes, digit_bits;
-    void* dw;                        // nullptr: nothing to fill
+    void* dw;
     int64_t cols, lddw;
     int elem_bytes, wide;
     int* dev_status;
@@ -189,6 +195,7 @@ __device__ void fill_rows(const SortArgs& a, uint32_t* bitmap, int part, int par
         const int64_t rows = min((int64_t)kWindowRows, end - r0);
         for (int i = tid; i < (rows + 31) / 32; i += kSortThreads) bitmap[i] = 0u;
         __syncthreads();
+#pragma unroll 4
         for (int64_t i = tid; i < a.tokens; i += kSortThreads) {
             const int64_t id = a.ids.at(i), r = id - r0;
             if (r >= 0 && r < rows && id != a.padding) atomicOr(&bitmap[r >> 5], 1u << (r & 31));
@@ -209,12 +216,20 @@ __device__ void fill_rows(const SortArgs& a, uint32_t* bitmap, int part, int par
     }
 }
 
-// Clusters of eight: the first sorts, the others fill.
+// One cluster.  What follows on the stream may start at once (the fill, which needs nothing of this kernel, and waits for
+// it at its end so that the launch behind it has both).
 __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __grid_constant__ SortArgs a) {
     grid_dependency_wait();
-    __shared__ union { SortShared sort; uint32_t bitmap[kWindowRows / 32]; } s;
-    if (blockIdx.x < kSortCtas) sort_tokens(a, s.sort);
-    else fill_rows(a, s.bitmap, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ SortShared s;
+    sort_tokens(a, s);
+}
+// Launched behind the sort: by the time its blocks run, every kernel before the sort has completed (the sort waited for
+// them before it let this one start), so the ids may be read and dW written.
+__global__ void __launch_bounds__(kSortThreads, 1) embed_fill_kernel(const __grid_constant__ SortArgs a) {
+    __shared__ uint32_t bitmap[kWindowRows / 32];
+    fill_rows(a, bitmap, blockIdx.x, gridDim.x);
+    grid_dependency_wait();
 }
 
 // ---- gradient, second launch: sums of chunks ---------------------------------------------------------------------------
@@ -245,8 +260,34 @@ __device__ __forceinline__ void put_row(const SumArgs& a, const Cols<kWide>& c, 
     c.store(row, x);
 }
 
+// Eight elements of a row as they lie in memory: what is in flight costs half the registers for bf16.
+template <typename T, bool kWide>
+struct RawRow {
+    static constexpr int kWords = !kWide || sizeof(T) == 4 ? 8 : 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const Cols<kWide>& c, const T* row) {
+        if constexpr (!kWide) {
+            float x[8];
+            c.load(row, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(x[j]);
+        } else if constexpr (sizeof(T) == 4) {
+            ld256(row + c.first, w);
+        } else {
+            const uint4 q = *reinterpret_cast<const uint4*>(row + c.first);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        }
+    }
+    __device__ __forceinline__ void add_to(f2 (&acc)[4]) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            acc[j] = add2(acc[j], kWords == 4 ? pair(bf16_lo(w[j]), bf16_hi(w[j]))
+                                              : pair(__uint_as_float(w[2 * j % kWords]), __uint_as_float(w[(2 * j + 1) % kWords])));
+    }
+};
+
 template <typename TY, typename TD, bool kWide>
-__global__ void __launch_bounds__(128) embed_sum_kernel(const __grid_constant__ SumArgs a) {
+__global__ void __launch_bounds__(128, kWide ? 6 : 4) embed_sum_kernel(const __grid_constant__ SumArgs a) {
     grid_dependency_wait();
     __shared__ uint32_t s_key[4][kChunk + 2], s_pos[4][kChunk];
     const int team = blockDim.x, ty = threadIdx.y;
@@ -266,64 +307,81 @@ __global__ void __launch_bounds__(128) embed_sum_kernel(const __grid_constant__ 
     if (c.count == 0) return;
     const TY* dy = static_cast<const TY*>(a.dy);
     float* partial = a.partial + chunk * 2 * a.ld_partial;
-    float acc[8] = {};
+    const uint32_t vocab = (uint32_t)a.vocab;
+    f2 acc[4] = {};
     bool from_front = key[-1] == key[0];
-    constexpr int kAhead = 8;
+    constexpr int kAhead = RawRow<TY, kWide>::kWords == 4 ? 8 : 4;
+#pragma unroll 1
     for (int i = 0; i < n; i += kAhead) {
-        float x[kAhead][8];
+        RawRow<TY, kWide> x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (i + u < n && key[i + u] < a.vocab) c.load(dy + (int64_t)s_pos[ty][i + u] * a.lddy, x[u]);
+            if (i + u < n && key[i + u] < vocab) x[u].load(c, dy + (int64_t)s_pos[ty][i + u] * a.lddy);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (i + u >= n || key[i + u] >= a.vocab) break;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] += x[u][j];
+            if (i + u >= n || key[i + u] >= vocab) break;
+            x[u].add_to(acc);
             const bool last = i + u + 1 == n, goes_on = key[i + u + 1] == key[i + u];
             if (!last && goes_on) continue;
-            if (from_front) c.store(partial, acc);
-            else if (goes_on) c.store(partial + a.ld_partial, acc);
-            else put_row<TD, kWide>(a, c, key[i + u], acc);
-            from_front = false;
+            float sum[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                unpair(acc[j], sum[2 * j], sum[2 * j + 1]);
+                acc[j] = pair(0.0f);
+            }
+            if (from_front) c.store(partial, sum);
+            else if (goes_on) c.store(partial + a.ld_partial, sum);
+            else put_row<TD, kWide>(a, c, key[i + u], sum);
+            from_front = false;
         }
     }
 }
 
 // ---- gradient, third launch: ids that cross chunks --------------------------------------------------------------------
-// The team of the chunk in which such an id begins adds that chunk's partial sum and those of the chunks it goes on in.
+// The block of the chunk in which such an id begins adds that chunk's partial sum and those of the chunks it goes on in:
+// its teams take consecutive shares of them, which are added in order.
+constexpr int kJoinTeams = 4;
 template <typename TD, bool kWide>
-__global__ void __launch_bounds__(128) embed_join_kernel(const __grid_constant__ SumArgs a) {
+__global__ void __launch_bounds__(128 * kJoinTeams) embed_join_kernel(const __grid_constant__ SumArgs a) {
     grid_dependency_wait();
-    const int64_t chunk = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    const int64_t end = (chunk + 1) * kChunk;
-    if (chunk >= a.chunks || end >= a.tokens) return;
+    __shared__ float s[kJoinTeams - 1][8][128];
+    const int64_t chunk = blockIdx.x, end = (chunk + 1) * kChunk;
+    if (end >= a.tokens) return;
     const uint32_t id = a.key[end - 1];
     if (id >= a.vocab || a.key[end] != id) return;                        // nothing leaves
     if (chunk > 0 && a.key[end - kChunk] == id && a.key[end - kChunk - 1] == id) return;   // began earlier
-    // the last chunk whose first key is this id
-    int64_t lo = chunk + 1, hi = a.chunks - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) >> 1;
-        if (a.key[mid * kChunk] == id) lo = mid; else hi = mid - 1;
+    // the last chunk whose first key is this id: every thread looks at one, as long as all of them are
+    const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
+    int64_t lo = chunk;
+    for (int found = threads; found == threads; lo += found) {
+        const int64_t k = lo + 1 + tid;
+        found = __syncthreads_count(k < a.chunks && a.key[k * kChunk] == id);
     }
     const Cols<kWide> c((int64_t)blockIdx.y * kSlab, a.cols, threadIdx.x, blockDim.x);
-    if (c.count == 0) return;
-    float acc[8];
-    c.load(a.partial + (chunk * 2 + 1) * a.ld_partial, acc);
+    const int64_t each = (lo - chunk + 1 + kJoinTeams - 1) / kJoinTeams;       // the first partial sum is the chunk's own
+    const int64_t first = chunk + each * threadIdx.y, last = min(lo + 1, first + each);
+    float acc[8] = {};
     constexpr int kAhead = 4;
-    for (int64_t k = chunk + 1; k <= lo; k += kAhead) {
-        float x[kAhead][8];
+    if (c.count)
+        for (int64_t k = first; k < last; k += kAhead) {
+            float x[kAhead][8];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (k + u <= lo) c.load(a.partial + (k + u) * 2 * a.ld_partial, x[u]);
+            for (int u = 0; u < kAhead; ++u)
+                if (k + u < last) c.load(a.partial + ((k + u) * 2 + (k + u == chunk)) * a.ld_partial, x[u]);
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (k + u <= lo)
+            for (int u = 0; u < kAhead; ++u)
+                if (k + u < last)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += x[u][j];
-    }
+                    for (int j = 0; j < 8; ++j) acc[j] += x[u][j];
+        }
+    if (threadIdx.y > 0)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[threadIdx.y - 1][j][threadIdx.x] = acc[j];
+    __syncthreads();
+    if (threadIdx.y > 0 || c.count == 0) return;
+    for (int t = 0; t < kJoinTeams - 1; ++t)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += s[t][j][threadIdx.x];
     put_row<TD, kWide>(a, c, id, acc);
 }
 
@@ -364,7 +422,7 @@ cudaError_t embed(Ids ids, int64_t tokens, const void* w, int64_t vocab, int64_t
     while (team < 256 && team * 16 < cols) team *= 2;
     const int rows = 256 / team;
     const int64_t pieces = (cols + team * 8 - 1) / (team * 8);
-    const dim3 grid((unsigned)((tokens + rows - 1) / rows), (unsigned)std::min<int64_t>((pieces + 1) / 2, 65535));
+    const dim3 grid((unsigned)((tokens + rows - 1) / rows), (unsigned)std::min<int64_t>(pieces / 2 + pieces % 2, 65535));
     auto kernel = wide ? &embed_kernel<TW, TO, true> : &embed_kernel<TW, TO, false>;
     return launch_dependent(kernel, grid, dim3(team, rows), 0, st, ids, tokens, static_cast<const TW*>(w), vocab, cols, ldw, scale,
                             static_cast<TO*>(out), ldo, dev_status);
@@ -377,12 +435,13 @@ cudaError_t sums(const SumArgs& a, bool wide, cudaStream_t st) {
     const dim3 grid((unsigned)((a.chunks + teams - 1) / teams), (unsigned)((a.cols + kSlab - 1) / kSlab)), block(team, teams);
     cudaError_t e = launch_dependent(wide ? &embed_sum_kernel<TY, TD, true> : &embed_sum_kernel<TY, TD, false>, grid, block, 0, st, a);
     if (e != cudaSuccess || a.chunks < 2) return e;
-    return launch_dependent(wide ? &embed_join_kernel<TD, true> : &embed_join_kernel<TD, false>, grid, block, 0, st, a);
+    return launch_dependent(wide ? &embed_join_kernel<TD, true> : &embed_join_kernel<TD, false>, dim3((unsigned)a.chunks, grid.y),
+                            dim3(team, kJoinTeams), 0, st, a);
 }
 
-cudaError_t launch_sort(const SortArgs& a, int clusters, cudaStream_t st) {
+cudaError_t launch_sort(const SortArgs& a, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(clusters * kSortCtas));
+    cfg.gridDim = dim3(kSortCtas);
     cfg.blockDim = dim3(kSortThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -394,29 +453,6 @@ cudaError_t launch_sort(const SortArgs& a, int clusters, cudaStream_t st) {
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, &embed_sort_kernel, a);
-}
-
-// clusters of the first launch that are resident at once, per device
-cudaError_t sort_clusters(int* clusters) {
-    static PerDeviceOnce once;
-    static int count[kMaxDevices];
-    const cudaError_t e = once_per_device(once, [](int dev) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(kSortCtas);
-        cfg.blockDim = dim3(kSortThreads);
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = kSortCtas;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        return cudaOccupancyMaxActiveClusters(&count[dev], &embed_sort_kernel, &cfg);
-    });
-    if (e != cudaSuccess) return e;
-    int dev = 0;
-    const cudaError_t e2 = cudaGetDevice(&dev);
-    if (e2 == cudaSuccess) *clusters = count[dev];
-    return e2;
 }
 
 }  // namespace
@@ -472,9 +508,6 @@ int mvue_embedding_grad(const void* ids, int id_bits, int64_t tokens, const void
     if (l.bytes > 0 && (!workspace || workspace_bytes < l.bytes || off(workspace, 32))) return MVUE_ERR_WORKSPACE;
     DeviceInfo dev;
     if (int s = current_device_info(&dev)) return s;
-    int clusters = 0;
-    cudaError_t e = sort_clusters(&clusters);
-    if (e != cudaSuccess) { set_cuda_error(e, "mvue_embedding_grad set-up"); return MVUE_ERR_CUDA; }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     char* ws = static_cast<char*>(workspace);
     SortArgs a = {};
@@ -490,14 +523,16 @@ int mvue_embedding_grad(const void* ids, int id_bits, int64_t tokens, const void
     while (bits < 32 && vocab >> bits) ++bits;
     a.passes = tokens == 0 ? 0 : (bits + kMaxDigitBits - 1) / kMaxDigitBits;
     a.digit_bits = a.passes ? (bits + a.passes - 1) / a.passes : 1;
-    a.dw = accumulate ? nullptr : dW;
+    a.dw = dW;
     a.cols = cols;
     a.lddw = lddW;
     a.elem_bytes = (int)size_of(dW_dtype);
     a.wide = !off(dW, 32) && cols * a.elem_bytes % 32 == 0 && lddW * a.elem_bytes % 32 == 0;
     a.dev_status = dev_status;
-    // with one cluster resident at a time the second would only begin when the sort is done, and that is all
-    e = launch_sort(a, accumulate ? 1 : std::max(2, clusters), st);
+    cudaError_t e = launch_sort(a, st);
+    // one block on every SM that the sort leaves
+    if (e == cudaSuccess && !accumulate)
+        e = launch_dependent(&embed_fill_kernel, dim3((unsigned)std::max(1, dev.sm_count - kSortCtas)), dim3(kSortThreads), 0, st, a);
     if (e == cudaSuccess && tokens > 0) {
         const int last = (a.passes - 1) & 1;
         SumArgs b = {a.key[last], a.pos[last], tokens, vocab, l.chunks, dy, cols, lddy, scale, dW, lddW, accumulate,
