@@ -106,8 +106,8 @@ MVUE_API int mvue_embedding(const void* ids, int id_bits, int64_t tokens, const 
  *  padding_idx   tokens with this id add nothing (a negative one: none does so).  Ids outside [0, vocab) add nothing and
  *           write MVUE_ERR_INDEX to *dev_status (optional).
  *  workspace     mvue_embedding_grad_workspace_bytes(tokens, cols) bytes, 32-byte aligned; contents scratch.
- * Sums are formed in binary32, within each run of 32 tokens of the list sorted by id in token order, the runs in order:
- * equal inputs give equal bits.  tokens = 0 gives zeros. */
+ * Sums are formed in binary32: the list sorted by id is cut into runs of 4 to 32 tokens (by the number of tokens), a run's
+ * rows are added in token order and an id's runs in a fixed order: equal inputs give equal bits.  tokens = 0 gives zeros. */
 MVUE_API int mvue_embedding_grad(const void* ids, int id_bits, int64_t tokens, const void* dy, int dy_dtype, int64_t cols, int64_t lddy,
                                  float scale, int64_t padding_idx, void* dW, int dW_dtype, int64_t vocab, int64_t lddW, int accumulate,
                                  void* workspace, size_t workspace_bytes, int* dev_status, void* stream);

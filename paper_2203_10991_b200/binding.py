@@ -111,12 +111,14 @@ def _stream_ptr() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+_DTYPE_CODES = {torch.float32: MVUE_F32, torch.bfloat16: MVUE_BF16}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return MVUE_F32
-    if t.dtype == torch.bfloat16:
-        return MVUE_BF16
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
 
 
 def mvue_packed_sizes(rows: int, cols: int, n: int, m: int, axis: int, layout: int = MVUE_LAYOUT_CANONICAL):
@@ -414,9 +416,9 @@ def _positions(t: torch.Tensor):
 
 def _affine(weight, bias, c: int) -> int:
     for t in (weight, bias):
-        if t is not None and (t.shape != (c,) or not t.is_contiguous() or not t.is_cuda):
+        if t is not None and (t.dim() != 1 or t.numel() != c or not t.is_contiguous() or not t.is_cuda):
             raise ValueError("weight and bias are contiguous CUDA tensors of one element per channel")
-    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+    if weight is not None and bias is not None and weight.dtype is not bias.dtype:
         raise TypeError("weight and bias have one dtype")
     return MVUE_F32 if weight is None and bias is None else _dtype_code(bias if weight is None else weight)
 
@@ -436,7 +438,7 @@ def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | Non
     assert x.is_cuda
     code = _affine(weight, bias, c)
     if out is None:
-        out = x.new_empty(x.shape)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
         ldy = c
     else:
         assert out.shape == x.shape and out.dtype == x.dtype
@@ -461,12 +463,12 @@ def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.
                                  dev_status: torch.Tensor | None = None):
     """Backward pass of mvue_group_norm_act.  Returns (dx, dweight, dbias); the last two [c] fp32."""
     n, s, c, ldx = _positions(x)
-    assert x.is_cuda and dy.shape == x.shape and dy.dtype == x.dtype
+    assert x.is_cuda and dy.shape == x.shape and dy.dtype is x.dtype
     for t in (mean, rstd):
-        assert t.shape == (n, groups) and t.dtype == torch.float32 and t.is_contiguous()
+        assert t.dim() == 2 and t.shape[1] == groups and t.numel() == n * groups and t.dtype is torch.float32 and t.is_contiguous()
     code = _affine(weight, bias, c)
     if out is None:
-        out = x.new_empty(x.shape)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
         lddx = c
     else:
         assert out.shape == x.shape and out.dtype == x.dtype

@@ -26,7 +26,7 @@ namespace cg = cooperative_groups;
 constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kKeysPerThread = 4;
 constexpr int kMaxDigitBits = 9, kMaxBins = 1 << kMaxDigitBits, kTileKeys = kSortThreads * kKeysPerThread;
 constexpr int kWindowRows = 65536;              // rows of dW that one pass over the tokens marks (an 8 KB bitmap)
-constexpr int kChunk = 32;                      // sorted tokens a team adds
+constexpr int kMaxChunk = 32;                   // sorted tokens a team adds at most
 constexpr int kSlab = 1024;                     // columns of a team at most: 128 threads of eight
 
 struct Ids {
@@ -186,7 +186,9 @@ __device__ void sort_tokens(const SortArgs& a, SortShared& s) {
     }
 }
 
-__device__ void fill_rows(const SortArgs& a, uint32_t* bitmap, int part, int parts) {
+// zeros into this block's share of the rows that no token names; `mark(f)` calls f with every token's key
+template <typename M>
+__device__ __forceinline__ void fill_rows(const SortArgs& a, uint32_t* bitmap, int part, int parts, M mark) {
     const int tid = threadIdx.x;
     const int64_t row_bytes = a.cols * a.elem_bytes;
     const int64_t each = (a.vocab + parts - 1) / parts;
@@ -195,11 +197,10 @@ __device__ void fill_rows(const SortArgs& a, uint32_t* bitmap, int part, int par
         const int64_t rows = min((int64_t)kWindowRows, end - r0);
         for (int i = tid; i < (rows + 31) / 32; i += kSortThreads) bitmap[i] = 0u;
         __syncthreads();
-#pragma unroll 4
-        for (int64_t i = tid; i < a.tokens; i += kSortThreads) {
-            const int64_t id = a.ids.at(i), r = id - r0;
+        mark([&](int64_t id) {
+            const int64_t r = id - r0;
             if (r >= 0 && r < rows && id != a.padding) atomicOr(&bitmap[r >> 5], 1u << (r & 31));
-        }
+        });
         __syncthreads();
         const uint32_t zero[8] = {};
         for (int64_t r = tid >> 5; r < rows; r += kSortWarps) {
@@ -228,14 +229,48 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(const __gri
 // them before it let this one start), so the ids may be read and dW written.
 __global__ void __launch_bounds__(kSortThreads, 1) embed_fill_kernel(const __grid_constant__ SortArgs a) {
     __shared__ uint32_t bitmap[kWindowRows / 32];
-    fill_rows(a, bitmap, blockIdx.x, gridDim.x);
+    fill_rows(a, bitmap, blockIdx.x, gridDim.x, [&](auto f) {
+#pragma unroll 4
+        for (int64_t i = threadIdx.x; i < a.tokens; i += kSortThreads) f(a.ids.at(i));
+    });
     grid_dependency_wait();
+}
+
+// Few tokens: every block holds all keys, a warp finds a token's place by counting those before it, and the same launch
+// fills.  4096^2 comparisons are a microsecond on 148 SMs, where the sort in a cluster and a launch for it take fifteen; 8192^2
+// would be four, which the fill hides less well than the sort beside it.
+constexpr int kRankTokens = 4096;
+__global__ void __launch_bounds__(kSortThreads, 1) embed_rank_kernel(const __grid_constant__ SortArgs a, int fill) {
+    grid_dependency_wait();
+    __shared__ __align__(16) uint32_t s_key[kRankTokens];
+    __shared__ uint32_t bitmap[kWindowRows / 32];
+    const int tokens = (int)a.tokens, padded = (tokens + 127) / 128 * 128, lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i < padded; i += kSortThreads) s_key[i] = i < tokens ? key_of(a, i) : 0xFFFFFFFFu;
+    __syncthreads();
+    for (int t = (threadIdx.x >> 5) * gridDim.x + blockIdx.x; t < tokens; t += gridDim.x * kSortWarps) {
+        const uint32_t key = s_key[t];
+        uint32_t before = 0u;
+        for (int j = lane * 4; j < padded; j += 128) {
+            const uint4 k = *reinterpret_cast<const uint4*>(s_key + j);
+            before += (k.x < key + (j < t)) + (k.y < key + (j + 1 < t)) + (k.z < key + (j + 2 < t)) + (k.w < key + (j + 3 < t));
+        }
+        before = __reduce_add_sync(0xFFFFFFFFu, before);
+        if (lane == 0) {
+            a.key[0][before] = key;
+            a.pos[0][before] = (uint32_t)t;
+        }
+    }
+    if (fill)
+        fill_rows(a, bitmap, blockIdx.x, gridDim.x, [&](auto f) {
+            for (int i = threadIdx.x; i < tokens; i += kSortThreads) f((int64_t)s_key[i] < a.vocab ? (int64_t)s_key[i] : -1);
+        });
 }
 
 // ---- gradient, second launch: sums of chunks ---------------------------------------------------------------------------
 struct SumArgs {
     const uint32_t *key, *pos;       // sorted
     int64_t tokens, vocab, chunks;
+    int chunk;                       // sorted tokens of a team
     const void* dy;
     int64_t cols, lddy;
     float scale;
@@ -289,13 +324,13 @@ struct RawRow {
 template <typename TY, typename TD, bool kWide>
 __global__ void __launch_bounds__(128, kWide ? 6 : 4) embed_sum_kernel(const __grid_constant__ SumArgs a) {
     grid_dependency_wait();
-    __shared__ uint32_t s_key[4][kChunk + 2], s_pos[4][kChunk];
+    __shared__ uint32_t s_key[4][kMaxChunk + 2], s_pos[4][kMaxChunk];
     const int team = blockDim.x, ty = threadIdx.y;
     const int64_t chunk = (int64_t)blockIdx.x * blockDim.y + ty;
-    const int64_t i0 = chunk * kChunk;
-    const int n = chunk < a.chunks ? (int)min((int64_t)kChunk, a.tokens - i0) : 0;
+    const int64_t i0 = chunk * a.chunk;
+    const int n = chunk < a.chunks ? (int)min((int64_t)a.chunk, a.tokens - i0) : 0;
     // keys of the chunk and of its neighbours on both sides (no id where there is none)
-    for (int i = threadIdx.x; i < kChunk + 2; i += team) {
+    for (int i = threadIdx.x; i < a.chunk + 2; i += team) {
         const int64_t at = i0 - 1 + i;
         s_key[ty][i] = n && at >= 0 && at < a.tokens ? a.key[at] : 0xFFFFFFFFu;
         if (i >= 1 && i <= n) s_pos[ty][i - 1] = a.pos[at];
@@ -345,17 +380,17 @@ template <typename TD, bool kWide>
 __global__ void __launch_bounds__(128 * kJoinTeams) embed_join_kernel(const __grid_constant__ SumArgs a) {
     grid_dependency_wait();
     __shared__ float s[kJoinTeams - 1][8][128];
-    const int64_t chunk = blockIdx.x, end = (chunk + 1) * kChunk;
+    const int64_t chunk = blockIdx.x, end = (chunk + 1) * a.chunk;
     if (end >= a.tokens) return;
     const uint32_t id = a.key[end - 1];
     if (id >= a.vocab || a.key[end] != id) return;                        // nothing leaves
-    if (chunk > 0 && a.key[end - kChunk] == id && a.key[end - kChunk - 1] == id) return;   // began earlier
+    if (chunk > 0 && a.key[end - a.chunk] == id && a.key[end - a.chunk - 1] == id) return;   // began earlier
     // the last chunk whose first key is this id: every thread looks at one, as long as all of them are
     const int threads = blockDim.x * blockDim.y, tid = threadIdx.y * blockDim.x + threadIdx.x;
     int64_t lo = chunk;
     for (int found = threads; found == threads; lo += found) {
         const int64_t k = lo + 1 + tid;
-        found = __syncthreads_count(k < a.chunks && a.key[k * kChunk] == id);
+        found = __syncthreads_count(k < a.chunks && a.key[k * a.chunk] == id);
     }
     const Cols<kWide> c((int64_t)blockIdx.y * kSlab, a.cols, threadIdx.x, blockDim.x);
     const int64_t each = (lo - chunk + 1 + kJoinTeams - 1) / kJoinTeams;       // the first partial sum is the chunk's own
@@ -389,17 +424,27 @@ __global__ void __launch_bounds__(128 * kJoinTeams) embed_join_kernel(const __gr
 struct Layout {
     size_t key[2], pos[2], partial, bytes;
     int64_t chunks, ld_partial;
+    int chunk;
 };
+
+// A team adds 32 tokens, fewer where that would leave SMs without teams (four for each of 148), but at least four: every
+// chunk may leave two partial sums.  2153 tokens of 426 bf16: the sums take 28 us in chunks of 32 (34 blocks) and the whole call 37 us; in chunks of four the call takes 22 us.
+int chunk_of(int64_t tokens) {
+    int chunk = 4;
+    while (chunk < kMaxChunk && tokens >= (int64_t)chunk * 2 * 4 * 148) chunk *= 2;
+    return chunk;
+}
 
 Layout layout_of(int64_t tokens, int64_t cols) {
     Layout l;
+    l.chunk = chunk_of(tokens);
     size_t at = 0;
     const auto take = [&](size_t n) { const size_t here = at; at += (n + 255) / 256 * 256; return here; };
     for (int i = 0; i < 2; ++i) {
         l.key[i] = take((size_t)tokens * 4);
         l.pos[i] = take((size_t)tokens * 4);
     }
-    l.chunks = (tokens + kChunk - 1) / kChunk;
+    l.chunks = (tokens + l.chunk - 1) / l.chunk;
     l.ld_partial = (cols + 7) / 8 * 8;
     l.partial = take((size_t)l.chunks * 2 * (size_t)l.ld_partial * 4);
     l.bytes = at;
@@ -529,13 +574,19 @@ int mvue_embedding_grad(const void* ids, int id_bits, int64_t tokens, const void
     a.elem_bytes = (int)size_of(dW_dtype);
     a.wide = !off(dW, 32) && cols * a.elem_bytes % 32 == 0 && lddW * a.elem_bytes % 32 == 0;
     a.dev_status = dev_status;
-    cudaError_t e = launch_sort(a, st);
+    cudaError_t e;
+    if (tokens <= kRankTokens) {
+        a.passes = 1;                                   // sorted into the first pair of lists
+        e = launch_dependent(&embed_rank_kernel, dim3((unsigned)dev.sm_count), dim3(kSortThreads), 0, st, a, (int)!accumulate);
+    } else {
+        e = launch_sort(a, st);
+    }
     // one block on every SM that the sort leaves
-    if (e == cudaSuccess && !accumulate)
+    if (e == cudaSuccess && !accumulate && tokens > kRankTokens)
         e = launch_dependent(&embed_fill_kernel, dim3((unsigned)std::max(1, dev.sm_count - kSortCtas)), dim3(kSortThreads), 0, st, a);
     if (e == cudaSuccess && tokens > 0) {
         const int last = (a.passes - 1) & 1;
-        SumArgs b = {a.key[last], a.pos[last], tokens, vocab, l.chunks, dy, cols, lddy, scale, dW, lddW, accumulate,
+        SumArgs b = {a.key[last], a.pos[last], tokens, vocab, l.chunks, l.chunk, dy, cols, lddy, scale, dW, lddW, accumulate,
                      reinterpret_cast<float*>(ws + l.partial), l.ld_partial};
         const bool wide = wide_rows(dy, lddy, cols, dy_dtype) && wide_rows(dW, lddW, cols, dW_dtype);
         if (dy_dtype == MVUE_BF16)

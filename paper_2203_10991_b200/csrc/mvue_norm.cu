@@ -127,6 +127,44 @@ struct Place {
     __device__ __forceinline__ int64_t channel(int j) const { return cols.first + (int64_t)j * cols.step; }
 };
 
+// Sums over a block's rows of what its threads left per channel: the block's threads share the channels (pieces x 8) and, where
+// that leaves threads over, the rows of each.
+struct Columns {
+    int piece, j, row0, rows, step, share;     // share: threads of a channel
+    bool first;
+    __device__ __forceinline__ Columns(int pieces) {
+        const int channels = pieces * 8, k = threadIdx.x % (unsigned)channels;
+        share = kThreads / channels;
+        row0 = threadIdx.x / (unsigned)channels;
+        piece = k % (unsigned)pieces;
+        j = k / (unsigned)pieces;
+        first = row0 == 0;
+        rows = row0 < share ? kThreads / pieces : 0;
+        step = pieces;
+    }
+    // f(thread, j) for the threads of this channel, added up; the sum on all threads of the channel
+    template <typename F> __device__ __forceinline__ float2 sum(F f) const {
+        __shared__ float2 s[kThreads];
+        __syncthreads();
+        float2 t = make_float2(0.0f, 0.0f);
+        for (int r = row0; r < rows; r += share) {
+            const float2 v = f(piece + r * step, j);
+            t.x += v.x;
+            t.y += v.y;
+        }
+        s[threadIdx.x] = t;
+        __syncthreads();
+        t = make_float2(0.0f, 0.0f);
+        if (rows)
+            for (int r = 0; r < share; ++r) {
+                const float2 v = s[threadIdx.x - (row0 - r) * step * 8];
+                t.x += v.x;
+                t.y += v.y;
+            }
+        return t;
+    }
+};
+
 // ---- forward through memory: means and M2 of a chunk of rows, per channel -------------------------------------------
 template <typename T, bool kWide>
 __global__ void __launch_bounds__(kThreads) norm_stats_kernel(const __grid_constant__ NormArgs a) {
@@ -162,32 +200,26 @@ __global__ void __launch_bounds__(kThreads) norm_stats_kernel(const __grid_const
         }
         count = all;
     }
-    // join the block's rows: thread k of the first pieces * 8 has channel k
+    // join the block's rows
+    __shared__ float s_count[kThreads];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         s_mean[j * kThreads + threadIdx.x] = mean[j];
         s_m2[j * kThreads + threadIdx.x] = m2[j];
     }
-    __shared__ float s_count[kThreads];
     s_count[threadIdx.x] = count;
-    __syncthreads();
-    for (int k = threadIdx.x; k < a.pieces * 8; k += kThreads) {
-        const int piece = k % a.pieces, j = k / a.pieces;
-        float total = 0.0f, sum = 0.0f, dev = 0.0f;
-        for (int t = piece; t < p.stride * a.pieces; t += a.pieces) {
-            total += s_count[t];
-            sum = fmaf(s_count[t], s_mean[j * kThreads + t], sum);
-        }
-        if (total == 0.0f) continue;
-        const float m = sum / total;
-        for (int t = piece; t < p.stride * a.pieces; t += a.pieces) {
-            const float d = s_mean[j * kThreads + t] - m;
-            dev += fmaf(s_count[t] * d, d, s_m2[j * kThreads + t]);
-        }
-        const Cols<kWide> mine(p.slab0, a.c, piece, a.pieces);
-        if (j < mine.count)
-            a.partial[(n * a.chunks + blockIdx.y) * a.c + mine.first + (int64_t)j * mine.step] = make_float2(m, dev);
-    }
+    const Columns col(a.pieces);
+    const float2 t = col.sum([&](int thread, int j) {
+        return make_float2(s_count[thread] * s_mean[j * kThreads + thread], s_count[thread]);
+    });
+    const float m = t.y > 0.0f ? t.x / t.y : 0.0f;
+    const float2 dev = col.sum([&](int thread, int j) {
+        const float d = s_mean[j * kThreads + thread] - m;
+        return make_float2(fmaf(s_count[thread] * d, d, s_m2[j * kThreads + thread]), 0.0f);
+    });
+    const Cols<kWide> mine(p.slab0, a.c, col.piece, a.pieces);
+    if (col.first && col.j < mine.count)
+        a.partial[(n * a.chunks + blockIdx.y) * a.c + mine.first + (int64_t)col.j * mine.step] = make_float2(m, dev.x);
 }
 
 __device__ __forceinline__ float warp_sum(float x) {
@@ -347,19 +379,12 @@ __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_c
         s_a[j * kThreads + threadIdx.x] = sum[j];
         s_b[j * kThreads + threadIdx.x] = along[j];
     }
-    __syncthreads();
-    for (int k = threadIdx.x; k < a.pieces * 8; k += kThreads) {
-        const int piece = k % a.pieces, j = k / a.pieces;
-        float ta = 0.0f, tb = 0.0f;
-        for (int t = piece; t < p.stride * a.pieces; t += a.pieces) {
-            ta += s_a[j * kThreads + t];
-            tb += s_b[j * kThreads + t];
-        }
-        const Cols<kWide> mine(p.slab0, a.c, piece, a.pieces);
-        if (j < mine.count) {
-            const int64_t c = mine.first + (int64_t)j * mine.step;
-            a.partial[(n * a.chunks + blockIdx.y) * a.c + c] = make_float2(ta, tb * a.rstd[n * a.groups + c / a.group_size]);
-        }
+    const Columns col(a.pieces);
+    const float2 t = col.sum([&](int thread, int j) { return make_float2(s_a[j * kThreads + thread], s_b[j * kThreads + thread]); });
+    const Cols<kWide> mine(p.slab0, a.c, col.piece, a.pieces);
+    if (col.first && col.j < mine.count) {
+        const int64_t c = mine.first + (int64_t)col.j * mine.step;
+        a.partial[(n * a.chunks + blockIdx.y) * a.c + c] = make_float2(t.x, t.y * a.rstd[n * a.groups + c / a.group_size]);
     }
 }
 
