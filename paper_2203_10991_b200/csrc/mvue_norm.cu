@@ -1216,7 +1216,8 @@ struct Split {
     int pieces, slabs;
     int64_t rows, chunks;
 };
-// Blocks of 256 threads, up to 32 along the channels: enough chunks of rows for six blocks on each of 148 SMs, but no
+// Blocks of 256 threads, up to 32 along the channels: as many chunks of rows as two blocks on each of 148 SMs take (six were
+// slower, 34 us against 28 us on 3 x 11811 x 320 fp32: every block joins its threads' sums at its end), but no
 // fewer rows than every thread has in flight at once.
 Split split_of(int64_t n, int64_t s, int64_t c) {
     Split p;
@@ -1224,7 +1225,7 @@ Split split_of(int64_t n, int64_t s, int64_t c) {
     p.slabs = (int)((all + kMaxPieces - 1) / kMaxPieces);
     p.pieces = (int)((all + p.slabs - 1) / p.slabs);
     const int64_t least = (int64_t)(kThreads / p.pieces) * kRowsAhead;
-    const int64_t want = (6 * 148 + n * p.slabs - 1) / std::max<int64_t>(1, n * p.slabs);
+    const int64_t want = 2 * 148 / std::max<int64_t>(1, n * p.slabs);
     p.chunks = std::max<int64_t>(1, std::min({want, (s + least - 1) / least, (int64_t)65535}));
     p.rows = (s + p.chunks - 1) / p.chunks;
     p.chunks = (s + p.rows - 1) / p.rows;
