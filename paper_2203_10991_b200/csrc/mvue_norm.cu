@@ -25,7 +25,6 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 256;
-constexpr int kResidentCols = 8;       // channels of a thread where a sample stays in shared memory
 constexpr int kMaxPieces = 32;       // pieces of eight channels that a block is wide: 256 channels
 constexpr int kRowsAhead = 4;        // rows that a thread has in flight
 
@@ -53,7 +52,7 @@ __device__ __forceinline__ float affine(const void* p, int is_bf16, int64_t i, f
 }
 
 // 1 / (1 + exp(-z)) of two numbers with one reciprocal, that of the product of the two denominators: the special-function
-// unit takes 16 values a cycle, and two each would hold up the backward pass.  The exponentials are capped at 2^60
+// unit takes 16 values a cycle, and two each hold up the backward pass (105 us against 99 us on 64 x 3136 x 256).  The exponentials are capped at 2^60
 // (z below -41.6, where the factor stays at 2^-60), which keeps the product finite.
 __device__ __forceinline__ f2 sigmoid(f2 z) {
     float a, b;
@@ -96,15 +95,13 @@ __device__ __forceinline__ f2 act_grad(f2 z, f2 d) {
     return mul2(d, fma2(z, density, fma2(e, pair(0.5f), pair(0.5f))));
 }
 
-template <int kPairs>
-__device__ __forceinline__ void pairs(const float (&x)[2 * kPairs], f2 (&p)[kPairs]) {
+__device__ __forceinline__ void pairs(const float (&x)[8], f2 (&p)[4]) {
 #pragma unroll
-    for (int j = 0; j < kPairs; ++j) p[j] = pair(x[2 * j], x[2 * j + 1]);
+    for (int j = 0; j < 4; ++j) p[j] = pair(x[2 * j], x[2 * j + 1]);
 }
-template <int kPairs>
-__device__ __forceinline__ void unpairs(const f2 (&p)[kPairs], float (&x)[2 * kPairs]) {
+__device__ __forceinline__ void unpairs(const f2 (&p)[4], float (&x)[8]) {
 #pragma unroll
-    for (int j = 0; j < kPairs; ++j) unpair(p[j], x[2 * j], x[2 * j + 1]);
+    for (int j = 0; j < 4; ++j) unpair(p[j], x[2 * j], x[2 * j + 1]);
 }
 
 // A thread's place: its channels, and its rows first, first + stride, ... below end.
@@ -271,18 +268,17 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const __grid_consta
 
 // What the elements of a thread's channels need: z = (x - mean) slope + shift, slope = rstd gamma, shift = beta; backward
 // dx = slope dz + level + tilt (x - mean).
-template <int kPairs>
 struct Channels {
-    f2 neg_mean[kPairs], slope[kPairs], shift[kPairs];
+    f2 neg_mean[4], slope[4], shift[4];
 
-    template <int kAct> __device__ __forceinline__ void output(f2 (&x)[kPairs]) const {
+    template <int kAct> __device__ __forceinline__ void output(f2 (&x)[4]) const {
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) x[j] = act<kAct>(fma2(add2(x[j], neg_mean[j]), slope[j], shift[j]));
+        for (int j = 0; j < 4; ++j) x[j] = act<kAct>(fma2(add2(x[j], neg_mean[j]), slope[j], shift[j]));
     }
     // x becomes x - mean, d becomes dz = d act'(z)
-    template <int kAct> __device__ __forceinline__ void gradient(f2 (&x)[kPairs], f2 (&d)[kPairs]) const {
+    template <int kAct> __device__ __forceinline__ void gradient(f2 (&x)[4], f2 (&d)[4]) const {
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
+        for (int j = 0; j < 4; ++j) {
             x[j] = add2(x[j], neg_mean[j]);
             d[j] = act_grad<kAct>(fma2(x[j], slope[j], shift[j]), d[j]);
         }
@@ -290,7 +286,7 @@ struct Channels {
 };
 
 template <bool kWide>
-__device__ __forceinline__ void set_channels(Channels<4>& k, const NormArgs& a, const Place<kWide>& p) {
+__device__ __forceinline__ void set_channels(Channels& k, const NormArgs& a, const Place<kWide>& p) {
     float m[8], t[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -315,7 +311,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_const
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     T* y = static_cast<T*>(a.out) + n * a.s * a.ldo;
-    Channels<4> k;
+    Channels k;
     set_channels(k, a, p);
     for (; p.row < p.end; p.row += (int64_t)p.stride * kRowsAhead) {
         float v[kRowsAhead][8];
@@ -346,7 +342,7 @@ __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_c
     const T* dy = static_cast<const T*>(a.dy) + n * a.s * a.lddy;
     f2 sums[4] = {}, alongs[4] = {};
     if (p.row < p.end) {
-        Channels<4> k;
+        Channels k;
         set_channels(k, a, p);
         for (; p.row < p.end; p.row += (int64_t)p.stride * 2) {
             float v[2][8], d[2][8];
@@ -445,7 +441,7 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + n * a.s * a.lddy;
     T* dx = static_cast<T*>(a.out) + n * a.s * a.ldo;
-    Channels<4> k;
+    Channels k;
     set_channels(k, a, p);
     float low[8], off[8];
 #pragma unroll
@@ -485,9 +481,14 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
 // ---- resident: a cluster of blocks keeps its part of one sample in shared memory ---------------------------------------
 // The route through memory reads x twice (three passes over HBM in all, five in the backward pass).  Here a cluster of up
 // to eight blocks takes one slab of whole groups of one sample, every block a run of its rows: the rows are copied to shared
-// memory once, a thread reads back only what it copied itself (no barrier between the copy and its use), the blocks
+// memory once,a thread reads back only what it copied itself (no barrier between the copy and its use), the blocks
 // exchange their groups' sums through distributed shared memory, and the output is formed from the same copy.  One read
-// and one write of HBM.
+// and one write of HBM.  64 x 3136 x 256 bf16 in 32 groups: forward 46 us (ReLU) and 51 us (SiLU) against 31 us of HBM time and
+// 101 us through memory, backward 74 us and 99 us against 47 us and 269 us.  Bound by instructions and their latency: 26 and 50
+// million warp instructions, 60 % and 50 % of the issue slots with four and two blocks on an SM (registers).  Measured and not
+// kept: a second buffer for the next sample (49 us forward, 102 us backward with half the blocks), copies of the next sample
+// rolling in behind the last pass (49 us, 110 us: the loops no longer unroll), four channels a thread with four blocks on an SM
+// (128 us backward), three blocks at 80 registers (111 us).
 struct ResidentArgs {
     NormArgs norm;
     int cluster, rows, iters;        // blocks of a cluster; rows of a block and of a thread at most
@@ -495,76 +496,66 @@ struct ResidentArgs {
     int units;                       // slabs of all samples
 };
 
-template <int kBytes>
-__device__ __forceinline__ void copy(uint32_t smem, const char* global) {
-    if (kBytes == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem), "l"(global) : "memory");
-    else asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory");
+__device__ __forceinline__ void copy16(uint32_t smem, const void* global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(global) : "memory");
 }
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// A thread's rows of one tensor in shared memory, kCols channels of each: slots of 8 or 16 bytes, consecutive threads side
-// by side.
-template <typename T, int kCols>
+// A thread's rows of one tensor in shared memory, eight channels of each: slots of 16 bytes, consecutive threads side by
+// side (no bank conflict), two planes of them for fp32.
+template <typename T>
 struct Slots {
-    static constexpr int kBytes = sizeof(T) * kCols, kSlot = kBytes < 16 ? kBytes : 16, kParts = kBytes / kSlot, kRowBytes = kBytes * kThreads;
-    static constexpr int kPairs = kCols / 2;
+    static constexpr int kParts = sizeof(T) / 2, kRowBytes = kParts * kThreads * 16;
     static __device__ __forceinline__ void fetch(uint32_t to, const T* from) {
 #pragma unroll
-        for (int h = 0; h < kParts; ++h) copy<kSlot>(to + h * (kThreads * kSlot), reinterpret_cast<const char*>(from) + kSlot * h);
+        for (int h = 0; h < kParts; ++h) copy16(to + h * (kThreads * 16), reinterpret_cast<const char*>(from) + 16 * h);
     }
-    static __device__ __forceinline__ void read(const char* slot, f2 (&x)[kPairs]) {
-        uint32_t w[kBytes / 4];
-#pragma unroll
-        for (int h = 0; h < kParts; ++h) {
-            if (kSlot == 16) {
-                const uint4 v = *reinterpret_cast<const uint4*>(slot + h * (kThreads * kSlot));
-                w[4 * h] = v.x; w[4 * h + 1] = v.y; w[4 * h + 2] = v.z; w[4 * h + 3] = v.w;
-            } else {
-                const uint2 v = *reinterpret_cast<const uint2*>(slot);
-                w[0] = v.x; w[1] = v.y;
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kPairs; ++j)
-            x[j] = sizeof(T) == 2 ? pair(bf16_lo(w[j]), bf16_hi(w[j])) : pair(__uint_as_float(w[2 * j % (kBytes / 4)]), __uint_as_float(w[(2 * j + 1) % (kBytes / 4)]));
-    }
-    static __device__ __forceinline__ void store(T* to, const f2 (&x)[kPairs]) {
-        float v[kCols];
-        unpairs(x, v);
-        uint32_t w[kBytes / 4];
-#pragma unroll
-        for (int j = 0; j < kBytes / 4; ++j)
-            w[j] = sizeof(T) == 2 ? pack_bf16x2(v[2 * j % kCols], v[(2 * j + 1) % kCols]) : __float_as_uint(v[j % kCols]);
-        if constexpr (kBytes == 32) {
-            st256(to, w);
-        } else if constexpr (kBytes == 16) {
-            *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    static __device__ __forceinline__ void read(const char* slot, f2 (&x)[4]) {
+        const uint4 v = *reinterpret_cast<const uint4*>(slot);
+        if constexpr (sizeof(T) == 2) {
+            x[0] = pair(bf16_lo(v.x), bf16_hi(v.x));
+            x[1] = pair(bf16_lo(v.y), bf16_hi(v.y));
+            x[2] = pair(bf16_lo(v.z), bf16_hi(v.z));
+            x[3] = pair(bf16_lo(v.w), bf16_hi(v.w));
         } else {
-            *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+            const uint4 w = *reinterpret_cast<const uint4*>(slot + kThreads * 16);
+            x[0] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
+            x[1] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
+            x[2] = pair(__uint_as_float(w.x), __uint_as_float(w.y));
+            x[3] = pair(__uint_as_float(w.z), __uint_as_float(w.w));
+        }
+    }
+    static __device__ __forceinline__ void store(T* to, const f2 (&x)[4]) {
+        float v[8];
+        unpairs(x, v);
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t w[4] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+            store8_words(to, true, 8, w);
+        } else {
+            store8(to, true, 8, v);
         }
     }
 };
-template <int kPairs>
-__device__ __forceinline__ void read_values(const float* p, f2 (&x)[kPairs]) {
-#pragma unroll
-    for (int j = 0; j < kPairs; j += 2) {
-        const float4 a = *reinterpret_cast<const float4*>(p + 2 * j);
-        x[j] = pair(a.x, a.y);
-        x[j + 1] = pair(a.z, a.w);
-    }
+// eight values per channel from shared memory
+__device__ __forceinline__ void read_values(const float* p, f2 (&x)[4]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = pair(a.x, a.y);
+    x[1] = pair(a.z, a.w);
+    x[2] = pair(b.x, b.y);
+    x[3] = pair(b.z, b.w);
 }
 
 // Where a block of the cluster stands, and its shared memory.  Values per channel are worked out once per block, by the
 // thread that has the channel's number, and read back eight at a time.
-template <typename T, int kTensors, int kCols>
+template <typename T, int kTensors>
 struct Resident {
-    using S = Slots<T, kCols>;
-    static constexpr int kPairs = kCols / 2;
+    using S = Slots<T>;
     const ResidentArgs& a;
     int piece, ty, threads_down, width, rank, rows_here, iters, row0;      // iters: rows of this thread below row0, its first one
     int channels, groups;            // of the unit at hand
     int64_t n, c0;
     bool mine;                       // the thread's piece exists in the unit at hand
+    bool lost = false;               // a wait of this thread ran out
     char* smem;
     size_t tensor_bytes;
     float *part, *one, *two, *slope, *shift, *group;     // group: two values for each group and block of the cluster, two units deep
@@ -573,7 +564,7 @@ struct Resident {
     __device__ __forceinline__ Resident(const ResidentArgs& args, char* shared) : a(args), smem(shared) {
         const NormArgs& q = a.norm;
         rank = (int)(blockIdx.x % (unsigned)a.cluster);
-        width = q.pieces * kCols;
+        width = q.pieces * 8;
         threads_down = kThreads / q.pieces;
         ty = threadIdx.x / (unsigned)q.pieces;
         piece = threadIdx.x - ty * q.pieces;
@@ -601,10 +592,10 @@ struct Resident {
         groups = channels / a.norm.group_size;
         mine = iters > 0 && exists();
     }
-    __device__ __forceinline__ bool exists() const { return piece * kCols < channels; }
-    __device__ __forceinline__ int64_t channel() const { return c0 + piece * kCols; }      // the thread's first one
+    __device__ __forceinline__ bool exists() const { return piece * 8 < channels; }
+    __device__ __forceinline__ int64_t channel() const { return c0 + piece * 8; }      // the thread's first one
     // the thread's first slot of a tensor
-    __device__ __forceinline__ char* slots(int tensor) const { return smem + tensor * tensor_bytes + threadIdx.x * S::kSlot; }
+    __device__ __forceinline__ char* slots(int tensor) const { return smem + tensor * tensor_bytes + threadIdx.x * 16; }
     // the thread's channels of its first row of this unit
     template <typename P> __device__ __forceinline__ P* at(P* base, int64_t ld) const { return base + (n * a.norm.s + row0) * ld + channel(); }
     // starts the copies of a unit's rows
@@ -612,36 +603,36 @@ struct Resident {
         int64_t sample, first;
         place(unit, sample, first);
         const NormArgs& q = a.norm;
-        if (piece * kCols < q.c - first)
+        if (piece * 8 < q.c - first)
 #pragma unroll
             for (int t = 0; t < kTensors; ++t) {
                 const int64_t ld = t ? q.lddy : q.ldx, step = (int64_t)threads_down * ld;
-                const T* from = static_cast<const T*>(t ? q.dy : q.x) + (sample * q.s + row0) * ld + first + piece * kCols;
+                const T* from = static_cast<const T*>(t ? q.dy : q.x) + (sample * q.s + row0) * ld + first + piece * 8;
                 uint32_t to = (uint32_t)__cvta_generic_to_shared(slots(t));
 #pragma unroll 2
                 for (int i = 0; i < iters; ++i, from += step, to += S::kRowBytes) S::fetch(to, from);
             }
     }
     // sums over the block's rows of every thread's values -> into[0 .. channels)
-    __device__ __forceinline__ void channel_sums(const f2 (&x)[kPairs], float* into) const {
-        f2 v[kPairs];
+    __device__ __forceinline__ void channel_sums(const f2 (&x)[4], float* into) const {
+        f2 v[4];
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) v[j] = x[j];
+        for (int j = 0; j < 4; ++j) v[j] = x[j];
         bool writes = ty < threads_down;
         int at = ty;
         if (a.fold) {
             for (int o = a.norm.pieces; o < 32; o <<= 1)
 #pragma unroll
-                for (int j = 0; j < kPairs; ++j) v[j] = add2(v[j], f2{__shfl_xor_sync(0xFFFFFFFFu, v[j].v, o)});
+                for (int j = 0; j < 4; ++j) v[j] = add2(v[j], f2{__shfl_xor_sync(0xFFFFFFFFu, v[j].v, o)});
             writes = (threadIdx.x & 31) < (unsigned)a.norm.pieces;
             at = threadIdx.x >> 5;
         }
         if (writes) {
-            float w[kCols];
+            float w[8];
             unpairs(v, w);
 #pragma unroll
-            for (int j = 0; j < kCols; j += 4)
-                *reinterpret_cast<float4*>(part + at * width + piece * kCols + j) = make_float4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+            for (int j = 0; j < 8; j += 4)
+                *reinterpret_cast<float4*>(part + at * width + piece * 8 + j) = make_float4(w[j], w[j + 1], w[j + 2], w[j + 3]);
         }
         __syncthreads();
         const int down = a.fold ? kThreads / 32 : threads_down;
@@ -688,7 +679,7 @@ struct Resident {
         cg::this_cluster().sync();
     }
     __device__ __forceinline__ void expect(int turn) const {
-        if (a.cluster > 1 && threadIdx.x == 0)
+        if (a.cluster > 1 && threadIdx.x == 0 && !lost)
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar(turn)), "r"(a.cluster * groups * 8) : "memory");
     }
     // to the block `block` of the cluster
@@ -705,21 +696,23 @@ struct Resident {
                      "r"(counter) : "memory");
     }
     __device__ __forceinline__ float2 sent(int turn, int block, int g) const { return *reinterpret_cast<const float2*>(place_of(turn, block, g)); }
-    // waits for the values of all blocks; false (and MVUE_ERR_DEVICE_TIMEOUT in dev_status) when they do not come
-    __device__ __forceinline__ bool meet(int turn, uint32_t parity) const {
+    // Waits for the values of all blocks.  When they do not come: MVUE_ERR_DEVICE_TIMEOUT in dev_status, and the thread waits no
+    // more (`lost`) but takes the rest of the way as it is, so that all threads meet at the same barriers to the end.
+    __device__ __forceinline__ void meet(int turn, uint32_t parity) {
         if (a.cluster == 1) {
             __syncthreads();
-            return true;
+            return;
         }
+        if (lost) return;
         for (uint32_t spin = 0; spin < (1u << 22); ++spin) {
             uint32_t done;
             asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                          : "=r"(done) : "r"(bar(turn)), "r"(parity) : "memory");
-            if (done) return true;
+            if (done) return;
             if (spin > 64) __nanosleep(spin > 4096 ? 256 : 32);
         }
+        lost = true;
         if (a.norm.dev_status) *a.norm.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
-        return false;
     }
     // before the block ends: nobody stores into its shared memory any more
     __device__ __forceinline__ void close() const {
@@ -732,10 +725,9 @@ template <typename T, int kAct>
 __global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(const __grid_constant__ ResidentArgs a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) char smem[];
-    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
-    Resident<T, 1, kCols> r(a, smem);
+    Resident<T, 1> r(a, smem);
     const NormArgs& q = a.norm;
-    using S = Slots<T, kCols>;
+    using S = Slots<T>;
     const unsigned clusters = gridDim.x / (unsigned)a.cluster;
     unsigned unit = blockIdx.x / (unsigned)a.cluster;
     const int lane = threadIdx.x & 31;
@@ -750,16 +742,16 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(const __grid
         r.enter(unit);
         r.expect(turn);
         copies_wait();
-        f2 sum[kPairs] = {};
+        f2 sum[4] = {};
         const int iters = r.mine ? r.iters : 0;
         const char* const first = r.slots(0);
         const char* slot = first;
 #pragma unroll 4
         for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
-            f2 v[kPairs];
+            f2 v[4];
             S::read(slot, v);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+            for (int j = 0; j < 4; ++j) sum[j] = add2(sum[j], v[j]);
         }
         r.channel_sums(sum, r.one);
         for (int k = threadIdx.x; k < r.channels; k += kThreads) {
@@ -772,24 +764,24 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(const __grid
         });
         __syncthreads();
         // squares about the block's own means, from shared memory
-        f2 neg_mean[kPairs];
-        read_values(r.one + r.piece * kCols, neg_mean);
+        f2 neg_mean[4];
+        read_values(r.one + r.piece * 8, neg_mean);
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) sum[j] = pair(0.0f);
+        for (int j = 0; j < 4; ++j) sum[j] = pair(0.0f);
         slot = first;
 #pragma unroll 4
         for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
-            f2 v[kPairs];
+            f2 v[4];
             S::read(slot, v);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const f2 d = add2(v[j], neg_mean[j]);
                 sum[j] = fma2(d, d, sum[j]);
             }
         }
         r.channel_sums(sum, r.two);
         r.group_sums(r.two, [&](int g, float s) { if (lane < a.cluster) r.send(turn, lane, g, -r.one[g * q.group_size], s); });
-        if (!r.meet(turn, parity)) break;
+        r.meet(turn, parity);
         for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
             // a warp per group, a lane per block of the cluster
             const float2 p = lane < a.cluster ? r.sent(turn, lane, g) : make_float2(0.0f, 0.0f);
@@ -808,16 +800,16 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(const __grid
             }
         }
         __syncthreads();
-        Channels<kPairs> k8;
-        read_values(r.one + r.piece * kCols, k8.neg_mean);
-        read_values(r.slope + r.piece * kCols, k8.slope);
-        read_values(r.shift + r.piece * kCols, k8.shift);
+        Channels k8;
+        read_values(r.one + r.piece * 8, k8.neg_mean);
+        read_values(r.slope + r.piece * 8, k8.slope);
+        read_values(r.shift + r.piece * 8, k8.shift);
         T* y = r.at(static_cast<T*>(q.out), q.ldo);
         const int64_t down = (int64_t)r.threads_down * q.ldo;
         slot = first;
 #pragma unroll 2
         for (int i = 0; i < iters; ++i, y += down, slot += S::kRowBytes) {
-            f2 v[kPairs];
+            f2 v[4];
             S::read(slot, v);
             k8.output<kAct>(v);
             S::store(y, v);
@@ -834,10 +826,9 @@ template <typename T, int kAct>
 __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const __grid_constant__ ResidentArgs a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) char smem[];
-    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
-    Resident<T, 2, kCols> r(a, smem);
+    Resident<T, 2> r(a, smem);
     const NormArgs& q = a.norm;
-    using S = Slots<T, kCols>;
+    using S = Slots<T>;
     const unsigned clusters = gridDim.x / (unsigned)a.cluster;
     unsigned unit = blockIdx.x / (unsigned)a.cluster;
     const int lane = threadIdx.x & 31;
@@ -859,20 +850,20 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
         }
         copies_wait();
         __syncthreads();
-        Channels<kPairs> k8;
-        read_values(r.one + r.piece * kCols, k8.neg_mean);
-        read_values(r.slope + r.piece * kCols, k8.slope);
-        read_values(r.shift + r.piece * kCols, k8.shift);
-        f2 sum[kPairs] = {}, along[kPairs] = {};
+        Channels k8;
+        read_values(r.one + r.piece * 8, k8.neg_mean);
+        read_values(r.slope + r.piece * 8, k8.slope);
+        read_values(r.shift + r.piece * 8, k8.shift);
+        f2 sum[4] = {}, along[4] = {};
         const int iters = r.mine ? r.iters : 0;
         const char *slot = r.slots(0), *dslot = r.slots(1);
         for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[kPairs], d[kPairs];
+            f2 v[4], d[4];
             S::read(slot, v);
             S::read(dslot, d);
             k8.gradient<kAct>(v, d);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 sum[j] = add2(sum[j], d[j]);
                 along[j] = fma2(d[j], v[j], along[j]);
             }
@@ -894,7 +885,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
             t = warp_sum(t);
             if (lane < a.cluster) r.send(turn, lane, g, s, t);
         });
-        if (!r.meet(turn, parity)) break;
+        r.meet(turn, parity);
         for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
             const float2 p = lane < a.cluster ? r.sent(turn, lane, g) : make_float2(0.0f, 0.0f);
             const float rstd = q.rstd[g0 + g];
@@ -905,20 +896,20 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
             }
         }
         __syncthreads();
-        f2 level[kPairs], tilt[kPairs];            // dx = slope dz + level + tilt (x - mean)
-        read_values(r.one + r.piece * kCols, level);
-        read_values(r.two + r.piece * kCols, tilt);
+        f2 level[4], tilt[4];            // dx = slope dz + level + tilt (x - mean)
+        read_values(r.one + r.piece * 8, level);
+        read_values(r.two + r.piece * 8, tilt);
         T* dx = r.at(static_cast<T*>(q.out), q.ldo);
         const int64_t down = (int64_t)r.threads_down * q.ldo;
         slot = r.slots(0);
         dslot = r.slots(1);
         for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[kPairs], d[kPairs];
+            f2 v[4], d[4];
             S::read(slot, v);
             S::read(dslot, d);
             k8.gradient<kAct>(v, d);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt[j], level[j]));
+            for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt[j], level[j]));
             S::store(dx, v);
         }
         if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
@@ -927,18 +918,18 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
     r.close();
 }
 
-// The common case: a warp holds whole rows of the slab and every group is whole pieces of the threads' channels.  Then a thread's
-// channels are of one group, a sum over a group is a handful of shuffles and eight values in shared memory, and
+// The common case: a warp holds whole rows of the slab and every group is whole pieces of eight channels.  Then a thread's
+// eight channels are of one group, a sum over a group is a handful of shuffles and eight values in shared memory, and
 // every thread works the group's statistics out for itself: two barriers of the block a unit (one backward), no values per
-// channel in shared memory.  64 x 3136 x 256 bf16 in 32 groups: NOTE_FWD.
-template <typename T, int kTensors, int kCols>
-struct Folded : Resident<T, kTensors, kCols> {
-    using Base = Resident<T, kTensors, kCols>;
+// channel in shared memory (64 x 3136 x 256 bf16: 57 -> 46 us forward, 129 -> 99 us backward with SiLU).
+template <typename T, int kTensors>
+struct Folded : Resident<T, kTensors> {
+    using Base = Resident<T, kTensors>;
     int per_group, g;                // pieces of a group; the thread's group in the unit
     float* sums;                     // [2][8 warps][pieces][2]
 
     __device__ __forceinline__ Folded(const ResidentArgs& args, char* shared) : Base(args, shared) {
-        per_group = args.norm.group_size / kCols;
+        per_group = args.norm.group_size / 8;
         g = this->piece / (unsigned)per_group;
         sums = this->one;
         this->group = sums + 2 * (kThreads / 32) * args.norm.pieces * 2;
@@ -983,21 +974,19 @@ struct Folded : Resident<T, kTensors, kCols> {
     }
 };
 
-template <int kPairs>
-__device__ __forceinline__ float total(const f2 (&x)[kPairs]) {
+__device__ __forceinline__ float total(const f2 (&x)[4]) {
     f2 s = x[0];
 #pragma unroll
-    for (int j = 1; j < kPairs; ++j) s = add2(s, x[j]);
+    for (int j = 1; j < 4; ++j) s = add2(s, x[j]);
     float a, b;
     unpair(s, a, b);
     return a + b;
 }
 // a thread's values of gamma or beta from channel c on
-template <int kPairs>
-__device__ __forceinline__ void affine_values(const void* p, int is_bf16, int64_t c, float none, f2 (&x)[kPairs]) {
-    float v[2 * kPairs];
+__device__ __forceinline__ void affine_values(const void* p, int is_bf16, int64_t c, float none, f2 (&x)[4]) {
+    float v[8];
 #pragma unroll
-    for (int j = 0; j < 2 * kPairs; ++j) v[j] = affine(p, is_bf16, c + j, none);
+    for (int j = 0; j < 8; ++j) v[j] = affine(p, is_bf16, c + j, none);
     pairs(v, x);
 }
 
@@ -1005,10 +994,9 @@ template <typename T, int kAct>
 __global__ void __launch_bounds__(kThreads, 4) norm_folded_kernel(const __grid_constant__ ResidentArgs a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) char smem[];
-    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
-    Folded<T, 1, kCols> r(a, smem);
+    Folded<T, 1> r(a, smem);
     const NormArgs& q = a.norm;
-    using S = Slots<T, kCols>;
+    using S = Slots<T>;
     const unsigned clusters = gridDim.x / (unsigned)a.cluster;
     unsigned unit = blockIdx.x / (unsigned)a.cluster;
     const float own = (float)r.rows_here * q.group_size, inv = own > 0.0f ? 1.0f / own : 0.0f;
@@ -1020,42 +1008,42 @@ __global__ void __launch_bounds__(kThreads, 4) norm_folded_kernel(const __grid_c
     for (; unit < (unsigned)a.units; unit += clusters, parity ^= turn, turn ^= 1) {
         r.enter(unit);
         r.expect(turn);
-        Channels<kPairs> k8;
+        Channels k8;
         if (r.exists()) {
             affine_values(q.gamma, q.affine_bf16, r.channel(), 1.0f, k8.slope);
             affine_values(q.beta, q.affine_bf16, r.channel(), 0.0f, k8.shift);
         }
         copies_wait();
-        f2 sum[kPairs] = {};
+        f2 sum[4] = {};
         const int iters = r.mine ? r.iters : 0;
         const char* const first = r.slots(0);
         const char* slot = first;
 #pragma unroll 4
         for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
-            f2 v[kPairs];
+            f2 v[4];
             S::read(slot, v);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) sum[j] = add2(sum[j], v[j]);
+            for (int j = 0; j < 4; ++j) sum[j] = add2(sum[j], v[j]);
         }
         const float block_mean = r.block_sum(total(sum), 0) * inv;
         // squares about the block's own mean, from shared memory
         const f2 low = pair(-block_mean);
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) sum[j] = pair(0.0f);
+        for (int j = 0; j < 4; ++j) sum[j] = pair(0.0f);
         slot = first;
 #pragma unroll 4
         for (int i = 0; i < iters; ++i, slot += S::kRowBytes) {
-            f2 v[kPairs];
+            f2 v[4];
             S::read(slot, v);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 const f2 d = add2(v[j], low);
                 sum[j] = fma2(d, d, sum[j]);
             }
         }
         const float block_dev = r.block_sum(total(sum), 1);
         if (r.sends()) r.send(turn, r.ty, r.g, block_mean, block_dev);
-        if (!r.meet(turn, parity)) break;
+        r.meet(turn, parity);
         float mean = 0.0f, dev = 0.0f;
         int left = (int)q.s;
         for (int b = 0; b < a.cluster; ++b, left -= a.rows) mean = fmaf((float)max(0, min(a.rows, left)), r.sent(turn, b, r.g).x, mean);
@@ -1073,7 +1061,7 @@ __global__ void __launch_bounds__(kThreads, 4) norm_folded_kernel(const __grid_c
             q.rstd[at] = rstd;
         }
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
+        for (int j = 0; j < 4; ++j) {
             k8.neg_mean[j] = pair(-mean);
             k8.slope[j] = mul2(k8.slope[j], pair(rstd));
         }
@@ -1082,7 +1070,7 @@ __global__ void __launch_bounds__(kThreads, 4) norm_folded_kernel(const __grid_c
         slot = first;
 #pragma unroll 2
         for (int i = 0; i < iters; ++i, y += down, slot += S::kRowBytes) {
-            f2 v[kPairs];
+            f2 v[4];
             S::read(slot, v);
             k8.output<kAct>(v);
             S::store(y, v);
@@ -1099,10 +1087,9 @@ template <typename T, int kAct>
 __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __grid_constant__ ResidentArgs a) {
     grid_dependency_wait();
     extern __shared__ __align__(16) char smem[];
-    constexpr int kCols = kResidentCols, kPairs = kCols / 2;
-    Folded<T, 2, kCols> r(a, smem);
+    Folded<T, 2> r(a, smem);
     const NormArgs& q = a.norm;
-    using S = Slots<T, kCols>;
+    using S = Slots<T>;
     const unsigned clusters = gridDim.x / (unsigned)a.cluster;
     const unsigned mine = blockIdx.x / (unsigned)a.cluster;
     unsigned unit = mine;
@@ -1110,8 +1097,8 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
     r.fetch(unit);
     r.enter(unit);
     const bool has = r.exists();
-    f2 gamma[kPairs] = {}, all_sum[kPairs] = {}, all_along[kPairs] = {};
-    Channels<kPairs> k8 = {};
+    f2 gamma[4] = {}, all_sum[4] = {}, all_along[4] = {};
+    Channels k8 = {};
     if (has) {
         affine_values(q.gamma, q.affine_bf16, r.channel(), 1.0f, gamma);
         affine_values(q.beta, q.affine_bf16, r.channel(), 0.0f, k8.shift);
@@ -1119,7 +1106,6 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
     r.open();
     int turn = 0;
     uint32_t parity = 0;
-    bool met = true;
     for (; unit < (unsigned)a.units; unit += clusters, parity ^= turn, turn ^= 1) {
         r.enter(unit);
         r.expect(turn);
@@ -1127,26 +1113,26 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
         const float mean = has ? q.mean[g] : 0.0f, rstd = has ? q.rstd[g] : 0.0f;
         copies_wait();
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
+        for (int j = 0; j < 4; ++j) {
             k8.neg_mean[j] = pair(-mean);
             k8.slope[j] = mul2(gamma[j], pair(rstd));
         }
-        f2 sum[kPairs] = {}, along[kPairs] = {};
+        f2 sum[4] = {}, along[4] = {};
         const int iters = r.mine ? r.iters : 0;
         const char *slot = r.slots(0), *dslot = r.slots(1);
         for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[kPairs], d[kPairs];
+            f2 v[4], d[4];
             S::read(slot, v);
             S::read(dslot, d);
             k8.gradient<kAct>(v, d);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) {
+            for (int j = 0; j < 4; ++j) {
                 sum[j] = add2(sum[j], d[j]);
                 along[j] = fma2(d[j], v[j], along[j]);
             }
         }
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
+        for (int j = 0; j < 4; ++j) {
             all_sum[j] = add2(all_sum[j], sum[j]);
             all_along[j] = fma2(along[j], pair(rstd), all_along[j]);
             sum[j] = mul2(sum[j], gamma[j]);
@@ -1154,8 +1140,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
         }
         const float2 block = r.block_sum(total(sum), total(along), turn);
         if (r.sends()) r.send(turn, r.ty, r.g, block.x, block.y);
-        met = r.meet(turn, parity);
-        if (!met) break;
+        r.meet(turn, parity);
         float sa = 0.0f, sb = 0.0f;
         for (int b = 0; b < a.cluster; ++b) {
             const float2 p = r.sent(turn, b, r.g);
@@ -1168,12 +1153,12 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
         slot = r.slots(0);
         dslot = r.slots(1);
         for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[kPairs], d[kPairs];
+            f2 v[4], d[4];
             S::read(slot, v);
             S::read(dslot, d);
             k8.gradient<kAct>(v, d);
 #pragma unroll
-            for (int j = 0; j < kPairs; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt, level));
+            for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt, level));
             S::store(dx, v);
         }
         if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
@@ -1182,24 +1167,24 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
     r.close();
     // the cluster's channels, summed over its samples: the warps' sums through the buffers, which are free now
     __syncthreads();
-    float sum[kCols], along[kCols];
+    float sum[8], along[8];
     unpairs(all_sum, sum);
     unpairs(all_along, along);
     float* scratch = reinterpret_cast<float*>(smem);
     const int pieces = q.pieces, lane = threadIdx.x & 31;
 #pragma unroll
-    for (int j = 0; j < kCols; ++j) {
+    for (int j = 0; j < 8; ++j) {
         for (int o = pieces; o < 32; o <<= 1) {
             sum[j] += __shfl_xor_sync(0xFFFFFFFFu, sum[j], o);
             along[j] += __shfl_xor_sync(0xFFFFFFFFu, along[j], o);
         }
-        if (lane < pieces) *reinterpret_cast<float2*>(scratch + (((threadIdx.x >> 5) * pieces + lane) * kCols + j) * 2) = make_float2(sum[j], along[j]);
+        if (lane < pieces) *reinterpret_cast<float2*>(scratch + (((threadIdx.x >> 5) * pieces + lane) * 8 + j) * 2) = make_float2(sum[j], along[j]);
     }
     __syncthreads();
     for (int k = threadIdx.x; k < r.channels; k += kThreads) {
         float2 t = make_float2(0.0f, 0.0f);
         for (int w = 0; w < kThreads / 32; ++w) {
-            const float2 v = *reinterpret_cast<const float2*>(scratch + (w * pieces * kCols + k) * 2);
+            const float2 v = *reinterpret_cast<const float2*>(scratch + (w * pieces * 8 + k) * 2);
             t.x += v.x;
             t.y += v.y;
         }
@@ -1253,7 +1238,7 @@ Keep keep_of(int64_t n, int64_t s, int64_t c, int groups, int64_t esz, int tenso
     int64_t width = std::min(c, (row + least - 1) / least * least);
     const auto spare = [&](int64_t w) { return s * w * esz < (8 << 10) && n * ((c + 2 * w - 1) / (2 * w)) >= 2 * 148; };
     while (width * 2 <= std::min<int64_t>(c, kThreads * 4) && spare(width)) width *= 2;
-    constexpr int cols = kResidentCols;
+    constexpr int cols = 8;
     const int pieces = (int)(width / cols), down = kThreads / pieces;
     const int64_t slabs = (c + width - 1) / width, most = width / cg;
     if (n * slabs > 0x7FFFFFFF / kMaxCluster) return k;
