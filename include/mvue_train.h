@@ -54,15 +54,15 @@ typedef struct {
  *   m' = beta1 m + (1 - beta1) g'
  *   v' = beta2 v + ((1 - beta2) g') g'
  *   param' = param (1 - lr weight_decay) - (lr / (1 - beta1^t)) * (m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
- * m' and v' with each operation rounded on its own; the param's root and quotient within 2 units in the last place, its
- * product by the decay fused with the sum.
+ * m' and v' with each operation rounded on its own; the root and the quotient within 2 units in the last place, the product
+ * by the decay fused with the sum.  (|g'| above 2^63 overflows v'.)
  * grad_scale: HOST value, 1 for none; dev_grad_scale: optional DEVICE float (a clipping factor or a loss scale's
  * inverse that the host does not know), read when the step runs.
  * state_bits: 32 or 8.  With 8 bits the new m and sqrt(v) of a block are divided by the block's new scale
  * top / 448 (top the largest magnitude; the new scale is top * fl(1/448), the factor 448 * fl(1/top), a magnitude
  * is capped at 448) and rounded to a neighbouring code at random so that the code's expectation is the value: an
  * average that moves by a thousandth per step, less than a hundredth of the distance of two codes, would otherwise never move.
- * A non-zero v keeps a code of at least the smallest.  Blocks whose largest |m| is below 2^-110 store zeros; a
+ * sqrt(v') is within one unit in the last place, the block's top rounded exactly.  A non-zero v keeps a code of at least the smallest.  Blocks whose largest |m| is below 2^-110 store zeros; a
  * non-finite value makes its block's scale NaN.
  * options: MVUE_OPT_STOCHASTIC_ROUNDING: a bf16 param without master is rounded to bf16 stochastically (as the
  * survivors of mvue_prune_opts) instead of to the nearest -- updates below half a unit in the last place then count in

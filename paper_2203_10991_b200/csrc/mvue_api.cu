@@ -84,7 +84,7 @@ using namespace mvue;
 
 extern "C" {
 
-int mvue_version(void) { return 140; }   // 1.4: prune options on the backward product that prunes its own output
+int mvue_version(void) { return 150; }   // 1.5: AdamW, embedding, group norm (mvue_train.h)
 
 const char* mvue_status_string(int status) {
     switch (status) {

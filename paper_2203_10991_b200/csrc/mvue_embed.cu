@@ -7,6 +7,12 @@
 // 32768 tokens and saves a dependent launch; (3) the sorted tokens are cut into chunks of equal length, a team adds the
 // rows of a chunk in token order and writes the sums of the ids that begin and end in it; what crosses a chunk's edge goes to
 // the workspace as a partial sum; (4) those are added in chunk order.  No atomics on data: equal inputs give equal bits.
+//
+// Measured (B200, HBM copy 6.55 TB/s).  Lookup of 16384 rows of 4096 bf16 out of 131072: 36 us against 29 us of HBM time
+// (6915 rows differ); four pieces in flight for two gave 37 us: bound by the mix of gathered reads and writes.  Gradient of
+// 32768 x 1024 bf16 into 65536 rows: 75 us against 51 us: fill 43 us (216 MB, 5 TB/s; a plain memset of as much takes 32 us;
+// bulk stores from shared memory gave the same), beside it the sort 29 us, sums 24 us (5 TB/s), joins 5 us.  8192 x 768 into
+// 50257 rows: 39 us against 26 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
