@@ -132,6 +132,16 @@ def test_empty_batch_stream_and_graph():
 
 
 @gpu
+def test_status_is_left_alone():
+    status = torch.full((1,), 7, dtype=torch.int32, device="cuda")
+    for shape in ((2, 3136, 64), (2, 20000, 64), (3, 10, 7)):
+        x = torch.randn(shape, device="cuda")
+        _, mean, rstd = binding.mvue_group_norm_act(x, 1, dev_status=status)
+        binding.mvue_group_norm_act_backward(x, x, mean, rstd, 1, dev_status=status)
+    assert int(status) == 7
+
+
+@gpu
 def test_a_bad_sample_stays_by_itself():
     x, dy, w, b = inputs(3, 40, 32, F32, F32, 5)
     clean = binding.mvue_group_norm_act(x, 4, w, b, act="relu")[0]
