@@ -96,7 +96,7 @@ MVUE_API int mvue_adamw_step(const mvue_adamw_tensor* tensors, int64_t count, co
  *           MVUE_ERR_INDEX to *dev_status (optional device int, otherwise left untouched).
  *  W        [vocab x cols], MVUE_F32 or MVUE_BF16, ldW >= cols;  out [tokens x cols], MVUE_F32 or MVUE_BF16, ldout >= cols.
  * The product is formed in binary32 and rounded once.  Rows whose base, cols and leading dimension are multiples of eight
- * elements (16 bytes of bf16, 32 of fp32) are moved in pieces of eight, others element by element. */
+ * elements (16 bytes of bf16, 32 of fp32) are moved in pieces of eight, others in pairs or element by element. */
 MVUE_API int mvue_embedding(const void* ids, int id_bits, int64_t tokens, const void* W, int w_dtype, int64_t vocab, int64_t cols,
                             int64_t ldW, float scale, void* out, int out_dtype, int64_t ldout, int* dev_status, void* stream);
 

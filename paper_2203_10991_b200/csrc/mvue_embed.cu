@@ -44,7 +44,7 @@ struct Ids {
 };
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
-template <typename TW, typename TO, bool kWide>
+template <typename TW, typename TO, int kVec>
 __global__ void __launch_bounds__(256) embed_kernel(Ids ids, int64_t tokens, const TW* __restrict__ w, int64_t vocab, int64_t cols,
                                                     int64_t ldw, float scale, TO* __restrict__ out, int64_t ldo, int* dev_status) {
     grid_dependency_wait();
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(256) embed_kernel(Ids ids, int64_t tokens, con
     out += t * ldo;
     // two pieces at a time: both loads are out before the first is used
     for (int64_t c0 = (int64_t)blockIdx.y * team * 16; c0 < cols; c0 += (int64_t)gridDim.y * team * 16) {
-        const Cols<kWide> a(c0, cols, threadIdx.x, team), b(c0 + team * 8, cols, threadIdx.x, team);
+        const Cols<kVec> a(c0, cols, threadIdx.x, team), b(c0 + team * 8, cols, threadIdx.x, team);
         float x[8] = {}, y[8] = {};
         if (known && a.count) a.load(w, x);
         if (known && b.count) b.load(w, y);
@@ -287,8 +287,8 @@ struct SumArgs {
     int64_t ld_partial;
 };
 
-template <typename TD, bool kWide>
-__device__ __forceinline__ void put_row(const SumArgs& a, const Cols<kWide>& c, uint32_t id, float (&x)[8]) {
+template <typename TD, int kVec>
+__device__ __forceinline__ void put_row(const SumArgs& a, const Cols<kVec>& c, uint32_t id, float (&x)[8]) {
     TD* row = static_cast<TD*>(a.dw) + (int64_t)id * a.lddw;
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] *= a.scale;
@@ -302,12 +302,12 @@ __device__ __forceinline__ void put_row(const SumArgs& a, const Cols<kWide>& c, 
 }
 
 // Eight elements of a row as they lie in memory: what is in flight costs half the registers for bf16.
-template <typename T, bool kWide>
+template <typename T, int kVec>
 struct RawRow {
-    static constexpr int kWords = !kWide || sizeof(T) == 4 ? 8 : 4;
+    static constexpr int kWords = kVec < 8 || sizeof(T) == 4 ? 8 : 4;
     uint32_t w[kWords];
-    __device__ __forceinline__ void load(const Cols<kWide>& c, const T* row) {
-        if constexpr (!kWide) {
+    __device__ __forceinline__ void load(const Cols<kVec>& c, const T* row) {
+        if constexpr (kVec < 8) {
             float x[8];
             c.load(row, x);
 #pragma unroll
@@ -327,8 +327,8 @@ struct RawRow {
     }
 };
 
-template <typename TY, typename TD, bool kWide>
-__global__ void __launch_bounds__(128, kWide ? 6 : 4) embed_sum_kernel(const __grid_constant__ SumArgs a) {
+template <typename TY, typename TD, int kVec>
+__global__ void __launch_bounds__(128, kVec == 8 ? 6 : 4) embed_sum_kernel(const __grid_constant__ SumArgs a) {
     grid_dependency_wait();
     __shared__ uint32_t s_key[4][kMaxChunk + 2], s_pos[4][kMaxChunk];
     const int team = blockDim.x, ty = threadIdx.y;
@@ -344,17 +344,17 @@ __global__ void __launch_bounds__(128, kWide ? 6 : 4) embed_sum_kernel(const __g
     __syncthreads();
     if (n == 0) return;
     const uint32_t* key = &s_key[ty][1];
-    const Cols<kWide> c((int64_t)blockIdx.y * kSlab, a.cols, threadIdx.x, team);
+    const Cols<kVec> c((int64_t)blockIdx.y * kSlab, a.cols, threadIdx.x, team);
     if (c.count == 0) return;
     const TY* dy = static_cast<const TY*>(a.dy);
     float* partial = a.partial + chunk * 2 * a.ld_partial;
     const uint32_t vocab = (uint32_t)a.vocab;
     f2 acc[4] = {};
     bool from_front = key[-1] == key[0];
-    constexpr int kAhead = RawRow<TY, kWide>::kWords == 4 ? 8 : 4;
+    constexpr int kAhead = RawRow<TY, kVec>::kWords == 4 ? 8 : 4;
 #pragma unroll 1
     for (int i = 0; i < n; i += kAhead) {
-        RawRow<TY, kWide> x[kAhead];
+        RawRow<TY, kVec> x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
             if (i + u < n && key[i + u] < vocab) x[u].load(c, dy + (int64_t)s_pos[ty][i + u] * a.lddy);
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(128, kWide ? 6 : 4) embed_sum_kernel(const __g
             }
             if (from_front) c.store(partial, sum);
             else if (goes_on) c.store(partial + a.ld_partial, sum);
-            else put_row<TD, kWide>(a, c, key[i + u], sum);
+            else put_row<TD, kVec>(a, c, key[i + u], sum);
             from_front = false;
         }
     }
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(128, kWide ? 6 : 4) embed_sum_kernel(const __g
 // The block of the chunk in which such an id begins adds that chunk's partial sum and those of the chunks it goes on in:
 // its teams take consecutive shares of them, which are added in order.
 constexpr int kJoinTeams = 4;
-template <typename TD, bool kWide>
+template <typename TD, int kVec>
 __global__ void __launch_bounds__(128 * kJoinTeams) embed_join_kernel(const __grid_constant__ SumArgs a) {
     grid_dependency_wait();
     __shared__ float s[kJoinTeams - 1][8][128];
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(128 * kJoinTeams) embed_join_kernel(const __gr
         const int64_t k = lo + 1 + tid;
         found = __syncthreads_count(k < a.chunks && a.key[k * a.chunk] == id);
     }
-    const Cols<kWide> c((int64_t)blockIdx.y * kSlab, a.cols, threadIdx.x, blockDim.x);
+    const Cols<kVec> c((int64_t)blockIdx.y * kSlab, a.cols, threadIdx.x, blockDim.x);
     const int64_t each = (lo - chunk + 1 + kJoinTeams - 1) / kJoinTeams;       // the first partial sum is the chunk's own
     const int64_t first = chunk + each * threadIdx.y, last = min(lo + 1, first + each);
     float acc[8] = {};
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(128 * kJoinTeams) embed_join_kernel(const __gr
     for (int t = 0; t < kJoinTeams - 1; ++t)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += s[t][j][threadIdx.x];
-    put_row<TD, kWide>(a, c, id, acc);
+    put_row<TD, kVec>(a, c, id, acc);
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------
@@ -457,36 +457,29 @@ Layout layout_of(int64_t tokens, int64_t cols) {
     return l;
 }
 
-bool off(const void* p, int64_t size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) != 0; }
-int64_t size_of(int dtype) { return dtype == MVUE_BF16 ? 2 : 4; }
-// rows whose eight-element pieces can be moved whole: 16 bytes of bf16, 32 of fp32
-bool wide_rows(const void* p, int64_t ld, int64_t cols, int dtype) {
-    const int64_t piece = 8 * size_of(dtype);
-    return !off(p, piece) && cols % 8 == 0 && ld % 8 == 0;
-}
-
 template <typename TW, typename TO>
 cudaError_t embed(Ids ids, int64_t tokens, const void* w, int64_t vocab, int64_t cols, int64_t ldw, float scale, void* out, int64_t ldo,
-                  bool wide, int* dev_status, cudaStream_t st) {
+                  int vec, int* dev_status, cudaStream_t st) {
     // a thread moves two pieces of eight; the team is a power of two of up to 256 threads
     int team = 32;
     while (team < 256 && team * 16 < cols) team *= 2;
     const int rows = 256 / team;
     const int64_t pieces = (cols + team * 8 - 1) / (team * 8);
     const dim3 grid((unsigned)((tokens + rows - 1) / rows), (unsigned)std::min<int64_t>(pieces / 2 + pieces % 2, 65535));
-    auto kernel = wide ? &embed_kernel<TW, TO, true> : &embed_kernel<TW, TO, false>;
+    auto kernel = vec == 8 ? &embed_kernel<TW, TO, 8> : vec == 2 ? &embed_kernel<TW, TO, 2> : &embed_kernel<TW, TO, 1>;
     return launch_dependent(kernel, grid, dim3(team, rows), 0, st, ids, tokens, static_cast<const TW*>(w), vocab, cols, ldw, scale,
                             static_cast<TO*>(out), ldo, dev_status);
 }
 
 template <typename TY, typename TD>
-cudaError_t sums(const SumArgs& a, bool wide, cudaStream_t st) {
+cudaError_t sums(const SumArgs& a, int vec, cudaStream_t st) {
     const int64_t slab = std::min<int64_t>(kSlab, (a.cols + 7) / 8 * 8);
     const int team = (int)((slab / 8 + 31) / 32 * 32), teams = team <= 32 ? 4 : team <= 64 ? 2 : 1;
     const dim3 grid((unsigned)((a.chunks + teams - 1) / teams), (unsigned)((a.cols + kSlab - 1) / kSlab)), block(team, teams);
-    cudaError_t e = launch_dependent(wide ? &embed_sum_kernel<TY, TD, true> : &embed_sum_kernel<TY, TD, false>, grid, block, 0, st, a);
+    cudaError_t e = launch_dependent(
+        vec == 8 ? &embed_sum_kernel<TY, TD, 8> : vec == 2 ? &embed_sum_kernel<TY, TD, 2> : &embed_sum_kernel<TY, TD, 1>, grid, block, 0, st, a);
     if (e != cudaSuccess || a.chunks < 2) return e;
-    return launch_dependent(wide ? &embed_join_kernel<TD, true> : &embed_join_kernel<TD, false>, dim3((unsigned)a.chunks, grid.y),
+    return launch_dependent(vec == 8 ? &embed_join_kernel<TD, 8> : vec == 2 ? &embed_join_kernel<TD, 2> : &embed_join_kernel<TD, 1>, dim3((unsigned)a.chunks, grid.y),
                             dim3(team, kJoinTeams), 0, st, a);
 }
 
@@ -523,16 +516,16 @@ int mvue_embedding(const void* ids, int id_bits, int64_t tokens, const void* W, 
     if (off(ids, id_bits / 8) || off(W, size_of(w_dtype)) || off(out, size_of(out_dtype)) || off(dev_status, 4)) return MVUE_ERR_ALIGN;
     DeviceInfo dev;
     if (int s = current_device_info(&dev)) return s;
-    const bool wide = wide_rows(W, ldW, cols, w_dtype) && wide_rows(out, ldout, cols, out_dtype);
+    const int vec = std::min(row_vector(W, ldW, cols, w_dtype), row_vector(out, ldout, cols, out_dtype));
     const Ids list{ids, id_bits == 64};
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (w_dtype == MVUE_BF16)
-        e = out_dtype == MVUE_BF16 ? embed<__nv_bfloat16, __nv_bfloat16>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, wide, dev_status, st)
-                                   : embed<__nv_bfloat16, float>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, wide, dev_status, st);
+        e = out_dtype == MVUE_BF16 ? embed<__nv_bfloat16, __nv_bfloat16>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, vec, dev_status, st)
+                                   : embed<__nv_bfloat16, float>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, vec, dev_status, st);
     else
-        e = out_dtype == MVUE_BF16 ? embed<float, __nv_bfloat16>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, wide, dev_status, st)
-                                   : embed<float, float>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, wide, dev_status, st);
+        e = out_dtype == MVUE_BF16 ? embed<float, __nv_bfloat16>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, vec, dev_status, st)
+                                   : embed<float, float>(list, tokens, W, vocab, cols, ldW, scale, out, ldout, vec, dev_status, st);
     if (e != cudaSuccess) { set_cuda_error(e, "mvue_embedding launch"); return MVUE_ERR_CUDA; }
     return MVUE_OK;
 }
@@ -594,11 +587,11 @@ int mvue_embedding_grad(const void* ids, int id_bits, int64_t tokens, const void
         const int last = (a.passes - 1) & 1;
         SumArgs b = {a.key[last], a.pos[last], tokens, vocab, l.chunks, l.chunk, dy, cols, lddy, scale, dW, lddW, accumulate,
                      reinterpret_cast<float*>(ws + l.partial), l.ld_partial};
-        const bool wide = wide_rows(dy, lddy, cols, dy_dtype) && wide_rows(dW, lddW, cols, dW_dtype);
+        const int vec = std::min(row_vector(dy, lddy, cols, dy_dtype), row_vector(dW, lddW, cols, dW_dtype));
         if (dy_dtype == MVUE_BF16)
-            e = dW_dtype == MVUE_BF16 ? sums<__nv_bfloat16, __nv_bfloat16>(b, wide, st) : sums<__nv_bfloat16, float>(b, wide, st);
+            e = dW_dtype == MVUE_BF16 ? sums<__nv_bfloat16, __nv_bfloat16>(b, vec, st) : sums<__nv_bfloat16, float>(b, vec, st);
         else
-            e = dW_dtype == MVUE_BF16 ? sums<float, __nv_bfloat16>(b, wide, st) : sums<float, float>(b, wide, st);
+            e = dW_dtype == MVUE_BF16 ? sums<float, __nv_bfloat16>(b, vec, st) : sums<float, float>(b, vec, st);
     }
     if (e != cudaSuccess) { set_cuda_error(e, "mvue_embedding_grad launch"); return MVUE_ERR_CUDA; }
     return MVUE_OK;

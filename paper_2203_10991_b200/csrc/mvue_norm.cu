@@ -105,10 +105,10 @@ __device__ __forceinline__ void unpairs(const f2 (&p)[4], float (&x)[8]) {
 }
 
 // A thread's place: its channels, and its rows first, first + stride, ... below end.
-template <bool kWide>
+template <int kVec>
 struct Place {
     int64_t n, slab0;
-    Cols<kWide> cols;
+    Cols<kVec> cols;
     int64_t row, end;
     int stride;
     __device__ __forceinline__ Place(const NormArgs& a)
@@ -121,7 +121,7 @@ struct Place {
         if (ty >= stride || cols.count == 0) row = end;          // threads beyond the last whole row of the block
     }
     // channel j of the thread
-    __device__ __forceinline__ int64_t channel(int j) const { return cols.first + (int64_t)j * cols.step; }
+    __device__ __forceinline__ int64_t channel(int j) const { return cols.at(j); }
 };
 
 // Sums over a block's rows of what its threads left per channel: the block's threads share the channels (pieces x 8) and, where
@@ -163,11 +163,11 @@ struct Columns {
 };
 
 // ---- forward through memory: means and M2 of a chunk of rows, per channel -------------------------------------------
-template <typename T, bool kWide>
+template <typename T, int kVec>
 __global__ void __launch_bounds__(kThreads) norm_stats_kernel(const __grid_constant__ NormArgs a) {
     grid_dependency_wait();
     __shared__ float s_mean[kThreads * 8], s_m2[kThreads * 8];
-    Place<kWide> p(a);
+    Place<kVec> p(a);
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     float mean[8] = {}, m2[8] = {}, count = 0.0f;
@@ -214,9 +214,9 @@ __global__ void __launch_bounds__(kThreads) norm_stats_kernel(const __grid_const
         const float d = s_mean[j * kThreads + thread] - m;
         return make_float2(fmaf(s_count[thread] * d, d, s_m2[j * kThreads + thread]), 0.0f);
     });
-    const Cols<kWide> mine(p.slab0, a.c, col.piece, a.pieces);
+    const Cols<kVec> mine(p.slab0, a.c, col.piece, a.pieces);
     if (col.first && col.j < mine.count)
-        a.partial[(n * a.chunks + blockIdx.y) * a.c + mine.first + (int64_t)col.j * mine.step] = make_float2(m, dev.x);
+        a.partial[(n * a.chunks + blockIdx.y) * a.c + mine.at(col.j)] = make_float2(m, dev.x);
 }
 
 __device__ __forceinline__ float warp_sum(float x) {
@@ -285,8 +285,8 @@ struct Channels {
     }
 };
 
-template <bool kWide>
-__device__ __forceinline__ void set_channels(Channels& k, const NormArgs& a, const Place<kWide>& p) {
+template <int kVec>
+__device__ __forceinline__ void set_channels(Channels& k, const NormArgs& a, const Place<kVec>& p) {
     float m[8], t[8], b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -303,10 +303,10 @@ __device__ __forceinline__ void set_channels(Channels& k, const NormArgs& a, con
     pairs(b, k.shift);
 }
 
-template <typename T, bool kWide, int kAct>
+template <typename T, int kVec, int kAct>
 __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_constant__ NormArgs a) {
     grid_dependency_wait();
-    Place<kWide> p(a);
+    Place<kVec> p(a);
     if (p.row >= p.end) return;
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
@@ -332,11 +332,11 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_const
 
 // ---- backward through memory -----------------------------------------------------------------------------------------
 // Sums per channel over a chunk of rows of dz = dy act'(z) and of dz (x - mean) rstd.
-template <typename T, bool kWide, int kAct>
+template <typename T, int kVec, int kAct>
 __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_constant__ NormArgs a) {
     grid_dependency_wait();
     __shared__ float s_a[kThreads * 8], s_b[kThreads * 8];
-    Place<kWide> p(a);
+    Place<kVec> p(a);
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + n * a.s * a.lddy;
@@ -377,9 +377,9 @@ __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_c
     }
     const Columns col(a.pieces);
     const float2 t = col.sum([&](int thread, int j) { return make_float2(s_a[j * kThreads + thread], s_b[j * kThreads + thread]); });
-    const Cols<kWide> mine(p.slab0, a.c, col.piece, a.pieces);
+    const Cols<kVec> mine(p.slab0, a.c, col.piece, a.pieces);
     if (col.first && col.j < mine.count) {
-        const int64_t c = mine.first + (int64_t)col.j * mine.step;
+        const int64_t c = mine.at(col.j);
         a.partial[(n * a.chunks + blockIdx.y) * a.c + c] = make_float2(t.x, t.y * a.rstd[n * a.groups + c / a.group_size]);
     }
 }
@@ -432,10 +432,10 @@ __global__ void __launch_bounds__(kThreads) norm_grad_join_kernel(const __grid_c
     }
 }
 
-template <typename T, bool kWide, int kAct>
+template <typename T, int kVec, int kAct>
 __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_constant__ NormArgs a) {
     grid_dependency_wait();
-    Place<kWide> p(a);
+    Place<kVec> p(a);
     if (p.row >= p.end) return;
     const int64_t n = p.n;
     const T* x = static_cast<const T*>(a.x) + n * a.s * a.ldx;
@@ -1193,9 +1193,6 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-int64_t size_of(int dtype) { return dtype == MVUE_BF16 ? 2 : 4; }
-bool off(const void* p, int64_t size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) != 0; }
-bool wide_rows(const void* p, int64_t ld, int64_t cols, int dtype) { return !off(p, 8 * size_of(dtype)) && cols % 8 == 0 && ld % 8 == 0; }
 
 struct Split {
     int pieces, slabs;
@@ -1334,26 +1331,26 @@ Layout layout_of(int64_t n, int64_t s, int64_t c, int groups) {
     return l;
 }
 
-template <typename T, bool kWide, int kAct>
+template <typename T, int kVec, int kAct>
 cudaError_t forward(const NormArgs& a, dim3 grid, cudaStream_t st) {
-    cudaError_t e = launch_dependent(&norm_stats_kernel<T, kWide>, grid, dim3(kThreads), 0, st, a);
+    cudaError_t e = launch_dependent(&norm_stats_kernel<T, kVec>, grid, dim3(kThreads), 0, st, a);
     const unsigned joins = (unsigned)(a.n * a.groups);
     if (e == cudaSuccess) e = launch_dependent(&norm_join_kernel, dim3(joins), dim3(kThreads), 0, st, a);
-    if (e == cudaSuccess) e = launch_dependent(&norm_apply_kernel<T, kWide, kAct>, grid, dim3(kThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_dependent(&norm_apply_kernel<T, kVec, kAct>, grid, dim3(kThreads), 0, st, a);
     return e;
 }
-template <typename T, bool kWide, int kAct>
+template <typename T, int kVec, int kAct>
 cudaError_t backward(const NormArgs& a, dim3 grid, cudaStream_t st) {
-    cudaError_t e = launch_dependent(&norm_grad_sums_kernel<T, kWide, kAct>, grid, dim3(kThreads), 0, st, a);
+    cudaError_t e = launch_dependent(&norm_grad_sums_kernel<T, kVec, kAct>, grid, dim3(kThreads), 0, st, a);
     const int64_t joins = a.n * a.groups;
     const int64_t sums = a.dgamma || a.dbeta ? (a.c + 31) / 32 : 0;
     if (e == cudaSuccess) e = launch_dependent(&norm_grad_join_kernel, dim3((unsigned)(joins + sums)), dim3(kThreads), 0, st, a, joins);
-    if (e == cudaSuccess) e = launch_dependent(&norm_grad_apply_kernel<T, kWide, kAct>, grid, dim3(kThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_dependent(&norm_grad_apply_kernel<T, kVec, kAct>, grid, dim3(kThreads), 0, st, a);
     return e;
 }
-template <typename T, bool kWide, int kAct>
+template <typename T, int kVec, int kAct>
 cudaError_t either(const NormArgs& a, dim3 grid, cudaStream_t st) {
-    if constexpr (kWide) {
+    if constexpr (kVec == 8) {
         const Keep k = keep_of(a.n, a.s, a.c, a.groups, sizeof(T), a.dy ? 2 : 1);
         if (k.pieces) {
             ResidentArgs r{a, k.cluster, k.rows, k.iters, k.fold, (int)(a.n * k.slabs)};
@@ -1377,15 +1374,15 @@ cudaError_t either(const NormArgs& a, dim3 grid, cudaStream_t st) {
             return e;
         }
     }
-    return a.dy ? backward<T, kWide, kAct>(a, grid, st) : forward<T, kWide, kAct>(a, grid, st);
+    return a.dy ? backward<T, kVec, kAct>(a, grid, st) : forward<T, kVec, kAct>(a, grid, st);
 }
-template <typename T, bool kWide>
+template <typename T, int kVec>
 cudaError_t by_act(const NormArgs& a, int act, dim3 grid, cudaStream_t st) {
     switch (act) {
-        case MVUE_ACT_RELU: return either<T, kWide, MVUE_ACT_RELU>(a, grid, st);
-        case MVUE_ACT_SILU: return either<T, kWide, MVUE_ACT_SILU>(a, grid, st);
-        case MVUE_ACT_GELU: return either<T, kWide, MVUE_ACT_GELU>(a, grid, st);
-        default: return either<T, kWide, MVUE_ACT_NONE>(a, grid, st);
+        case MVUE_ACT_RELU: return either<T, kVec, MVUE_ACT_RELU>(a, grid, st);
+        case MVUE_ACT_SILU: return either<T, kVec, MVUE_ACT_SILU>(a, grid, st);
+        case MVUE_ACT_GELU: return either<T, kVec, MVUE_ACT_GELU>(a, grid, st);
+        default: return either<T, kVec, MVUE_ACT_NONE>(a, grid, st);
     }
 }
 
@@ -1401,9 +1398,9 @@ int check(int dtype, int64_t n, int64_t s, int64_t c, int groups, int affine_dty
     return MVUE_OK;
 }
 
-int run(NormArgs& a, int dtype, int act, bool wide, void* workspace, size_t workspace_bytes, void* stream, const char* what) {
+int run(NormArgs& a, int dtype, int act, int vec, void* workspace, size_t workspace_bytes, void* stream, const char* what) {
     // a forward pass whose samples stay in shared memory leaves nothing outside when it is given room for mean and rstd
-    const bool none = wide && !a.dy && a.mean && a.rstd && keep_of(a.n, a.s, a.c, a.groups, size_of(dtype), 1).pieces;
+    const bool none = vec == 8 && !a.dy && a.mean && a.rstd && keep_of(a.n, a.s, a.c, a.groups, size_of(dtype), 1).pieces;
     const Layout l = layout_of(a.n, a.s, a.c, a.groups);
     if (!none && (!workspace || workspace_bytes < l.bytes || off(workspace, 16))) return MVUE_ERR_WORKSPACE;
     DeviceInfo dev;
@@ -1421,8 +1418,8 @@ int run(NormArgs& a, int dtype, int act, bool wide, void* workspace, size_t work
     const dim3 grid((unsigned)(a.n * sp.slabs), (unsigned)sp.chunks);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     cudaError_t e;
-    if (dtype == MVUE_BF16) e = wide ? by_act<__nv_bfloat16, true>(a, act, grid, st) : by_act<__nv_bfloat16, false>(a, act, grid, st);
-    else e = wide ? by_act<float, true>(a, act, grid, st) : by_act<float, false>(a, act, grid, st);
+    if (dtype == MVUE_BF16) e = vec == 8 ? by_act<__nv_bfloat16, 8>(a, act, grid, st) : vec == 2 ? by_act<__nv_bfloat16, 2>(a, act, grid, st) : by_act<__nv_bfloat16, 1>(a, act, grid, st);
+    else e = vec == 8 ? by_act<float, 8>(a, act, grid, st) : vec == 2 ? by_act<float, 2>(a, act, grid, st) : by_act<float, 1>(a, act, grid, st);
     if (e != cudaSuccess) { set_cuda_error(e, what); return MVUE_ERR_CUDA; }
     return MVUE_OK;
 }
@@ -1455,7 +1452,7 @@ int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t 
     a.groups = groups; a.group_size = (int)(c / groups);
     a.gamma = gamma; a.beta = beta; a.affine_bf16 = affine_dtype == MVUE_BF16;
     a.eps = eps; a.mean = mean; a.rstd = rstd; a.dev_status = dev_status;
-    return run(a, dtype, act, wide_rows(x, ldx, c, dtype) && wide_rows(y, ldy, c, dtype), workspace, workspace_bytes, stream,
+    return run(a, dtype, act, std::min(row_vector(x, ldx, c, dtype), row_vector(y, ldy, c, dtype)), workspace, workspace_bytes, stream,
                "mvue_group_norm_act launch");
 }
 
@@ -1483,7 +1480,7 @@ int mvue_group_norm_act_backward(const void* dy, int64_t lddy, const void* x, in
     a.gamma = gamma; a.beta = beta; a.affine_bf16 = affine_dtype == MVUE_BF16;
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);      // only read here
     a.dgamma = dgamma; a.dbeta = dbeta; a.dev_status = dev_status;
-    return run(a, dtype, act, wide_rows(x, ldx, c, dtype) && wide_rows(dy, lddy, c, dtype) && wide_rows(dx, lddx, c, dtype), workspace,
+    return run(a, dtype, act, std::min({row_vector(x, ldx, c, dtype), row_vector(dy, lddy, c, dtype), row_vector(dx, lddx, c, dtype)}), workspace,
                workspace_bytes, stream, "mvue_group_norm_act_backward launch");
 }
 

@@ -106,45 +106,81 @@ __device__ __forceinline__ void store8_words(__nv_bfloat16* p, bool wide, int co
     }
 }
 
-// Eight elements of a row per thread: consecutive ones where the rows allow wide accesses, else one of every
-// `stride` (the team's threads), so that a warp's accesses stay together.
-template <bool kWide>
+// Eight elements of a row per thread in groups of kVec neighbours: 8 where the rows allow wide accesses (then they are
+// consecutive), 2 where they allow those, else 1; the groups lie the team's threads apart, so that a warp's accesses stay
+// together.
+template <typename T> struct Two;
+template <> struct Two<float> { using Type = float2; };
+template <> struct Two<__nv_bfloat16> { using Type = __nv_bfloat162; };
+
+template <int kVec>
 struct Cols {
     int64_t first;
-    int step, count;
+    int step, count;                 // elements from one group to the next; elements that exist
     __device__ __forceinline__ Cols(int64_t slab0, int64_t cols, int lane, int team) {
-        first = slab0 + (kWide ? (int64_t)lane * 8 : lane);
-        step = kWide ? 1 : team;
+        first = slab0 + (int64_t)lane * kVec;
+        step = team * kVec;
         const int64_t left = cols - first;
-        count = left <= 0 ? 0 : (int)min((int64_t)8, kWide ? left : (left + team - 1) / team);
+        count = left <= 0 ? 0 : (int)min((int64_t)8, kVec == 8 ? left : (left + step - 1) / step * kVec);
     }
+    __device__ __forceinline__ int64_t at(int j) const { return first + (int64_t)(j / kVec) * step + j % kVec; }
     template <typename T> __device__ __forceinline__ void load(const T* row, float (&x)[8]) const {
-        if (kWide) {
+        if constexpr (kVec == 8) {
             load8(row + first, true, 8, x);
+        } else if constexpr (kVec == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                float2 v = make_float2(0.0f, 0.0f);
+                if (j < count) {
+                    const typename Two<T>::Type q = *reinterpret_cast<const typename Two<T>::Type*>(row + at(j));
+                    v = make_float2((float)q.x, (float)q.y);
+                }
+                x[j] = v.x;
+                x[j + 1] = v.y;
+            }
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = j < count ? (float)row[first + (int64_t)j * step] : 0.0f;
+            for (int j = 0; j < 8; ++j) x[j] = j < count ? (float)row[at(j)] : 0.0f;
         }
     }
     __device__ __forceinline__ void store(float* row, const float (&x)[8]) const {
-        if (kWide) {
+        if constexpr (kVec == 8) {
             store8(row + first, true, 8, x);
+        } else if constexpr (kVec == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2)
+                if (j < count) *reinterpret_cast<float2*>(row + at(j)) = make_float2(x[j], x[j + 1]);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j < count) row[first + (int64_t)j * step] = x[j];
+                if (j < count) row[at(j)] = x[j];
         }
     }
     __device__ __forceinline__ void store(__nv_bfloat16* row, const float (&x)[8]) const {
-        if (kWide) {
+        if constexpr (kVec == 8) {
             const uint32_t w[4] = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
             store8_words(row + first, true, 8, w);
+        } else if constexpr (kVec == 2) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 2)
+                if (j < count) *reinterpret_cast<uint32_t*>(row + at(j)) = pack_bf16x2(x[j], x[j + 1]);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (j < count) row[first + (int64_t)j * step] = __float2bfloat16_rn(x[j]);
+                if (j < count) row[at(j)] = __float2bfloat16_rn(x[j]);
         }
     }
 };
+
+// ---- host: how many neighbouring elements of a matrix's rows one access may take: eight (16 bytes of bf16, 32 of fp32), two, or
+// one, by the alignment of base, leading dimension and columns.  Pairs against single elements, group norm on 16 x 3000 x 90
+// bf16: backward 33 us against 38 us, forward 27 us either way. ----
+inline bool off(const void* p, int64_t size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) != 0; }
+inline int64_t size_of(int dtype) { return dtype == 1 ? 2 : 4; }                 // MVUE_BF16, MVUE_F32
+inline int row_vector(const void* p, int64_t ld, int64_t cols, int dtype) {
+    for (int v = 8; v > 1; v /= 4)
+        if (!off(p, v * size_of(dtype)) && cols % v == 0 && ld % v == 0) return v;
+    return 1;
+}
 
 }  // namespace mvue

@@ -57,6 +57,22 @@ def test_lookup_strides_shapes_and_unknown_ids():
     assert torch.equal(got[1], big[3]) and float(got[[0, 2, 3]].abs().max()) == 0
 
 
+@gpu
+@pytest.mark.parametrize("lo,cols", [(2, 34), (2, 64), (1, 34), (4, 1030), (0, 90)])
+def test_rows_that_allow_pairs(lo, cols):
+    # even widths on even and odd offsets: pieces of eight, pairs, single elements
+    big = torch.randn(60, 1040, device="cuda")
+    ids = torch.randint(0, 60, (500,), device="cuda")
+    for dtype in (F32, BF16):
+        w = big.to(dtype)[:, lo:lo + cols]
+        assert torch.equal(binding.mvue_embedding(ids, w), w[ids])
+        wide = torch.randn(500, 1040, device="cuda").to(dtype)
+        out = torch.full((60, 1040), 5.0, device="cuda")
+        binding.mvue_embedding_grad(ids, wide[:, lo:lo + cols], 60, out=out[:, lo:lo + cols])
+        check_grad(out[:, lo:lo + cols], ids, wide[:, lo:lo + cols], 60, 1.0)
+        assert bool((out[:, :lo] == 5).all()) and bool((out[:, lo + cols:] == 5).all())
+
+
 def sums64(ids, dy, vocab, scale, padding):
     """(sum, sum of magnitudes, count) for each id, in 64 bits."""
     keep = (ids >= 0) & (ids < vocab) & (ids != padding)

@@ -107,6 +107,21 @@ def test_channel_slices_images_and_in_place(dtype, lo):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lo,c,groups", [(2, 90, 30), (2, 64, 8), (1, 34, 17), (0, 10, 1), (4, 258, 6)])
+def test_rows_that_allow_pairs(dtype, lo, c, groups):
+    big, dyb, w, b = inputs(2, 333, c + 6, dtype, F32, c)
+    w, b = w[:c].contiguous(), b[:c].contiguous()
+    x, dy = big[..., lo:lo + c], dyb[..., lo:lo + c]
+    got = binding.mvue_group_norm_act(x, groups, w, b, act="silu")
+    check_forward(got, x, groups, w, b, "silu")
+    out = torch.full_like(big, 4.0)
+    back = binding.mvue_group_norm_act_backward(dy, x, got[1], got[2], groups, w, b, act="silu", out=out[..., lo:lo + c])
+    check_backward(back, dy, x, got[1], got[2], groups, w, b, "silu")
+    assert bool((out[..., :lo] == 4).all()) and bool((out[..., lo + c:] == 4).all())
+
+
+@gpu
 def test_empty_batch_stream_and_graph():
     w = torch.ones(16, device="cuda")
     x = torch.empty(0, 4, 16, device="cuda")
