@@ -8,12 +8,14 @@
 // eight 16-bit random numbers are one generator call.
 //
 // Measured (B200, HBM copy 6.55 TB/s).  24 matrices of 4 M elements, 32-bit states, bf16 + float copy: 438 us for 3.02 GB,
-// 105 % of the copy rate: bound by HBM.  Two matrices of 59 M elements, 8-bit states, bf16: 315 us against 180 us of HBM
-// time: bound by instructions, 62 per element of which 8 are the generator, 67 % of the issue slots, the integer/logic pipe half
-// busy.  What brought it down: the code taken from the bit pattern instead of by way of a step and a rounded sum (400 ->
-// 341 us), packed pairs and hardware decoding (457 -> 400 us), five blocks an SM (341 -> 315 us).  Six blocks spill (368 us);
-// loads of the next block ahead of the arithmetic cost more registers than they hide (351 us).  96 vectors of 2500 elements:
-// 7 to 9 us, the launch.
+// 105 % of the copy rate: bound by HBM.  Two matrices of 59 M elements, 8-bit states, bf16: 327 us against 180 us of HBM
+// time: bound by instructions, above 60 per element of which 8 are the generator.  What brought it down: the code taken from
+// the bit pattern instead of by way of a step and a rounded sum (400 -> 341 us), packed pairs and hardware decoding
+// (457 -> 400 us), five blocks an SM (341 -> 315 us, although 17 words a thread spill).  Six blocks spill more (368 us); loads of the
+// next block ahead of the arithmetic cost more registers than they hide (351 us).  Finding the lanes whose code may differ
+// between the approximate root and the correctly rounded one costs 12 of the 327 us; the correctly rounded root for every element
+// would take 374 us.  It depends on the data: lanes with a code below 2^-6, zeros among them, take the longer way.  Every second block
+// zero 358 us, all zero 394 us, one zero in every lane 427 us.  96 vectors of 2500 elements: 7 to 9 us, the launch.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -73,7 +75,7 @@ __device__ __forceinline__ f2 e4m3_values(uint32_t half) {
 // Code of a magnitude y <= 448 (a few units in its last place above are no matter), any y: steps of 2^-3 of its power of
 // two (2^-9 below 2^-6), rounded up where the fraction plus the random number r 2^-16 reaches one.  The product by a power
 // of two is exact; adding 2^23 rounded down leaves the whole steps in the low bits.
-__device__ __noinline__ uint32_t e4m3_code(float y, uint32_t r) {
+__device__ __forceinline__ uint32_t e4m3_code(float y, uint32_t r) {
     const uint32_t e = max(__float_as_uint(y) & 0x7F800000u, 121u << 23);
     const float steps = __fmaf_rn(y, __uint_as_float((257u << 23) - e), (float)r * 1.52587890625e-05f);
     return (e >> 20) - (121u << 3) + (__float_as_uint(__fadd_rd(steps, 8388608.0f)) - 0x4B000000u);
@@ -116,8 +118,8 @@ __device__ __forceinline__ float block_scale(float top, float* factor) {
 // A NaN whose lower half is zero: random bits added to it do not carry into the sign.
 __device__ __forceinline__ float short_nan(float x) { return x != x ? __uint_as_float(0x7FC00000u) : x; }
 
-// The new moments of eight elements (v: the second moment, root: its square root within one unit in the last place, which
-// moves a code only where the random number falls within 2^-20 of its threshold) and the new param.
+// The new moments of eight elements (v: the second moment, root: its square root with a relative error of at most 2^-23)
+// and the new param.
 struct Step {
     f2 m[4], v[4], root[4], p[4];
     __device__ __forceinline__ void take(const Constants& c, const f2 (&g)[4], float gs) {
@@ -260,8 +262,15 @@ __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constan
                 r8[2 * j] = __byte_perm(rw[j], 0u, 0x4014);              // the half-words with their bytes exchanged, << 8
                 r8[2 * j + 1] = __byte_perm(rw[j], 0u, 0x4234);
             }
+            // The code of sqrt(v) is that of the correctly rounded root, also where the approximate one is on the other side of
+            // a threshold.  The two roots are at most 2^-23 + 2^-24 apart (relative), z with its rounding 5 units of its last place:
+            // a lane with an element whose z plus random number is within 8 units of a carry takes the second way, one lane
+            // in eight thousand. 
+            uint32_t nearest = 0xFFFFFFFFu;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) nearest = min(nearest, (__float_as_uint(z[i]) * 16u + r8[i]) * 256u + 0x8000u);
             uint32_t mw[2], vw[2];
-            if (least >= 0.015625f) {
+            if (least >= 0.015625f && nearest >= 0x10000u) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t signs = __byte_perm(__byte_perm(__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), 0x0073),
@@ -274,7 +283,8 @@ __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constan
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t cm = e4m3_code(fminf(fabsf(y[i]), 448.0f), r8[i] >> 8) | (y[i] < 0.0f ? 0x80u : 0u);
-                    const uint32_t cv = max(e4m3_code(fminf(z[i], 448.0f), r8[i] >> 8), v[i] > 0.0f ? 1u : 0u);
+                    const float exact = vf > 0.0f ? __fmul_rn(__fsqrt_rn(v[i]), vf) : 0.0f;
+                    const uint32_t cv = max(e4m3_code(fminf(exact, 448.0f), r8[i] >> 8), v[i] > 0.0f ? 1u : 0u);
                     mw[i >> 2] |= cm << (8 * (i & 3));
                     vw[i >> 2] |= cv << (8 * (i & 3));
                 }
