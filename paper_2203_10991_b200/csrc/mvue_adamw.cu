@@ -8,14 +8,14 @@
 // eight 16-bit random numbers are one generator call.
 //
 // Measured (B200, HBM copy 6.55 TB/s).  24 matrices of 4 M elements, 32-bit states, bf16 + float copy: 438 us for 3.02 GB,
-// 105 % of the copy rate: bound by HBM.  Two matrices of 59 M elements, 8-bit states, bf16: 327 us against 180 us of HBM
+// 105 % of the copy rate: bound by HBM.  Two matrices of 59 M elements, 8-bit states, bf16: 333 us against 180 us of HBM
 // time: bound by instructions, above 60 per element of which 8 are the generator.  What brought it down: the code taken from
 // the bit pattern instead of by way of a step and a rounded sum (400 -> 341 us), packed pairs and hardware decoding
 // (457 -> 400 us), five blocks an SM (341 -> 315 us, although 17 words a thread spill).  Six blocks spill more (368 us); loads of the
 // next block ahead of the arithmetic cost more registers than they hide (351 us).  Finding the lanes whose code may differ
-// between the approximate root and the correctly rounded one costs 12 of the 327 us; the correctly rounded root for every element
-// would take 374 us.  It depends on the data: lanes with a code below 2^-6, zeros among them, take the longer way.  Every second block
-// zero 358 us, all zero 394 us, one zero in every lane 427 us.  96 vectors of 2500 elements: 7 to 9 us, the launch.
+// between the approximate root and the correctly rounded one costs 12 of the 333 us; the correctly rounded root for every element
+// would take 375 us.  It depends on the data: lanes with a code below 2^-6, zeros among them, take the longer way.  Every second block
+// zero 366 us, all zero 404 us, one zero in every lane 438 us.  96 vectors of 2500 elements: 7 to 9 us, the launch.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -92,9 +92,12 @@ __device__ __forceinline__ uint32_t e4m3_codes_normal(const float* y, const uint
     return (bytes ^ 0x40404040u) & 0x7F7F7F7Fu;              // less 120 << 3: the top two bits are 11 or 00, to become 00 or 01
 }
 
+// Square root with a relative error of at most 2^-23, subnormal arguments included: v' below 2^-126 (|g'| below 3e-18 on
+// a fresh state) has an ordinary root, and with a small eps that is what the step is divided by.  Flushing them to zero saves 6 of
+// 333 us on 2 x 59 M elements with 8-bit states.
 __device__ __forceinline__ float fast_root(float x) {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 // the larger magnitude, NaN if there is one
