@@ -14,7 +14,7 @@
 // (457 -> 400 us), five blocks an SM (341 -> 315 us, although 17 words a thread spill).  Six blocks spill more (368 us); loads of the
 // next block ahead of the arithmetic cost more registers than they hide (351 us).  Finding the lanes whose code may differ
 // between the approximate root and the correctly rounded one costs 12 of the 333 us; the correctly rounded root for every element
-// would take 375 us.  It depends on the data: lanes with a code below 2^-6, zeros among them, take the longer way.  Every second block
+// would take 374 us.  It depends on the data: lanes with a code below 2^-6, zeros among them, take the longer way.  Every second block
 // zero 366 us, all zero 404 us, one zero in every lane 438 us.  96 vectors of 2500 elements: 7 to 9 us, the launch.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

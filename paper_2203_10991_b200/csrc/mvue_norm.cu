@@ -51,20 +51,41 @@ __device__ __forceinline__ float affine(const void* p, int is_bf16, int64_t i, f
     return is_bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
 }
 
-// 1 / (1 + exp(-z)) of two numbers with one reciprocal, that of the product of the two denominators: the special-function
-// unit takes 16 values a cycle, and two each hold up the backward pass (105 us against 99 us on 64 x 3136 x 256).  The exponentials are capped at 2^60
-// (z below -41.6, where the factor stays at 2^-60), which keeps the product finite.
-__device__ __forceinline__ f2 sigmoid(f2 z) {
-    float a, b;
-    unpair(mul2(z, pair(-1.4426950408889634f)), a, b);
-    unpair(add2(pair(fast_exp2(fminf(a, 60.0f)), fast_exp2(fminf(b, 60.0f))), pair(1.0f)), a, b);
-    return mul2(pair(fast_reciprocal(a * b)), pair(b, a));
-}
+// 1 / (1 + exp(-z)) of two numbers.  Each: by itself, from the exponential of -|z|, which does not overflow; subnormal results
+// included, and what is not finite stays on its side.
+struct Each {
+    static __device__ __forceinline__ float one(float t) {              // t = -z in powers of two
+        float e;
+        asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-fabsf(t)));
+        return (t > 0.0f ? e : 1.0f) * fast_reciprocal(1.0f + e);
+    }
+    __device__ __forceinline__ f2 sigmoid(f2 z) {
+        float a, b;
+        unpair(mul2(z, pair(-1.4426950408889634f)), a, b);
+        return pair(one(a), one(b));
+    }
+};
+// Both with one reciprocal, that of the product of the two denominators: the special-function unit takes 16 values a cycle, and
+// two each hold up the folded kernels (64 x 3136 x 256 bf16: 53 us against 52 us forward, 107 us against 100 us backward).
+// The product is finite while both exponentials are at most 2^60 (z above -41.6); where `held` says that they were not, or
+// that there was a NaN, the caller goes over its rows again with Each.  A test of every pair on the way costs 119 us, one of every
+// four pairs 108 us.
+struct Shared {
+    float top = 0.0f;
+    __device__ __forceinline__ f2 sigmoid(f2 z) {
+        float a, b;
+        unpair(mul2(z, pair(-1.4426950408889634f)), a, b);
+        asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(a), "f"(b));
+        unpair(add2(pair(fast_exp2(a), fast_exp2(b)), pair(1.0f)), a, b);
+        return mul2(pair(fast_reciprocal(a * b)), pair(b, a));
+    }
+    __device__ __forceinline__ bool held() const { return top <= 60.0f; }
+};
 
-template <int kAct>
-__device__ __forceinline__ f2 act(f2 z) {
+template <int kAct, typename How>
+__device__ __forceinline__ f2 act(f2 z, How& how) {
     if (kAct == MVUE_ACT_NONE) return z;
-    if (kAct == MVUE_ACT_SILU) return mul2(z, sigmoid(z));
+    if (kAct == MVUE_ACT_SILU) return mul2(z, how.sigmoid(z));
     float a, b;
     unpair(z, a, b);
     if (kAct == MVUE_ACT_RELU) {                                                            // NaN stays
@@ -76,11 +97,11 @@ __device__ __forceinline__ f2 act(f2 z) {
     return mul2(mul2(z, pair(0.5f)), add2(e, pair(1.0f)));
 }
 // d act'(z)
-template <int kAct>
-__device__ __forceinline__ f2 act_grad(f2 z, f2 d) {
+template <int kAct, typename How>
+__device__ __forceinline__ f2 act_grad(f2 z, f2 d, How& how) {
     if (kAct == MVUE_ACT_NONE) return d;
     if (kAct == MVUE_ACT_SILU) {                       // s + z s (1 - s)
-        const f2 s = sigmoid(z);
+        const f2 s = how.sigmoid(z);
         return mul2(d, fma2(mul2(z, s), fma2(s, pair(-1.0f), pair(1.0f)), s));
     }
     float a, b, da, db;
@@ -271,16 +292,16 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const __grid_consta
 struct Channels {
     f2 neg_mean[4], slope[4], shift[4];
 
-    template <int kAct> __device__ __forceinline__ void output(f2 (&x)[4]) const {
+    template <int kAct, typename How> __device__ __forceinline__ void output(f2 (&x)[4], How& how) const {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = act<kAct>(fma2(add2(x[j], neg_mean[j]), slope[j], shift[j]));
+        for (int j = 0; j < 4; ++j) x[j] = act<kAct>(fma2(add2(x[j], neg_mean[j]), slope[j], shift[j]), how);
     }
     // x becomes x - mean, d becomes dz = d act'(z)
-    template <int kAct> __device__ __forceinline__ void gradient(f2 (&x)[4], f2 (&d)[4]) const {
+    template <int kAct, typename How> __device__ __forceinline__ void gradient(f2 (&x)[4], f2 (&d)[4], How& how) const {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             x[j] = add2(x[j], neg_mean[j]);
-            d[j] = act_grad<kAct>(fma2(x[j], slope[j], shift[j]), d[j]);
+            d[j] = act_grad<kAct>(fma2(x[j], slope[j], shift[j]), d[j], how);
         }
     }
 };
@@ -313,6 +334,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_const
     T* y = static_cast<T*>(a.out) + n * a.s * a.ldo;
     Channels k;
     set_channels(k, a, p);
+    Each each;
     for (; p.row < p.end; p.row += (int64_t)p.stride * kRowsAhead) {
         float v[kRowsAhead][8];
 #pragma unroll
@@ -323,7 +345,7 @@ __global__ void __launch_bounds__(kThreads) norm_apply_kernel(const __grid_const
             if (p.row + (int64_t)u * p.stride < p.end) {
                 f2 z[4];
                 pairs(v[u], z);
-                k.output<kAct>(z);
+                k.output<kAct>(z, each);
                 unpairs(z, v[u]);
                 p.cols.store(y + (p.row + (int64_t)u * p.stride) * a.ldo, v[u]);
             }
@@ -344,27 +366,37 @@ __global__ void __launch_bounds__(kThreads) norm_grad_sums_kernel(const __grid_c
     if (p.row < p.end) {
         Channels k;
         set_channels(k, a, p);
-        for (; p.row < p.end; p.row += (int64_t)p.stride * 2) {
-            float v[2][8], d[2][8];
+        const auto add_up = [&](auto& how) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-                if (p.row + (int64_t)u * p.stride < p.end) {
-                    p.cols.load(x + (p.row + (int64_t)u * p.stride) * a.ldx, v[u]);
-                    p.cols.load(dy + (p.row + (int64_t)u * p.stride) * a.lddy, d[u]);
-                }
+            for (int j = 0; j < 4; ++j) sums[j] = alongs[j] = pair(0.0f);
+            for (int64_t row = p.row; row < p.end; row += (int64_t)p.stride * 2) {
+                float v[2][8], d[2][8];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-                if (p.row + (int64_t)u * p.stride < p.end) {
-                    f2 xc[4], dz[4];
-                    pairs(v[u], xc);
-                    pairs(d[u], dz);
-                    k.gradient<kAct>(xc, dz);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        sums[j] = add2(sums[j], dz[j]);
-                        alongs[j] = fma2(dz[j], xc[j], alongs[j]);
+                for (int u = 0; u < 2; ++u)
+                    if (row + (int64_t)u * p.stride < p.end) {
+                        p.cols.load(x + (row + (int64_t)u * p.stride) * a.ldx, v[u]);
+                        p.cols.load(dy + (row + (int64_t)u * p.stride) * a.lddy, d[u]);
                     }
-                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (row + (int64_t)u * p.stride < p.end) {
+                        f2 xc[4], dz[4];
+                        pairs(v[u], xc);
+                        pairs(d[u], dz);
+                        k.gradient<kAct>(xc, dz, how);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            sums[j] = add2(sums[j], dz[j]);
+                            alongs[j] = fma2(dz[j], xc[j], alongs[j]);
+                        }
+                    }
+            }
+        };
+        Shared shared;
+        add_up(shared);
+        if (kAct == MVUE_ACT_SILU && !shared.held()) {
+            Each each;
+            add_up(each);
         }
     }
     float sum[8], along[8];
@@ -455,6 +487,7 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
     f2 level[4], tilt[4];
     pairs(low, level);
     pairs(off, tilt);
+    Each each;
     for (; p.row < p.end; p.row += (int64_t)p.stride * 2) {
         float v[2][8], d[2][8];
 #pragma unroll
@@ -469,7 +502,7 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
                 f2 xc[4], dz[4];
                 pairs(v[u], xc);
                 pairs(d[u], dz);
-                k.gradient<kAct>(xc, dz);
+                k.gradient<kAct>(xc, dz, each);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) xc[j] = fma2(k.slope[j], dz[j], fma2(xc[j], tilt[j], level[j]));
                 unpairs(xc, v[u]);
@@ -804,15 +837,24 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(const __grid
         read_values(r.one + r.piece * 8, k8.neg_mean);
         read_values(r.slope + r.piece * 8, k8.slope);
         read_values(r.shift + r.piece * 8, k8.shift);
-        T* y = r.at(static_cast<T*>(q.out), q.ldo);
+        T* const y0 = r.at(static_cast<T*>(q.out), q.ldo);
         const int64_t down = (int64_t)r.threads_down * q.ldo;
-        slot = first;
+        const auto output = [&](auto& how) {
+            T* y = y0;
+            const char* from = first;
 #pragma unroll 2
-        for (int i = 0; i < iters; ++i, y += down, slot += S::kRowBytes) {
-            f2 v[4];
-            S::read(slot, v);
-            k8.output<kAct>(v);
-            S::store(y, v);
+            for (int i = 0; i < iters; ++i, y += down, from += S::kRowBytes) {
+                f2 v[4];
+                S::read(from, v);
+                k8.output<kAct>(v, how);
+                S::store(y, v);
+            }
+        };
+        Shared shared;
+        output(shared);
+        if (kAct == MVUE_ACT_SILU && !shared.held()) {
+            Each each;
+            output(each);
         }
         if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
     }
@@ -854,20 +896,29 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
         read_values(r.one + r.piece * 8, k8.neg_mean);
         read_values(r.slope + r.piece * 8, k8.slope);
         read_values(r.shift + r.piece * 8, k8.shift);
-        f2 sum[4] = {}, along[4] = {};
+        f2 sum[4], along[4];
         const int iters = r.mine ? r.iters : 0;
-        const char *slot = r.slots(0), *dslot = r.slots(1);
-        for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[4], d[4];
-            S::read(slot, v);
-            S::read(dslot, d);
-            k8.gradient<kAct>(v, d);
+        const auto sums = [&](auto& how) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                sum[j] = add2(sum[j], d[j]);
-                along[j] = fma2(d[j], v[j], along[j]);
+            for (int j = 0; j < 4; ++j) sum[j] = along[j] = pair(0.0f);
+            const char *slot = r.slots(0), *dslot = r.slots(1);
+            for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
+                f2 v[4], d[4];
+                S::read(slot, v);
+                S::read(dslot, d);
+                k8.gradient<kAct>(v, d, how);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sum[j] = add2(sum[j], d[j]);
+                    along[j] = fma2(d[j], v[j], along[j]);
+                }
             }
-        }
+        };
+        Shared shared;
+        Each each;
+        sums(shared);
+        const bool held = kAct != MVUE_ACT_SILU || shared.held();
+        if (!held) sums(each);
         __syncthreads();             // all have read r.one
         r.channel_sums(sum, r.one);
         r.channel_sums(along, r.two);
@@ -899,19 +950,22 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
         f2 level[4], tilt[4];            // dx = slope dz + level + tilt (x - mean)
         read_values(r.one + r.piece * 8, level);
         read_values(r.two + r.piece * 8, tilt);
-        T* dx = r.at(static_cast<T*>(q.out), q.ldo);
         const int64_t down = (int64_t)r.threads_down * q.ldo;
-        slot = r.slots(0);
-        dslot = r.slots(1);
-        for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[4], d[4];
-            S::read(slot, v);
-            S::read(dslot, d);
-            k8.gradient<kAct>(v, d);
+        const auto output = [&](auto& how) {
+            T* dx = r.at(static_cast<T*>(q.out), q.ldo);
+            const char *slot = r.slots(0), *dslot = r.slots(1);
+            for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
+                f2 v[4], d[4];
+                S::read(slot, v);
+                S::read(dslot, d);
+                k8.gradient<kAct>(v, d, how);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt[j], level[j]));
-            S::store(dx, v);
-        }
+                for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt[j], level[j]));
+                S::store(dx, v);
+            }
+        };
+        if (held) output(shared);
+        else output(each);
         if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
     }
     copies_wait();
@@ -1065,15 +1119,24 @@ __global__ void __launch_bounds__(kThreads, 4) norm_folded_kernel(const __grid_c
             k8.neg_mean[j] = pair(-mean);
             k8.slope[j] = mul2(k8.slope[j], pair(rstd));
         }
-        T* y = r.at(static_cast<T*>(q.out), q.ldo);
+        T* const y0 = r.at(static_cast<T*>(q.out), q.ldo);
         const int64_t down = (int64_t)r.threads_down * q.ldo;
-        slot = first;
+        const auto output = [&](auto& how) {
+            T* y = y0;
+            const char* from = first;
 #pragma unroll 2
-        for (int i = 0; i < iters; ++i, y += down, slot += S::kRowBytes) {
-            f2 v[4];
-            S::read(slot, v);
-            k8.output<kAct>(v);
-            S::store(y, v);
+            for (int i = 0; i < iters; ++i, y += down, from += S::kRowBytes) {
+                f2 v[4];
+                S::read(from, v);
+                k8.output<kAct>(v, how);
+                S::store(y, v);
+            }
+        };
+        Shared shared;
+        output(shared);
+        if (kAct == MVUE_ACT_SILU && !shared.held()) {
+            Each each;
+            output(each);
         }
         if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
     }
@@ -1117,20 +1180,29 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
             k8.neg_mean[j] = pair(-mean);
             k8.slope[j] = mul2(gamma[j], pair(rstd));
         }
-        f2 sum[4] = {}, along[4] = {};
+        f2 sum[4], along[4];
         const int iters = r.mine ? r.iters : 0;
-        const char *slot = r.slots(0), *dslot = r.slots(1);
-        for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[4], d[4];
-            S::read(slot, v);
-            S::read(dslot, d);
-            k8.gradient<kAct>(v, d);
+        const auto sums = [&](auto& how) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                sum[j] = add2(sum[j], d[j]);
-                along[j] = fma2(d[j], v[j], along[j]);
+            for (int j = 0; j < 4; ++j) sum[j] = along[j] = pair(0.0f);
+            const char *slot = r.slots(0), *dslot = r.slots(1);
+            for (int i = 0; i < iters; ++i, slot += S::kRowBytes, dslot += S::kRowBytes) {
+                f2 v[4], d[4];
+                S::read(slot, v);
+                S::read(dslot, d);
+                k8.gradient<kAct>(v, d, how);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    sum[j] = add2(sum[j], d[j]);
+                    along[j] = fma2(d[j], v[j], along[j]);
+                }
             }
-        }
+        };
+        Shared shared;
+        Each each;
+        sums(shared);
+        const bool held = kAct != MVUE_ACT_SILU || shared.held();
+        if (!held) sums(each);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             all_sum[j] = add2(all_sum[j], sum[j]);
@@ -1148,19 +1220,22 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
             sb += p.y;
         }
         const f2 level = pair(-rstd * (sa * inv)), tilt = pair(-rstd * rstd * (rstd * sb * inv));    // dx = slope dz + level + tilt (x - mean)
-        T* dx = r.at(static_cast<T*>(q.out), q.ldo);
         const int64_t down = (int64_t)r.threads_down * q.ldo;
-        slot = r.slots(0);
-        dslot = r.slots(1);
-        for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
-            f2 v[4], d[4];
-            S::read(slot, v);
-            S::read(dslot, d);
-            k8.gradient<kAct>(v, d);
+        const auto output = [&](auto& how) {
+            T* dx = r.at(static_cast<T*>(q.out), q.ldo);
+            const char *slot = r.slots(0), *dslot = r.slots(1);
+            for (int i = 0; i < iters; ++i, dx += down, slot += S::kRowBytes, dslot += S::kRowBytes) {
+                f2 v[4], d[4];
+                S::read(slot, v);
+                S::read(dslot, d);
+                k8.gradient<kAct>(v, d, how);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt, level));
-            S::store(dx, v);
-        }
+                for (int j = 0; j < 4; ++j) v[j] = fma2(k8.slope[j], d[j], fma2(v[j], tilt, level));
+                S::store(dx, v);
+            }
+        };
+        if (held) output(shared);
+        else output(each);
         if (unit + clusters < (unsigned)a.units) r.fetch(unit + clusters);     // each thread has read what it replaces
     }
     copies_wait();
