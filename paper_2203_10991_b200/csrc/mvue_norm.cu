@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) norm_stats_kernel(const __grid_const
             }
             const float delta = m - mean[j];
             mean[j] = fmaf(delta, share, mean[j]);
-            m2[j] += fmaf(delta * delta, weight, dev);
+            m2[j] += fmaf(delta * weight, delta, dev);          // weight first: it is 0 with the first rows, where delta^2 may overflow
         }
         count = all;
     }
