@@ -1,0 +1,41 @@
+"""AdamWPlan as an object: seeds, refused gradients."""
+import pytest
+import torch
+
+from paper_2203_10991_b200 import optim
+
+gpu = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+@gpu
+def test_slow_average_moves_without_a_seed_of_ones_own():
+    # sqrt(v) = 4 q, gradients of size q: v falls to q^2 at the rate beta2 = 0.999.  With the same random numbers each step
+    # every element has a fixed threshold, and the average stays where it is.
+    n, q = 4096, 1e-3
+    plan = optim.AdamWPlan.zeros([torch.zeros(n, device="cuda")], state_bits=8)
+    plan.exp_avg_sqs[0].view(torch.uint8).fill_(0x60)                       # 2^(12-7) = 32 in units of the scale
+    plan.exp_avg_sq_scales[0].fill_(4 * q / 32)
+    g = [torch.full((n,), q, device="cuda")]
+    g[0][::256] = 40 * q                                                    # one large value a block keeps the scale up
+    for t in range(1, 1001):
+        plan.step(g, step=t, lr=0.0, weight_decay=0.0)
+    root = (plan.exp_avg_sqs[0].double() * plan.exp_avg_sq_scales[0].double().repeat_interleave(256)).reshape(-1, 256)[:, 1:]
+    exact = (16 * 0.999 ** 1000 + (1 - 0.999 ** 1000)) ** 0.5 * q
+    # v follows the average of the squared codes, which the rounding's spread (a few per cent of sqrt(v) a step) raises a little
+    assert abs(float(root.mean()) / exact - 1) < 0.15
+
+
+@gpu
+def test_bf16_params_drift_in_the_mean_without_a_seed_of_ones_own():
+    # updates of 2^-16 on params of 1 (half a unit there is 2^-9): 256 steps move the mean by 2^-8 (32-bit states, v' = m'^2 = 1)
+    n, steps, lr = 65536, 256, 2.0 ** -16
+    p = [torch.ones(n, device="cuda", dtype=BF16)]
+    plan = optim.AdamWPlan.zeros(p)
+    g = [torch.ones(n, device="cuda")]
+    for t in range(1, steps + 1):
+        plan.step(g, step=t, lr=lr, weight_decay=0.0, stochastic_rounding=True)
+    # each element falls by 2^-8 with probability 2^-8 a step: the mean's deviation is 2^-8 sqrt(256 / 256 / 65536) = 2^-16
+    assert abs(float((1 - p[0].double()).mean()) - steps * lr) < 8 * 2.0 ** -16
+    # and is not the same for all: with fixed thresholds 1 in 256 would fall at every step
+    assert float((1 - p[0].double()).max()) < 0.1
