@@ -91,10 +91,13 @@ class AdamWPlan:
     def _point(self, grads) -> None:
         if len(grads) != len(self._array):
             raise ValueError("one gradient for each param")
-        for e, p, g in zip(self._array, self.params, grads):
+        found = []
+        for p, g in zip(self.params, grads):
             if g.device != self._device or not _same_layout(g, p):
                 raise ValueError("a gradient has its param's device, size and strides")
-            e.grad_dtype, e.grad = binding._dtype_code(g), g.data_ptr()
+            found.append((binding._dtype_code(g), g.data_ptr()))
+        for e, (code, ptr) in zip(self._array, found):                       # nothing was refused
+            e.grad_dtype, e.grad = code, ptr
         self._grads = list(grads)
 
     def step(self, grads=None, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,

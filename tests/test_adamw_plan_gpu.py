@@ -39,3 +39,25 @@ def test_bf16_params_drift_in_the_mean_without_a_seed_of_ones_own():
     assert abs(float((1 - p[0].double()).mean()) - steps * lr) < 8 * 2.0 ** -16
     # and is not the same for all: with fixed thresholds 1 in 256 would fall at every step
     assert float((1 - p[0].double()).max()) < 0.1
+
+
+@gpu
+def test_refused_gradients_leave_the_plan_as_it_is():
+    def plan_of():
+        p = [torch.full((300,), 0.5, device="cuda"), torch.full((8, 64), 0.5, device="cuda")]
+        return p, optim.AdamWPlan.zeros(p)
+
+    first = [torch.full((300,), 0.1, device="cuda"), torch.full((8, 64), 0.2, device="cuda")]
+    other = torch.full((300,), -7.0, device="cuda")
+    p, plan = plan_of()
+    q, want = plan_of()
+    plan.step(first, step=1, lr=1e-2)
+    want.step(first, step=1, lr=1e-2)
+    for bad in ([other, torch.zeros(8, 128, device="cuda")[:, ::2]], [other, torch.zeros(8, 64)], [other, torch.zeros(8, 65, device="cuda")], [other]):
+        with pytest.raises(ValueError):
+            plan.step(bad, step=2, lr=1e-2)
+    with pytest.raises(TypeError):
+        plan.step([other, torch.zeros(8, 64, device="cuda", dtype=torch.float16)], step=2, lr=1e-2)
+    plan.step(step=2, lr=1e-2)
+    want.step(first, step=2, lr=1e-2)
+    assert all(torch.equal(a, b) for a, b in zip(p, q))
