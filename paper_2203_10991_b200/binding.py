@@ -324,6 +324,24 @@ def mvue_adamw_step(tensors: ctypes.Array, count: int, config: AdamWConfig) -> N
     _check(lib().mvue_adamw_step(tensors, count, config, _stream_ptr()), "mvue_adamw_step")
 
 
+def _operands(first: torch.Tensor, *others: torch.Tensor | None, workspace: torch.Tensor | None = None,
+              dev_status: torch.Tensor | None = None) -> None:
+    """Raises unless all tensors are on one CUDA device and that is the current one, whose stream the call goes to: the
+    library reads every address on the device."""
+    device = first.get_device()                              # -1 on the CPU
+    if device < 0:
+        raise ValueError("wants CUDA tensors")
+    for t in (*others, workspace, dev_status):
+        if t is not None and t.get_device() != device:
+            raise ValueError("the operands are on different devices")
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the operands are on device {device}, the current device is {torch.cuda.current_device()}")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("the workspace is contiguous")
+    if dev_status is not None and (dev_status.dtype is not torch.int32 or dev_status.numel() == 0):
+        raise ValueError("dev_status is an int32 tensor")
+
+
 def _id_list(ids: torch.Tensor) -> tuple[torch.Tensor, int]:
     if ids.dtype is torch.int64:
         return ids.contiguous(), 64
@@ -337,8 +355,9 @@ def mvue_embedding(ids: torch.Tensor, W: torch.Tensor, *, scale: float = 1.0, ou
     """scale * W[ids]: ids int32 or int64 of any shape, W [vocab, cols] fp32 or bf16 (unit column stride).  Ids outside the
     vocabulary give rows of zeros and write MVUE_ERR_INDEX (-13) to dev_status (int32 CUDA tensor).  Returns
     [*ids.shape, cols] of out_dtype (W's own unless given); out: [tokens, cols] with unit column stride instead."""
+    _operands(ids, W, out, dev_status=dev_status)
     flat, id_bits = _id_list(ids)
-    assert ids.is_cuda and W.dim() == 2 and W.stride(1) == 1
+    assert W.dim() == 2 and W.stride(1) == 1
     vocab, cols = W.shape
     tokens = flat.numel()
     if out is None:
@@ -364,12 +383,13 @@ def mvue_embedding_grad(ids: torch.Tensor, dy: torch.Tensor, vocab: int, *, scal
                         workspace: torch.Tensor | None = None, dev_status: torch.Tensor | None = None) -> torch.Tensor:
     """dW[v] (+)= scale * sum of dy[t] over ids[t] = v: dy [*ids.shape, cols] fp32 or bf16, or [tokens, cols] with a row
     stride.  Rows that no token names are zero (accumulate: out, fp32, is added to).  Returns dW [vocab, cols]."""
+    _operands(ids, dy, out, workspace=workspace, dev_status=dev_status)
     flat, id_bits = _id_list(ids)
     cols = dy.shape[-1]
     tokens = flat.numel()
     if dy.dim() != 2:
         dy = dy.reshape(tokens, cols)
-    assert ids.is_cuda and dy.shape[0] == tokens and dy.stride(1) == 1
+    assert dy.shape[0] == tokens and dy.stride(1) == 1
     if out is None:
         if accumulate:
             raise ValueError("accumulate adds to a given out")
@@ -416,7 +436,7 @@ def _positions(t: torch.Tensor):
 
 def _affine(weight, bias, c: int) -> int:
     for t in (weight, bias):
-        if t is not None and (t.dim() != 1 or t.numel() != c or not t.is_contiguous() or not t.is_cuda):
+        if t is not None and (t.dim() != 1 or t.numel() != c or not t.is_contiguous()):
             raise ValueError("weight and bias are contiguous CUDA tensors of one element per channel")
     if weight is not None and bias is not None and weight.dtype is not bias.dtype:
         raise TypeError("weight and bias have one dtype")
@@ -434,8 +454,8 @@ def mvue_group_norm_act(x: torch.Tensor, groups: int, weight: torch.Tensor | Non
                         workspace: torch.Tensor | None = None, dev_status: torch.Tensor | None = None):
     """act(group_norm(x) * weight + bias) on a channels-last CUDA tensor x [n, ..., c], fp32 or bf16 (act: none, relu, silu,
     gelu).  Returns (y, mean, rstd); mean and rstd [n, groups] fp32 are what the backward pass takes."""
+    _operands(x, weight, bias, out, workspace=workspace, dev_status=dev_status)
     n, s, c, ldx = _positions(x)
-    assert x.is_cuda
     code = _affine(weight, bias, c)
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -462,8 +482,9 @@ def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.
                                  out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
                                  dev_status: torch.Tensor | None = None):
     """Backward pass of mvue_group_norm_act.  Returns (dx, dweight, dbias); the last two [c] fp32."""
+    _operands(x, dy, mean, rstd, weight, bias, out, workspace=workspace, dev_status=dev_status)
     n, s, c, ldx = _positions(x)
-    assert x.is_cuda and dy.shape == x.shape and dy.dtype is x.dtype
+    assert dy.shape == x.shape and dy.dtype is x.dtype
     for t in (mean, rstd):
         assert t.dim() == 2 and t.shape[1] == groups and t.numel() == n * groups and t.dtype is torch.float32 and t.is_contiguous()
     code = _affine(weight, bias, c)
