@@ -27,8 +27,14 @@ def _dense(t: torch.Tensor) -> bool:
     return True
 
 
+def _addresses(tensors) -> list[int]:
+    return list(map(torch.Tensor.data_ptr, tensors))
+
+
 class AdamWPlan:
-    """The tensors of an optimiser, marshalled once.  It keeps references to them; the step updates them in place.
+    """The tensors of an optimiser, marshalled once.  The step updates them in place, in the memory that they had when the plan
+    was made: the plan keeps that memory (do not resize it), and once a param's memory has been exchanged (p.data = ..., a
+    move to another device) the model wants a new plan.  step() with gradients raises then; without, it goes on with the old memory.
 
     params:     list of CUDA tensors, fp32 or bf16, dense (any dimension order).
     exp_avgs, exp_avg_sqs: 32-bit states: fp32 tensors; 8-bit states: torch.float8_e4m3fn tensors (of m and of sqrt(v)) with
@@ -69,10 +75,15 @@ class AdamWPlan:
                 setattr(e, field, t.data_ptr())
         self.params, self.exp_avgs, self.exp_avg_sqs, self.masters = list(params), list(exp_avgs), list(exp_avg_sqs), list(masters)
         self.exp_avg_scales, self.exp_avg_sq_scales = (list(scales[0]), list(scales[1]))
+        # tensors of the plan's own over the same memory, which outlives an exchange of a tensor's data thereby
+        self._memory = [t.detach() for ts in (params, masters, exp_avgs, exp_avg_sqs, *scales) for t in ts if t is not None]
+        self._addresses = _addresses(self.params)
         self._config = binding.AdamWConfig(state_bits=self.state_bits)
-        self._grads = None
+        self._grads = self._grad_addresses = None
         if grads is not None:
             self._point(grads)
+            self._memory += [g.detach() for g in grads]
+            self._grad_addresses = None
 
     @classmethod
     def zeros(cls, params, *, state_bits: int = 32, master: bool = False, grads=None) -> "AdamWPlan":
@@ -91,6 +102,8 @@ class AdamWPlan:
     def _point(self, grads) -> None:
         if len(grads) != len(self._array):
             raise ValueError("one gradient for each param")
+        if _addresses(self.params) != self._addresses:
+            raise ValueError("a param's memory has been exchanged since the plan was made: make a new plan")
         found = []
         for p, g in zip(self.params, grads):
             if g.device != self._device or not _same_layout(g, p):
@@ -98,7 +111,7 @@ class AdamWPlan:
             found.append((binding._dtype_code(g), g.data_ptr()))
         for e, (code, ptr) in zip(self._array, found):                       # nothing was refused
             e.grad_dtype, e.grad = code, ptr
-        self._grads = list(grads)
+        self._grads, self._grad_addresses = list(grads), [ptr for _, ptr in found]
 
     def step(self, grads=None, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
              weight_decay: float = 0.01, grad_scale: float = 1.0, dev_grad_scale: torch.Tensor | None = None, seed: int | None = None,
@@ -112,6 +125,8 @@ class AdamWPlan:
             self._point(grads)
         elif self._grads is None and len(self._array):
             raise ValueError("no gradients")
+        elif self._grad_addresses is not None and _addresses(self._grads) != self._grad_addresses:
+            raise ValueError("a gradient's memory has been exchanged since it was given")
         if dev_grad_scale is not None and (dev_grad_scale.dtype != torch.float32 or dev_grad_scale.device != self._device
                                            or dev_grad_scale.numel() != 1):
             raise ValueError("dev_grad_scale is one fp32 element on the params' device")

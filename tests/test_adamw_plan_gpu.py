@@ -61,3 +61,26 @@ def test_refused_gradients_leave_the_plan_as_it_is():
     plan.step(step=2, lr=1e-2)
     want.step(first, step=2, lr=1e-2)
     assert all(torch.equal(a, b) for a, b in zip(p, q))
+
+
+@gpu
+def test_exchanged_memory_is_refused_and_never_written_after_it_was_freed():
+    p = [torch.full((4096,), 0.5, device="cuda"), torch.full((4096,), 0.5, device="cuda")]
+    g = [torch.full((4096,), 0.1, device="cuda") for _ in p]
+    plan = optim.AdamWPlan.zeros(p, grads=g)
+    plan.step(step=1, lr=1e-2)
+    after = p[1].clone()
+    p[1].data = p[1].data.clone()
+    with pytest.raises(ValueError):
+        plan.step(g, step=2, lr=1e-2)
+    # the old memory is the plan's: nothing else is given it, and the step without gradients stays inside
+    others = [torch.full((4096,), 7.0, device="cuda") for _ in range(64)]
+    plan.step(step=2, lr=1e-2)
+    assert all(bool((t == 7).all()) for t in others) and torch.equal(p[1], after)
+    again = optim.AdamWPlan(p, plan.exp_avgs, plan.exp_avg_sqs)
+    again.step(g, step=3, lr=1e-2)
+    assert not torch.equal(p[1], after)
+    g[0].data = g[0].data.clone()
+    with pytest.raises(ValueError):
+        again.step(step=4, lr=1e-2)
+    again.step(g, step=4, lr=1e-2)
