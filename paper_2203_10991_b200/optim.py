@@ -116,7 +116,7 @@ class AdamWPlan:
     def step(self, grads=None, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
              weight_decay: float = 0.01, grad_scale: float = 1.0, dev_grad_scale: torch.Tensor | None = None, seed: int | None = None,
              stochastic_rounding: bool = False) -> None:
-        """One step (step >= 1 counts them) on the current stream.  grads: this step's gradients (they stay the plan's
+        """One step (step >= 1 counts them) on the current stream of the params' device.  grads: this step's gradients (they stay the plan's
         until others are given); None reads the buffers the plan has.  seed keys what is rounded at random (8-bit states; bf16
         params without a float copy when stochastic_rounding): None takes the step's number; a seed of one's own has to be another
         one each step, since the same random numbers every time are a fixed threshold for each element, which averages and
@@ -135,4 +135,8 @@ class AdamWPlan:
         c.dev_grad_scale = None if dev_grad_scale is None else dev_grad_scale.data_ptr()
         c.seed = (step if seed is None else seed) & (2**64 - 1)
         c.options = binding.MVUE_OPT_STOCHASTIC_ROUNDING if stochastic_rounding else binding.MVUE_OPT_NONE
-        binding.mvue_adamw_step(self._array, len(self._array), c)
+        if self._device is None or self._device.index == torch.cuda.current_device():
+            binding.mvue_adamw_step(self._array, len(self._array), c)
+        else:
+            with torch.cuda.device(self._device):
+                binding.mvue_adamw_step(self._array, len(self._array), c)
