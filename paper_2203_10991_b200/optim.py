@@ -14,11 +14,18 @@ BLOCK = 256                       # elements that share one scale of the 8-bit s
 
 def _same_layout(a: torch.Tensor, b: torch.Tensor) -> bool:
     """Whether element i in memory of one is element i in memory of the other (all dense)."""
-    return a.numel() == b.numel() and ((a.is_contiguous() and b.is_contiguous()) or (a.shape == b.shape and a.stride() == b.stride()))
+    if a.numel() != b.numel():
+        return False
+    if a.is_contiguous() and b.is_contiguous():
+        return True
+    # the stride of a dimension of size one says nothing
+    return a.shape == b.shape and all(n == 1 or s == t for n, s, t in zip(a.shape, a.stride(), b.stride()))
 
 
 def _dense(t: torch.Tensor) -> bool:
     """Whether the tensor covers its memory without gaps or overlaps, in any order of its dimensions."""
+    if t.numel() == 0:
+        return True
     want = 1
     for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda d: d[1]):
         if stride != want:
