@@ -131,8 +131,9 @@ typedef enum { MVUE_ACT_NONE = 0, MVUE_ACT_RELU = 1, MVUE_ACT_SILU = 2, MVUE_ACT
  *  workspace  mvue_group_norm_workspace_bytes(n, s, c, groups) bytes, 16-byte aligned; contents scratch.  A call that
  *             gives mean and rstd and whose samples stay in shared memory (x and y aligned for wide accesses, whole groups
  *             that fit eight thread blocks) uses none and accepts NULL; others return MVUE_ERR_WORKSPACE without it.
- *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait between the blocks of a cluster expires
- *             (then the outputs are unspecified); otherwise left untouched.
+ *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait between the blocks of a cluster expires;
+ *             otherwise left untouched.  What depended on the wait is NaN then: y, mean and rstd of the samples concerned, or dx
+ *             in the backward pass.
  * Arithmetic in binary32; the output is rounded once.  n = 0: nothing.  s >= 1. */
 MVUE_API int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t c, int64_t ldx, int groups, const void* gamma,
                                  const void* beta, int affine_dtype, float eps, int act, void* y, int64_t ldy, float* mean, float* rstd,
@@ -148,6 +149,16 @@ MVUE_API int mvue_group_norm_act_backward(const void* dy, int64_t lddy, const vo
                                           const void* beta, int affine_dtype, int act, void* dx, int64_t lddx, float* dgamma,
                                           float* dbeta, void* workspace, size_t workspace_bytes, int* dev_status, void* stream);
 MVUE_API int mvue_group_norm_workspace_bytes(int64_t n, int64_t s, int64_t c, int groups, size_t* bytes);   /* bytes: HOST */
+
+/* Self-test of that bounded wait.  One forward launch (dy = NULL) or one backward launch, without affine and activation and
+ * with eps = 1, on contiguous tensors whose samples stay in the shared memory of two or more thread blocks (else
+ * MVUE_ERR_SHAPE), in which the blocks send one another nothing: every wait gives up after `polls` polls
+ * (1 <= polls <= 65536, else MVUE_ERR_SHAPE; each takes about 4 us) and the blocks leave the ordinary way.
+ * MVUE_ERR_DEVICE_TIMEOUT is written to *dev_status (required) and NaN to the outputs.  Nothing is in flight, nothing
+ * traps or faults, and the next call must be correct.  The other arguments are those of the two calls above. */
+MVUE_API int mvue_selftest_group_norm_timeout(int polls, const void* x, const void* dy, int dtype, int64_t n, int64_t s, int64_t c,
+                                              int groups, float* mean, float* rstd, void* out, void* workspace,
+                                              size_t workspace_bytes, int* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -28,7 +28,8 @@ EXPORTS = ("mvue_version", "mvue_status_string", "mvue_last_cuda_error", "mvue_p
            "mvue_gemm_workspace_bytes", "mvue_sparse_update_gemm_noalloc", "mvue_fused_update_gemm", "mvue_fused_update_gemm_joint",
            "mvue_probe_sparse_mma", "mvue_selftest_wait_timeout",
            "mvue_adamw_step", "mvue_embedding", "mvue_embedding_grad", "mvue_embedding_grad_workspace_bytes",
-           "mvue_group_norm_act", "mvue_group_norm_act_backward", "mvue_group_norm_workspace_bytes")
+           "mvue_group_norm_act", "mvue_group_norm_act_backward", "mvue_group_norm_workspace_bytes",
+           "mvue_selftest_group_norm_timeout")
 
 
 class AdamWTensor(ctypes.Structure):
@@ -96,6 +97,7 @@ def lib() -> ctypes.CDLL:
         L.mvue_group_norm_act_backward.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, ci, vp, vp, vp, vp, ci, ci, vp, i64, vp, vp,
                                                    vp, csz, vp, vp]
         L.mvue_group_norm_workspace_bytes.argtypes = [i64, i64, i64, ci, szp]
+        L.mvue_selftest_group_norm_timeout.argtypes = [ci, vp, vp, ci, i64, i64, i64, ci, vp, vp, vp, vp, csz, vp, vp]
         L.mvue_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, ctypes.POINTER(AdamWConfig), vp]
         _lib = L
     return _lib
@@ -504,3 +506,17 @@ def mvue_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.
                                               workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream_ptr()),
            "mvue_group_norm_act_backward")
     return out, dweight, dbias
+
+
+def mvue_selftest_group_norm_timeout(polls: int, x: torch.Tensor, groups: int, mean: torch.Tensor, rstd: torch.Tensor, out: torch.Tensor,
+                                     dev_status: torch.Tensor, dy: torch.Tensor | None = None) -> None:
+    """A forward launch (or, with dy, a backward one) on contiguous x [n, s, c] whose blocks send one another nothing, so that
+    their bounded waits run out: MVUE_ERR_DEVICE_TIMEOUT in dev_status, NaN in the outputs."""
+    _operands(x, dy, mean, rstd, out, dev_status=dev_status)
+    n, s, c = x.shape
+    assert all(t is None or (t.shape == x.shape and t.dtype is x.dtype and t.is_contiguous()) for t in (x, dy, out))
+    assert all(t.shape == (n, groups) and t.dtype is torch.float32 and t.is_contiguous() for t in (mean, rstd))
+    workspace = x.new_empty(mvue_group_norm_workspace_bytes(n, s, c, groups), dtype=torch.uint8)
+    _check(lib().mvue_selftest_group_norm_timeout(polls, x.data_ptr(), _ptr(dy), _dtype_code(x), n, s, c, groups, mean.data_ptr(),
+                                                  rstd.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                                  dev_status.data_ptr(), _stream_ptr()), "mvue_selftest_group_norm_timeout")

@@ -44,7 +44,10 @@ struct NormArgs {
     float2* coef;                    // backward: [n, groups]: means over the group of gamma dz and of gamma dz xh
     float *dgamma, *dbeta;
     int* dev_status;
+    uint32_t polls;                  // after which a wait between the blocks of a cluster gives up
+    int mute;                        // nothing is sent between them (the self-test of that exit)
 };
+constexpr uint32_t kPolls = 1u << 22;         // of 4 us each (measured): 17 s
 
 __device__ __forceinline__ float affine(const void* p, int is_bf16, int64_t i, float none) {
     if (!p) return none;
@@ -722,6 +725,7 @@ struct Resident {
             *reinterpret_cast<float2*>(to) = make_float2(x, y);
             return;
         }
+        if (lost || a.norm.mute) return;                     // after a wait that ran out nobody counts any more
         uint32_t there, counter;
         asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((uint32_t)__cvta_generic_to_shared(to)), "r"(block));
         asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(counter) : "r"(bar(turn)), "r"(block));
@@ -730,14 +734,15 @@ struct Resident {
     }
     __device__ __forceinline__ float2 sent(int turn, int block, int g) const { return *reinterpret_cast<const float2*>(place_of(turn, block, g)); }
     // Waits for the values of all blocks.  When they do not come: MVUE_ERR_DEVICE_TIMEOUT in dev_status, and the thread waits no
-    // more (`lost`) but takes the rest of the way as it is, so that all threads meet at the same barriers to the end.
+    // more (`lost`) but takes the rest of the way as it is, with NaN in the place of what it has not got, so that all threads
+    // meet at the same barriers to the end and nobody takes the outputs for results.
     __device__ __forceinline__ void meet(int turn, uint32_t parity) {
         if (a.cluster == 1) {
             __syncthreads();
             return;
         }
         if (lost) return;
-        for (uint32_t spin = 0; spin < (1u << 22); ++spin) {
+        for (uint32_t spin = 0; spin < a.norm.polls; ++spin) {
             uint32_t done;
             asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                          : "=r"(done) : "r"(bar(turn)), "r"(parity) : "memory");
@@ -747,9 +752,17 @@ struct Resident {
         lost = true;
         if (a.norm.dev_status) *a.norm.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
     }
-    // before the block ends: nobody stores into its shared memory any more
+    // x, or NaN where the wait before it ran out
+    __device__ __forceinline__ float got(float x) const { return lost ? __uint_as_float(0x7FC00000u) : x; }
+    // Before the block ends: nobody stores into its shared memory any more.  Behind the cluster's barrier nothing more is sent,
+    // and where every wait of the block has ended all that was sent has arrived.  After one that ran out some of it may
+    // still be on its way, for a microsecond or so: the block stays for 200 more.
     __device__ __forceinline__ void close() const {
-        if (a.cluster > 1) cg::this_cluster().sync();
+        if (a.cluster == 1) return;
+        cg::this_cluster().sync();
+        if (!__syncthreads_or(lost)) return;
+        const long long from = clock64();
+        for (int i = 0; i < (1 << 16) && clock64() - from < 400000; ++i) __nanosleep(100);
     }
 };
 
@@ -818,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_kernel(const __grid
         for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
             // a warp per group, a lane per block of the cluster
             const float2 p = lane < a.cluster ? r.sent(turn, lane, g) : make_float2(0.0f, 0.0f);
-            const float mean = warp_sum(lane_rows * p.x) / (float)q.s;
+            const float mean = warp_sum(r.got(lane_rows * p.x)) / (float)q.s;
             const float d = p.x - mean;
             const float dev = warp_sum(fmaf(lane_rows * q.group_size * d, d, p.y));
             const float rstd = 1.0f / sqrtf(dev / all + q.eps);
@@ -940,7 +953,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
         for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
             const float2 p = lane < a.cluster ? r.sent(turn, lane, g) : make_float2(0.0f, 0.0f);
             const float rstd = q.rstd[g0 + g];
-            const float level = -rstd * (warp_sum(p.x) * inv), tilt = -rstd * rstd * (warp_sum(p.y) * inv);
+            const float level = -rstd * (warp_sum(r.got(p.x)) * inv), tilt = -rstd * rstd * (warp_sum(p.y) * inv);
             for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
                 r.one[c] = level;
                 r.two[c] = tilt;
@@ -1101,7 +1114,7 @@ __global__ void __launch_bounds__(kThreads, 4) norm_folded_kernel(const __grid_c
         float mean = 0.0f, dev = 0.0f;
         int left = (int)q.s;
         for (int b = 0; b < a.cluster; ++b, left -= a.rows) mean = fmaf((float)max(0, min(a.rows, left)), r.sent(turn, b, r.g).x, mean);
-        mean /= (float)q.s;
+        mean = r.got(mean / (float)q.s);
         left = (int)q.s;
         for (int b = 0; b < a.cluster; ++b, left -= a.rows) {
             const float2 p = r.sent(turn, b, r.g);
@@ -1219,7 +1232,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_folded_grad_kernel(const __g
             sa += p.x;
             sb += p.y;
         }
-        const f2 level = pair(-rstd * (sa * inv)), tilt = pair(-rstd * rstd * (rstd * sb * inv));    // dx = slope dz + level + tilt (x - mean)
+        const f2 level = pair(-rstd * (r.got(sa) * inv)), tilt = pair(-rstd * rstd * (rstd * sb * inv));    // dx = slope dz + level + tilt (x - mean)
         const int64_t down = (int64_t)r.threads_down * q.ldo;
         const auto output = [&](auto& how) {
             T* dx = r.at(static_cast<T*>(q.out), q.ldo);
@@ -1526,7 +1539,7 @@ int mvue_group_norm_act(const void* x, int dtype, int64_t n, int64_t s, int64_t 
     a.x = x; a.out = y; a.n = n; a.s = s; a.c = c; a.ldx = ldx; a.ldo = ldy;
     a.groups = groups; a.group_size = (int)(c / groups);
     a.gamma = gamma; a.beta = beta; a.affine_bf16 = affine_dtype == MVUE_BF16;
-    a.eps = eps; a.mean = mean; a.rstd = rstd; a.dev_status = dev_status;
+    a.eps = eps; a.mean = mean; a.rstd = rstd; a.dev_status = dev_status; a.polls = kPolls;
     return run(a, dtype, act, std::min(row_vector(x, ldx, c, dtype), row_vector(y, ldy, c, dtype)), workspace, workspace_bytes, stream,
                "mvue_group_norm_act launch");
 }
@@ -1554,9 +1567,26 @@ int mvue_group_norm_act_backward(const void* dy, int64_t lddy, const void* x, in
     a.groups = groups; a.group_size = (int)(c / groups);
     a.gamma = gamma; a.beta = beta; a.affine_bf16 = affine_dtype == MVUE_BF16;
     a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);      // only read here
-    a.dgamma = dgamma; a.dbeta = dbeta; a.dev_status = dev_status;
+    a.dgamma = dgamma; a.dbeta = dbeta; a.dev_status = dev_status; a.polls = kPolls;
     return run(a, dtype, act, std::min({row_vector(x, ldx, c, dtype), row_vector(dy, lddy, c, dtype), row_vector(dx, lddx, c, dtype)}), workspace,
                workspace_bytes, stream, "mvue_group_norm_act_backward launch");
+}
+
+int mvue_selftest_group_norm_timeout(int polls, const void* x, const void* dy, int dtype, int64_t n, int64_t s, int64_t c, int groups,
+                                     float* mean, float* rstd, void* out, void* workspace, size_t workspace_bytes, int* dev_status,
+                                     void* stream) {
+    if (int e = check(dtype, n, s, c, groups, MVUE_F32, nullptr, nullptr, MVUE_ACT_NONE)) return e;
+    if (polls <= 0 || polls > (1 << 16) || n == 0) return MVUE_ERR_SHAPE;
+    if (!x || !mean || !rstd || !out || !dev_status) return MVUE_ERR_NULL;
+    const int64_t esz = size_of(dtype);
+    if (off(x, 8 * esz) || off(dy, 8 * esz) || off(out, 8 * esz) || off(mean, 4) || off(rstd, 4) || off(dev_status, 4)) return MVUE_ERR_ALIGN;
+    const Keep k = keep_of(n, s, c, groups, esz, dy ? 2 : 1);
+    if (!k.pieces || k.cluster < 2) return MVUE_ERR_SHAPE;
+    NormArgs a = {};
+    a.x = x; a.dy = dy; a.out = out; a.n = n; a.s = s; a.c = c; a.ldx = a.lddy = a.ldo = c;
+    a.groups = groups; a.group_size = (int)(c / groups);
+    a.eps = 1.0f; a.mean = mean; a.rstd = rstd; a.dev_status = dev_status; a.polls = (uint32_t)polls; a.mute = 1;
+    return run(a, dtype, MVUE_ACT_NONE, 8, workspace, workspace_bytes, stream, "mvue_selftest_group_norm_timeout launch");
 }
 
 }  // extern "C"
