@@ -290,6 +290,10 @@ __global__ void __launch_bounds__(kThreads) norm_join_kernel(const __grid_consta
     }
 }
 
+// The factor of dx: 0 where a group is one element, whose output does not depend on it (the sum of its terms is then the difference
+// of two roundings of one product, times rstd).
+__device__ __forceinline__ float more_than_one(const NormArgs& a) { return a.s * a.group_size > 1 ? 1.0f : 0.0f; }
+
 // What the elements of a thread's channels need: z = (x - mean) slope + shift, slope = rstd gamma, shift = beta; backward
 // dx = slope dz + level + tilt (x - mean).
 struct Channels {
@@ -478,18 +482,21 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
     T* dx = static_cast<T*>(a.out) + n * a.s * a.ldo;
     Channels k;
     set_channels(k, a, p);
+    const float some = more_than_one(a);
     float low[8], off[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int64_t g = n * a.groups + (j < p.cols.count ? p.channel(j) : 0) / a.group_size;
-        const float r = a.rstd[g];
+        const float r = a.rstd[g] * some;
         const float2 q = a.coef[g];
         low[j] = -r * q.x;
-        off[j] = -r * r * q.y;
+        off[j] = -r * a.rstd[g] * q.y;
     }
     f2 level[4], tilt[4];
     pairs(low, level);
     pairs(off, tilt);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) k.slope[j] = mul2(k.slope[j], pair(some));
     Each each;
     for (; p.row < p.end; p.row += (int64_t)p.stride * 2) {
         float v[2][8], d[2][8];
@@ -887,6 +894,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
     const unsigned clusters = gridDim.x / (unsigned)a.cluster;
     unsigned unit = blockIdx.x / (unsigned)a.cluster;
     const int lane = threadIdx.x & 31;
+    const float some = more_than_one(q);
     const float inv = 1.0f / ((float)q.s * q.group_size);
     r.fetch(unit);
     r.open();
@@ -952,7 +960,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
         r.meet(turn, parity);
         for (int g = threadIdx.x >> 5; g < r.groups; g += kThreads / 32) {
             const float2 p = lane < a.cluster ? r.sent(turn, lane, g) : make_float2(0.0f, 0.0f);
-            const float rstd = q.rstd[g0 + g];
+            const float rstd = q.rstd[g0 + g] * some;
             const float level = -rstd * (warp_sum(r.got(p.x)) * inv), tilt = -rstd * rstd * (warp_sum(p.y) * inv);
             for (int c = g * q.group_size + lane; c < (g + 1) * q.group_size; c += 32) {
                 r.one[c] = level;
@@ -963,6 +971,8 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
         f2 level[4], tilt[4];            // dx = slope dz + level + tilt (x - mean)
         read_values(r.one + r.piece * 8, level);
         read_values(r.two + r.piece * 8, tilt);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k8.slope[j] = mul2(k8.slope[j], pair(some));
         const int64_t down = (int64_t)r.threads_down * q.ldo;
         const auto output = [&](auto& how) {
             T* dx = r.at(static_cast<T*>(q.out), q.ldo);
