@@ -8,14 +8,14 @@
 // eight 16-bit random numbers are one generator call.
 //
 // Measured (B200, HBM copy 6.55 TB/s).  24 matrices of 4 M elements, 32-bit states, bf16 + float copy: 438 us for 3.02 GB,
-// 105 % of the copy rate: bound by HBM.  Two matrices of 59 M elements, 8-bit states, bf16: 333 us against 180 us of HBM
+// 105 % of the copy rate: bound by HBM.  Two matrices of 59 M elements, 8-bit states, bf16: 315 us against 180 us of HBM
 // time: bound by instructions, above 60 per element of which 8 are the generator.  What brought it down: the code taken from
 // the bit pattern instead of by way of a step and a rounded sum (400 -> 341 us), packed pairs and hardware decoding
-// (457 -> 400 us), five blocks an SM (341 -> 315 us, although 17 words a thread spill).  Six blocks spill more (368 us); loads of the
-// next block ahead of the arithmetic cost more registers than they hide (351 us).  Finding the lanes whose code may differ
-// between the approximate root and the correctly rounded one costs 12 of the 333 us; the correctly rounded root for every element
-// would take 374 us.  It depends on the data: lanes with a code below 2^-6, zeros among them, take the longer way.  Every second block
-// zero 366 us, all zero 404 us, one zero in every lane 438 us.  96 vectors of 2500 elements: 7 to 9 us, the launch.
+// (457 -> 400 us), five blocks an SM (341 -> 315 us, although eight words a thread spill).  Six blocks spill more (368 us); loads of
+// the next block ahead of the arithmetic cost more registers than they hide (351 us).  The root is approximate; the correctly
+// rounded one for every element would take 374 us, finding the lanes whose code may differ between the two costs what codes below
+// 2^-6 in line have saved.  The time depends on the data: lanes with such codes, zeros among them, take longer.  Every second block
+// zero 354 us, all zero 408 us, one zero in every lane 441 us.  96 vectors of 2500 elements: 7 to 9 us, the launch.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -53,7 +53,7 @@ struct Constants {
     bool round_up_at_random;   // a bf16 param without master
 };
 
-// Kernel parameters may take 32764 bytes: 300 tensors of 84 bytes.  Short lists go in a small block, since the
+// Kernel parameters may take 32764 bytes: 320 tensors of 84 bytes take 27 KB.  Short lists go in a small block, since the
 // parameters of every launch are copied.
 template <int kCapacity>
 struct Params {
@@ -84,20 +84,24 @@ __device__ __forceinline__ uint32_t e4m3_code(float y, uint32_t r) {
 // r to the 16 bits below the three mantissa bits of a binary32 carries into them exactly that often, and the code is the
 // low five exponent bits and the three mantissa bits less a constant.  r8: r << 8, which is r's place four bits further up,
 // where the code fills the highest byte; the sign is shifted out.
-__device__ __forceinline__ uint32_t e4m3_codes_normal(const float* y, const uint32_t* r8) {
-    uint32_t t[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = __float_as_uint(y[i]) * 16u + r8[i];
+__device__ __forceinline__ uint32_t carried(float y, uint32_t r8) { return __float_as_uint(y) * 16u + r8; }
+__device__ __forceinline__ uint32_t e4m3_codes_normal(const uint32_t* t) {
     const uint32_t bytes = __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410);
     return (bytes ^ 0x40404040u) & 0x7F7F7F7Fu;              // less 120 << 3: the top two bits are 11 or 00, to become 00 or 01
 }
 
-// Square root with a relative error of at most 2^-23, subnormal arguments included: v' below 2^-126 (|g'| below 3e-18 on
-// a fresh state) has an ordinary root, and with a small eps that is what the step is divided by.  Flushing them to zero saves 6 of
-// 333 us on 2 x 59 M elements with 8-bit states.
+__device__ __forceinline__ uint32_t min_halves(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Square root with a relative error of at most 2^-23; without kSubnormal, arguments below 2^-126 have the root 0 (v' of |g'| below
+// 3e-18 on a fresh state).
+template <bool kSubnormal>
 __device__ __forceinline__ float fast_root(float x) {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    if (kSubnormal) asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    else asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 // the larger magnitude, NaN if there is one
@@ -121,8 +125,8 @@ __device__ __forceinline__ float block_scale(float top, float* factor) {
 // A NaN whose lower half is zero: random bits added to it do not carry into the sign.
 __device__ __forceinline__ float short_nan(float x) { return x != x ? __uint_as_float(0x7FC00000u) : x; }
 
-// The new moments of eight elements (v: the second moment, root: its square root with a relative error of at most 2^-23)
-// and the new param.
+// The new moments of eight elements (v: the second moment, root: its square root, fast_root's) and the new param.
+template <bool kSubnormal>
 struct Step {
     f2 m[4], v[4], root[4], p[4];
     __device__ __forceinline__ void take(const Constants& c, const f2 (&g)[4], float gs) {
@@ -137,7 +141,7 @@ struct Step {
             v[j] = add2(fma2(b2, v[j], nothing), fma2(mul2(c2, x), x, nothing));
             float r0, r1, d0, d1;
             unpair(v[j], r0, r1);
-            root[j] = pair(fast_root(r0), fast_root(r1));
+            root[j] = pair(fast_root<kSubnormal>(r0), fast_root<kSubnormal>(r1));
             unpair(add2(mul2(root[j], inv_root), eps), d0, d1);
             p[j] = fma2(p[j], decay, mul2(size, mul2(m[j], pair(fast_reciprocal(d0), fast_reciprocal(d1)))));
         }
@@ -176,7 +180,7 @@ __device__ __forceinline__ void store_codes(uint8_t* to, bool wide, int count, c
 }
 
 // kRuns: blocks of 256 elements that a warp takes one after another; the search for the tensor is shared by them.
-template <int kBits, int kCapacity, int kRuns>
+template <int kBits, int kCapacity, int kRuns, bool kSubnormal>
 __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constant__ Params<kCapacity> a) {
     grid_dependency_wait();
     const int tile = blockIdx.x;
@@ -201,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constan
 
         // all loads first
         f2 g[4];
-        Step s;
+        Step<kSubnormal> s;
         uint2 mc = make_uint2(0u, 0u), vc = mc;
         float ms = 0.0f, vs = 0.0f;
         if (flags & kGradBf16) load_pairs(static_cast<const __nv_bfloat16*>(t.grad) + i0, wide, count, g);
@@ -254,42 +258,53 @@ __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constan
             float mf, vf;
             ms = block_scale(warp_largest(m_top), &mf);
             vs = block_scale(__fsqrt_rn(warp_largest(v_top)), &vf);
+            // The code of sqrt(v) is that of the correctly rounded root also where the approximate one is on the other side of a
+            // threshold.  z is raised by 10 2^-24 of itself, against at most 6 2^-24 for the two roots' distance and the roundings: it
+            // is above the z of the correctly rounded root by at most 16 units of its last place, and gives the same code unless
+            // its sum with the random number is less than that above a carry.  Lanes where one is within 32 units
+            // (one in four thousand) take the second way.
+            const float raised = vf * 1.00000059604644775390625f;
             float y[8], z[8];
             uint32_t r8[8];
-            float least = 1.0f;
+            float least_y = 1.0f, least_z = 1.0f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 unpair(mul2(s.m[j], pair(mf)), y[2 * j], y[2 * j + 1]);
-                unpair(mul2(s.root[j], pair(vf)), z[2 * j], z[2 * j + 1]);
-                least = fminf(least, fminf(fminf(fabsf(y[2 * j]), z[2 * j]), fminf(fabsf(y[2 * j + 1]), z[2 * j + 1])));
+                unpair(mul2(s.root[j], pair(raised)), z[2 * j], z[2 * j + 1]);
+                least_y = fminf(least_y, fminf(fabsf(y[2 * j]), fabsf(y[2 * j + 1])));
+                least_z = fminf(least_z, fminf(z[2 * j], z[2 * j + 1]));
                 r8[2 * j] = __byte_perm(rw[j], 0u, 0x4014);              // the half-words with their bytes exchanged, << 8
                 r8[2 * j + 1] = __byte_perm(rw[j], 0u, 0x4234);
             }
-            // The code of sqrt(v) is that of the correctly rounded root, also where the approximate one is on the other side of
-            // a threshold.  The two roots are at most 2^-23 + 2^-24 apart (relative), z with its rounding 5 units of its last place:
-            // a lane with an element whose z plus random number is within 8 units of a carry takes the second way, one lane
-            // in eight thousand. 
-            uint32_t nearest = 0xFFFFFFFFu;
+            // bits 8 .. 23 of the sums, two to a word: below 2 within 32 units above a carry
+            uint32_t ty[8], tz[8], nearest = 0xFFFFFFFFu;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) nearest = min(nearest, (__float_as_uint(z[i]) * 16u + r8[i]) * 256u + 0x8000u);
+            for (int i = 0; i < 8; ++i) {
+                ty[i] = carried(y[i], r8[i]);
+                tz[i] = carried(z[i], r8[i]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) nearest = min_halves(nearest, __byte_perm(tz[2 * j], tz[2 * j + 1], 0x6521));
             uint32_t mw[2], vw[2];
-            if (least >= 0.015625f && nearest >= 0x10000u) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t signs = __byte_perm(__byte_perm(__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), 0x0073),
-                                                       __byte_perm(__float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3]), 0x0073), 0x5410);
-                    mw[h] = e4m3_codes_normal(y + 4 * h, r8 + 4 * h) | (signs & 0x80808080u);
-                    vw[h] = e4m3_codes_normal(z + 4 * h, r8 + 4 * h);
-                }
-            } else {
-                mw[0] = mw[1] = vw[0] = vw[1] = 0u;
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t signs = __byte_perm(__byte_perm(__float_as_uint(y[4 * h]), __float_as_uint(y[4 * h + 1]), 0x0073),
+                                                   __byte_perm(__float_as_uint(y[4 * h + 2]), __float_as_uint(y[4 * h + 3]), 0x0073), 0x5410);
+                mw[h] = e4m3_codes_normal(ty + 4 * h) | (signs & 0x80808080u);
+                vw[h] = e4m3_codes_normal(tz + 4 * h);
+            }
+            if (least_y < 0.015625f) {
+                mw[0] = mw[1] = 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    mw[i >> 2] |= (e4m3_code(fminf(fabsf(y[i]), 448.0f), r8[i] >> 8) | (y[i] < 0.0f ? 0x80u : 0u)) << (8 * (i & 3));
+            }
+            if (least_z < 0.01563f || (nearest & 0xFFFFu) < 2u || nearest < 0x20000u) {
+                vw[0] = vw[1] = 0u;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint32_t cm = e4m3_code(fminf(fabsf(y[i]), 448.0f), r8[i] >> 8) | (y[i] < 0.0f ? 0x80u : 0u);
                     const float exact = vf > 0.0f ? __fmul_rn(__fsqrt_rn(v[i]), vf) : 0.0f;
-                    const uint32_t cv = max(e4m3_code(fminf(exact, 448.0f), r8[i] >> 8), v[i] > 0.0f ? 1u : 0u);
-                    mw[i >> 2] |= cm << (8 * (i & 3));
-                    vw[i >> 2] |= cv << (8 * (i & 3));
+                    vw[i >> 2] |= max(e4m3_code(fminf(exact, 448.0f), r8[i] >> 8), v[i] > 0.0f ? 1u : 0u) << (8 * (i & 3));
                 }
             }
             store_codes(static_cast<uint8_t*>(t.m) + i0, wide, count, mw);
@@ -325,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constan
     }
 }
 
-template <int kBits, int kCapacity, int kRuns>
+template <int kBits, int kCapacity, int kRuns, bool kSubnormal>
 cudaError_t launch(const mvue_adamw_tensor* ts, int64_t count, const Constants& c, uint64_t seed,
                    int64_t* first_block, int64_t* used, cudaStream_t stream) {
     Params<kCapacity> a;
@@ -355,7 +370,7 @@ cudaError_t launch(const mvue_adamw_tensor* ts, int64_t count, const Constants& 
     *used = i;
     if (n == 0) return cudaSuccess;
     a.count = n;
-    return launch_dependent(&adamw_kernel<kBits, kCapacity, kRuns>, dim3((unsigned)tiles), dim3(kThreads), 0, stream, a);
+    return launch_dependent(&adamw_kernel<kBits, kCapacity, kRuns, kSubnormal>, dim3((unsigned)tiles), dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace
@@ -404,14 +419,20 @@ extern "C" int mvue_adamw_step(const mvue_adamw_tensor* tensors, int64_t count, 
     int64_t elements = 0, first_block = 0;
     for (int64_t i = 0; i < count; ++i) elements += tensors[i].numel;
     const bool runs = elements / (4 * kTile) >= 16 * dev.sm_count;
+    // 8-bit states: a v' below 2^-126 counts in the step's divisor only where its root, 2^-63 at most, is not lost beside eps: else
+    // the root may flush it (2 x 59 M elements: 318 us with such roots, 312 us without; the codes' own root is exact either way).
+    // 32-bit states are bound by memory and always take it (439 us either way on 24 matrices of 4 M).
+    const bool subnormal = std::ldexp(1.0 / std::sqrt(1.0 - std::pow(cfg->beta2, t)), -63) > std::ldexp(cfg->eps, -26);
     while (count > 0) {
         int64_t used = 0;
         cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
         const auto go = [&](auto kernel) { return kernel(tensors, count, c, cfg->seed, &first_block, &used, st); };
         cudaError_t e;
-        if (cfg->state_bits == 32) e = go(count <= 32 ? &launch<32, 32, 1> : &launch<32, 320, 1>);
-        else if (runs) e = go(count <= 32 ? &launch<8, 32, 4> : &launch<8, 320, 4>);
-        else e = go(count <= 32 ? &launch<8, 32, 1> : &launch<8, 320, 1>);
+        if (cfg->state_bits == 32) e = go(count <= 32 ? &launch<32, 32, 1, true> : &launch<32, 320, 1, true>);
+        else if (runs && subnormal) e = go(count <= 32 ? &launch<8, 32, 4, true> : &launch<8, 320, 4, true>);
+        else if (runs) e = go(count <= 32 ? &launch<8, 32, 4, false> : &launch<8, 320, 4, false>);
+        else if (subnormal) e = go(count <= 32 ? &launch<8, 32, 1, true> : &launch<8, 320, 1, true>);
+        else e = go(count <= 32 ? &launch<8, 32, 1, false> : &launch<8, 320, 1, false>);
         if (e != cudaSuccess) { set_cuda_error(e, "mvue_adamw_step launch"); return MVUE_ERR_CUDA; }
         tensors += used;
         count -= used;

@@ -11,7 +11,7 @@
 // Measured (B200, HBM copy 6.55 TB/s).  Lookup of 16384 rows of 4096 bf16 out of 131072: 36 us against 29 us of HBM time
 // (6915 rows differ); four pieces in flight for two gave 37 us: bound by the mix of gathered reads and writes.  Gradient of
 // 32768 x 1024 bf16 into 65536 rows: 75 us against 51 us: fill 43 us (216 MB, 5 TB/s; a plain memset of as much takes 32 us;
-// bulk stores from shared memory gave the same), beside it the sort 29 us, sums 24 us (5 TB/s), joins 5 us.  8192 x 768 into
+// bulk stores from shared memory gave the same), beside it the sort 29 us, sums 24 us (5 TB/s), joins 11 us (each launch by itself).  8192 x 768 into
 // 50257 rows: 39 us against 26 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
