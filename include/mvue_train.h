@@ -62,6 +62,7 @@ typedef struct {
  * top / 448 (top the largest magnitude; the new scale is top * fl(1/448), the factor 448 * fl(1/top), a magnitude
  * is capped at 448) and rounded to a neighbouring code at random so that the code's expectation is the value: an
  * average that moves by a thousandth per step, less than a hundredth of the distance of two codes, would otherwise never move.
+ * (The magnitude in steps of its binade, of 2^-9 below 2^-6, plus the random number, in binary32, is cut to whole steps.)
  * sqrt(v') is the root rounded to the nearest binary32 number here.  A non-zero v keeps a code of at least the smallest.  Blocks whose largest |m| is below 2^-110 store zeros; a
  * non-finite value makes its block's scale NaN.
  * options: MVUE_OPT_STOCHASTIC_ROUNDING: a bf16 param without master is rounded to bf16 stochastically (as the

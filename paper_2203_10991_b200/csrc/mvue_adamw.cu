@@ -299,6 +299,7 @@ __global__ void __launch_bounds__(kThreads, 5) adamw_kernel(const __grid_constan
                 for (int i = 0; i < 8; ++i)
                     mw[i >> 2] |= (e4m3_code(fminf(fabsf(y[i]), 448.0f), r8[i] >> 8) | (y[i] < 0.0f ? 0x80u : 0u)) << (8 * (i & 3));
             }
+            // below 2^-6 without the raise, or near a carry
             if (least_z < 0.01563f || (nearest & 0xFFFFu) < 2u || nearest < 0x20000u) {
                 vw[0] = vw[1] = 0u;
 #pragma unroll

@@ -26,8 +26,8 @@ def quantise(x: torch.Tensor, random: torch.Tensor, floor_one: bool):
     factor = torch.where(large, top.reciprocal() * 448.0, 0.0)
     y = (x.view(-1, BLOCK).abs() * factor).clamp_(max=448.0).reshape(-1)
     e = (y.view(torch.int32) >> 23).clamp_(min=121)                   # of the power of two, 2^-6 at least
-    # in 64 bits nothing is rounded from here on: y has 24 bits, a step's 2^-16 parts 16 more
-    steps = torch.floor(y.double() * torch.exp2(130.0 - e.double()) + random.double() * 2.0 ** -16)
+    # the product by a power of two is exact; the sum is rounded to binary32 (below 2^-6 it may have more digits)
+    steps = torch.floor(y * ((257 - e) << 23).view(torch.float32) + random.float() * 2.0 ** -16)
     codes = ((e - 121) << 3) + steps.int()
     if floor_one:
         codes = torch.where(x > 0, codes.clamp(min=1), codes)

@@ -36,8 +36,8 @@ def test_the_two_references_agree():
 
 
 @gpu
-@pytest.mark.parametrize("zero_blocks", [False, True])
-def test_codes_and_scales_of_a_large_tensor_over_eight_steps(zero_blocks):
+@pytest.mark.parametrize("kind", ["dense", "zero blocks", "wide"])
+def test_codes_and_scales_of_a_large_tensor_over_eight_steps(kind):
     # 2^25 elements: a root that is one unit off where it should be rounded moves about ten codes a step
     n = 1 << 25
     gen = torch.Generator(device="cuda").manual_seed(7)
@@ -46,7 +46,9 @@ def test_codes_and_scales_of_a_large_tensor_over_eight_steps(zero_blocks):
     want = adamw_torch.States(n, "cuda")
     for step in range(1, 9):
         g = torch.randn(n, generator=gen, device="cuda").mul_(1e-3)
-        if zero_blocks:                                     # rows of a table that no batch has named, single zeros in the others
+        if kind == "wide":                                  # magnitudes over many binades: codes below 2^-6 are common
+            g *= torch.exp(4 * torch.randn(n, generator=gen, device="cuda"))
+        if kind == "zero blocks":                           # rows of a table that no batch has named, single zeros in the others
             g.view(-1, 2, 256)[:, 0] = 0.0
             g[300::512] = 0.0
         plan.step([g], step=step, lr=1e-3, seed=1000 + step)
