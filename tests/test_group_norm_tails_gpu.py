@@ -68,3 +68,26 @@ def test_a_neighbour_that_is_not_finite(n, s, c, groups, bad):
     dy[0, s // 2] = 1.0
     _, _, dbeta = binding.mvue_group_norm_act_backward(dy, x, mean, rstd, groups, gamma, z.cuda(), act="silu")
     assert bool(((dbeta.double().cpu() - slope).abs() <= slope_bound)[fine].all())
+
+
+@gpu
+@pytest.mark.parametrize("n,s,c,groups", ROUTES)
+def test_in_place(n, s, c, groups):
+    z = arguments(c)
+    z[3::16] = float("nan")
+    fine = torch.isfinite(z)
+    x = torch.randn(n, s, c, generator=torch.Generator().manual_seed(1)).cuda()
+    gamma = torch.zeros(c, device="cuda")
+    want, bound, _, _ = silu64(torch.where(fine, z, torch.zeros_like(z)))
+    y = x.clone()
+    _, mean, rstd = binding.mvue_group_norm_act(y, groups, gamma, z.cuda(), act="silu", out=y)
+    assert bool(((y.double().cpu() - want).abs() <= bound)[..., fine].all()) and bool(torch.isnan(y[..., ~fine.cuda()]).all())
+    # gamma of ordinary size and the far arguments in beta: dx in the place of dy as well as beside it
+    gamma = torch.ones(c, device="cuda")
+    z = arguments(c).cuda()
+    dy = torch.randn(n, s, c, generator=torch.Generator().manual_seed(2)).cuda()
+    apart = binding.mvue_group_norm_act_backward(dy, x, mean, rstd, groups, gamma, z, act="silu")
+    inside = binding.mvue_group_norm_act_backward(dy, x, mean, rstd, groups, gamma, z, act="silu", out=dy)
+    # the two ways differ by the sigmoids' last places, 8 units of the largest term at most
+    assert float((apart[0] - inside[0]).abs().max()) <= 8 * 2.0 ** -23 * float(apart[0].abs().max())
+    assert all(torch.equal(p, q) for p, q in zip(apart[1:], inside[1:]))
