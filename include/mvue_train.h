@@ -54,8 +54,8 @@ typedef struct {
  *   m' = beta1 m + (1 - beta1) g'
  *   v' = beta2 v + ((1 - beta2) g') g'
  *   param' = param (1 - lr weight_decay) - (lr / (1 - beta1^t)) * (m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
- * m' and v' with each operation rounded on its own; the root and the quotient within 2 units in the last place, the product
- * by the decay fused with the sum.  (|g'| above 2^63 overflows v'.)
+ * m' and v' with each operation rounded on its own; the root and the quotient within 2 units in the last place (with 8-bit states
+ * a root below 2^-63 may count as 0 where it is lost beside eps), the product by the decay fused with the sum.  (|g'| above 2^63 overflows v'.)
  * grad_scale: HOST value, 1 for none; dev_grad_scale: optional DEVICE float (a clipping factor or a loss scale's
  * inverse that the host does not know), read when the step runs.
  * state_bits: 32 or 8.  With 8 bits the new m and sqrt(v) of a block are divided by the block's new scale
@@ -63,8 +63,8 @@ typedef struct {
  * is capped at 448) and rounded to a neighbouring code at random so that the code's expectation is the value: an
  * average that moves by a thousandth per step, less than a hundredth of the distance of two codes, would otherwise never move.
  * (The magnitude in steps of its binade, of 2^-9 below 2^-6, plus the random number, in binary32, is cut to whole steps.)
- * sqrt(v') is the root rounded to the nearest binary32 number here.  A non-zero v keeps a code of at least the smallest.  Blocks whose largest |m| is below 2^-110 store zeros; a
- * non-finite value makes its block's scale NaN.
+ * sqrt(v') is the root rounded to the nearest binary32 number here.  A non-zero v keeps a code of at least the smallest.
+ * Blocks whose largest |m| is below 2^-110 store zeros; a non-finite value makes its block's scale NaN.
  * options: MVUE_OPT_STOCHASTIC_ROUNDING: a bf16 param without master is rounded to bf16 stochastically (as the
  * survivors of mvue_prune_opts) instead of to the nearest -- updates below half a unit in the last place then count in
  * the mean.  Other bits: MVUE_ERR_OPTION.

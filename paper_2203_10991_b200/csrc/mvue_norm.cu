@@ -69,7 +69,7 @@ struct Each {
     }
 };
 // Both with one reciprocal, that of the product of the two denominators: the special-function unit takes 16 values a cycle, and
-// two each hold up the folded kernels (64 x 3136 x 256 bf16: 53 us against 52 us forward, 107 us against 100 us backward).
+// two each hold up the folded kernels (64 x 3136 x 256 bf16: 53 us against 52 us forward, 107 us against 102 us backward).
 // The product is finite while both exponentials are at most 2^60 (z above -41.6); where `held` says that they were not, or
 // that there was a NaN, the caller goes over its rows again with Each.  A test of every pair on the way costs 119 us, one of every
 // four pairs 108 us.  (3 x 11811 x 320 fp32 through memory: forward 30.6 us against 31.8 us with Each throughout.)
@@ -542,9 +542,9 @@ __global__ void __launch_bounds__(kThreads) norm_grad_apply_kernel(const __grid_
 // to eight blocks takes one slab of whole groups of one sample, every block a run of its rows: the rows are copied to shared
 // memory once,a thread reads back only what it copied itself (no barrier between the copy and its use), the blocks
 // exchange their groups' sums through distributed shared memory, and the output is formed from the same copy.  One read
-// and one write of HBM.  64 x 3136 x 256 bf16 in 32 groups: forward 46 us (ReLU) and 51 us (SiLU) against 31 us of HBM time and
-// 101 us through memory, backward 74 us and 99 us against 47 us and 269 us.  Bound by instructions and their latency: 26 and 50
-// million warp instructions, 60 % and 50 % of the issue slots with four and two blocks on an SM (registers).  Measured and not
+// and one write of HBM.  64 x 3136 x 256 bf16 in 32 groups: forward 46 us (ReLU) and 52 us (SiLU) against 31 us of HBM time and
+// 101 us through memory, backward 75 us and 102 us against 47 us and 269 us.  Bound by instructions and their latency: 26 and 47
+// million warp instructions, 59 % and 45 % of the issue slots with four and two blocks on an SM (registers).  Measured and not
 // kept: a second buffer for the next sample (49 us forward, 102 us backward with half the blocks), copies of the next sample
 // rolling in behind the last pass (49 us, 110 us: the loops no longer unroll), four channels a thread with four blocks on an SM
 // (128 us backward), three blocks at 80 registers (111 us).
@@ -1014,7 +1014,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_resident_grad_kernel(const _
 // The common case: a warp holds whole rows of the slab and every group is whole pieces of eight channels.  Then a thread's
 // eight channels are of one group, a sum over a group is a handful of shuffles and eight values in shared memory, and
 // every thread works the group's statistics out for itself: two barriers of the block a unit (one backward), no values per
-// channel in shared memory (64 x 3136 x 256 bf16: 57 -> 46 us forward, 129 -> 99 us backward with SiLU).
+// channel in shared memory (64 x 3136 x 256 bf16: 57 -> 46 us forward, 129 -> 102 us backward with SiLU).
 template <typename T, int kTensors>
 struct Folded : Resident<T, kTensors> {
     using Base = Resident<T, kTensors>;
