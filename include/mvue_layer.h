@@ -1,0 +1,85 @@
+/*
+ * mvue_layer.h -- the rest of a layer's own arithmetic beside the pruned products of mvue.h: layer normalisation and its
+ * backward pass, the dense products (the forward product, and the backward product where the gradient is not pruned) in
+ * 8-bit floating point with block scales, and the quantiser that feeds them.
+ *
+ * The rules of mvue_train.h hold: device pointers, caller-owned buffers, work enqueued on `stream`, argument errors found on
+ * the host before anything is launched, tensors aligned to their element type unless a call says more.
+ */
+#ifndef MVUE_LAYER_H_
+#define MVUE_LAYER_H_
+
+#include "mvue_train.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Layer normalisation
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* For each row of x [rows, cols]:
+ *   mean = sum x / cols;  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps);  y_c = (x_c - mean) rstd gamma_c + beta_c
+ *  x, y       MVUE_F32 or MVUE_BF16 (the same); ldx, ldy >= cols.  y may be x.
+ *  gamma, beta   [cols], MVUE_F32 or MVUE_BF16 (affine_dtype), either may be NULL (ones, zeros).
+ *  mean, rstd [rows] float outputs for the backward pass, either may be NULL.
+ * Arithmetic in binary32; the output is rounded once.  rows = 0: nothing.  cols >= 1. */
+MVUE_API int mvue_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* gamma, const void* beta,
+                             int affine_dtype, float eps, void* y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Its backward pass, from x and the forward pass's mean and rstd; xh = (x - mean) rstd, sums over a row's columns:
+ *   dx_c = rstd (gamma_c dy_c - sum(gamma dy) / cols - xh_c sum(gamma dy xh) / cols)
+ *   dgamma_c = sum over rows of dy_c xh_c;  dbeta_c = sum over rows of dy_c
+ *  dgamma, dbeta   [cols] float, either may be NULL; rows = 0 sets them to zero.
+ *  workspace  mvue_layer_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned; contents scratch.  None is needed without
+ *             dgamma and dbeta.
+ * dx may be dy or x (and is what mvue_prune takes as the neural gradient of the layer below).  Equal inputs give equal bits. */
+MVUE_API int mvue_layer_norm_backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, int dtype, int64_t rows, int64_t cols,
+                                      const float* mean, const float* rstd, const void* gamma, int affine_dtype, void* dx, int64_t lddx,
+                                      float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+MVUE_API int mvue_layer_norm_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);   /* bytes: HOST */
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * 8-bit floating point with block scales
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* Elements along the reduction axis of a product that share a scale (and, in a weight, along the other axis too). */
+#define MVUE_SCALE_BLOCK 128
+
+/* Codes of x [rows, cols] (MVUE_F32 or MVUE_BF16, ldx >= cols) as 8-bit floats of four exponent and three mantissa bits (e4m3:
+ * largest 448, no infinities, 0x7F and 0xFF are NaN), one scale for each block of block_rows x 128 elements (block_rows 1 or 128;
+ * blocks at the right and lower edges may be short):
+ *   scale = 2^(e - 127), e the least byte >= 1 for which the block's largest finite magnitude is at most 448 scale
+ *   code = e4m3(x / scale), to the nearest, ties to even
+ * Elements that are infinite or NaN get a NaN code and do not count for the scale.
+ *  codes      [rows, cols] bytes, ldq >= cols (the products want codes 16-byte aligned and ldq a multiple of 16).
+ *  scales     exponent bytes e: [ceil(cols / 128), rows] for block_rows = 1 (a block's rows are neighbours),
+ *             [ceil(rows / 128), ceil(cols / 128)] for block_rows = 128.
+ * options: MVUE_OPT_STOCHASTIC_ROUNDING rounds without bias: with z = |x| / scale cut (to the nearest) to a multiple of 2^-20 of the
+ * distance of the two codes around it, the larger code is taken where the fraction of that distance plus r 2^-16 reaches one, and the
+ * expectation is z.  r: elements 8j .. 8j + 7 of row i take the eight halves (low first) of the words of Philox4x32-10 with counter
+ * (lo32(u), hi32(u), 3, 0), u = i ceil(cols / 8) + j, under the key `seed` (pass another one each step).  Other bits: MVUE_ERR_OPTION.
+ * rows = 0 or cols = 0: nothing. */
+MVUE_API int mvue_quantize_e4m3(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int block_rows, unsigned options,
+                                uint64_t seed, void* codes, int64_t ldq, void* scales, void* stream);
+
+/* Products of such codes, each multiplied by its scale, summed in binary32 on the tensor cores and rounded once to the output type:
+ *   forward    C[tokens x out] = x W^T     x [tokens, in] with one scale per 1 x 128, W [out, in] with one per 128 x 128
+ *   backward   C[tokens x in]  = g W       g [tokens, out] with one scale per 1 x 128, the same W and scales
+ *  x, g, W    e4m3 codes, 16-byte aligned, leading dimensions multiples of 16 bytes (MVUE_ERR_ALIGN); any extents.
+ *  scales     as mvue_quantize_e4m3 leaves them; the byte 255 stands for NaN.
+ *  C          MVUE_F32 or MVUE_BF16, ldc >= its columns; 32-byte aligned rows take the wide stores.
+ *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires; otherwise left untouched.
+ * tokens = 0: nothing.  Equal inputs give equal bits. */
+MVUE_API int mvue_scaled_forward_gemm(const void* x, const void* x_scales, int64_t tokens, int64_t in, int64_t ldx, const void* W,
+                                      const void* W_scales, int64_t out, int64_t ldW, void* C, int c_dtype, int64_t ldc, int* dev_status,
+                                      void* stream);
+MVUE_API int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int64_t tokens, int64_t out, int64_t ldg, const void* W,
+                                       const void* W_scales, int64_t in, int64_t ldW, void* C, int c_dtype, int64_t ldc, int* dev_status,
+                                       void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MVUE_LAYER_H_ */

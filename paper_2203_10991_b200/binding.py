@@ -29,7 +29,9 @@ EXPORTS = ("mvue_version", "mvue_status_string", "mvue_last_cuda_error", "mvue_p
            "mvue_probe_sparse_mma", "mvue_selftest_wait_timeout",
            "mvue_adamw_step", "mvue_embedding", "mvue_embedding_grad", "mvue_embedding_grad_workspace_bytes",
            "mvue_group_norm_act", "mvue_group_norm_act_backward", "mvue_group_norm_workspace_bytes",
-           "mvue_selftest_group_norm_timeout")
+           "mvue_selftest_group_norm_timeout",
+           "mvue_layer_norm", "mvue_layer_norm_backward", "mvue_layer_norm_workspace_bytes",
+           "mvue_quantize_e4m3", "mvue_scaled_forward_gemm", "mvue_scaled_backward_gemm")
 
 
 class AdamWTensor(ctypes.Structure):
@@ -98,6 +100,12 @@ def lib() -> ctypes.CDLL:
                                                    vp, csz, vp, vp]
         L.mvue_group_norm_workspace_bytes.argtypes = [i64, i64, i64, ci, szp]
         L.mvue_selftest_group_norm_timeout.argtypes = [ci, vp, vp, ci, i64, i64, i64, ci, vp, vp, vp, vp, csz, vp, vp]
+        L.mvue_layer_norm.argtypes = [vp, ci, i64, i64, i64, vp, vp, ci, cf, vp, i64, vp, vp, vp]
+        L.mvue_layer_norm_backward.argtypes = [vp, i64, vp, i64, ci, i64, i64, vp, vp, vp, ci, vp, i64, vp, vp, vp, csz, vp]
+        L.mvue_layer_norm_workspace_bytes.argtypes = [i64, i64, szp]
+        L.mvue_quantize_e4m3.argtypes = [vp, ci, i64, i64, i64, ci, ctypes.c_uint, u64, vp, i64, vp, vp]
+        for product in (L.mvue_scaled_forward_gemm, L.mvue_scaled_backward_gemm):
+            product.argtypes = [vp, vp, i64, i64, i64, vp, vp, i64, i64, vp, ci, i64, vp, vp]
         L.mvue_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, ctypes.POINTER(AdamWConfig), vp]
         _lib = L
     return _lib
@@ -520,3 +528,141 @@ def mvue_selftest_group_norm_timeout(polls: int, x: torch.Tensor, groups: int, m
     _check(lib().mvue_selftest_group_norm_timeout(polls, x.data_ptr(), _ptr(dy), _dtype_code(x), n, s, c, groups, mean.data_ptr(),
                                                   rstd.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                                   dev_status.data_ptr(), _stream_ptr()), "mvue_selftest_group_norm_timeout")
+
+
+def _rows(t: torch.Tensor):
+    """(rows, cols, ld) of a tensor [..., cols] whose rows lie one stride apart."""
+    if t.dim() == 0:
+        raise ValueError("wants [..., columns]")
+    cols = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // cols if cols else 0), cols, cols
+    if t.dim() == 1:
+        t = t[None]
+    n, s, cols, ld = _positions(t)
+    return n * s, cols, ld
+
+
+def mvue_layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, *, eps: float = 1e-5,
+                    out: torch.Tensor | None = None):
+    """layer_norm(x) * weight + bias over the last dimension of a CUDA tensor x [..., cols], fp32 or bf16, whose rows lie one stride
+    apart.  Returns (y, mean, rstd); mean and rstd [...] fp32 are what the backward pass takes.  out may be x."""
+    _operands(x, weight, bias, out)
+    rows, cols, ldx = _rows(x)
+    code = _affine(weight, bias, cols)
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        ldy = cols
+    else:
+        assert out.shape == x.shape and out.dtype == x.dtype
+        ldy = _rows(out)[2]
+    mean, rstd = x.new_empty(x.shape[:-1], dtype=torch.float32), x.new_empty(x.shape[:-1], dtype=torch.float32)
+    _check(lib().mvue_layer_norm(x.data_ptr(), _dtype_code(x), rows, cols, ldx, _ptr(weight), _ptr(bias), code, eps, out.data_ptr(), ldy,
+                                 mean.data_ptr(), rstd.data_ptr(), _stream_ptr()), "mvue_layer_norm")
+    return out, mean, rstd
+
+
+def mvue_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().mvue_layer_norm_workspace_bytes(rows, cols, ctypes.byref(b)), "mvue_layer_norm_workspace_bytes")
+    return b.value
+
+
+def mvue_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor | None = None, *,
+                             out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Backward pass of mvue_layer_norm.  Returns (dx, dweight, dbias); the last two [cols] fp32.  out may be dy or x."""
+    _operands(x, dy, mean, rstd, weight, out, workspace=workspace)
+    rows, cols, ldx = _rows(x)
+    assert dy.shape == x.shape and dy.dtype is x.dtype
+    for t in (mean, rstd):
+        assert t.numel() == rows and t.dtype is torch.float32 and t.is_contiguous()
+    code = _affine(weight, None, cols)
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        lddx = cols
+    else:
+        assert out.shape == x.shape and out.dtype == x.dtype
+        lddx = _rows(out)[2]
+    dweight, dbias = x.new_empty(cols, dtype=torch.float32), x.new_empty(cols, dtype=torch.float32)
+    need = mvue_layer_norm_workspace_bytes(rows, cols)
+    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+        workspace = x.new_empty(need, dtype=torch.uint8)
+    _check(lib().mvue_layer_norm_backward(dy.data_ptr(), _rows(dy)[2], x.data_ptr(), ldx, _dtype_code(x), rows, cols, mean.data_ptr(),
+                                          rstd.data_ptr(), _ptr(weight), code, out.data_ptr(), lddx, dweight.data_ptr(), dbias.data_ptr(),
+                                          _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                          _stream_ptr()), "mvue_layer_norm_backward")
+    return out, dweight, dbias
+
+
+SCALE_BLOCK = 128                 # elements along the reduction axis that share a scale (MVUE_SCALE_BLOCK)
+
+
+def mvue_quantize_e4m3(x: torch.Tensor, block_rows: int = 1, *, seed: int | None = None, codes: torch.Tensor | None = None,
+                       scales: torch.Tensor | None = None):
+    """e4m3 codes of a matrix x [rows, cols] (fp32 or bf16, unit column stride) with one power-of-two scale for each block of
+    block_rows x 128 elements (block_rows: 1 for activations and gradients, 128 for weights).  seed: None rounds to the nearest code, ties
+    to even; a number rounds at random without bias, keyed by it (another one each step).
+    Returns (codes float8_e4m3fn [rows, cols], its rows 16-byte aligned; scales uint8: the exponent byte e of a scale 2^(e - 127),
+    [ceil(cols / 128), rows] for block_rows = 1, [ceil(rows / 128), ceil(cols / 128)] for 128)."""
+    _operands(x, codes, scales)
+    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] != 1):
+        raise ValueError("wants a matrix with unit column stride")
+    rows, cols = x.shape
+    blocks = -(-cols // SCALE_BLOCK)
+    shape = (blocks, rows) if block_rows == 1 else (-(-rows // SCALE_BLOCK), blocks)
+    if codes is None:
+        codes = x.new_empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn)[:, :cols]
+    elif codes.shape != x.shape:
+        raise ValueError("codes have the shape of x")
+    if scales is None:
+        scales = x.new_empty(shape, dtype=torch.uint8)
+    else:
+        _scale_bytes(scales, shape)
+    _check(lib().mvue_quantize_e4m3(x.data_ptr(), _dtype_code(x), rows, cols, x.stride(0) if rows > 1 else cols, block_rows,
+                                    MVUE_OPT_NONE if seed is None else MVUE_OPT_STOCHASTIC_ROUNDING, (seed or 0) & (2**64 - 1),
+                                    codes.data_ptr(), _code_pitch(codes), scales.data_ptr(), _stream_ptr()), "mvue_quantize_e4m3")
+    return codes, scales
+
+
+def _code_pitch(codes: torch.Tensor) -> int:
+    """Bytes from row to row of a matrix of e4m3 codes."""
+    if codes.dim() != 2 or codes.dtype not in (torch.float8_e4m3fn, torch.uint8) or (codes.stride(1) != 1 and codes.shape[1] != 1):
+        raise ValueError("codes are a float8_e4m3fn matrix with unit column stride")
+    return codes.stride(0) if codes.shape[0] > 1 else -(-codes.shape[1] // 16) * 16
+
+
+def _scale_bytes(scales: torch.Tensor, shape: tuple[int, int]) -> None:
+    if scales.dtype is not torch.uint8 or tuple(scales.shape) != shape or not scales.is_contiguous():
+        raise ValueError(f"wants contiguous uint8 scales {list(shape)}")
+
+
+def _scaled_gemm(name, a, a_scales, W, W_scales, n, k, w_k, out, out_dtype, dev_status):
+    _operands(a, a_scales, W, W_scales, out, dev_status=dev_status)
+    lda, ldw = _code_pitch(a), _code_pitch(W)
+    if k != w_k:
+        raise ValueError("the operands differ along the reduction axis")
+    rows = a.shape[0]
+    _scale_bytes(a_scales, (-(-k // SCALE_BLOCK), rows))
+    _scale_bytes(W_scales, tuple(-(-d // SCALE_BLOCK) for d in W.shape))
+    if out is None:
+        out = a.new_empty((rows, n), dtype=out_dtype)
+        ldc = n
+    else:
+        assert out.shape == (rows, n) and (out.stride(1) == 1 or n == 1)
+        ldc = out.stride(0) if rows > 1 else n
+    _check(getattr(lib(), name)(a.data_ptr(), a_scales.data_ptr(), rows, k, lda, W.data_ptr(), W_scales.data_ptr(), n, ldw, out.data_ptr(),
+                                _dtype_code(out), ldc, _ptr(dev_status), _stream_ptr()), name)
+    return out
+
+
+def mvue_scaled_forward_gemm(x: torch.Tensor, x_scales: torch.Tensor, W: torch.Tensor, W_scales: torch.Tensor, *,
+                             out: torch.Tensor | None = None, out_dtype=torch.bfloat16, dev_status: torch.Tensor | None = None) -> torch.Tensor:
+    """x . W^T from e4m3 codes: x [tokens, in] with scales [ceil(in / 128), tokens], W [out, in] with scales
+    [ceil(out / 128), ceil(in / 128)] (what mvue_quantize_e4m3 returns for block_rows = 1 and 128).  bf16 or fp32 out."""
+    return _scaled_gemm("mvue_scaled_forward_gemm", x, x_scales, W, W_scales, W.shape[0], x.shape[-1], W.shape[-1], out, out_dtype, dev_status)
+
+
+def mvue_scaled_backward_gemm(g: torch.Tensor, g_scales: torch.Tensor, W: torch.Tensor, W_scales: torch.Tensor, *,
+                              out: torch.Tensor | None = None, out_dtype=torch.bfloat16, dev_status: torch.Tensor | None = None) -> torch.Tensor:
+    """g . W from e4m3 codes: g [tokens, out] with scales [ceil(out / 128), tokens]; W and its scales as in the forward product."""
+    return _scaled_gemm("mvue_scaled_backward_gemm", g, g_scales, W, W_scales, W.shape[-1], g.shape[-1], W.shape[0], out, out_dtype, dev_status)

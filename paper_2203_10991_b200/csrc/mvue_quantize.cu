@@ -1,0 +1,256 @@
+// e4m3 codes with a power-of-two scale for each block of 1 x 128 or 128 x 128 elements: what the products of mvue_scaled.cu take.
+//
+// Bytes: one pass, the input read once and one byte per element written; a block's elements wait in registers for its largest
+// magnitude.  Sixteen lanes of eight neighbours each hold 128 columns.  The scale is a power of two, so dividing by it is
+// exact and both roundings act on the element itself.
+// Rounding at random: the element over its scale, times 2^-120, has its binary32 subnormals where e4m3 has its own, so the
+// code is the upper bits of the bit pattern for subnormal, normal and zero alike; adding a random number to the 16 bits below
+// them carries into them as often as the element is nearer to its upper neighbour.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "../../include/mvue_layer.h"
+#include "mvue_device.cuh"
+#include "mvue_internal.h"
+#include "mvue_train.cuh"
+
+namespace mvue {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRowsPerWarp = 4;                       // 1 x 128: rows of a warp, two blocks each
+constexpr uint32_t kInf = 0x7F800000u;
+
+struct Params {
+    const void* x;
+    int64_t rows, cols, ldx;
+    uint8_t* codes;
+    int64_t ldq;
+    uint8_t* scales;
+    int64_t scale_pitch;       // 1 x 128: bytes from one block of columns to the next (rows); 128 x 128: from one block of rows
+    int64_t units;             // ceil(cols / 8): generator calls of a row
+    bool wide_x, wide_q;       // eight elements, eight codes in one access
+    int64_t tiles_x;
+    RoundKeys keys;
+};
+
+// Eight elements of a lane as they were read.
+template <typename T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool wide, int count) {
+        if (wide && count == 8) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = (2 * i < count ? (uint32_t)q[2 * i] : 0u) | (2 * i + 1 < count ? (uint32_t)q[2 * i + 1] << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ float at(int i) const { return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
+    // bit pattern of the largest magnitude (as binary32); an infinity or a NaN is above all others
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t m = w[0] & 0x7FFF7FFFu;
+#pragma unroll
+        for (int i = 1; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+        return max(m << 16, m & 0xFFFF0000u);
+    }
+};
+template <> struct Eight<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const float* p, bool wide, int count) {
+        if (wide && count == 8) {
+            ld256(p, w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = i < count ? __float_as_uint(p[i]) : 0u;
+        }
+    }
+    __device__ __forceinline__ float at(int i) const { return __uint_as_float(w[i]); }
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t m = 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+        return m;
+    }
+};
+
+// the largest finite magnitude: where top() met something else
+template <typename T> __device__ __noinline__ uint32_t finite_top(const Eight<T>& x) {
+    uint32_t m = 0u;
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __float_as_uint(x.at(i)) & 0x7FFFFFFFu;
+        if (b < kInf) m = max(m, b);
+    }
+    return m;
+}
+
+// Exponent byte of the least power of two, 2^-126 or above, that brings the magnitude with these bits to 448 = 1.75 2^8 or less.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+    return (uint32_t)max((int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0), 1);
+}
+
+template <typename T, bool kRandom>
+__device__ __forceinline__ uint2 encode(const Eight<T>& x, uint32_t byte, bool finite, uint4 random) {
+    const f2 factor = pair(__uint_as_float((254u - byte) << 23));          // 2^(127 - byte)
+    uint32_t out[2];
+    if constexpr (kRandom) {
+        const uint32_t rw[4] = {random.x, random.y, random.z, random.w};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t t[4], s[4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float lo, hi;
+                unpair(mul2(mul2(pair(x.at(4 * h + 2 * j), x.at(4 * h + 2 * j + 1)), factor), pair(7.52316384526264005e-37f)), lo, hi);   // 2^-120
+                s[2 * j] = __float_as_uint(lo);
+                s[2 * j + 1] = __float_as_uint(hi);
+                // the code fills the highest byte of the bits four places up, the sign falls out; the random number is below it
+                t[2 * j] = s[2 * j] * 16u + __byte_perm(rw[2 * h + j], 0u, 0x4104);
+                t[2 * j + 1] = s[2 * j + 1] * 16u + __byte_perm(rw[2 * h + j], 0u, 0x4324);
+            }
+            const uint32_t signs = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410) & 0x80808080u;
+            out[h] = __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410) | signs;
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t half[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float lo, hi;
+                unpair(mul2(pair(x.at(4 * h + 2 * j), x.at(4 * h + 2 * j + 1)), factor), lo, hi);
+                asm("{\n\t.reg .b16 c;\n\tcvt.rn.satfinite.e4m3x2.f32 c, %1, %2;\n\tcvt.u32.u16 %0, c;\n\t}" : "=r"(half[j]) : "f"(hi), "f"(lo));
+            }
+            out[h] = __byte_perm(half[0], half[1], 0x5410);
+        }
+    }
+    if (!finite) {                                                            // NaN for what has no code
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((__float_as_uint(x.at(i)) & 0x7FFFFFFFu) >= kInf) out[i >> 2] |= 0x7Fu << (8 * (i & 3));
+    }
+    return make_uint2(out[0], out[1]);
+}
+
+__device__ __forceinline__ void store_codes(uint8_t* to, bool wide, int count, uint2 v) {
+    if (wide && count == 8) {
+        *reinterpret_cast<uint2*>(to) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) to[i] = (uint8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
+    }
+}
+
+// 1 x 128: a warp takes two blocks (256 columns) of kRowsPerWarp rows, a thread block 32 rows.
+template <typename T, bool kRandom>
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const __grid_constant__ Params p) {
+    grid_dependency_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t tile_y = blockIdx.x / p.tiles_x, tile_x = blockIdx.x - tile_y * p.tiles_x;
+    const int64_t row0 = (tile_y * (kThreads / 32) + (threadIdx.x >> 5)) * kRowsPerWarp, col = tile_x * 256 + lane * 8;
+    const int count = (int)min((int64_t)8, max((int64_t)0, p.cols - col));
+    Eight<T> x[kRowsPerWarp];
+#pragma unroll
+    for (int r = 0; r < kRowsPerWarp; ++r)
+        x[r].load(static_cast<const T*>(p.x) + (row0 + r) * p.ldx + col, p.wide_x, row0 + r < p.rows ? count : 0);
+#pragma unroll
+    for (int r = 0; r < kRowsPerWarp; ++r) {
+        const int64_t row = row0 + r;
+        if (row >= p.rows) return;                                            // a whole warp
+        uint32_t top = x[r].top();
+        const bool finite = top < kInf;
+        if (!finite) top = finite_top(x[r]);
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        const uint32_t byte = scale_byte(top);
+        uint4 random = make_uint4(0u, 0u, 0u, 0u);
+        if (kRandom) random = philox4x32_10((uint64_t)(row * p.units + (col >> 3)), p.keys, 3u);
+        const uint2 v = encode<T, kRandom>(x[r], byte, finite, random);
+        store_codes(p.codes + row * p.ldq + col, p.wide_q, count, v);
+        if ((lane & 15) == 0 && count > 0) p.scales[(col >> 7) * p.scale_pitch + row] = (uint8_t)byte;
+    }
+}
+
+// 128 x 128: a thread block takes one, a thread eight rows of eight columns.
+template <typename T, bool kRandom>
+__global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(const __grid_constant__ Params p) {
+    grid_dependency_wait();
+    __shared__ uint32_t tops[kThreads / 32];
+    const int64_t tile_y = blockIdx.x / p.tiles_x, tile_x = blockIdx.x - tile_y * p.tiles_x;
+    const int64_t row0 = tile_y * 128 + (threadIdx.x >> 4), col = tile_x * 128 + (threadIdx.x & 15) * 8;
+    const int count = (int)min((int64_t)8, max((int64_t)0, p.cols - col));
+    Eight<T> x[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        x[r].load(static_cast<const T*>(p.x) + (row0 + 16 * r) * p.ldx + col, p.wide_x, row0 + 16 * r < p.rows ? count : 0);
+    uint32_t top = 0u;
+    bool finite = true;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        uint32_t t = x[r].top();
+        if (t >= kInf) {
+            finite = false;
+            t = finite_top(x[r]);
+        }
+        top = max(top, t);
+    }
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kThreads / 32; ++i) top = max(top, tops[i]);
+    const uint32_t byte = scale_byte(top);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const int64_t row = row0 + 16 * r;
+        if (row >= p.rows) break;
+        uint4 random = make_uint4(0u, 0u, 0u, 0u);
+        if (kRandom) random = philox4x32_10((uint64_t)(row * p.units + (col >> 3)), p.keys, 3u);
+        store_codes(p.codes + row * p.ldq + col, p.wide_q, count, encode<T, kRandom>(x[r], byte, finite, random));
+    }
+    if (threadIdx.x == 0) p.scales[tile_y * p.scale_pitch + tile_x] = (uint8_t)byte;
+}
+
+}  // namespace
+}  // namespace mvue
+
+using namespace mvue;
+
+extern "C" int mvue_quantize_e4m3(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int block_rows, unsigned options,
+                                  uint64_t seed, void* codes, int64_t ldq, void* scales, void* stream) {
+    if (dtype != MVUE_F32 && dtype != MVUE_BF16) return MVUE_ERR_DTYPE;
+    if (options & ~(unsigned)MVUE_OPT_STOCHASTIC_ROUNDING) return MVUE_ERR_OPTION;
+    if ((block_rows != 1 && block_rows != MVUE_SCALE_BLOCK) || rows < 0 || cols < 0 || ldx < cols || ldq < cols) return MVUE_ERR_SHAPE;
+    if (rows == 0 || cols == 0) return MVUE_OK;
+    if (!x || !codes || !scales) return MVUE_ERR_NULL;
+    if (off(x, size_of(dtype))) return MVUE_ERR_ALIGN;
+    const bool random = (options & MVUE_OPT_STOCHASTIC_ROUNDING) != 0;
+    Params p;
+    p.x = x; p.rows = rows; p.cols = cols; p.ldx = ldx;
+    p.codes = static_cast<uint8_t*>(codes); p.ldq = ldq;
+    p.scales = static_cast<uint8_t*>(scales);
+    p.units = (cols + 7) / 8;
+    p.wide_x = !off(x, 8 * size_of(dtype)) && (ldx % 8 == 0 || rows == 1);
+    p.wide_q = !off(codes, 8) && (ldq % 8 == 0 || rows == 1);
+    p.keys = make_round_keys(seed);
+    const int width = block_rows == 1 ? 256 : 128, height = block_rows == 1 ? kThreads / 32 * kRowsPerWarp : 128;
+    p.tiles_x = (cols + width - 1) / width;
+    p.scale_pitch = block_rows == 1 ? rows : p.tiles_x;
+    const int64_t tiles_y = (rows + height - 1) / height;
+    if (tiles_y > 0x7FFFFFFF / p.tiles_x) return MVUE_ERR_SHAPE;
+    DeviceInfo dev;
+    if (int s = current_device_info(&dev)) return s;
+    using Kernel = void (*)(Params);
+    const Kernel kernels[2][2][2] = {{{quantize_rows_kernel<float, false>, quantize_rows_kernel<float, true>},
+                                      {quantize_rows_kernel<__nv_bfloat16, false>, quantize_rows_kernel<__nv_bfloat16, true>}},
+                                     {{quantize_tiles_kernel<float, false>, quantize_tiles_kernel<float, true>},
+                                      {quantize_tiles_kernel<__nv_bfloat16, false>, quantize_tiles_kernel<__nv_bfloat16, true>}}};
+    const cudaError_t e = launch_dependent(kernels[block_rows != 1][dtype == MVUE_BF16][random], dim3((unsigned)(tiles_y * p.tiles_x)), dim3(kThreads),
+                                           0, reinterpret_cast<cudaStream_t>(stream), p);
+    if (e != cudaSuccess) { set_cuda_error(e, "mvue_quantize_e4m3 launch"); return MVUE_ERR_CUDA; }
+    return MVUE_OK;
+}

@@ -1,0 +1,104 @@
+// Dense products in 8-bit floating point with block scales: the forward product of a layer, C = x W^T, and its backward
+// product, C = g W.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "../../include/mvue_layer.h"
+#include "mvue_dense.cuh"
+#include "mvue_train.cuh"
+
+namespace mvue {
+namespace {
+
+// 32 consecutive results of a row.
+template <bool kBf16>
+struct Store {
+    void* C;
+    int64_t ldc;
+    int vec;                                 // bytes that one access may take: 32, 16, or an element
+    __device__ __forceinline__ void store(const dense::Params& p, int, int row, int, int, int col, const uint32_t (&v)[32]) const {
+        if (row >= p.M || col >= p.N) return;
+        const int left = p.N - col;
+        if constexpr (kBf16) {
+            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(C) + (int64_t)row * ldc + col;
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack_bf16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+            if (left >= 32 && vec >= 16) {
+                if (vec == 32) {
+                    store8_b32(to, w);
+                    store8_b32(to + 16, w + 8);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(to)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                }
+            } else {
+                unsigned short* q = reinterpret_cast<unsigned short*>(to);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i < left) q[i] = (unsigned short)(w[i >> 1] >> (16 * (i & 1)));
+            }
+        } else {
+            float* to = static_cast<float*>(C) + (int64_t)row * ldc + col;
+            if (left >= 32 && vec >= 16) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) store8_b32(to + i, v + i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i < left) to[i] = __uint_as_float(v[i]);
+            }
+        }
+    }
+};
+
+template <bool kBf16>
+cudaError_t launch(const dense::Params& p, const dense::Operand& a, const dense::Operand& b, bool n_major, const Store<kBf16>& out, cudaStream_t stream) {
+    if (n_major) return dense::launch_pair<dense::Shape<true, true, 256>>(p, a, b, out, stream);
+    return dense::launch_pair<dense::Shape<true, false, 256>>(p, a, b, out, stream);
+}
+
+int scaled_gemm(const void* a, int64_t M, int64_t K, int64_t lda, const void* a_scales, const void* w, int64_t N, int64_t ldw,
+                const void* w_scales, bool n_major, void* C, int c_dtype, int64_t ldc, int* dev_status, void* stream) {
+    if (c_dtype != MVUE_F32 && c_dtype != MVUE_BF16) return MVUE_ERR_DTYPE;
+    if (M < 0 || N <= 0 || K <= 0 || M > 0x7FFFFF00 || N > 0x7FFFFF00 || K > 0x7FFFFF00) return MVUE_ERR_SHAPE;
+    if (lda < K || ldw < (n_major ? N : K) || ldc < N) return MVUE_ERR_SHAPE;
+    if (!w || !w_scales || (M > 0 && (!a || !a_scales || !C))) return MVUE_ERR_NULL;
+    if (off(a, 16) || off(w, 16) || lda % 16 != 0 || ldw % 16 != 0 || off(C, size_of(c_dtype))) return MVUE_ERR_ALIGN;
+    if (M == 0) return MVUE_OK;
+    DeviceInfo dev;
+    if (int s = current_device_info(&dev)) return s;
+    dense::Params p = {};
+    p.M = (int)M; p.N = (int)N; p.K = (int)K; p.batch = 1;
+    p.a_scales = static_cast<const uint8_t*>(a_scales);
+    p.b_scales = static_cast<const uint8_t*>(w_scales);
+    const int64_t blocks_n = (N + 127) / 128, blocks_k = (K + 127) / 128;
+    p.b_scales_n = n_major ? 1 : blocks_k;
+    p.b_scales_k = n_major ? blocks_n : 1;
+    p.dev_status = dev_status;
+    const dense::Operand oa = {a, lda, lda * M}, ob = {w, ldw, ldw * (n_major ? K : N)};
+    const int64_t pitch = ldc * size_of(c_dtype);
+    const int vec = !off(C, 32) && pitch % 32 == 0 ? 32 : !off(C, 16) && pitch % 16 == 0 ? 16 : (int)size_of(c_dtype);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const cudaError_t e = c_dtype == MVUE_BF16 ? launch(p, oa, ob, n_major, Store<true>{C, ldc, vec}, st)
+                                               : launch(p, oa, ob, n_major, Store<false>{C, ldc, vec}, st);
+    if (e != cudaSuccess) { set_cuda_error(e, "scaled product launch"); return MVUE_ERR_CUDA; }
+    return MVUE_OK;
+}
+
+}  // namespace
+}  // namespace mvue
+
+using namespace mvue;
+
+extern "C" int mvue_scaled_forward_gemm(const void* x, const void* x_scales, int64_t tokens, int64_t in, int64_t ldx, const void* W,
+                                        const void* W_scales, int64_t out, int64_t ldW, void* C, int c_dtype, int64_t ldc, int* dev_status,
+                                        void* stream) {
+    return scaled_gemm(x, tokens, in, ldx, x_scales, W, out, ldW, W_scales, false, C, c_dtype, ldc, dev_status, stream);
+}
+
+extern "C" int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int64_t tokens, int64_t out, int64_t ldg, const void* W,
+                                         const void* W_scales, int64_t in, int64_t ldW, void* C, int c_dtype, int64_t ldc, int* dev_status,
+                                         void* stream) {
+    return scaled_gemm(g, tokens, out, ldg, g_scales, W, in, ldW, W_scales, true, C, c_dtype, ldc, dev_status, stream);
+}
