@@ -5,6 +5,8 @@
  *
  * The rules of mvue_train.h hold: device pointers, caller-owned buffers, work enqueued on `stream`, argument errors found on
  * the host before anything is launched, tensors aligned to their element type unless a call says more.
+ *
+ * And the Muon step, for the weights that are matrices: it takes the dW of the update products as mvue_adamw_step does.
  */
 #ifndef MVUE_LAYER_H_
 #define MVUE_LAYER_H_
@@ -78,6 +80,73 @@ MVUE_API int mvue_scaled_forward_gemm(const void* x, const void* x_scales, int64
 MVUE_API int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int64_t tokens, int64_t out, int64_t ldg, const void* W,
                                        const void* W_scales, int64_t in, int64_t ldW, void* C, int c_dtype, int64_t ldc, int* dev_status,
                                        void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Muon
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* The polynomial 3.4445 s - 4.7750 s^3 + 2.0315 s^5 applied ns_steps times (1 .. 16) to the singular values of x / (||x|| + 1e-7),
+ * ||x|| the root of the sum of squares: five steps bring those above a hundredth or so between 0.7 and 1.2 and leave the
+ * singular vectors as they are.
+ *   X = x / (||x|| + 1e-7);  ns_steps times:  A = X X^T,  X = 3.4445 X + (-4.7750 A + 2.0315 A A) X
+ * (X^T X where rows > cols).  Products of binary16 values with binary32 sums; in all steps but the last two the first term is taken
+ * from 22 bits of X.  Against exact arithmetic, five steps: 1e-3 to 2.5e-3 of the result's norm (gradients of any spectrum).
+ * A matrix with an element that is not finite, or whose sum of squares overflows binary32 in eight neighbours, becomes NaN throughout.
+ *  x          [batch, rows, cols], MVUE_F32 or MVUE_BF16, ldx >= cols, x_stride elements between matrices.
+ *  out        the same, MVUE_F32 or MVUE_BF16; it may be x.
+ *  workspace  mvue_orthogonalize_workspace_bytes(batch, rows, cols) bytes, 256-byte aligned; contents scratch.
+ *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires; otherwise left untouched.
+ * min(rows, cols) <= 2^20.  An empty extent: nothing.  Equal inputs give equal bits. */
+MVUE_API int mvue_orthogonalize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ldx, int64_t x_stride, int ns_steps,
+                                void* out, int out_dtype, int64_t ldo, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                                int* dev_status, void* stream);
+MVUE_API int mvue_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t* bytes);   /* bytes: HOST */
+
+/* One matrix of the step: rows x cols, contiguous.
+ *  param      MVUE_F32 or MVUE_BF16 (param_dtype), updated in place.
+ *  master     optional float copy of a bf16 param, as in mvue_adamw_tensor.
+ *  grad       MVUE_F32 or MVUE_BF16 (grad_dtype), read only.
+ *  momentum   float, updated in place.
+ * Buffers of one call must not overlap. */
+typedef struct {
+    void* param;
+    void* master;
+    const void* grad;
+    void* momentum;
+    int64_t rows, cols;
+    int32_t param_dtype;
+    int32_t grad_dtype;
+} mvue_muon_tensor;
+
+typedef enum {
+    MVUE_MUON_SCALE_RMS = 0,      /* 0.2 sqrt(max(rows, cols)): the update is as large as AdamW's */
+    MVUE_MUON_SCALE_SHAPE = 1     /* sqrt(max(1, rows / cols)) */
+} mvue_muon_scale;
+
+#define MVUE_OPT_NESTEROV 16u
+
+/* The step:
+ *   g' = g * grad_scale (* *dev_grad_scale);  M' = momentum M + (1 - momentum) g'
+ *   U = M', or with MVUE_OPT_NESTEROV momentum M' + (1 - momentum) g'
+ *   param' = param (1 - lr weight_decay) - lr scale orthogonalize(U)          (scale: scale_rule)
+ * Arithmetic in binary32 outside the products.  options: MVUE_OPT_NESTEROV; MVUE_OPT_STOCHASTIC_ROUNDING rounds a bf16 param without
+ * master stochastically, with the random numbers of mvue_adamw_step (matrices of a call numbered through in order, each padded to a
+ * multiple of 256 elements).  Other bits: MVUE_ERR_OPTION. */
+typedef struct {
+    double lr, momentum, weight_decay, grad_scale;
+    const float* dev_grad_scale;
+    uint64_t seed;
+    int32_t ns_steps;
+    int32_t scale_rule;
+    uint32_t options;
+} mvue_muon_config;
+
+/* tensors: HOST array of `count` entries (0, and empty matrices, are accepted); it may be freed on return.  Matrices of equal extents go
+ * through the products together, up to 64 and 2^27 elements at a time.  workspace: mvue_muon_workspace_bytes(tensors, count) bytes (only the
+ * extents are looked at), 256-byte aligned; contents scratch.  Errors as mvue_adamw_step's, MVUE_ERR_WORKSPACE beside them. */
+MVUE_API int mvue_muon_step(const mvue_muon_tensor* tensors, int64_t count, const mvue_muon_config* config, void* workspace,
+                            size_t workspace_bytes, int* dev_status, void* stream);
+MVUE_API int mvue_muon_workspace_bytes(const mvue_muon_tensor* tensors, int64_t count, size_t* bytes);   /* bytes: HOST */
 
 #ifdef __cplusplus
 }

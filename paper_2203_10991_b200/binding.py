@@ -19,6 +19,8 @@ MVUE_LAYOUT_CANONICAL = 0
 MVUE_LAYOUT_TC = 1
 MVUE_JOINT_TABLE, MVUE_JOINT_SYSTEMATIC, MVUE_JOINT_APPROX = 0, 1, 2
 MVUE_OPT_NONE, MVUE_OPT_STOCHASTIC_ROUNDING, MVUE_OPT_EPS16 = 0, 1, 2
+MVUE_OPT_NESTEROV = 16            # of mvue_muon_step
+MVUE_MUON_SCALES = {"rms": 0, "shape": 1}
 MVUE_ERR_WORKSPACE = -7
 MVUE_ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
@@ -31,7 +33,8 @@ EXPORTS = ("mvue_version", "mvue_status_string", "mvue_last_cuda_error", "mvue_p
            "mvue_group_norm_act", "mvue_group_norm_act_backward", "mvue_group_norm_workspace_bytes",
            "mvue_selftest_group_norm_timeout",
            "mvue_layer_norm", "mvue_layer_norm_backward", "mvue_layer_norm_workspace_bytes",
-           "mvue_quantize_e4m3", "mvue_scaled_forward_gemm", "mvue_scaled_backward_gemm")
+           "mvue_quantize_e4m3", "mvue_scaled_forward_gemm", "mvue_scaled_backward_gemm",
+           "mvue_orthogonalize", "mvue_orthogonalize_workspace_bytes", "mvue_muon_step", "mvue_muon_workspace_bytes")
 
 
 class AdamWTensor(ctypes.Structure):
@@ -46,6 +49,19 @@ class AdamWConfig(ctypes.Structure):
     _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")] + \
                [("step", ctypes.c_int64), ("grad_scale", ctypes.c_double), ("dev_grad_scale", ctypes.c_void_p),
                 ("seed", ctypes.c_uint64), ("state_bits", ctypes.c_int32), ("options", ctypes.c_uint32)]
+
+
+class MuonTensor(ctypes.Structure):
+    """mvue_muon_tensor"""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("param", "master", "grad", "momentum")] + \
+               [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32)]
+
+
+class MuonConfig(ctypes.Structure):
+    """mvue_muon_config"""
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "momentum", "weight_decay", "grad_scale")] + \
+               [("dev_grad_scale", ctypes.c_void_p), ("seed", ctypes.c_uint64), ("ns_steps", ctypes.c_int32),
+                ("scale_rule", ctypes.c_int32), ("options", ctypes.c_uint32)]
 
 
 class MvueError(RuntimeError):
@@ -104,6 +120,10 @@ def lib() -> ctypes.CDLL:
         L.mvue_layer_norm_backward.argtypes = [vp, i64, vp, i64, ci, i64, i64, vp, vp, vp, ci, vp, i64, vp, vp, vp, csz, vp]
         L.mvue_layer_norm_workspace_bytes.argtypes = [i64, i64, szp]
         L.mvue_quantize_e4m3.argtypes = [vp, ci, i64, i64, i64, ci, ctypes.c_uint, u64, vp, i64, vp, vp]
+        L.mvue_orthogonalize.argtypes = [vp, ci, i64, i64, i64, i64, i64, ci, vp, ci, i64, i64, vp, csz, vp, vp]
+        L.mvue_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, szp]
+        L.mvue_muon_step.argtypes = [ctypes.POINTER(MuonTensor), i64, ctypes.POINTER(MuonConfig), vp, csz, vp, vp]
+        L.mvue_muon_workspace_bytes.argtypes = [ctypes.POINTER(MuonTensor), i64, szp]
         for product in (L.mvue_scaled_forward_gemm, L.mvue_scaled_backward_gemm):
             product.argtypes = [vp, vp, i64, i64, i64, vp, vp, i64, i64, vp, ci, i64, vp, vp]
         L.mvue_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, ctypes.POINTER(AdamWConfig), vp]
@@ -666,3 +686,59 @@ def mvue_scaled_backward_gemm(g: torch.Tensor, g_scales: torch.Tensor, W: torch.
                               out: torch.Tensor | None = None, out_dtype=torch.bfloat16, dev_status: torch.Tensor | None = None) -> torch.Tensor:
     """g . W from e4m3 codes: g [tokens, out] with scales [ceil(out / 128), tokens]; W and its scales as in the forward product."""
     return _scaled_gemm("mvue_scaled_backward_gemm", g, g_scales, W, W_scales, W.shape[-1], g.shape[-1], W.shape[0], out, out_dtype, dev_status)
+
+
+def _matrices(t: torch.Tensor):
+    """(batch, rows, cols, ld, stride) of a tensor [..., rows, cols] whose matrices lie one stride apart."""
+    if t.dim() < 2 or (t.stride(-1) != 1 and t.shape[-1] != 1):
+        raise ValueError("wants [..., rows, columns] with unit column stride")
+    rows, cols = t.shape[-2:]
+    ld = t.stride(-2) if rows > 1 else cols
+    batch, stride, step = 1, rows * ld, None
+    for size, s in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):                # innermost matrix first
+        if size != 1 and t.numel():
+            if step is None:
+                stride = s
+            elif s != step:
+                raise ValueError("matrices are not one stride apart")
+            step = s * size
+        batch *= size
+    return batch, rows, cols, ld, stride
+
+
+def mvue_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().mvue_orthogonalize_workspace_bytes(batch, rows, cols, ctypes.byref(b)), "mvue_orthogonalize_workspace_bytes")
+    return b.value
+
+
+def mvue_orthogonalize(x: torch.Tensor, *, steps: int = 5, out: torch.Tensor | None = None, out_dtype=None,
+                       workspace: torch.Tensor | None = None, dev_status: torch.Tensor | None = None) -> torch.Tensor:
+    """Each matrix of x [..., rows, cols] (fp32 or bf16) with its singular values brought towards one by `steps` Newton-Schulz steps, its
+    singular vectors kept.  Returns a tensor of out_dtype (x's own unless given); out may be x."""
+    _operands(x, out, workspace=workspace, dev_status=dev_status)
+    batch, rows, cols, ldx, stride = _matrices(x)
+    if out is None:
+        out = torch.empty_like(x, dtype=out_dtype, memory_format=torch.contiguous_format)
+    assert out.shape == x.shape
+    _, _, _, ldo, out_stride = _matrices(out)
+    need = mvue_orthogonalize_workspace_bytes(batch, rows, cols)
+    if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
+        workspace = x.new_empty(need, dtype=torch.uint8)
+    _check(lib().mvue_orthogonalize(x.data_ptr(), _dtype_code(x), batch, rows, cols, ldx, stride, steps, out.data_ptr(), _dtype_code(out), ldo,
+                                    out_stride, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                    _ptr(dev_status), _stream_ptr()), "mvue_orthogonalize")
+    return out
+
+
+def mvue_muon_workspace_bytes(tensors: ctypes.Array, count: int) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().mvue_muon_workspace_bytes(tensors, count, ctypes.byref(b)), "mvue_muon_workspace_bytes")
+    return b.value
+
+
+def mvue_muon_step(tensors: ctypes.Array, count: int, config: MuonConfig, workspace: torch.Tensor | None,
+                   dev_status: torch.Tensor | None = None) -> None:
+    """One Muon step over `count` entries of a ctypes array of MuonTensor (optim.MuonPlan fills and keeps one)."""
+    _check(lib().mvue_muon_step(tensors, count, config, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                _ptr(dev_status), _stream_ptr()), "mvue_muon_step")

@@ -16,7 +16,8 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libmvue_b200.so"
 SOURCES = ["mvue_api.cu", "mvue_prune.cu", "mvue_gemm.cu", "mvue_adamw.cu", "mvue_embed.cu",
-           "mvue_norm.cu", "mvue_layer_norm.cu", "mvue_quantize.cu", "mvue_scaled.cu"]
+           "mvue_norm.cu", "mvue_layer_norm.cu", "mvue_quantize.cu", "mvue_scaled.cu",
+           "mvue_muon.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--cudart", "static", "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden"]
 

@@ -1,0 +1,598 @@
+// The Muon step: momentum, the update's orthogonalisation by Newton-Schulz products, the param.
+//
+// With X the update over its norm, transposed where it has more rows than columns ([m x n], m <= n), a step of the iteration is
+//   A = X X^T;  B = b A + c A A;  X' = a X + B X
+// Products are binary16 on the tensor cores with fp32 accumulators: binary16 and not bf16, since the polynomial's slope of a = 3.4
+// at zero multiplies what a rounding adds to small singular values by up to 485 in five steps (an update of sixteen large
+// directions and noise a tenth as strong comes out 9 % off with bf16, 1 % with binary16).  The same update is 0.08 % off if, in all
+// steps but the last two, the term a X is taken from a second binary16 beside the first (x = hi + lo 2^-11): the error of B X lies in
+// few directions, that of a X in all.
+// A and B are symmetric: only tiles on and above the diagonal are computed, and stored twice.
+// X is stored times xs, A and B times S, powers of two near the root of n, so that entries of 1 / sqrt(n) stay normal numbers; xs is larger for
+// an update far below eps.
+//
+// Matrices of equal extents go through the products together.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/mvue_layer.h"
+#include "mvue_dense.cuh"
+#include "mvue_train.cuh"
+
+namespace mvue {
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr double kEps = 1e-7;
+constexpr int kBatch = 64;                          // matrices that go together
+constexpr int64_t kBatchElements = 1 << 27;         // unless they have more elements than this
+constexpr int kMaxParts = 128;                      // blocks that share a matrix's norm
+constexpr int kThreads = 256, kTile = 64;
+constexpr float kLo = 2048.0f;                      // 2^11: lo holds what hi lost, times this
+
+enum : uint32_t { kTransposed = 1, kGradBf16 = 2, kParamBf16 = 4, kWideIn = 8, kWideOut = 16 };
+
+struct Matrix {
+    const void* grad;
+    float* momentum;            // NULL: orthogonalise grad itself
+    void* param;                // or the output
+    float* master;
+    int64_t first_block;        // the call's 256-element blocks before this matrix
+    uint32_t flags, pad;
+};
+
+struct Group {
+    int count, m, n;            // m <= n
+    int64_t ld_grad, ld_param;  // of a matrix as the caller holds it; momentum and master lie as the param does
+    // workspace
+    __half *hi, *lo;            // [count][m][n_pitch]
+    int64_t n_pitch;
+    double* parts;              // [count][n_parts]
+    int n_parts;
+    float* xs;                  // [count]
+    float S, growth;            // growth: 3.4445^steps
+    // the step
+    float mu, one_mu, grad_scale, decay, size;      // size: lr times the scale of the update
+    const float* dev_grad_scale;
+    int nesterov, random;
+    RoundKeys keys;
+    Matrix matrix[kBatch];
+
+    __device__ __forceinline__ int rows(const Matrix& t) const { return t.flags & kTransposed ? n : m; }
+    __device__ __forceinline__ int cols(const Matrix& t) const { return t.flags & kTransposed ? m : n; }
+    __device__ __forceinline__ float scale() const { return dev_grad_scale ? __fmul_rn(grad_scale, *dev_grad_scale) : grad_scale; }
+};
+
+__device__ __forceinline__ void load_grad(const Matrix& t, int64_t at, bool wide, int count, float gs, float (&g)[8]) {
+    if (t.flags & kGradBf16) load8(static_cast<const __nv_bfloat16*>(t.grad) + at, wide, count, g);
+    else load8(static_cast<const float*>(t.grad) + at, wide, count, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] *= gs;
+}
+
+// The new momentum, and a share of the squared norm of the update.  Grid: n_parts x count.
+__global__ void __launch_bounds__(kThreads) momentum_kernel(const __grid_constant__ Group q) {
+    __shared__ double warps[kThreads / 32];
+    grid_dependency_wait();
+    const Matrix& t = q.matrix[blockIdx.y];
+    const float gs = q.scale();
+    const int cols = q.cols(t);
+    // rows without gaps are one long row
+    const bool dense = q.ld_grad == cols;
+    const int64_t len = dense ? (int64_t)q.m * q.n : cols, pieces = (len + 8 * kThreads - 1) / (8 * kThreads), rows = dense ? 1 : q.rows(t);
+    double sum = 0.0;
+    for (int64_t w = blockIdx.x; w < rows * pieces; w += gridDim.x) {
+        const int64_t row = w / pieces, i0 = (w - row * pieces) * 8 * kThreads + threadIdx.x * 8;
+        const int count = (int)min((int64_t)8, len - i0);
+        if (count <= 0) continue;
+        const bool wide = (t.flags & kWideIn) && count == 8;
+        float g[8], u[8];
+        load_grad(t, row * q.ld_grad + i0, wide, count, gs, g);
+        if (t.momentum) {
+            load8(t.momentum + row * q.ld_param + i0, wide, count, u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = fmaf(q.mu, u[i], q.one_mu * g[i]);
+            store8(t.momentum + row * q.ld_param + i0, wide, count, u);
+            if (q.nesterov) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = fmaf(q.mu, u[i], q.one_mu * g[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = g[i];
+        }
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(u[i], u[i], s);
+        sum += (double)s;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kThreads / 32; ++w) sum += warps[w];
+        q.parts[(int64_t)blockIdx.y * q.n_parts + blockIdx.x] = sum;
+    }
+}
+
+// hi and lo of eight values.
+__device__ __forceinline__ void split8(const float (&x)[8], uint4* hi, uint4* lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 a = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+        const float2 f = __half22float2(a);
+        const __half2 b = __floats2half2_rn((x[2 * i] - f.x) * kLo, (x[2 * i + 1] - f.y) * kLo);
+        h[i] = *reinterpret_cast<const uint32_t*>(&a);
+        l[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    *hi = make_uint4(h[0], h[1], h[2], h[3]);
+    *lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// X = update / (norm + eps) in tiles of 64 x 64 of the caller's matrix, which is turned over where it has more rows than columns.
+// Eight neighbours a thread; n_pitch is a multiple of eight, so what is written in X's rows is whole pieces of it.
+__global__ void __launch_bounds__(kThreads) start_kernel(const __grid_constant__ Group q) {
+    __shared__ float tile[kTile][kTile + 1];
+    __shared__ float factor;
+    grid_dependency_wait();
+    const int z = blockIdx.y;
+    const Matrix& t = q.matrix[z];
+    const int rows = q.rows(t), cols = q.cols(t);
+    if (threadIdx.x < 32) {                        // every block adds the shares in the same order
+        double s = 0.0;
+        for (int i = threadIdx.x; i < q.n_parts; i += 32) s += q.parts[(int64_t)z * q.n_parts + i];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+        if (threadIdx.x == 0) {
+            const double norm = sqrt(s);
+            // xs: S, or more where even the last X stays below one (eps outweighs the update): S 2^k, k at most 60
+            const float last = fminf((float)(norm / (norm + kEps)) * q.growth, 1.25f);
+            const float xs = last < 1.25f ? q.S * exp2f(fminf(floorf(log2f(1.25f / fmaxf(last, 1e-37f))), 60.0f)) : q.S;
+            factor = isfinite(norm) ? (float)((double)xs / (norm + kEps)) : __uint_as_float(0x7FFFFFFFu);
+            if (blockIdx.x == 0) q.xs[z] = xs;
+        }
+    }
+    __syncthreads();
+    const float gs = q.scale(), f = factor;
+    const int tiles_x = (cols + kTile - 1) / kTile, tiles = tiles_x * ((rows + kTile - 1) / kTile);
+    __half *hi = q.hi + (int64_t)z * q.m * q.n_pitch, *lo = q.lo + (int64_t)z * q.m * q.n_pitch;
+    for (int w = blockIdx.x; w < tiles; w += gridDim.x) {
+        const int row0 = w / tiles_x * kTile, col0 = w % tiles_x * kTile;
+        const int c = (threadIdx.x & 7) * 8;
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+            const int r = (threadIdx.x >> 3) + 32 * it, row = row0 + r, col = col0 + c;
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
+            const int count = row < rows ? max(0, min(8, cols - col)) : 0;
+            if (count > 0) {
+                const bool wide = (t.flags & kWideIn) && count == 8;
+                load_grad(t, (int64_t)row * q.ld_grad + col, wide, count, gs, x);
+                if (t.momentum) {
+                    float u[8];
+                    load8(t.momentum + (int64_t)row * q.ld_param + col, wide, count, u);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = q.nesterov ? fmaf(q.mu, u[i], q.one_mu * x[i]) : u[i];
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] *= f;
+            }
+            if (t.flags & kTransposed) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) tile[r][c + i] = x[i];
+            } else if (count > 0) {
+                const int64_t at = (int64_t)row * q.n_pitch + col;
+                split8(x, reinterpret_cast<uint4*>(hi + at), reinterpret_cast<uint4*>(lo + at));
+            }
+        }
+        if (t.flags & kTransposed) {
+            __syncthreads();
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int r = (threadIdx.x >> 3) + 32 * it, row = col0 + r, col = row0 + c;       // of X
+                if (row < q.m && col < q.n) {
+                    float x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = tile[c + i][r];
+                    const int64_t at = (int64_t)row * q.n_pitch + col;
+                    split8(x, reinterpret_cast<uint4*>(hi + at), reinterpret_cast<uint4*>(lo + at));
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// What comes of the last X (hi / xs): the output, or the param's step.  Tiles as above.
+__global__ void __launch_bounds__(kThreads) finish_kernel(const __grid_constant__ Group q) {
+    __shared__ float tile[kTile][kTile + 1];
+    grid_dependency_wait();
+    const int z = blockIdx.y;
+    const Matrix& t = q.matrix[z];
+    const int rows = q.rows(t), cols = q.cols(t);
+    const float inv = 1.0f / q.xs[z];
+    const int tiles_x = (cols + kTile - 1) / kTile, tiles = tiles_x * ((rows + kTile - 1) / kTile);
+    const __half* hi = q.hi + (int64_t)z * q.m * q.n_pitch;
+    const auto take = [&](int row, int col, float (&x)[8]) {          // eight neighbours in a row of X
+        const uint4 v = *reinterpret_cast<const uint4*>(hi + (int64_t)row * q.n_pitch + col);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            x[2 * i] = f.x * inv;
+            x[2 * i + 1] = f.y * inv;
+        }
+    };
+    for (int w = blockIdx.x; w < tiles; w += gridDim.x) {
+        const int row0 = w / tiles_x * kTile, col0 = w % tiles_x * kTile;
+        const int c = (threadIdx.x & 7) * 8;
+        if (t.flags & kTransposed) {
+            __syncthreads();
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int r = (threadIdx.x >> 3) + 32 * it, row = col0 + r, col = row0 + c;       // of X
+                if (row < q.m && col < q.n) {
+                    float x[8];
+                    take(row, col, x);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) tile[c + i][r] = x[i];
+                }
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+            const int r = (threadIdx.x >> 3) + 32 * it, row = row0 + r, col = col0 + c;
+            const int count = row < rows ? max(0, min(8, cols - col)) : 0;
+            if (count == 0) continue;
+            const bool wide = (t.flags & kWideOut) && count == 8;
+            float x[8];
+            if (t.flags & kTransposed) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = tile[r][c + i];
+            } else {
+                take(row, col, x);
+            }
+            const int64_t at = (int64_t)row * q.ld_param + col;
+            uint32_t random[8];
+            bool rounds = false;
+            if (t.momentum) {
+                float p[8];
+                if (t.master) load8(t.master + at, wide, count, p);
+                else if (t.flags & kParamBf16) load8(static_cast<const __nv_bfloat16*>(t.param) + at, wide, count, p);
+                else load8(static_cast<const float*>(t.param) + at, wide, count, p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = fmaf(p[i], q.decay, -q.size * x[i]);
+                if (t.master) store8(t.master + at, wide, count, x);
+                rounds = q.random && (t.flags & kParamBf16) && !t.master;
+                if (rounds) {
+                    // elements 8u .. 8u + 7 of the padded list share a call; a piece that starts inside one takes two
+                    const uint64_t first = (uint64_t)t.first_block * 256u + (uint64_t)at;
+                    const int shift = (int)(first & 7u);
+                    const uint4 a = philox4x32_10(first >> 3, q.keys, 2u);
+                    const uint4 b = shift ? philox4x32_10((first >> 3) + 1u, q.keys, 2u) : a;
+                    const uint32_t words[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t v = 0u;
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            if (s == shift) v = words[(i + s) >> 1] >> (16 * ((i + s) & 1));
+                        random[i] = v & 0xFFFFu;
+                    }
+                }
+            }
+            if (t.flags & kParamBf16) {
+                uint32_t o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (rounds) {
+                        // (a NaN whose lower half is zero: random bits do not carry into its sign)
+                        const float lo = x[2 * i] == x[2 * i] ? x[2 * i] : __uint_as_float(0x7FC00000u);
+                        const float hi2 = x[2 * i + 1] == x[2 * i + 1] ? x[2 * i + 1] : __uint_as_float(0x7FC00000u);
+                        o[i] = pack_out<true>(lo, hi2, random[2 * i] | random[2 * i + 1] << 16);
+                    } else {
+                        o[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                    }
+                }
+                store8_words(static_cast<__nv_bfloat16*>(t.param) + at, wide, count, o);
+            } else {
+                store8(static_cast<float*>(t.param) + at, wide, count, x);
+            }
+        }
+    }
+}
+
+// ---- epilogues of the products -----------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// 32 halves of a row whose pitch is a multiple of eight; columns beyond `left` are the pitch's own or not touched
+__device__ __forceinline__ void load_row(const __half* from, int left, uint32_t (&w)[16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint4 v = 8 * i < left ? *reinterpret_cast<const uint4*>(from + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+    }
+}
+__device__ __forceinline__ void store_row(__half* to, int left, const uint32_t (&w)[16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (8 * i < left) *reinterpret_cast<uint4*>(to + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+
+// A S = acc S / xs^2 (kPoly false), B S = b (A S) + c acc / S (true); symmetric, the tile's mirror image is stored too.
+template <bool kPoly>
+struct StoreSymmetric {
+    const __half* A;
+    __half* out;
+    int64_t pitch;
+    const float* xs;
+    float S;
+    __device__ __forceinline__ void store(const dense::Params& p, int z, int row, int m0, int n0, int col, const uint32_t (&v)[32]) const {
+        const int left = p.N - col;
+        const bool there = row < p.M && left > 0;
+        const int64_t matrix = (int64_t)z * p.M * pitch;
+        float alpha;
+        uint32_t w[16];
+        if (kPoly) {
+            alpha = kC / S;
+            if (there) load_row(A + matrix + (int64_t)row * pitch + col, left, w);
+        } else {
+            const float x = xs[z];
+            alpha = S / x / x;
+        }
+        if (!there) return;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float lo = __uint_as_float(v[2 * i]) * alpha, hi = __uint_as_float(v[2 * i + 1]) * alpha;
+            if (kPoly) {
+                const float2 a = halves(w[i]);
+                lo = fmaf(kB, a.x, lo);
+                hi = fmaf(kB, a.y, hi);
+            }
+            w[i] = half_pair(lo, hi);
+        }
+        store_row(out + matrix + (int64_t)row * pitch + col, left, w);
+        if (m0 != n0) {
+            __half* to = out + matrix + (int64_t)col * pitch + row;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < left) reinterpret_cast<unsigned short*>(to)[i * pitch] = (unsigned short)(w[i >> 1] >> (16 * (i & 1)));
+        }
+    }
+};
+
+// X' xs = a (X xs) + acc / S.  lo (the same place in both) is read and written where asked for.
+struct StoreApply {
+    const __half* hi;
+    __half* lo;
+    __half* out;
+    int64_t pitch;
+    float inv_S;
+    int read_lo, write_lo;
+    __device__ __forceinline__ void store(const dense::Params& p, int z, int row, int, int, int col, const uint32_t (&v)[32]) const {
+        const int left = p.N - col;
+        if (row >= p.M || left <= 0) return;
+        const int64_t at = ((int64_t)z * p.M + row) * pitch + col;
+        uint32_t h[16], l[16];
+        load_row(hi + at, left, h);
+        if (read_lo) load_row(lo + at, left, l);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float2 x = halves(h[i]);
+            if (read_lo) {
+                const float2 y = halves(l[i]);
+                x.x = fmaf(y.x, 1.0f / kLo, x.x);
+                x.y = fmaf(y.y, 1.0f / kLo, x.y);
+            }
+            const float a = fmaf(kA, x.x, __uint_as_float(v[2 * i]) * inv_S), b = fmaf(kA, x.y, __uint_as_float(v[2 * i + 1]) * inv_S);
+            h[i] = half_pair(a, b);
+            const float2 r = halves(h[i]);
+            l[i] = half_pair((a - r.x) * kLo, (b - r.y) * kLo);
+        }
+        store_row(out + at, left, h);
+        if (write_lo) store_row(lo + at, left, l);
+    }
+};
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+int64_t pitch_of(int64_t n) { return (n + 7) / 8 * 8; }
+
+// Bytes of a group's workspace, in the order X (two), lo, A, B, shares of the norms, xs.
+int64_t group_bytes(int64_t count, int64_t m, int64_t n) {
+    return 3 * padded(count * m * pitch_of(n) * 2) + 2 * padded(count * m * pitch_of(m) * 2) + padded(count * kMaxParts * 8) + padded(count * 4);
+}
+int64_t batch_of(int64_t m, int64_t n) { return std::max<int64_t>(1, std::min<int64_t>(kBatch, kBatchElements / (m * n))); }
+
+bool extents_ok(int64_t rows, int64_t cols) {
+    return rows >= 0 && cols >= 0 && rows <= 0x7FFFFF00 && cols <= 0x7FFFFF00 && (rows == 0 || cols <= ((int64_t)1 << 40) / rows) &&
+           std::min(rows, cols) <= (1 << 20);
+}
+
+// The whole step of the q.count matrices of q, which have the extents q.m <= q.n.
+cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_count, cudaStream_t st) {
+    const int64_t m = q.m, n = q.n, mp = pitch_of(m);
+    q.n_pitch = pitch_of(n);
+    const int64_t x_bytes = padded(q.count * m * q.n_pitch * 2), a_bytes = padded(q.count * m * mp * 2);
+    __half* X[2] = {reinterpret_cast<__half*>(ws), reinterpret_cast<__half*>(ws + x_bytes)};
+    q.lo = reinterpret_cast<__half*>(ws + 2 * x_bytes);
+    __half *A = reinterpret_cast<__half*>(ws + 3 * x_bytes), *B = reinterpret_cast<__half*>(ws + 3 * x_bytes + a_bytes);
+    q.parts = reinterpret_cast<double*>(ws + 3 * x_bytes + 2 * a_bytes);
+    q.xs = reinterpret_cast<float*>(ws + 3 * x_bytes + 2 * a_bytes + padded((int64_t)q.count * kMaxParts * 8));
+    q.hi = X[0];
+    q.S = (float)std::ldexp(1.0, (int)std::lround(0.5 * std::log2((double)n)));
+    q.growth = (float)std::pow((double)kA, (double)steps);
+    const int64_t pieces = (m * n + 8 * kThreads - 1) / (8 * kThreads);
+    q.n_parts = (int)std::max<int64_t>(1, std::min<int64_t>({pieces, (int64_t)kMaxParts, 8 * (int64_t)sm_count / q.count}));
+    cudaError_t e = launch_dependent(&momentum_kernel, dim3(q.n_parts, q.count), dim3(kThreads), 0, st, q);
+    const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
+    const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 8 * sm_count / q.count));
+    if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
+    using KMajor = dense::Shape<false, false, 256>;
+    using NMajor = dense::Shape<false, true, 256>;
+    for (int k = 0; k < steps && e == cudaSuccess; ++k) {
+        __half *x = X[k & 1], *y = X[(k + 1) & 1];
+        const dense::Operand ox = {x, q.n_pitch * 2, m * q.n_pitch * 2}, oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2};
+        dense::Params p = {};
+        p.batch = q.count;
+        p.dev_status = dev_status;
+        p.M = p.N = (int)m;
+        p.K = (int)n;
+        p.symmetric = 1;
+        e = dense::launch_pair<KMajor>(p, ox, ox, StoreSymmetric<false>{nullptr, A, mp, q.xs, q.S}, st);
+        p.K = (int)m;
+        if (e == cudaSuccess) e = dense::launch_pair<KMajor>(p, oa, oa, StoreSymmetric<true>{A, B, mp, q.xs, q.S}, st);
+        p.symmetric = 0;
+        p.N = (int)n;
+        if (e == cudaSuccess)
+            e = dense::launch_pair<NMajor>(p, ob, ox, StoreApply{x, q.lo, y, q.n_pitch, 1.0f / q.S, k < steps - 2, k + 1 < steps - 2}, st);
+        q.hi = y;
+    }
+    if (e == cudaSuccess) e = launch_dependent(&finish_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
+    return e;
+}
+
+bool wide(const void* p, int64_t size, int64_t ld) { return !off(p, 8 * size) && ld % 8 == 0; }
+
+}  // namespace
+}  // namespace mvue
+
+using namespace mvue;
+
+extern "C" int mvue_muon_workspace_bytes(const mvue_muon_tensor* tensors, int64_t count, size_t* bytes) {
+    if (!bytes || (count > 0 && !tensors)) return MVUE_ERR_NULL;
+    if (count < 0) return MVUE_ERR_SHAPE;
+    int64_t most = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (!extents_ok(tensors[i].rows, tensors[i].cols)) return MVUE_ERR_SHAPE;
+        const int64_t m = std::min(tensors[i].rows, tensors[i].cols), n = std::max(tensors[i].rows, tensors[i].cols);
+        if (m == 0) continue;
+        int64_t same = 0;
+        for (int64_t j = 0; j < count; ++j) same += std::min(tensors[j].rows, tensors[j].cols) == m && std::max(tensors[j].rows, tensors[j].cols) == n;
+        most = std::max(most, group_bytes(std::min(same, batch_of(m, n)), m, n));
+    }
+    *bytes = (size_t)most;
+    return MVUE_OK;
+}
+
+extern "C" int mvue_muon_step(const mvue_muon_tensor* tensors, int64_t count, const mvue_muon_config* cfg, void* workspace,
+                              size_t workspace_bytes, int* dev_status, void* stream) {
+    if (!cfg || (count > 0 && !tensors)) return MVUE_ERR_NULL;
+    if (count < 0 || cfg->ns_steps < 1 || cfg->ns_steps > 16) return MVUE_ERR_SHAPE;
+    if (cfg->options & ~(uint32_t)(MVUE_OPT_STOCHASTIC_ROUNDING | MVUE_OPT_NESTEROV)) return MVUE_ERR_OPTION;
+    if (cfg->scale_rule != MVUE_MUON_SCALE_RMS && cfg->scale_rule != MVUE_MUON_SCALE_SHAPE) return MVUE_ERR_OPTION;
+    if (!(cfg->momentum >= 0.0 && cfg->momentum < 1.0)) return MVUE_ERR_OPTION;
+    for (int64_t i = 0; i < count; ++i) {
+        const mvue_muon_tensor& t = tensors[i];
+        if (!extents_ok(t.rows, t.cols)) return MVUE_ERR_SHAPE;
+        if ((t.param_dtype != MVUE_F32 && t.param_dtype != MVUE_BF16) || (t.grad_dtype != MVUE_F32 && t.grad_dtype != MVUE_BF16) ||
+            (t.master && t.param_dtype != MVUE_BF16))
+            return MVUE_ERR_DTYPE;
+        if (t.rows == 0 || t.cols == 0) continue;
+        if (!t.param || !t.grad || !t.momentum) return MVUE_ERR_NULL;
+        if (off(t.param, size_of(t.param_dtype)) || off(t.grad, size_of(t.grad_dtype)) || off(t.master, 4) || off(t.momentum, 4)) return MVUE_ERR_ALIGN;
+    }
+    size_t need = 0;
+    if (int s = mvue_muon_workspace_bytes(tensors, count, &need)) return s;
+    if (need == 0) return MVUE_OK;
+    if (!workspace || off(workspace, 256) || workspace_bytes < need) return MVUE_ERR_WORKSPACE;
+    DeviceInfo dev;
+    if (int s = current_device_info(&dev)) return s;
+
+    Group q = {};
+    q.mu = (float)cfg->momentum;
+    q.one_mu = (float)(1.0 - cfg->momentum);
+    q.grad_scale = (float)cfg->grad_scale;
+    q.dev_grad_scale = cfg->dev_grad_scale;
+    q.decay = (float)(1.0 - cfg->lr * cfg->weight_decay);
+    q.nesterov = (cfg->options & MVUE_OPT_NESTEROV) != 0;
+    q.random = (cfg->options & MVUE_OPT_STOCHASTIC_ROUNDING) != 0;
+    q.keys = make_round_keys(cfg->seed);
+    for (int64_t i = 0; i < count; ++i) {
+        const int64_t rows = tensors[i].rows, cols = tensors[i].cols;
+        if (rows == 0 || cols == 0) continue;
+        bool seen = false;                                      // rows and cols both, since the scale rule may tell them apart
+        for (int64_t j = 0; j < i && !seen; ++j) seen = tensors[j].rows == rows && tensors[j].cols == cols;
+        if (seen) continue;
+        const int64_t m = std::min(rows, cols), n = std::max(rows, cols), batch = batch_of(m, n);
+        q.m = (int)m;
+        q.n = (int)n;
+        q.ld_grad = q.ld_param = cols;
+        const double s = cfg->scale_rule == MVUE_MUON_SCALE_RMS ? 0.2 * std::sqrt((double)n) : std::sqrt(std::max(1.0, (double)rows / (double)cols));
+        q.size = (float)(cfg->lr * s);
+        q.count = 0;
+        int64_t blocks = 0;
+        for (int64_t j = 0; j < count; ++j) {
+            const mvue_muon_tensor& t = tensors[j];
+            const int64_t numel = t.rows * t.cols;
+            if (t.rows == rows && t.cols == cols) {
+                Matrix& x = q.matrix[q.count++];
+                x = {t.grad, static_cast<float*>(t.momentum), t.param, static_cast<float*>(t.master), blocks, 0u, 0u};
+                x.flags = (rows > cols ? kTransposed : 0u) | (t.grad_dtype == MVUE_BF16 ? kGradBf16 : 0u) | (t.param_dtype == MVUE_BF16 ? kParamBf16 : 0u);
+                if (wide(t.grad, size_of(t.grad_dtype), cols) && wide(t.momentum, 4, cols)) x.flags |= kWideIn;
+                if (wide(t.param, size_of(t.param_dtype), cols) && wide(t.master, 4, cols)) x.flags |= kWideOut;
+            }
+            blocks += (numel + 255) / 256;
+            if (q.count == batch || (j + 1 == count && q.count > 0)) {
+                const cudaError_t e = run_group(q, cfg->ns_steps, static_cast<uint8_t*>(workspace), dev_status, dev.sm_count, reinterpret_cast<cudaStream_t>(stream));
+                if (e != cudaSuccess) { set_cuda_error(e, "mvue_muon_step launch"); return MVUE_ERR_CUDA; }
+                q.count = 0;
+            }
+        }
+    }
+    return MVUE_OK;
+}
+
+extern "C" int mvue_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t* bytes) {
+    if (!bytes) return MVUE_ERR_NULL;
+    if (batch < 0 || !extents_ok(rows, cols)) return MVUE_ERR_SHAPE;
+    const int64_t m = std::min(rows, cols), n = std::max(rows, cols);
+    *bytes = batch == 0 || m == 0 ? 0 : (size_t)group_bytes(std::min(batch, batch_of(m, n)), m, n);
+    return MVUE_OK;
+}
+
+extern "C" int mvue_orthogonalize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ldx, int64_t x_stride, int ns_steps,
+                                  void* out, int out_dtype, int64_t ldo, int64_t out_stride, void* workspace, size_t workspace_bytes,
+                                  int* dev_status, void* stream) {
+    if ((dtype != MVUE_F32 && dtype != MVUE_BF16) || (out_dtype != MVUE_F32 && out_dtype != MVUE_BF16)) return MVUE_ERR_DTYPE;
+    if (ns_steps < 1 || ns_steps > 16 || ldx < cols || ldo < cols || x_stride < 0 || out_stride < 0) return MVUE_ERR_SHAPE;
+    size_t need = 0;
+    if (int s = mvue_orthogonalize_workspace_bytes(batch, rows, cols, &need)) return s;
+    if (need == 0) return MVUE_OK;
+    if (!x || !out) return MVUE_ERR_NULL;
+    if (off(x, size_of(dtype)) || off(out, size_of(out_dtype))) return MVUE_ERR_ALIGN;
+    if (!workspace || off(workspace, 256) || workspace_bytes < need) return MVUE_ERR_WORKSPACE;
+    DeviceInfo dev;
+    if (int s = current_device_info(&dev)) return s;
+    Group q = {};
+    q.m = (int)std::min(rows, cols);
+    q.n = (int)std::max(rows, cols);
+    q.ld_grad = ldx;
+    q.ld_param = ldo;
+    q.grad_scale = 1.0f;
+    const int64_t most = batch_of(q.m, q.n);
+    for (int64_t z = 0; z < batch;) {
+        for (q.count = 0; q.count < most && z < batch; ++z) {
+            Matrix& t = q.matrix[q.count++];
+            t = {static_cast<const uint8_t*>(x) + z * x_stride * size_of(dtype), nullptr,
+                 static_cast<uint8_t*>(out) + z * out_stride * size_of(out_dtype), nullptr, 0, 0u, 0u};
+            t.flags = (rows > cols ? kTransposed : 0u) | (dtype == MVUE_BF16 ? kGradBf16 : 0u) | (out_dtype == MVUE_BF16 ? kParamBf16 : 0u);
+            if (wide(t.grad, size_of(dtype), ldx)) t.flags |= kWideIn;
+            if (wide(t.param, size_of(out_dtype), ldo)) t.flags |= kWideOut;
+        }
+        const cudaError_t e = run_group(q, ns_steps, static_cast<uint8_t*>(workspace), dev_status, dev.sm_count, reinterpret_cast<cudaStream_t>(stream));
+        if (e != cudaSuccess) { set_cuda_error(e, "mvue_orthogonalize launch"); return MVUE_ERR_CUDA; }
+    }
+    return MVUE_OK;
+}

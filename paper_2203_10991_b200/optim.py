@@ -1,7 +1,12 @@
-"""AdamW over the tensors of a model: one library call (one launch for up to 320 tensors) per step.
+"""Optimisers over the tensors of a model.  AdamW: one library call (one launch for up to 320 tensors) per step.
 
     plan = AdamWPlan.zeros(params, state_bits=8)            # or AdamWPlan(params, exp_avgs, exp_avg_sqs, ...)
     plan.step(grads, step=t, lr=1e-3)                       # grads: as mvue_sparse_update_gemm left them
+
+Muon, for the weights that are matrices: one library call per step.
+
+    plan = MuonPlan.zeros(weights)                          # or MuonPlan(weights, momentums, ...)
+    plan.step(grads, lr=1e-3)
 """
 from __future__ import annotations
 
@@ -147,3 +152,100 @@ class AdamWPlan:
         else:
             with torch.cuda.device(self._device):
                 binding.mvue_adamw_step(self._array, len(self._array), c)
+
+
+class MuonPlan:
+    """The matrices of a Muon optimiser, marshalled once, and the workspace of its steps.  As AdamWPlan, the plan keeps the memory that
+    its tensors had when it was made, and a param whose memory has been exchanged is refused with the next gradients.
+
+    params:     list of 2-D CUDA tensors, fp32 or bf16, contiguous.
+    momentums:  fp32 tensors of the same shapes.
+    masters:    optional list of fp32 copies for bf16 params (None entries allowed).
+    grads:      optional list of gradient buffers (fp32 or bf16) that every step reads; otherwise step() takes them.
+    """
+
+    def __init__(self, params, momentums, *, masters=None, grads=None):
+        n = len(params)
+        masters = [None] * n if masters is None else masters
+        if len(momentums) != n or len(masters) != n:
+            raise ValueError("the lists differ in length")
+        self._array = (binding.MuonTensor * n)()
+        self._device = params[0].device if n else None
+        for e, p, w, m in zip(self._array, params, masters, momentums):
+            if not p.is_cuda or p.device != self._device or p.dim() != 2 or not p.is_contiguous():
+                raise ValueError("params are contiguous matrices on one CUDA device")
+            e.param_dtype, e.rows, e.cols, e.param = binding._dtype_code(p), p.shape[0], p.shape[1], p.data_ptr()
+            for t, field in ((w, "master"), (m, "momentum")):
+                if t is None and field == "master":
+                    continue
+                if t.dtype != torch.float32 or t.device != p.device or t.shape != p.shape or not t.is_contiguous():
+                    raise ValueError(f"{field}: wants a contiguous fp32 tensor of the param's shape on its device")
+                setattr(e, field, t.data_ptr())
+            if w is not None and p.dtype != torch.bfloat16:
+                raise ValueError("a float copy belongs to a bf16 param")
+        self.params, self.momentums, self.masters = list(params), list(momentums), list(masters)
+        self._memory = [t.detach() for ts in (params, masters, momentums) for t in ts if t is not None]
+        self._addresses = _addresses(self.params)
+        self._config = binding.MuonConfig()
+        need = binding.mvue_muon_workspace_bytes(self._array, n)
+        self._workspace = torch.empty(need, dtype=torch.uint8, device=self._device) if need else None
+        self._grads = self._grad_addresses = None
+        if grads is not None:
+            self._point(grads)
+            self._memory += [g.detach() for g in grads]
+            self._grad_addresses = None
+
+    @classmethod
+    def zeros(cls, params, *, master: bool = False, grads=None) -> "MuonPlan":
+        """A plan with fresh (zero) momentum, and float copies of the bf16 params if asked for."""
+        momentums = [torch.zeros_like(p, dtype=torch.float32) for p in params]
+        masters = [p.float() if p.dtype == torch.bfloat16 else None for p in params] if master else None
+        return cls(params, momentums, masters=masters, grads=grads)
+
+    def _point(self, grads) -> None:
+        if len(grads) != len(self._array):
+            raise ValueError("one gradient for each param")
+        if _addresses(self.params) != self._addresses:
+            raise ValueError("a param's memory has been exchanged since the plan was made: make a new plan")
+        found = []
+        for p, g in zip(self.params, grads):
+            if g.device != self._device or g.shape != p.shape or not g.is_contiguous():
+                raise ValueError("a gradient is contiguous and has its param's device and shape")
+            found.append((binding._dtype_code(g), g.data_ptr()))
+        for e, (code, ptr) in zip(self._array, found):                       # nothing was refused
+            e.grad_dtype, e.grad = code, ptr
+        self._grads, self._grad_addresses = list(grads), [ptr for _, ptr in found]
+
+    def step(self, grads=None, *, lr: float, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.01, ns_steps: int = 5,
+             scale: str = "rms", grad_scale: float = 1.0, dev_grad_scale: torch.Tensor | None = None, stochastic_rounding: bool = False,
+             seed: int | None = None, dev_status: torch.Tensor | None = None) -> None:
+        """One step on the current stream of the params' device.  grads: this step's gradients (they stay the plan's until others are
+        given); None reads the buffers the plan has.  scale: "rms" multiplies the orthogonal update by 0.2 sqrt(max(rows, cols)), which makes
+        it as large as AdamW's; "shape" by sqrt(max(1, rows / cols)).  stochastic_rounding (bf16 params without a float copy)
+        wants a seed, another one each step.  Steps of one plan share its workspace: they run in the order of one stream."""
+        if grads is not None:
+            self._point(grads)
+        elif self._grads is None and len(self._array):
+            raise ValueError("no gradients")
+        elif self._grad_addresses is not None and _addresses(self._grads) != self._grad_addresses:
+            raise ValueError("a gradient's memory has been exchanged since it was given")
+        if dev_grad_scale is not None and (dev_grad_scale.dtype != torch.float32 or dev_grad_scale.device != self._device
+                                           or dev_grad_scale.numel() != 1):
+            raise ValueError("dev_grad_scale is one fp32 element on the params' device")
+        if dev_status is not None and (dev_status.dtype is not torch.int32 or dev_status.device != self._device or dev_status.numel() == 0):
+            raise ValueError("dev_status is an int32 tensor on the params' device")
+        if stochastic_rounding and seed is None:
+            raise ValueError("stochastic rounding wants a seed, another one each step")
+        if scale not in binding.MVUE_MUON_SCALES:
+            raise ValueError(f"scale is one of {', '.join(binding.MVUE_MUON_SCALES)}")
+        c = self._config
+        c.lr, c.momentum, c.weight_decay, c.grad_scale = lr, momentum, weight_decay, grad_scale
+        c.dev_grad_scale = None if dev_grad_scale is None else dev_grad_scale.data_ptr()
+        c.seed = (seed or 0) & (2**64 - 1)
+        c.ns_steps, c.scale_rule = ns_steps, binding.MVUE_MUON_SCALES[scale]
+        c.options = (binding.MVUE_OPT_NESTEROV if nesterov else 0) | (binding.MVUE_OPT_STOCHASTIC_ROUNDING if stochastic_rounding else 0)
+        if self._device is None or self._device.index == torch.cuda.current_device():
+            binding.mvue_muon_step(self._array, len(self._array), c, self._workspace, dev_status)
+        else:
+            with torch.cuda.device(self._device):
+                binding.mvue_muon_step(self._array, len(self._array), c, self._workspace, dev_status)
