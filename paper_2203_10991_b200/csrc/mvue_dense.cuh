@@ -34,8 +34,14 @@ constexpr int kPairThreads = 384;
 constexpr int kEpiWarps = 8;
 constexpr int kBand = 8;                     // row tiles per band of the tile order
 
+// Epilogues.  Direct ones (kSlabs false) are handed 32 consecutive results of a row and store them themselves.  The others
+// read and write matrices of binary16 in slabs of 128 rows x 64 columns, which an own warp moves by TMA through a ring in shared
+// memory while the main loop runs: a thread owns a row, and its accesses to global memory would touch as many lines as there are lanes.
+constexpr int kSlabBufs = 3;
+constexpr int kSlabBytes = kRowsA * 64 * 2;  // 16 KiB; two matrices in a buffer
+
 // How a product's operands lie and how large its tiles are.
-template <bool kScaledT, bool kNMajorT, int kBNT>
+template <bool kScaledT, bool kNMajorT, int kBNT, int kStagesT, bool kSlabsT = false>
 struct Shape {
     static constexpr bool kScaled = kScaledT, kNMajor = kNMajorT;
     static constexpr int kBN = kBNT;
@@ -50,7 +56,8 @@ struct Shape {
     static constexpr int kBoxLine = kNMajor ? kColsBox * (kScaled ? 1 : 2) : kLine;   // bytes of a shared-memory line: 128, or 64
     static constexpr int kBStep = (kNMajor ? kMmaK * kBoxLine : 32) / 16;             // from one instruction's B to the next, in 16 bytes
     static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = kBN == 256 ? 6 : 8;
+    static constexpr int kStages = kStagesT;
+    static constexpr int kSlabBase = kSlabsT ? kSlabBufs * 2 * kSlabBytes : 0;        // bytes of that ring
     // Scales of kGroup stages travel together, four bytes of a row in a word, through rings of kGroups in shared and tensor memory.
     static constexpr int kGroup = 4, kGroups = kScaled ? 3 : 0;
     static constexpr int kScaleParts = 1 + kBN / 128;                                 // 128 rows of A, the columns of B
@@ -60,7 +67,7 @@ struct Shape {
     static constexpr bool kOverlap = kScaled && kBN == 256;
     static constexpr int kAcc1 = kOverlap ? kTmemScale - kBN : kBN;                   // first column of the second accumulator
     static constexpr int kShared = kOverlap ? kBN - kAcc1 : 0;                        // columns that the accumulators share
-    static constexpr int kSmem = kStages * kStageBytes + kGroups * kGroupBytes + 1024 /*alignment*/ + 256 /*barriers*/;
+    static constexpr int kSmem = kStages * kStageBytes + kGroups * kGroupBytes + kSlabBase + 1024 /*alignment*/ + 256 /*barriers*/;
     static constexpr uint32_t kInstr = (kScaled ? (1u << 23) /*scales: powers of two*/ : (1u << 4) /*D = f32*/) |
                                        ((kNMajor ? 1u : 0u) << 16) | ((uint32_t)(kBN >> 3) << 17);      // + M >> 4 at bit 24
     static_assert(kSmem <= 227 * 1024 && kStageBytes % 1024 == 0 && kAcc1 + kBN <= kTmemScale && kShared <= 64, "does not fit");
@@ -101,6 +108,21 @@ __device__ __forceinline__ void scales_to_tmem_pair(uint32_t tmem, uint32_t smem
     asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(make_smem_desc(smem, 16, 128, kSwizzleNone)) : "memory");
 }
 
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+// The matrices of a slab epilogue: up to two read, two written (the second may be the mirror image of the first).
+struct SlabMaps {
+    CUtensorMap in[2], out[2];
+};
+struct NoMaps {};
+
 struct Params {
     int M, N, K, batch;
     int tiles_m, tiles_n;                    // of one matrix
@@ -132,11 +154,11 @@ __device__ __forceinline__ Tile tile_at(const Params& p, int64_t w, int bn) {
 template <class S, class Epilogue>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Params p,
-            const __grid_constant__ Epilogue epi) {
+            const __grid_constant__ typename Epilogue::Maps maps, const __grid_constant__ Epilogue epi) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
-    constexpr int kScaleBase = S::kStages * S::kStageBytes, kBars = kScaleBase + S::kGroups * S::kGroupBytes;
+    constexpr int kSlabs = S::kStages * S::kStageBytes, kScaleBase = kSlabs + S::kSlabBase, kBars = kScaleBase + S::kGroups * S::kGroupBytes;
     const uint32_t bar_base = smem_base + kBars;
     const auto full_bar = [&](int s) { return bar_base + 8u * s; };                // used in the leader only
     const auto empty_bar = [&](int s) { return bar_base + 8u * (S::kStages + s); };
@@ -144,7 +166,9 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     const auto free_bar = [&](int b) { return bar_base + 8u * (2 * S::kStages + 2 + b); };     // accumulator drained (leader only)
     const auto scale_full_bar = [&](int s) { return bar_base + 8u * (2 * S::kStages + 4 + s); };                 // leader only
     const auto scale_empty_bar = [&](int s) { return bar_base + 8u * (2 * S::kStages + 4 + S::kGroups + s); };
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + kBars + 8 * (2 * S::kStages + 4 + 2 * S::kGroups));
+    const auto slab_in_bar = [&](int b) { return bar_base + 8u * (2 * S::kStages + 4 + 2 * S::kGroups + b); };       // free, and its matrices read
+    const auto slab_out_bar = [&](int b) { return bar_base + 8u * (2 * S::kStages + 4 + 2 * S::kGroups + kSlabBufs + b); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + kBars + 8 * (2 * S::kStages + 4 + 2 * S::kGroups + 2 * kSlabBufs));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -164,6 +188,10 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         for (int s = 0; s < S::kGroups; ++s) {
             mbar_init(scale_full_bar(s), 2);                 // both blocks' scales
             mbar_init(scale_empty_bar(s), 1);
+        }
+        for (int b = 0; b < kSlabBufs; ++b) {
+            mbar_init(slab_in_bar(b), 1);
+            mbar_init(slab_out_bar(b), kEpiWarps);
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -291,7 +319,113 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 if (++slot == S::kGroups) { slot = 0; parity ^= 1u; }
             }
         }
-    } else if (warp >= 4) {
+    } else if (Epilogue::kSlabs && warp == 3) {
+        // ------------------------------------------------------------ slabs of the epilogue (both blocks, own rows)
+        if constexpr (Epilogue::kSlabs) {
+            if (lane == 0) {
+                constexpr int kPer = S::kBN / 64;                // slabs of a tile
+                // reads run two slabs ahead of writes; a buffer is free when the write before the last has been taken from it
+                int64_t w_in = first, w_out = first;
+                int at_in = 0, at_out = 0, buf_in = 0, buf_out = 0;
+                uint32_t parity = 0u;
+                const auto read = [&] {
+                    if (w_in >= p.n_work) return;
+                    if (Epilogue::kIn > 0) {
+                        const Tile t = tile_at(p, w_in, S::kBN);
+                        const uint32_t to = smem_base + kSlabs + buf_in * 2 * kSlabBytes;
+                        mbar_expect_tx(slab_in_bar(buf_in), Epilogue::kIn * kSlabBytes);
+                        tma_load_3d(to, &maps.in[0], t.n + 64 * at_in, t.m + (int)rank * kRowsA, t.z, slab_in_bar(buf_in));
+                        if (Epilogue::kIn > 1)
+                            tma_load_3d(to + kSlabBytes, &maps.in[1], t.n + 64 * at_in, t.m + (int)rank * kRowsA, t.z, slab_in_bar(buf_in));
+                    } else {
+                        mbar_arrive(slab_in_bar(buf_in));
+                    }
+                    if (++buf_in == kSlabBufs) buf_in = 0;
+                    if (++at_in == kPer) { at_in = 0; w_in += n_pairs; }
+                };
+                read();
+                read();
+                while (w_out < p.n_work) {
+                    if (!mbar_wait(slab_out_bar(buf_out), parity, abort_flag)) break;
+                    const Tile t = tile_at(p, w_out, S::kBN);
+                    const int m = t.m + (int)rank * kRowsA, n = t.n + 64 * at_out;
+                    const uint32_t from = smem_base + kSlabs + buf_out * 2 * kSlabBytes;
+                    if (m < p.M && n < p.N) {
+                        tma_store_3d(&maps.out[0], n, m, t.z, from);
+                        if (Epilogue::kMirror) {
+                            if (t.m != t.n) tma_store_3d(&maps.out[1], m, n, t.z, from + kSlabBytes);
+                        } else if (epi.two_out()) {
+                            tma_store_3d(&maps.out[1], n, m, t.z, from + kSlabBytes);
+                        }
+                    }
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    read();
+                    if (++buf_out == kSlabBufs) { buf_out = 0; parity ^= 1u; }
+                    if (++at_out == kPer) { at_out = 0; w_out += n_pairs; }
+                }
+                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+            }
+        }
+    } else if (Epilogue::kSlabs && warp >= 4) {
+        // ------------------------------------------------------------ epilogue in slabs: a warp 32 rows and 32 of the 64 columns
+        if constexpr (Epilogue::kSlabs) {
+            const int q = warp & 3, half = (warp - 4) >> 2, row = 32 * q + lane;
+            const uint32_t rows_at = (uint32_t)(32 * q) << 16;
+            const uint32_t leader_free[2] = {map_to_cta(free_bar(0), 0), map_to_cta(free_bar(1), 0)};
+            uint32_t done = 0, parity = 0u;
+            int buf = 0;
+            bool ok = true;
+            for (int64_t w = first; w < p.n_work && ok; w += n_pairs, ++done) {
+                const Tile t = tile_at(p, w, S::kBN);
+                const auto values = epi.values(t.z);
+                const int par = done & 1;
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(par), (done >> 1) & 1u, abort_flag))) break;
+                tc_fence_after();
+                const uint32_t acc = tmem_base + rows_at + (par ? S::kAcc1 : 0) + 32 * half;
+                for (int c = 0; c < S::kBN / 64; ++c) {
+                    uint32_t v[32];
+                    tmem_ld_32x32b_x32(acc + 64 * c, v);
+                    if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(slab_in_bar(buf), parity, abort_flag)))) break;
+                    uint8_t* slab = smem_gen + kSlabs + buf * 2 * kSlabBytes;
+                    uint4 x[2][4];
+                    const auto piece = [&](int i) { return reinterpret_cast<uint4*>(slab + row * 128 + (((4 * half + i) ^ (row & 7)) << 4)); };
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (Epilogue::kIn > 0) x[0][i] = *piece(i);
+                        if (Epilogue::kIn > 1) x[1][i] = *(piece(i) + kSlabBytes / 16);
+                    }
+                    tmem_ld_wait();
+                    if (c == S::kBN / 64 - 1) {                  // the accumulator is in registers: it may be overwritten
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0)
+                            asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_free[par]) : "memory");
+                    }
+                    epi.compute(values, v, x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        *piece(i) = x[0][i];
+                        if (!Epilogue::kMirror) *(piece(i) + kSlabBytes / 16) = x[1][i];
+                    }
+                    if (Epilogue::kMirror && t.m != t.n) {       // [64 columns][128 rows]
+                        unsigned short* to = reinterpret_cast<unsigned short*>(slab + kSlabBytes) + 32 * half * kRowsA + row;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t word[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w};
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) to[(8 * i + j) * kRowsA] = (unsigned short)(word[j >> 1] >> (16 * (j & 1)));
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(slab_out_bar(buf));
+                    if (++buf == kSlabBufs) { buf = 0; parity ^= 1u; }
+                }
+            }
+        }
+    } else if (!Epilogue::kSlabs && warp >= 4) {
+        if constexpr (!Epilogue::kSlabs) {
         // ------------------------------------------------------------ epilogue (both blocks, own rows)
         const int q = warp & 3, half = (warp - 4) >> 2;          // a quarter of the lanes, half of the columns
         const uint32_t rows_at = (uint32_t)(32 * q) << 16;
@@ -321,7 +455,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 tmem_ld_wait();
                 if (shares) arrive(0);
 #pragma unroll
-                for (int c = 0; c < kFirst; ++c) epi.store(p, t.z, row, t.m, t.n, t.n + chunk_at(c), v[c]);
+                for (int c = 0; c < kFirst; ++c) epi.store(p, row, t.n + chunk_at(c), v[c]);
             }
             {
                 uint32_t v[kFirst][32];
@@ -330,8 +464,9 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 tmem_ld_wait();
                 if (!S::kOverlap) arrive(par);
 #pragma unroll
-                for (int c = 0; c < kFirst; ++c) epi.store(p, t.z, row, t.m, t.n, t.n + chunk_at(kFirst + c), v[c]);
+                for (int c = 0; c < kFirst; ++c) epi.store(p, row, t.n + chunk_at(kFirst + c), v[c]);
             }
+        }
         }
     }
 
@@ -341,6 +476,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         // copies that may still be in flight get a bounded chance to land before the pair exits
         for (int s = 0; s < S::kStages; ++s)
             for (uint32_t spin = 0; spin < 4096 && !mbar_try_wait(full_bar(s), 0) && !mbar_try_wait(full_bar(s), 1); ++spin) __nanosleep(64);
+        for (int b = 0; b < (Epilogue::kSlabs ? kSlabBufs : 0); ++b)
+            for (uint32_t spin = 0; spin < 4096 && !mbar_try_wait(slab_in_bar(b), 0) && !mbar_try_wait(slab_in_bar(b), 1); ++spin) __nanosleep(64);
         if (p.dev_status) *p.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
     }
     cluster_sync();                          // neither block leaves while the other may still touch it
@@ -369,6 +506,12 @@ struct Operand {
     int64_t pitch, matrix;                   // bytes from row to row, from matrix to matrix (multiples of 16)
 };
 
+// A slab's map of binary16 matrices [rows x cols]; the mirror image of a slab is 128 columns of 64 rows, as it lies.
+inline bool make_slab_map(CUtensorMap* map, const Operand& x, int64_t rows, int64_t cols, int64_t batch, bool mirror) {
+    return make_map_3d(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x.base, cols, rows, batch, x.pitch, x.matrix, mirror ? kRowsA : 64, mirror ? 64 : kRowsA,
+                       mirror ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
 template <class S, class Epilogue>
 struct PairSetup {
     PerDeviceOnce once;
@@ -377,7 +520,7 @@ struct PairSetup {
 
 // Launches the pair kernel for p (M, N, K, batch, scales and symmetric set; the rest is filled in here).
 template <class S, class Epilogue>
-cudaError_t launch_pair(Params p, const Operand& a, const Operand& b, const Epilogue& epi, cudaStream_t stream) {
+cudaError_t launch_pair(Params p, const Operand& a, const Operand& b, const typename Epilogue::Maps& maps, const Epilogue& epi, cudaStream_t stream) {
     static PairSetup<S, Epilogue> st;
     cudaError_t e = once_per_device(st.once, [](int dev) {
         const cudaError_t err = cudaFuncSetAttribute(pair_kernel<S, Epilogue>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
@@ -406,7 +549,7 @@ cudaError_t launch_pair(Params p, const Operand& a, const Operand& b, const Epil
         return cudaErrorInvalidValue;
     int64_t pairs = st.max_pairs[dev] > 0 ? st.max_pairs[dev] : 1;
     if (pairs > p.n_work) pairs = p.n_work;
-    return launch_dependent(&pair_kernel<S, Epilogue>, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), S::kSmem, stream, map_a, map_b, p, epi);
+    return launch_dependent(&pair_kernel<S, Epilogue>, dim3((unsigned)(2 * pairs)), dim3(kPairThreads), S::kSmem, stream, map_a, map_b, p, maps, epi);
 }
 
 }  // namespace dense

@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const __grid_constant_
                 take(row, col, x);
             }
             const int64_t at = (int64_t)row * q.ld_param + col;
-            uint32_t random[8];
+            uint32_t random[4];
             bool rounds = false;
             if (t.momentum) {
                 float p[8];
@@ -277,15 +277,17 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const __grid_constant_
                     const uint64_t first = (uint64_t)t.first_block * 256u + (uint64_t)at;
                     const int shift = (int)(first & 7u);
                     const uint4 a = philox4x32_10(first >> 3, q.keys, 2u);
-                    const uint4 b = shift ? philox4x32_10((first >> 3) + 1u, q.keys, 2u) : a;
-                    const uint32_t words[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    random[0] = a.x; random[1] = a.y; random[2] = a.z; random[3] = a.w;
+                    if (shift) {
+                        const uint4 b = philox4x32_10((first >> 3) + 1u, q.keys, 2u);
+                        const uint32_t words[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        uint32_t v = 0u;
+                        for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                        for (int s = 0; s < 8; ++s)
-                            if (s == shift) v = words[(i + s) >> 1] >> (16 * ((i + s) & 1));
-                        random[i] = v & 0xFFFFu;
+                            for (int s = 1; s < 8; ++s)
+                                if (s == shift)
+                                    random[i] = s & 1 ? words[i + s / 2] >> 16 | words[i + s / 2 + 1] << 16 : words[i + s / 2];
+                        }
                     }
                 }
             }
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const __grid_constant_
                         // (a NaN whose lower half is zero: random bits do not carry into its sign)
                         const float lo = x[2 * i] == x[2 * i] ? x[2 * i] : __uint_as_float(0x7FC00000u);
                         const float hi2 = x[2 * i + 1] == x[2 * i + 1] ? x[2 * i + 1] : __uint_as_float(0x7FC00000u);
-                        o[i] = pack_out<true>(lo, hi2, random[2 * i] | random[2 * i + 1] << 16);
+                        o[i] = pack_out<true>(lo, hi2, random[i]);
                     } else {
                         o[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
                     }
@@ -316,92 +318,68 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-// 32 halves of a row whose pitch is a multiple of eight; columns beyond `left` are the pitch's own or not touched
-__device__ __forceinline__ void load_row(const __half* from, int left, uint32_t (&w)[16]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint4 v = 8 * i < left ? *reinterpret_cast<const uint4*>(from + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
-        w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
-    }
-}
-__device__ __forceinline__ void store_row(__half* to, int left, const uint32_t (&w)[16]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (8 * i < left) *reinterpret_cast<uint4*>(to + 8 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-}
-
 // A S = acc S / xs^2 (kPoly false), B S = b (A S) + c acc / S (true); symmetric, the tile's mirror image is stored too.
 template <bool kPoly>
-struct StoreSymmetric {
-    const __half* A;
-    __half* out;
-    int64_t pitch;
+struct Symmetric {
+    using Maps = dense::SlabMaps;
+    static constexpr bool kSlabs = true, kMirror = true;
+    static constexpr int kIn = kPoly ? 1 : 0;
     const float* xs;
     float S;
-    __device__ __forceinline__ void store(const dense::Params& p, int z, int row, int m0, int n0, int col, const uint32_t (&v)[32]) const {
-        const int left = p.N - col;
-        const bool there = row < p.M && left > 0;
-        const int64_t matrix = (int64_t)z * p.M * pitch;
-        float alpha;
-        uint32_t w[16];
-        if (kPoly) {
-            alpha = kC / S;
-            if (there) load_row(A + matrix + (int64_t)row * pitch + col, left, w);
-        } else {
-            const float x = xs[z];
-            alpha = S / x / x;
-        }
-        if (!there) return;
+    __device__ __forceinline__ bool two_out() const { return true; }
+    __device__ __forceinline__ float values(int z) const { return kPoly ? kC / S : S / xs[z] / xs[z]; }
+    __device__ __forceinline__ void compute(float alpha, const uint32_t (&v)[32], uint4 (&x)[2][4]) const {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float lo = __uint_as_float(v[2 * i]) * alpha, hi = __uint_as_float(v[2 * i + 1]) * alpha;
-            if (kPoly) {
-                const float2 a = halves(w[i]);
-                lo = fmaf(kB, a.x, lo);
-                hi = fmaf(kB, a.y, hi);
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float lo = __uint_as_float(v[8 * i + 2 * j]) * alpha, hi = __uint_as_float(v[8 * i + 2 * j + 1]) * alpha;
+                if (kPoly) {
+                    const float2 a = halves(w[j]);
+                    lo = fmaf(kB, a.x, lo);
+                    hi = fmaf(kB, a.y, hi);
+                }
+                w[j] = half_pair(lo, hi);
             }
-            w[i] = half_pair(lo, hi);
-        }
-        store_row(out + matrix + (int64_t)row * pitch + col, left, w);
-        if (m0 != n0) {
-            __half* to = out + matrix + (int64_t)col * pitch + row;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) reinterpret_cast<unsigned short*>(to)[i * pitch] = (unsigned short)(w[i >> 1] >> (16 * (i & 1)));
+            x[0][i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
 };
 
-// X' xs = a (X xs) + acc / S.  lo (the same place in both) is read and written where asked for.
-struct StoreApply {
-    const __half* hi;
-    __half* lo;
-    __half* out;
-    int64_t pitch;
+// X' xs = a (X xs) + acc / S, with (kLo) or without the second half of X.
+template <bool kWithLo>
+struct Apply {
+    using Maps = dense::SlabMaps;
+    static constexpr bool kSlabs = true, kMirror = false;
+    static constexpr int kIn = kWithLo ? 2 : 1;
     float inv_S;
-    int read_lo, write_lo;
-    __device__ __forceinline__ void store(const dense::Params& p, int z, int row, int, int, int col, const uint32_t (&v)[32]) const {
-        const int left = p.N - col;
-        if (row >= p.M || left <= 0) return;
-        const int64_t at = ((int64_t)z * p.M + row) * pitch + col;
-        uint32_t h[16], l[16];
-        load_row(hi + at, left, h);
-        if (read_lo) load_row(lo + at, left, l);
+    int write_lo;
+    __device__ __forceinline__ bool two_out() const { return kWithLo && write_lo; }
+    __device__ __forceinline__ float values(int) const { return inv_S; }
+    __device__ __forceinline__ void compute(float scale, const uint32_t (&v)[32], uint4 (&x)[2][4]) const {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float2 x = halves(h[i]);
-            if (read_lo) {
-                const float2 y = halves(l[i]);
-                x.x = fmaf(y.x, 1.0f / kLo, x.x);
-                x.y = fmaf(y.y, 1.0f / kLo, x.y);
+        for (int i = 0; i < 4; ++i) {
+            uint32_t h[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w}, l[4] = {};
+            if (kWithLo) { l[0] = x[1][i].x; l[1] = x[1][i].y; l[2] = x[1][i].z; l[3] = x[1][i].w; }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float2 f = halves(h[j]);
+                if (kWithLo) {
+                    const float2 y = halves(l[j]);
+                    f.x = fmaf(y.x, 1.0f / kLo, f.x);
+                    f.y = fmaf(y.y, 1.0f / kLo, f.y);
+                }
+                const float a = fmaf(kA, f.x, __uint_as_float(v[8 * i + 2 * j]) * scale), b = fmaf(kA, f.y, __uint_as_float(v[8 * i + 2 * j + 1]) * scale);
+                h[j] = half_pair(a, b);
+                if (kWithLo) {
+                    const float2 r = halves(h[j]);
+                    l[j] = half_pair((a - r.x) * kLo, (b - r.y) * kLo);
+                }
             }
-            const float a = fmaf(kA, x.x, __uint_as_float(v[2 * i]) * inv_S), b = fmaf(kA, x.y, __uint_as_float(v[2 * i + 1]) * inv_S);
-            h[i] = half_pair(a, b);
-            const float2 r = halves(h[i]);
-            l[i] = half_pair((a - r.x) * kLo, (b - r.y) * kLo);
+            x[0][i] = make_uint4(h[0], h[1], h[2], h[3]);
+            x[1][i] = make_uint4(l[0], l[1], l[2], l[3]);
         }
-        store_row(out + at, left, h);
-        if (write_lo) store_row(lo + at, left, l);
     }
 };
 
@@ -439,25 +417,35 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
     const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 8 * sm_count / q.count));
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
-    using KMajor = dense::Shape<false, false, 256>;
-    using NMajor = dense::Shape<false, true, 256>;
+    using KMajor = dense::Shape<false, false, 256, 4, true>;
+    using NMajor = dense::Shape<false, true, 256, 4, true>;
+    const dense::Operand oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2}, olo = {q.lo, q.n_pitch * 2, m * q.n_pitch * 2};
     for (int k = 0; k < steps && e == cudaSuccess; ++k) {
-        __half *x = X[k & 1], *y = X[(k + 1) & 1];
-        const dense::Operand ox = {x, q.n_pitch * 2, m * q.n_pitch * 2}, oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2};
+        const dense::Operand ox = {X[k & 1], q.n_pitch * 2, m * q.n_pitch * 2}, oy = {X[(k + 1) & 1], ox.pitch, ox.matrix};
+        const bool read_lo = k < steps - 2, write_lo = k + 1 < steps - 2;
+        dense::SlabMaps gram, poly, apply;
+        if (!dense::make_slab_map(&gram.out[0], oa, m, m, q.count, false) || !dense::make_slab_map(&gram.out[1], oa, m, m, q.count, true) ||
+            !dense::make_slab_map(&poly.out[0], ob, m, m, q.count, false) || !dense::make_slab_map(&poly.out[1], ob, m, m, q.count, true) ||
+            !dense::make_slab_map(&apply.in[0], ox, m, n, q.count, false) || !dense::make_slab_map(&apply.out[0], oy, m, n, q.count, false) ||
+            !dense::make_slab_map(&apply.in[1], olo, m, n, q.count, false))
+            return cudaErrorInvalidValue;
+        gram.in[0] = gram.in[1] = poly.in[0] = poly.in[1] = gram.out[0];
+        apply.out[1] = apply.in[1];
         dense::Params p = {};
         p.batch = q.count;
         p.dev_status = dev_status;
         p.M = p.N = (int)m;
         p.K = (int)n;
         p.symmetric = 1;
-        e = dense::launch_pair<KMajor>(p, ox, ox, StoreSymmetric<false>{nullptr, A, mp, q.xs, q.S}, st);
+        e = dense::launch_pair<KMajor>(p, ox, ox, gram, Symmetric<false>{q.xs, q.S}, st);
         p.K = (int)m;
-        if (e == cudaSuccess) e = dense::launch_pair<KMajor>(p, oa, oa, StoreSymmetric<true>{A, B, mp, q.xs, q.S}, st);
+        if (e == cudaSuccess) e = dense::launch_pair<KMajor>(p, oa, oa, poly, Symmetric<true>{q.xs, q.S}, st);
         p.symmetric = 0;
         p.N = (int)n;
         if (e == cudaSuccess)
-            e = dense::launch_pair<NMajor>(p, ob, ox, StoreApply{x, q.lo, y, q.n_pitch, 1.0f / q.S, k < steps - 2, k + 1 < steps - 2}, st);
-        q.hi = y;
+            e = read_lo ? dense::launch_pair<NMajor>(p, ob, ox, apply, Apply<true>{1.0f / q.S, write_lo}, st)
+                        : dense::launch_pair<NMajor>(p, ob, ox, apply, Apply<false>{1.0f / q.S, 0}, st);
+        q.hi = X[(k + 1) & 1];
     }
     if (e == cudaSuccess) e = launch_dependent(&finish_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     return e;

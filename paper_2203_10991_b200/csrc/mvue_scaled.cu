@@ -16,7 +16,10 @@ struct Store {
     void* C;
     int64_t ldc;
     int vec;                                 // bytes that one access may take: 32, 16, or an element
-    __device__ __forceinline__ void store(const dense::Params& p, int, int row, int, int, int col, const uint32_t (&v)[32]) const {
+    using Maps = dense::NoMaps;
+    static constexpr bool kSlabs = false, kMirror = false;
+    static constexpr int kIn = 0;
+    __device__ __forceinline__ void store(const dense::Params& p, int row, int col, const uint32_t (&v)[32]) const {
         if (row >= p.M || col >= p.N) return;
         const int left = p.N - col;
         if constexpr (kBf16) {
@@ -54,8 +57,8 @@ struct Store {
 
 template <bool kBf16>
 cudaError_t launch(const dense::Params& p, const dense::Operand& a, const dense::Operand& b, bool n_major, const Store<kBf16>& out, cudaStream_t stream) {
-    if (n_major) return dense::launch_pair<dense::Shape<true, true, 256>>(p, a, b, out, stream);
-    return dense::launch_pair<dense::Shape<true, false, 256>>(p, a, b, out, stream);
+    if (n_major) return dense::launch_pair<dense::Shape<true, true, 256, 6>>(p, a, b, {}, out, stream);
+    return dense::launch_pair<dense::Shape<true, false, 256, 6>>(p, a, b, {}, out, stream);
 }
 
 int scaled_gemm(const void* a, int64_t M, int64_t K, int64_t lda, const void* a_scales, const void* w, int64_t N, int64_t ldw,
