@@ -12,6 +12,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/mvue_layer.h"
 #include "mvue_device.cuh"
@@ -21,7 +22,7 @@
 namespace mvue {
 namespace {
 
-constexpr int kMaxTeam = 1024;                   // threads; eight columns each
+constexpr int kMaxTeam = 512;                    // threads; eight columns each in the kernels for any alignment
 constexpr int kWideThreads = 1024;
 constexpr int kColumnRows = 8;                   // wide: teams of a warp in a column block
 
@@ -53,44 +54,388 @@ __device__ __forceinline__ void team_barrier(int team, int threads) {
     else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory");
 }
 
-// Sums of four values over a team.  Within a warp the lanes fold: after two exchanges a lane holds one of the four values for
-// its four neighbours, and three more add up.  `sums`: the team's slots, four for each of its warps; not used again before another
-// barrier of the team.
-__device__ __forceinline__ void team_sum4(float (&v)[4], float (*sums)[4], int team, int threads, int warp, int lane) {
-    const bool b0 = lane & 1, b1 = lane & 2;
-    float p = (b0 ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? v[0] : v[2], 1);
-    float q = (b0 ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? v[1] : v[3], 1);
-    float t = (b1 ? q : p) + __shfl_xor_sync(0xFFFFFFFFu, b1 ? p : q, 2);           // value 2 (lane & 1) + (lane >> 1 & 1)
+// Sums of kN (1, 2 or 4) values over a team.  Within a warp the lanes fold: each exchange leaves a lane with half of the values, and
+// the last ones are added up (four values: six shuffles instead of twenty).  `sums`: the team's slots, four for each of its warps; not
+// used again before another barrier of the team.
+template <int kN>
+__device__ __forceinline__ void team_sum(float (&v)[kN], float (*sums)[4], int team, int threads, int warp, int lane) {
+    float t;
+    if constexpr (kN == 4) {
+        const bool b0 = lane & 1, b1 = lane & 2;
+        const float p = (b0 ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? v[0] : v[2], 1);
+        const float q = (b0 ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? v[1] : v[3], 1);
+        t = (b1 ? q : p) + __shfl_xor_sync(0xFFFFFFFFu, b1 ? p : q, 2);             // value 2 (lane & 1) + (lane >> 1 & 1)
+    } else if constexpr (kN == 2) {
+        t = (lane & 1 ? v[1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, lane & 1 ? v[0] : v[1], 1);
+    } else {
+        t = v[0];
+    }
 #pragma unroll
-    for (int d = 4; d < 32; d <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
+    for (int d = kN; d < 32; d <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
     if (threads > 32) {
-        if (lane < 4) sums[warp][lane] = t;
+        if (lane < kN) sums[warp][lane] = t;
         team_barrier(team, threads);
         t = 0.0f;
-        for (int w = lane >> 2; w < (threads >> 5); w += 8) t += sums[w][lane & 3];
+        for (int w = lane / kN; w < (threads >> 5); w += 32 / kN) t += sums[w][lane % kN];
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
+        for (int d = kN; d < 32; d <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, d);
     }
-    v[0] = __shfl_sync(0xFFFFFFFFu, t, 0);
-    v[1] = __shfl_sync(0xFFFFFFFFu, t, 2);
-    v[2] = __shfl_sync(0xFFFFFFFFu, t, 1);
-    v[3] = __shfl_sync(0xFFFFFFFFu, t, 3);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, t, kN == 4 ? (i >> 1) | (i & 1) << 1 : i);
 }
-__device__ __forceinline__ void team_sum1(float& v, float (*sums)[4], int team, int threads, int warp, int lane) {
+
+// Eight neighbours as they lie in memory.
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    }
+    __device__ __forceinline__ f2 two(int i) const { return pair(bf16_lo(w[i]), bf16_hi(w[i])); }          // elements 2i, 2i + 1
+};
+template <> struct Raw<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const float* p) { ld256(p, w); }
+    __device__ __forceinline__ f2 two(int i) const { return pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])); }
+};
+__device__ __forceinline__ void floats_of(const f2 (&p)[4], float (&x)[8]) {
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    for (int i = 0; i < 4; ++i) unpair(p[i], x[2 * i], x[2 * i + 1]);
+}
+__device__ __forceinline__ void store_eight(float* to, const f2 (&p)[4]) {
+    float x[8];
+    floats_of(p, x);
+    store8(to, true, 8, x);
+}
+__device__ __forceinline__ void store_eight(__nv_bfloat16* to, const f2 (&p)[4]) {
+    float x[8];
+    floats_of(p, x);
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+__device__ __forceinline__ float both(f2 a) {
+    float lo, hi;
+    unpair(a, lo, hi);
+    return lo + hi;
+}
+// Weight or bias in shared memory as binary32, in the order in which a team's threads read it without conflicts: the piece of eight columns
+// with number i lies as two quarters of 16 bytes, `pieces` such quarters apart.
+__device__ __forceinline__ void stage_quarters(float* to, const void* from, int bf16, float none, int cols) {
+    const int pieces = cols >> 3;
+    for (int i = threadIdx.y * blockDim.x + threadIdx.x; i < cols; i += blockDim.x * blockDim.y)
+        to[((i >> 2 & 1) * pieces + (i >> 3)) * 4 + (i & 3)] =
+            !from ? none : bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(from)[i]) : static_cast<const float*>(from)[i];
+}
+__device__ __forceinline__ void quarters_of(const float* from, int piece, int pieces, f2 (&x)[4]) {
+    const float4 a = reinterpret_cast<const float4*>(from)[piece], b = reinterpret_cast<const float4*>(from)[pieces + piece];
+    x[0] = pair(a.x, a.y);
+    x[1] = pair(a.z, a.w);
+    x[2] = pair(b.x, b.y);
+    x[3] = pair(b.z, b.w);
+}
+
+// Means and sums of squares about them of kR rows over a team whose threads have `count` elements of each.  Equal counts n join as
+// m = (m_a + m_b) / 2, M2 = M2_a + M2_b + (m_b - m_a)^2 n / 2; in a warp the lanes fold as in team_sum.
+template <int kR>
+__device__ __forceinline__ void team_moments(float (&mean)[kR], float (&m2)[kR], float2 (*slots)[kR], int team, int threads, int warp, int lane, float count) {
+    const auto join = [](float& m, float& q, float om, float oq, float half_n) {
+        const float delta = om - m;
+        q = fmaf(delta * delta, half_n, q + oq);
+        m = fmaf(0.5f, delta, m);
+    };
+    float m = mean[0], q = m2[0], half_n = 0.5f * count;
+    int d = 1;
+    if constexpr (kR == 4) {
+        const bool up = lane & 1;
+        float ma = up ? mean[2] : mean[0], qa = up ? m2[2] : m2[0], mb = up ? mean[3] : mean[1], qb = up ? m2[3] : m2[1];
+        join(ma, qa, __shfl_xor_sync(0xFFFFFFFFu, up ? mean[0] : mean[2], 1), __shfl_xor_sync(0xFFFFFFFFu, up ? m2[0] : m2[2], 1), half_n);
+        join(mb, qb, __shfl_xor_sync(0xFFFFFFFFu, up ? mean[1] : mean[3], 1), __shfl_xor_sync(0xFFFFFFFFu, up ? m2[1] : m2[3], 1), half_n);
+        half_n *= 2.0f;
+        const bool up2 = lane & 2;
+        m = up2 ? mb : ma;
+        q = up2 ? qb : qa;
+        join(m, q, __shfl_xor_sync(0xFFFFFFFFu, up2 ? ma : mb, 2), __shfl_xor_sync(0xFFFFFFFFu, up2 ? qa : qb, 2), half_n);
+        half_n *= 2.0f;
+        d = 4;
+    } else if constexpr (kR == 2) {
+        const bool up = lane & 1;
+        m = up ? mean[1] : mean[0];
+        q = up ? m2[1] : m2[0];
+        join(m, q, __shfl_xor_sync(0xFFFFFFFFu, up ? mean[0] : mean[1], 1), __shfl_xor_sync(0xFFFFFFFFu, up ? m2[0] : m2[1], 1), half_n);
+        half_n *= 2.0f;
+        d = 2;
+    }
+#pragma unroll
+    for (; d < 32; d <<= 1) {
+        join(m, q, __shfl_xor_sync(0xFFFFFFFFu, m, d), __shfl_xor_sync(0xFFFFFFFFu, q, d), half_n);
+        half_n *= 2.0f;
+    }
     if (threads > 32) {
-        if (lane == 0) sums[warp][0] = v;
+        const int warps = threads >> 5;
+        if (lane < kR) slots[warp][lane] = make_float2(m, q);
         team_barrier(team, threads);
-        v = lane < (threads >> 5) ? sums[lane][0] : 0.0f;
+        // lane r + kR w holds row r of warp w (several where there are more warps than that)
+        float2 own[kR];
+        float total = 0.0f;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+        for (int i = 0; i < kR; ++i) {
+            const int w = lane / kR + i * (32 / kR);
+            own[i] = w < warps ? slots[w][lane % kR] : make_float2(0.0f, 0.0f);
+            total += own[i].x;
+        }
+#pragma unroll
+        for (int e = kR; e < 32; e <<= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, e);
+        m = total / (float)warps;
+        q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kR; ++i)
+            if (lane / kR + i * (32 / kR) < warps) q += fmaf((own[i].x - m) * (own[i].x - m), 32.0f * count, own[i].y);
+#pragma unroll
+        for (int e = kR; e < 32; e <<= 1) q += __shfl_xor_sync(0xFFFFFFFFu, q, e);
+    }
+#pragma unroll
+    for (int i = 0; i < kR; ++i) {
+        const int from = kR == 4 ? (i >> 1) | (i & 1) << 1 : i;
+        mean[i] = __shfl_sync(0xFFFFFFFFu, m, from);
+        m2[i] = __shfl_sync(0xFFFFFFFFu, q, from);
+    }
+}
+
+// Many rows that the team's threads cover exactly, kC pieces of eight columns each: a thread holds its pieces of kR rows while the next
+// rows' are on their way; weight and bias wait in shared memory and are read once for the kR rows.  One barrier for the kR rows: each thread
+// takes mean and squares about it of its own elements.
+// 16384 x 4096 bf16: a row at a time, with the weight's pieces in their own order (bank conflicts), took 71 us.
+constexpr int kEightThreads = 512;
+template <typename T, int kC, int kR, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 1) forward8_kernel(const __grid_constant__ Params p) {
+    __shared__ float2 slots[2][kThreads / 32][kR];
+    extern __shared__ float affine[];
+    const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cols = (int)p.cols, pieces = cols >> 3, step = threads * 8;
+    const int64_t first = ((int64_t)blockIdx.x * blockDim.y + team) * kR, stride = (int64_t)gridDim.x * blockDim.y * kR;
+    const T* from = static_cast<const T*>(p.x) + first * p.ldx + threadIdx.x * 8;
+    T* to = static_cast<T*>(p.y) + first * p.ldy + threadIdx.x * 8;
+    Raw<T> next[kR][kC];
+    const auto fetch = [&](int64_t row) {                    // (rows beyond the last: the last, which nobody stores)
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            const T* at = from + (row + r < p.rows ? r : p.rows - 1 - row) * p.ldx;
+#pragma unroll
+            for (int c = 0; c < kC; ++c) next[r][c].load(at + c * step);
+        }
+    };
+    grid_dependency_wait();
+    if (first < p.rows) fetch(first);
+    stage_quarters(affine, p.gamma, p.affine_bf16, 1.0f, cols);
+    stage_quarters(affine + cols, p.beta, p.affine_bf16, 0.0f, cols);
+    __syncthreads();
+    int turn = 0;
+    for (int64_t row = first; row < p.rows; row += stride, turn ^= 1) {
+        f2 v[kR][kC][4];
+        float own[kR], mean[kR], m2[kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            f2 sum = pair(0.0f);
+#pragma unroll
+            for (int c = 0; c < kC; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[r][c][j] = next[r][c].two(j);
+                    sum = add2(sum, v[r][c][j]);
+                }
+            own[r] = both(sum) * (1.0f / (8 * kC));
+        }
+        from += stride * p.ldx;
+        if (row + stride < p.rows) fetch(row + stride);
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            f2 sum = pair(0.0f);
+#pragma unroll
+            for (int c = 0; c < kC; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[r][c][j] = add2(v[r][c][j], pair(-own[r]));
+                    sum = fma2(v[r][c][j], v[r][c][j], sum);
+                }
+            mean[r] = own[r];
+            m2[r] = both(sum);
+        }
+        team_moments<kR>(mean, m2, slots[turn] + team * (threads >> 5), team, threads, warp, lane, (float)(8 * kC));
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            m2[r] = rsqrtf(fmaf(m2[r], p.inv_cols, p.eps));
+            if (threadIdx.x == 0 && row + r < p.rows) {
+                if (p.mean) p.mean[row + r] = mean[r];
+                if (p.rstd) p.rstd[row + r] = m2[r];
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            f2 gamma[4], beta[4], o[4];
+            quarters_of(affine, threadIdx.x + c * threads, pieces, gamma);
+            quarters_of(affine + cols, threadIdx.x + c * threads, pieces, beta);
+#pragma unroll
+            for (int r = 0; r < kR; ++r) {
+                if (row + r >= p.rows) break;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = fma2(mul2(add2(v[r][c][j], pair(own[r] - mean[r])), pair(m2[r])), gamma[j], beta[j]);
+                store_eight(to + r * p.ldy + c * step, o);
+            }
+        }
+        to += stride * p.ldy;
+    }
+}
+
+// The teams of a block add up their column sums in order, each thread its own places, and the block leaves its partial sum.
+template <int kN>
+__device__ __forceinline__ bool join_teams(float (&dgamma)[kN], float (&dbeta)[kN], float* joined, int team, int threads) {
+    if (blockDim.y > 1) {
+        float* at = joined + threadIdx.x;
+        for (int t = 0; t < (int)blockDim.y; ++t) {
+            if (t == team) {
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    at[2 * j * threads] = t == 0 ? dgamma[j] : at[2 * j * threads] + dgamma[j];
+                    at[(2 * j + 1) * threads] = t == 0 ? dbeta[j] : at[(2 * j + 1) * threads] + dbeta[j];
+                }
+            }
+            __syncthreads();
+        }
+        if (team != 0) return false;
+#pragma unroll
+        for (int j = 0; j < kN; ++j) {
+            dgamma[j] = at[2 * j * threads];
+            dbeta[j] = at[(2 * j + 1) * threads];
+        }
+    }
+    return true;
+}
+
+// The same for the backward pass: kR rows, two sums each.  kFull: the team's threads cover a row exactly.
+template <typename T, int kC, int kR, bool kSums, bool kFull>
+__global__ void __launch_bounds__(kEightThreads, 1) backward8_kernel(const __grid_constant__ Params p) {
+    __shared__ float slots[2][32][4];
+    extern __shared__ float affine[];                        // the weight; at the end the teams' sums
+    const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cols = (int)p.cols, pieces = cols >> 3, c0 = threadIdx.x * 8, step = threads * 8;
+    const T *x = static_cast<const T*>(p.x), *dy = static_cast<const T*>(p.dy);
+    T* dx = static_cast<T*>(p.dx);
+    const int64_t stride = (int64_t)gridDim.x * blockDim.y * kR;
+    int64_t row = ((int64_t)blockIdx.x * blockDim.y + team) * kR;
+    Raw<T> next_x[kR][kC], next_g[kR][kC];
+    float next_mean[kR], next_rstd[kR];
+    f2 dgamma[4 * kC], dbeta[4 * kC];
+#pragma unroll
+    for (int j = 0; j < 4 * kC; ++j) dgamma[j] = dbeta[j] = pair(0.0f);
+    const auto fetch = [&](int64_t from) {
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            const bool there = from + r < p.rows;
+            next_mean[r] = there ? p.mean_in[from + r] : 0.0f;
+            next_rstd[r] = there ? p.rstd_in[from + r] : 0.0f;
+#pragma unroll
+            for (int c = 0; c < kC; ++c)
+                if (there && (kFull || c0 + c * step < cols)) {
+                    next_x[r][c].load(x + (from + r) * p.ldx + c0 + c * step);
+                    next_g[r][c].load(dy + (from + r) * p.lddy + c0 + c * step);
+                } else {
+#pragma unroll
+                    for (uint32_t& w : next_x[r][c].w) w = 0u;
+#pragma unroll
+                    for (uint32_t& w : next_g[r][c].w) w = 0u;
+                }
+        }
+    };
+    grid_dependency_wait();
+    fetch(row);
+    stage_quarters(affine, p.gamma, p.affine_bf16, 1.0f, cols);
+    __syncthreads();
+    int turn = 0;
+    for (; row < p.rows; row += stride, turn ^= 1) {
+        f2 xh[kR][kC][4], w[kR][kC][4];
+        float rstd[kR], s[2 * kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            rstd[r] = next_rstd[r];
+            const f2 minus = pair(-next_mean[r]), scale = pair(rstd[r]);
+#pragma unroll
+            for (int c = 0; c < kC; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    xh[r][c][j] = mul2(add2(next_x[r][c].two(j), minus), scale);
+                    w[r][c][j] = next_g[r][c].two(j);
+                }
+        }
+        fetch(row + stride);
+        f2 s0[kR], s1[kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r) s0[r] = s1[r] = pair(0.0f);
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            if (!kFull && c0 + c * step >= cols) break;
+            f2 gamma[4];
+            quarters_of(affine, threadIdx.x + c * threads, pieces, gamma);
+#pragma unroll
+            for (int r = 0; r < kR; ++r) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (kSums) {
+                        dgamma[4 * c + j] = fma2(w[r][c][j], xh[r][c][j], dgamma[4 * c + j]);
+                        dbeta[4 * c + j] = add2(dbeta[4 * c + j], w[r][c][j]);
+                    }
+                    w[r][c][j] = mul2(w[r][c][j], gamma[j]);
+                    s0[r] = add2(s0[r], w[r][c][j]);
+                    s1[r] = fma2(w[r][c][j], xh[r][c][j], s1[r]);
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kR; ++r) {
+            s[2 * r] = both(s0[r]);
+            s[2 * r + 1] = both(s1[r]);
+        }
+        team_sum<2 * kR>(s, slots[turn] + team * (threads >> 5), team, threads, warp, lane);
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            if (!kFull && c0 + c * step >= cols) break;
+#pragma unroll
+            for (int r = 0; r < kR; ++r) {
+                if (row + r >= p.rows) break;
+                const f2 m0 = pair(-s[2 * r] * p.inv_cols), m1 = pair(-s[2 * r + 1] * p.inv_cols), scale = pair(rstd[r]);
+                f2 o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = mul2(scale, add2(w[r][c][j], fma2(xh[r][c][j], m1, m0)));
+                store_eight(dx + (row + r) * p.ldy + c0 + c * step, o);
+            }
+        }
+    }
+    if constexpr (kSums) {
+        float a[8 * kC], b[8 * kC];
+#pragma unroll
+        for (int j = 0; j < 4 * kC; ++j) {
+            unpair(dgamma[j], a[2 * j], a[2 * j + 1]);
+            unpair(dbeta[j], b[2 * j], b[2 * j + 1]);
+        }
+        __syncthreads();
+        if (!join_teams(a, b, affine, team, threads)) return;
+        float* out = p.partial + (int64_t)blockIdx.x * 2 * p.cols;
+#pragma unroll
+        for (int c = 0; c < kC; ++c) {
+            if (c0 + c * step >= cols) break;
+            float o[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = a[8 * c + j];
+            store8(out + c0 + c * step, true, 8, o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = b[8 * c + j];
+            store8(out + p.cols + c0 + c * step, true, 8, o);
+        }
     }
 }
 
 // Block: blockDim.x threads a team, blockDim.y teams.  kR rows at a time: 4, or 1 where there are few.
 template <typename T, int kVec, int kR>
-__global__ void __launch_bounds__(1024) forward_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kMaxTeam) forward_kernel(const __grid_constant__ Params p) {
     __shared__ float slots[2][32][4];
     grid_dependency_wait();
     const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -115,8 +460,7 @@ __global__ void __launch_bounds__(1024) forward_kernel(const __grid_constant__ P
         }
 #pragma unroll
         for (int r = 0; r < kR; ++r) s[r] = ((v[r][0] + v[r][1]) + (v[r][2] + v[r][3])) + ((v[r][4] + v[r][5]) + (v[r][6] + v[r][7]));
-        if constexpr (kR == 4) team_sum4(s, sums0, team, threads, warp, lane);
-        else team_sum1(s[0], sums0, team, threads, warp, lane);
+        team_sum<kR>(s, sums0, team, threads, warp, lane);
         float mean[kR];
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
@@ -128,8 +472,7 @@ __global__ void __launch_bounds__(1024) forward_kernel(const __grid_constant__ P
                 s[r] = fmaf(v[r][j], v[r][j], s[r]);
             }
         }
-        if constexpr (kR == 4) team_sum4(s, sums1, team, threads, warp, lane);
-        else team_sum1(s[0], sums1, team, threads, warp, lane);
+        team_sum<kR>(s, sums1, team, threads, warp, lane);
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
             if (row + r >= p.rows) break;
@@ -149,7 +492,7 @@ __global__ void __launch_bounds__(1024) forward_kernel(const __grid_constant__ P
 
 // Two rows at a time.  kSums: the column sums are wanted too.
 template <typename T, int kVec, bool kSums>
-__global__ void __launch_bounds__(1024) backward_kernel(const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kMaxTeam) backward_kernel(const __grid_constant__ Params p) {
     __shared__ float slots[2][32][4];
     extern __shared__ float joined[];                       // [2][blockDim.x * 8] where there are several teams
     grid_dependency_wait();
@@ -190,7 +533,7 @@ __global__ void __launch_bounds__(1024) backward_kernel(const __grid_constant__ 
                 s[2 * r + 1] = fmaf(g[r][j], xh[r][j], s[2 * r + 1]);
             }
         }
-        team_sum4(s, slots[turn] + team * (threads >> 5), team, threads, warp, lane);
+        team_sum<4>(s, slots[turn] + team * (threads >> 5), team, threads, warp, lane);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             if (row + r >= p.rows || !mine) break;
@@ -202,26 +545,7 @@ __global__ void __launch_bounds__(1024) backward_kernel(const __grid_constant__ 
     }
     if constexpr (kSums) {
         float* out = p.partial + (int64_t)blockIdx.x * 2 * p.cols;
-        if (blockDim.y > 1) {
-            // the teams add up in order, each thread its own places
-            float* at = joined + threadIdx.x * 8;
-            for (int t = 0; t < (int)blockDim.y; ++t) {
-                if (t == team) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        at[j] = t == 0 ? dgamma[j] : at[j] + dgamma[j];
-                        at[threads * 8 + j] = t == 0 ? dbeta[j] : at[threads * 8 + j] + dbeta[j];
-                    }
-                }
-                __syncthreads();
-            }
-            if (team != 0) return;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                dgamma[j] = at[j];
-                dbeta[j] = at[threads * 8 + j];
-            }
-        }
+        if (!join_teams(dgamma, dbeta, joined, team, threads)) return;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < c.count) {
@@ -400,50 +724,125 @@ __global__ void __launch_bounds__(32 * kColumnRows) wide_column_kernel(const __g
 }
 
 // ---- host ----
+// Which kernel: `eight` where every access is of eight elements (forward: and a row whole pieces of a team) and there are rows enough to
+// fill the device with them; wide where a row does not fit the threads of a block; else the one for any alignment.
 struct Plan {
-    bool wide;
-    int team, teams, blocks;                  // wide: blocks of rows
+    enum Kind { kAny, kEight, kWide } kind;
+    bool full;                                // kEight, backward: the team covers a row exactly
+    int pieces, at_once;                      // kEight: pieces of eight columns per thread; rows at once
+    int team, teams, blocks;                  // kWide: blocks of rows
     int parts;                                // partial sums of the backward pass
-    dim3 columns;                             // wide: grid of the column sums
+    dim3 columns;                             // kWide: grid of the column sums
 };
-Plan plan(int64_t rows, int64_t cols, int rows_at_once, int sm_count) {
+int round_up(int64_t x, int to) { return (int)((x + to - 1) / to * to); }
+
+Plan plan(bool backward, int64_t rows, int64_t cols, int dtype, int vec, int sm_count) {
     Plan q = {};
-    q.wide = cols > 8 * kMaxTeam;
-    if (q.wide) {
+    if (vec == 8 && !backward && cols % 256 == 0 && cols <= 32 * kEightThreads) {
+        // bf16 two rows of two pieces of eight, fp32 two rows of one, where the columns allow it
+        const int64_t eights = cols / 256, most = kEightThreads / 32;
+        const int room = dtype == MVUE_BF16 ? 4 : 2;
+        q.pieces = eights <= most && (room == 2 || eights % 2 != 0) ? 1 : eights <= 2 * most ? 2 : 4;
+        q.at_once = std::max(1, room / q.pieces);
+        q.team = (int)(eights / q.pieces * 32);
+        q.teams = std::max(1, 512 / q.team);
+        const int64_t per_block = (int64_t)q.teams * q.at_once, blocks = (rows + per_block - 1) / per_block;
+        if (eights % q.pieces == 0 && blocks >= sm_count) {
+            q.kind = Plan::kEight;
+            q.blocks = (int)std::min<int64_t>(blocks, (int64_t)sm_count);
+            return q;
+        }
+    }
+    if (vec == 8 && backward && cols <= 16 * kEightThreads) {
+        const int room = dtype == MVUE_BF16 ? 2 : 1;                       // pieces of two tensors that the registers have room for
+        q.pieces = cols > 8 * kEightThreads || (room == 2 && cols > 2048 && cols % 512 == 0) ? 2 : 1;
+        q.at_once = std::max(1, room / q.pieces);
+        q.team = round_up((cols + 8 * q.pieces - 1) / (8 * q.pieces), 32);
+        q.teams = std::max(1, 512 / q.team);
+        q.full = (int64_t)q.team * 8 * q.pieces == cols;
+        const int64_t per_block = (int64_t)q.teams * q.at_once, blocks = (rows + per_block - 1) / per_block;
+        if (blocks >= sm_count) {
+            q.kind = Plan::kEight;
+            q.blocks = q.parts = sm_count;
+            return q;
+        }
+    }
+    if (cols > 8 * kMaxTeam) {
+        q.kind = Plan::kWide;
         q.blocks = (int)std::min<int64_t>(rows, 2 * (int64_t)sm_count);
         const int64_t slabs = (cols + 255) / 256;
         q.parts = (int)std::max<int64_t>(1, std::min<int64_t>((rows + 4 * kColumnRows - 1) / (4 * kColumnRows), 8 * (int64_t)sm_count / slabs));
         q.columns = dim3((unsigned)slabs, (unsigned)q.parts);
         return q;
     }
-    q.team = (int)((cols + 255) / 256 * 32);
-    q.teams = std::max(1, 256 / q.team);
-    const int64_t per_block = (int64_t)q.teams * rows_at_once;
-    q.blocks = (int)std::min<int64_t>((rows + per_block - 1) / per_block, (int64_t)sm_count * std::max(1, 1024 / (q.team * q.teams)));
-    q.parts = q.blocks;
+    q.kind = Plan::kAny;
+    q.team = round_up((cols + 7) / 8, 32);
+    q.teams = std::max(1, 512 / q.team);
+    q.at_once = backward ? 2 : rows >= (int64_t)4 * q.teams * sm_count ? 4 : 1;
+    if (q.at_once == 1) q.teams = 1;
+    const int64_t per_block = (int64_t)q.teams * q.at_once;
+    q.blocks = q.parts = (int)std::min<int64_t>((rows + per_block - 1) / per_block, (int64_t)sm_count * std::max(1, (backward ? 512 : 1024) / (q.team * q.teams)));
     return q;
 }
 
-template <typename T, int kVec> cudaError_t forward(const Plan& q, int at_once, const Params& p, cudaStream_t st) {
-    if (q.wide) return launch_dependent(&wide_forward_kernel<T, kVec>, dim3(q.blocks), dim3(kWideThreads), 0, st, p);
+template <typename K> cudaError_t roomy(PerDeviceOnce& once, K kernel) {
+    return once_per_device(once, [&](int) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kEightThreads * 4 * 8); });
+}
+template <typename T, int kC, int kR, int kThreads> cudaError_t forward8(const Plan& q, const Params& p, cudaStream_t st) {
+    static PerDeviceOnce once;
+    if (cudaError_t e = roomy(once, &forward8_kernel<T, kC, kR, kThreads>)) return e;
+    return launch_dependent(&forward8_kernel<T, kC, kR, kThreads>, dim3(q.blocks), dim3(q.team, q.teams), (size_t)p.cols * 8, st, p);
+}
+template <typename T, int kC, int kR, bool kSums, bool kFull> cudaError_t backward8(const Plan& q, const Params& p, cudaStream_t st) {
+    static PerDeviceOnce once;
+    if (cudaError_t e = roomy(once, &backward8_kernel<T, kC, kR, kSums, kFull>)) return e;
+    const size_t joined = kSums && q.teams > 1 ? (size_t)q.team * 16 * kC * 4 : 0;
+    return launch_dependent(&backward8_kernel<T, kC, kR, kSums, kFull>, dim3(q.blocks), dim3(q.team, q.teams), std::max((size_t)p.cols * 4, joined), st, p);
+}
+
+template <typename T, int kVec> cudaError_t forward(const Plan& q, const Params& p, cudaStream_t st) {
+    if constexpr (kVec == 8) {
+        if (q.kind == Plan::kEight) {
+            const auto go = [&](auto threads) {
+                constexpr int kThreads = decltype(threads)::value;
+                constexpr int kRoom = sizeof(T) == 2 ? 4 : 2;
+                return q.pieces == 1   ? forward8<T, 1, kRoom, kThreads>(q, p, st)
+                       : q.pieces == 2 ? forward8<T, 2, kRoom / 2, kThreads>(q, p, st)
+                                       : forward8<T, 4, 1, kThreads>(q, p, st);
+            };
+            return q.team * q.teams <= 256 ? go(std::integral_constant<int, 256>()) : go(std::integral_constant<int, kEightThreads>());
+        }
+    }
+    if (q.kind == Plan::kWide) return launch_dependent(&wide_forward_kernel<T, kVec>, dim3(q.blocks), dim3(kWideThreads), 0, st, p);
     const dim3 block(q.team, q.teams);
-    if (at_once == 4) return launch_dependent(&forward_kernel<T, kVec, 4>, dim3(q.blocks), block, 0, st, p);
+    if (q.at_once == 4) return launch_dependent(&forward_kernel<T, kVec, 4>, dim3(q.blocks), block, 0, st, p);
     return launch_dependent(&forward_kernel<T, kVec, 1>, dim3(q.blocks), block, 0, st, p);
 }
-template <typename T, int kVec> cudaError_t backward(const Plan& q, bool sums, const Params& p, cudaStream_t st) {
-    if (q.wide) {
+template <typename T, int kVec, bool kSums> cudaError_t backward(const Plan& q, const Params& p, cudaStream_t st) {
+    if constexpr (kVec == 8) {
+        if (q.kind == Plan::kEight) {
+            constexpr int kRoom = sizeof(T) == 2 ? 2 : 1;
+            if (q.full) return q.pieces == 1 ? backward8<T, 1, kRoom, kSums, true>(q, p, st) : backward8<T, 2, 1, kSums, true>(q, p, st);
+            return q.pieces == 1 ? backward8<T, 1, kRoom, kSums, false>(q, p, st) : backward8<T, 2, 1, kSums, false>(q, p, st);
+        }
+    }
+    if (q.kind == Plan::kWide) {
         cudaError_t e = cudaSuccess;
-        if (sums) e = launch_dependent(&wide_column_kernel<T, kVec>, q.columns, dim3(32, kColumnRows), 0, st, p);
+        if (kSums) e = launch_dependent(&wide_column_kernel<T, kVec>, q.columns, dim3(32, kColumnRows), 0, st, p);
         if (e != cudaSuccess) return e;
         return launch_dependent(&wide_backward_kernel<T, kVec>, dim3(q.blocks), dim3(kWideThreads), 0, st, p);
     }
-    const dim3 block(q.team, q.teams);
-    if (!sums) return launch_dependent(&backward_kernel<T, kVec, false>, dim3(q.blocks), block, 0, st, p);
-    return launch_dependent(&backward_kernel<T, kVec, true>, dim3(q.blocks), block, q.teams > 1 ? q.team * 64 : 0, st, p);
+    return launch_dependent(&backward_kernel<T, kVec, kSums>, dim3(q.blocks), dim3(q.team, q.teams), kSums && q.teams > 1 ? q.team * 64 : 0, st, p);
 }
 int widest(int v, const void* p, int64_t ld, int64_t cols, int64_t rows, int dtype) { return std::min(v, row_vector(p, rows > 1 ? ld : cols, cols, dtype)); }
 
-size_t workspace_bytes_of(int64_t rows, int64_t cols, int sm_count) { return (size_t)plan(rows, cols, 2, sm_count).parts * 2 * (size_t)cols * sizeof(float); }
+// enough for any alignment and type
+size_t workspace_bytes_of(int64_t rows, int64_t cols, int sm_count) {
+    int parts = 0;
+    for (const int dtype : {MVUE_F32, MVUE_BF16})
+        for (const int vec : {8, 1}) parts = std::max(parts, plan(true, rows, cols, dtype, vec, sm_count).parts);
+    return (size_t)parts * 2 * (size_t)cols * sizeof(float);
+}
 
 int check(const void* x, int dtype, int64_t rows, int64_t cols, int affine_dtype, const void* gamma, const void* beta) {
     if (dtype != MVUE_F32 && dtype != MVUE_BF16) return MVUE_ERR_DTYPE;
@@ -472,15 +871,12 @@ extern "C" int mvue_layer_norm(const void* x, int dtype, int64_t rows, int64_t c
     p.x = x; p.y = y; p.gamma = gamma; p.beta = beta; p.mean = mean; p.rstd = rstd;
     p.rows = rows; p.cols = cols; p.ldx = ldx; p.ldy = ldy;
     p.eps = eps; p.inv_cols = (float)(1.0 / (double)cols); p.affine_bf16 = affine_dtype == MVUE_BF16;
-    // four rows at a time where that leaves every SM a block's worth of them
-    Plan q = plan(rows, cols, 4, dev.sm_count);
-    const int at_once = q.wide || q.blocks >= dev.sm_count ? 4 : 1;
-    if (at_once == 1) q = plan(rows, cols, 1, dev.sm_count);
     const int v = widest(widest(8, x, ldx, cols, rows, dtype), y, ldy, cols, rows, dtype);
+    const Plan q = plan(false, rows, cols, dtype, v, dev.sm_count);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const auto pick = [&](auto t) {
         using T = decltype(t);
-        return v == 8 ? forward<T, 8>(q, at_once, p, st) : v == 2 ? forward<T, 2>(q, at_once, p, st) : forward<T, 1>(q, at_once, p, st);
+        return v == 8 ? forward<T, 8>(q, p, st) : v == 2 ? forward<T, 2>(q, p, st) : forward<T, 1>(q, p, st);
     };
     const cudaError_t e = dtype == MVUE_BF16 ? pick(__nv_bfloat16()) : pick(float());
     if (e != cudaSuccess) { set_cuda_error(e, "mvue_layer_norm launch"); return MVUE_ERR_CUDA; }
@@ -509,11 +905,15 @@ extern "C" int mvue_layer_norm_backward(const void* dy, int64_t lddy, const void
     p.x = x; p.dy = dy; p.dx = dx; p.gamma = gamma; p.mean_in = mean; p.rstd_in = rstd; p.partial = static_cast<float*>(workspace);
     p.rows = rows; p.cols = cols; p.ldx = ldx; p.lddy = lddy; p.ldy = lddx;
     p.inv_cols = (float)(1.0 / (double)cols); p.affine_bf16 = affine_dtype == MVUE_BF16;
-    const Plan q = plan(rows, cols, 2, dev.sm_count);
     const int v = widest(widest(widest(8, x, ldx, cols, rows, dtype), dy, lddy, cols, rows, dtype), dx, lddx, cols, rows, dtype);
+    const Plan q = plan(true, rows, cols, dtype, v, dev.sm_count);
     const auto pick = [&](auto t) {
         using T = decltype(t);
-        return v == 8 ? backward<T, 8>(q, sums, p, st) : v == 2 ? backward<T, 2>(q, sums, p, st) : backward<T, 1>(q, sums, p, st);
+        const auto go = [&](auto s) {
+            constexpr bool kSums = decltype(s)::value;
+            return v == 8 ? backward<T, 8, kSums>(q, p, st) : v == 2 ? backward<T, 2, kSums>(q, p, st) : backward<T, 1, kSums>(q, p, st);
+        };
+        return sums ? go(std::true_type()) : go(std::false_type());
     };
     cudaError_t e = dtype == MVUE_BF16 ? pick(__nv_bfloat16()) : pick(float());
     if (e == cudaSuccess && sums)

@@ -50,13 +50,19 @@ template <> struct Eight<__nv_bfloat16> {
         }
     }
     __device__ __forceinline__ float at(int i) const { return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
-    // bit pattern of the largest magnitude (as binary32); an infinity or a NaN is above all others
-    __device__ __forceinline__ uint32_t top() const {
+    // upper halves of the magnitudes, two neighbours' largest in each half of the word
+    __device__ __forceinline__ uint32_t tops() const {
         uint32_t m = w[0] & 0x7FFF7FFFu;
 #pragma unroll
         for (int i = 1; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7FFF7FFFu);
+        return m;
+    }
+    // bit pattern of the largest magnitude (as binary32); an infinity or a NaN is above all others
+    __device__ __forceinline__ uint32_t top() const {
+        const uint32_t m = tops();
         return max(m << 16, m & 0xFFFF0000u);
     }
+    __device__ __forceinline__ uint32_t signs(int h) const { return __byte_perm(w[2 * h], w[2 * h + 1], 0x7531); }      // bit 7 of each byte
 };
 template <> struct Eight<float> {
     uint32_t w[8];
@@ -75,11 +81,38 @@ template <> struct Eight<float> {
         for (int i = 0; i < 8; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
         return m;
     }
+    __device__ __forceinline__ uint32_t signs(int h) const {
+        return __byte_perm(__byte_perm(w[4 * h], w[4 * h + 1], 0x0073), __byte_perm(w[4 * h + 2], w[4 * h + 3], 0x0073), 0x5410);
+    }
 };
 
+// The largest magnitudes of the blocks that kRows rows have in a lane's sixteen lanes.  bf16: two rows share a word.
+template <typename T, int kRows>
+__device__ __forceinline__ void block_tops(const Eight<T> (&x)[kRows], uint32_t (&top)[kRows]) {
+    if constexpr (sizeof(T) == 2 && kRows % 2 == 0) {
+#pragma unroll
+        for (int r = 0; r < kRows; r += 2) {
+            const uint32_t a = x[r].tops(), b = x[r + 1].tops();
+            uint32_t m = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            top[r] = m << 16;
+            top[r + 1] = m & 0xFFFF0000u;
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            top[r] = x[r].top();
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) top[r] = max(top[r], __shfl_xor_sync(0xFFFFFFFFu, top[r], d));
+        }
+    }
+}
+
 // the largest finite magnitude: where top() met something else
-template <typename T> __device__ __noinline__ uint32_t finite_top(const Eight<T>& x) {
+template <typename T> __device__ __forceinline__ uint32_t finite_top(const Eight<T>& x) {
     uint32_t m = 0u;
+#pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t b = __float_as_uint(x.at(i)) & 0x7FFFFFFFu;
         if (b < kInf) m = max(m, b);
@@ -92,29 +125,43 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
     return (uint32_t)max((int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0), 1);
 }
 
+// NaN codes for elements that have none other.
+template <typename T> __device__ __forceinline__ void put_nan(const Eight<T>& x, uint2& v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if ((__float_as_uint(x.at(i)) & 0x7FFFFFFFu) >= kInf) (i < 4 ? v.x : v.y) |= 0x7Fu << (8 * (i & 3));
+}
+
+// Four codes rounded at random: y = the elements over their scale, times 2^-120.  The code fills the highest byte of the bits four
+// places up, the sign falls out, the random number is below it.
+__device__ __forceinline__ uint32_t random_codes(f2 y0, f2 y1, uint32_t r0, uint32_t r1) {
+    float y[4];
+    unpair(y0, y[0], y[1]);
+    unpair(y1, y[2], y[3]);
+    const uint32_t t0 = (__float_as_uint(y[0]) << 4) + __byte_perm(r0, 0u, 0x4104), t1 = (__float_as_uint(y[1]) << 4) + __byte_perm(r0, 0u, 0x4324);
+    const uint32_t t2 = (__float_as_uint(y[2]) << 4) + __byte_perm(r1, 0u, 0x4104), t3 = (__float_as_uint(y[3]) << 4) + __byte_perm(r1, 0u, 0x4324);
+    return __byte_perm(__byte_perm(t0, t1, 0x0073), __byte_perm(t2, t3, 0x0073), 0x5410);
+}
+
 template <typename T, bool kRandom>
-__device__ __forceinline__ uint2 encode(const Eight<T>& x, uint32_t byte, bool finite, uint4 random) {
-    const f2 factor = pair(__uint_as_float((254u - byte) << 23));          // 2^(127 - byte)
+__device__ __forceinline__ uint2 encode(const Eight<T>& x, uint32_t byte, uint4 random) {
     uint32_t out[2];
     if constexpr (kRandom) {
         const uint32_t rw[4] = {random.x, random.y, random.z, random.w};
+        // 2^(7 - byte) in one product where that is a normal number (blocks of magnitudes up to 2^14), else in two
+        const bool one = byte <= 133u;
+        const f2 first = pair(__uint_as_float(one ? (134u - byte) << 23 : (254u - byte) << 23)), second = pair(7.52316384526264005e-37f);       // 2^-120
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            uint32_t t[4], s[4];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float lo, hi;
-                unpair(mul2(mul2(pair(x.at(4 * h + 2 * j), x.at(4 * h + 2 * j + 1)), factor), pair(7.52316384526264005e-37f)), lo, hi);   // 2^-120
-                s[2 * j] = __float_as_uint(lo);
-                s[2 * j + 1] = __float_as_uint(hi);
-                // the code fills the highest byte of the bits four places up, the sign falls out; the random number is below it
-                t[2 * j] = s[2 * j] * 16u + __byte_perm(rw[2 * h + j], 0u, 0x4104);
-                t[2 * j + 1] = s[2 * j + 1] * 16u + __byte_perm(rw[2 * h + j], 0u, 0x4324);
+            f2 y0 = mul2(pair(x.at(4 * h), x.at(4 * h + 1)), first), y1 = mul2(pair(x.at(4 * h + 2), x.at(4 * h + 3)), first);
+            if (!one) {
+                y0 = mul2(y0, second);
+                y1 = mul2(y1, second);
             }
-            const uint32_t signs = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410) & 0x80808080u;
-            out[h] = __byte_perm(__byte_perm(t[0], t[1], 0x0073), __byte_perm(t[2], t[3], 0x0073), 0x5410) | signs;
+            out[h] = random_codes(y0, y1, rw[2 * h], rw[2 * h + 1]) | (x.signs(h) & 0x80808080u);
         }
     } else {
+        const f2 factor = pair(__uint_as_float((254u - byte) << 23));          // 2^(127 - byte)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             uint32_t half[2];
@@ -126,11 +173,6 @@ __device__ __forceinline__ uint2 encode(const Eight<T>& x, uint32_t byte, bool f
             }
             out[h] = __byte_perm(half[0], half[1], 0x5410);
         }
-    }
-    if (!finite) {                                                            // NaN for what has no code
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if ((__float_as_uint(x.at(i)) & 0x7FFFFFFFu) >= kInf) out[i >> 2] |= 0x7Fu << (8 * (i & 3));
     }
     return make_uint2(out[0], out[1]);
 }
@@ -157,21 +199,27 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const __grid_co
 #pragma unroll
     for (int r = 0; r < kRowsPerWarp; ++r)
         x[r].load(static_cast<const T*>(p.x) + (row0 + r) * p.ldx + col, p.wide_x, row0 + r < p.rows ? count : 0);
+    uint32_t top[kRowsPerWarp];
+    block_tops(x, top);
+    uint8_t* to = p.codes + row0 * p.ldq + col;
+    uint8_t* scale = p.scales + (col >> 7) * p.scale_pitch + row0;
+    uint64_t unit = (uint64_t)(row0 * p.units + (col >> 3));
 #pragma unroll
-    for (int r = 0; r < kRowsPerWarp; ++r) {
-        const int64_t row = row0 + r;
-        if (row >= p.rows) return;                                            // a whole warp
-        uint32_t top = x[r].top();
-        const bool finite = top < kInf;
-        if (!finite) top = finite_top(x[r]);
+    for (int r = 0; r < kRowsPerWarp; ++r, to += p.ldq, unit += (uint64_t)p.units) {
+        if (row0 + r >= p.rows) return;                                       // a whole warp
+        const bool finite = __all_sync(0xFFFFFFFFu, top[r] < kInf);           // (the branches below are the warp's, and rarely taken)
+        if (!finite) {
+            top[r] = finite_top(x[r]);
 #pragma unroll
-        for (int d = 8; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-        const uint32_t byte = scale_byte(top);
+            for (int d = 8; d > 0; d >>= 1) top[r] = max(top[r], __shfl_xor_sync(0xFFFFFFFFu, top[r], d));
+        }
+        const uint32_t byte = scale_byte(top[r]);
         uint4 random = make_uint4(0u, 0u, 0u, 0u);
-        if (kRandom) random = philox4x32_10((uint64_t)(row * p.units + (col >> 3)), p.keys, 3u);
-        const uint2 v = encode<T, kRandom>(x[r], byte, finite, random);
-        store_codes(p.codes + row * p.ldq + col, p.wide_q, count, v);
-        if ((lane & 15) == 0 && count > 0) p.scales[(col >> 7) * p.scale_pitch + row] = (uint8_t)byte;
+        if (kRandom) random = philox4x32_10(unit, p.keys, 3u);
+        uint2 v = encode<T, kRandom>(x[r], byte, random);
+        if (!finite) put_nan(x[r], v);
+        store_codes(to, p.wide_q, count, v);
+        if ((lane & 15) == 0 && count > 0) scale[r] = (uint8_t)byte;
     }
 }
 
@@ -188,29 +236,31 @@ __global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(const __grid_c
     for (int r = 0; r < 8; ++r)
         x[r].load(static_cast<const T*>(p.x) + (row0 + 16 * r) * p.ldx + col, p.wide_x, row0 + 16 * r < p.rows ? count : 0);
     uint32_t top = 0u;
-    bool finite = true;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        uint32_t t = x[r].top();
-        if (t >= kInf) {
-            finite = false;
-            t = finite_top(x[r]);
-        }
-        top = max(top, t);
-    }
+    for (int r = 0; r < 8; ++r) top = max(top, x[r].top());
     top = __reduce_max_sync(0xFFFFFFFFu, top);
+    const bool finite = top < kInf;                                           // of the warp
+    if (!finite) {
+        top = 0u;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) top = max(top, finite_top(x[r]));
+        top = __reduce_max_sync(0xFFFFFFFFu, top);
+    }
     if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kThreads / 32; ++i) top = max(top, tops[i]);
     const uint32_t byte = scale_byte(top);
+    uint8_t* to = p.codes + row0 * p.ldq + col;
+    uint64_t unit = (uint64_t)(row0 * p.units + (col >> 3));
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const int64_t row = row0 + 16 * r;
-        if (row >= p.rows) break;
+    for (int r = 0; r < 8; ++r, to += 16 * p.ldq, unit += 16 * (uint64_t)p.units) {
+        if (row0 + 16 * r >= p.rows) break;
         uint4 random = make_uint4(0u, 0u, 0u, 0u);
-        if (kRandom) random = philox4x32_10((uint64_t)(row * p.units + (col >> 3)), p.keys, 3u);
-        store_codes(p.codes + row * p.ldq + col, p.wide_q, count, encode<T, kRandom>(x[r], byte, finite, random));
+        if (kRandom) random = philox4x32_10(unit, p.keys, 3u);
+        uint2 v = encode<T, kRandom>(x[r], byte, random);
+        if (!finite) put_nan(x[r], v);
+        store_codes(to, p.wide_q, count, v);
     }
     if (threadIdx.x == 0) p.scales[tile_y * p.scale_pitch + tile_x] = (uint8_t)byte;
 }
