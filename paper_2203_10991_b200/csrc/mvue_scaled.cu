@@ -5,6 +5,7 @@
 
 #include "../../include/mvue_layer.h"
 #include "mvue_dense.cuh"
+#include "mvue_few.cuh"
 #include "mvue_train.cuh"
 
 namespace mvue {
@@ -61,6 +62,14 @@ cudaError_t launch(const dense::Params& p, const dense::Operand& a, const dense:
     return dense::launch_pair<dense::Shape<true, false, 256, 6>>(p, a, b, {}, out, stream);
 }
 
+template <int kTN> cudaError_t launch_few(const dense::FewParams& p, const dense::Operand& t, const dense::Operand& w, bool n_major, cudaStream_t stream) {
+    return n_major ? dense::launch_few<dense::FewShape<true, kTN>>(p, t, w, stream) : dense::launch_few<dense::FewShape<false, kTN>>(p, t, w, stream);
+}
+
+// Tiles of 128 outs and a cluster along the reduction where a token tile of the pair kernel would be half empty or its tiles would leave
+// SMs without work.
+bool few(int64_t tokens, int64_t pair_tiles, int sm_count) { return tokens <= 128 || 2 * pair_tiles < sm_count * 3 / 4; }
+
 int scaled_gemm(const void* a, int64_t M, int64_t K, int64_t lda, const void* a_scales, const void* w, int64_t N, int64_t ldw,
                 const void* w_scales, bool n_major, void* C, int c_dtype, int64_t ldc, int* dev_status, void* stream) {
     if (c_dtype != MVUE_F32 && c_dtype != MVUE_BF16) return MVUE_ERR_DTYPE;
@@ -71,20 +80,36 @@ int scaled_gemm(const void* a, int64_t M, int64_t K, int64_t lda, const void* a_
     if (M == 0) return MVUE_OK;
     DeviceInfo dev;
     if (int s = current_device_info(&dev)) return s;
-    dense::Params p = {};
-    p.M = (int)M; p.N = (int)N; p.K = (int)K; p.batch = 1;
-    p.a_scales = static_cast<const uint8_t*>(a_scales);
-    p.b_scales = static_cast<const uint8_t*>(w_scales);
-    const int64_t blocks_n = (N + 127) / 128, blocks_k = (K + 127) / 128;
-    p.b_scales_n = n_major ? 1 : blocks_k;
-    p.b_scales_k = n_major ? blocks_n : 1;
-    p.dev_status = dev_status;
     const dense::Operand oa = {a, lda, lda * M}, ob = {w, ldw, ldw * (n_major ? K : N)};
     const int64_t pitch = ldc * size_of(c_dtype);
     const int vec = !off(C, 32) && pitch % 32 == 0 ? 32 : !off(C, 16) && pitch % 16 == 0 ? 16 : (int)size_of(c_dtype);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const cudaError_t e = c_dtype == MVUE_BF16 ? launch(p, oa, ob, n_major, Store<true>{C, ldc, vec}, st)
-                                               : launch(p, oa, ob, n_major, Store<false>{C, ldc, vec}, st);
+    const int64_t blocks_n = (N + 127) / 128, blocks_k = (K + 127) / 128;
+    const int64_t scales_n = n_major ? 1 : blocks_k, scales_k = n_major ? blocks_n : 1;
+    const uint8_t *as = static_cast<const uint8_t*>(a_scales), *ws = static_cast<const uint8_t*>(w_scales);
+    cudaError_t e;
+    const int64_t pair_tiles = ((M + 255) / 256) * ((N + 255) / 256);
+    if (few(M, pair_tiles, dev.sm_count)) {
+        dense::FewParams p = {};
+        p.tokens = (int)M; p.outs = (int)N; p.K = (int)K;
+        p.tiles_o = (int)blocks_n;
+        p.t_scales = as; p.w_scales = ws; p.w_scales_o = scales_n; p.w_scales_k = scales_k;
+        p.C = C; p.ldc = ldc; p.bf16 = c_dtype == MVUE_BF16; p.vec = vec >= 16 ? 16 : 1;
+        p.dev_status = dev_status;
+        const int tn = M <= 16 ? 16 : M <= 64 ? 64 : 128;
+        const int64_t tiles = blocks_n * ((M + tn - 1) / tn);
+        // as many parts as two blocks an SM have room for, of four steps at least
+        p.split = 1;
+        while (p.split < 8 && tiles * p.split * 2 <= 2 * (int64_t)dev.sm_count && blocks_k >= 8 * p.split) p.split *= 2;
+        p.steps_per_part = (int)((blocks_k + p.split - 1) / p.split);
+        e = tn == 16 ? launch_few<16>(p, oa, ob, n_major, st) : tn == 64 ? launch_few<64>(p, oa, ob, n_major, st) : launch_few<128>(p, oa, ob, n_major, st);
+    } else {
+        dense::Params p = {};
+        p.M = (int)M; p.N = (int)N; p.K = (int)K; p.batch = 1;
+        p.a_scales = as; p.b_scales = ws; p.b_scales_n = scales_n; p.b_scales_k = scales_k;
+        p.dev_status = dev_status;
+        e = c_dtype == MVUE_BF16 ? launch(p, oa, ob, n_major, Store<true>{C, ldc, vec}, st) : launch(p, oa, ob, n_major, Store<false>{C, ldc, vec}, st);
+    }
     if (e != cudaSuccess) { set_cuda_error(e, "scaled product launch"); return MVUE_ERR_CUDA; }
     return MVUE_OK;
 }
