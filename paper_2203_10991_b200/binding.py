@@ -576,7 +576,8 @@ def mvue_layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: t
     else:
         assert out.shape == x.shape and out.dtype == x.dtype
         ldy = _rows(out)[2]
-    mean, rstd = x.new_empty(x.shape[:-1], dtype=torch.float32), x.new_empty(x.shape[:-1], dtype=torch.float32)
+    mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     _check(lib().mvue_layer_norm(x.data_ptr(), _dtype_code(x), rows, cols, ldx, _ptr(weight), _ptr(bias), code, eps, out.data_ptr(), ldy,
                                  mean.data_ptr(), rstd.data_ptr(), _stream_ptr()), "mvue_layer_norm")
     return out, mean, rstd

@@ -14,7 +14,7 @@
 namespace mvue {
 namespace dense {
 
-constexpr int kFewThreads = 192;
+constexpr int kFewThreads = 192, kMaxSplit = 8;
 
 template <bool kMMajorT, int kTNT>
 struct FewShape {
@@ -212,13 +212,22 @@ few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     for (int i = threadIdx.x; i < share * 16; i += kFewThreads) {
         const int token = first + (i >> 4), o = (i & 15) * 8;
         if (token0 + token >= p.tokens || out0 + o >= p.outs) continue;
-        float x[8] = {};
         const uint32_t at = smem_base + (uint32_t)(token * 128 + o) * 4;
-        for (int r = 0; r < p.split; ++r) {
-            const uint32_t from = p.split > 1 ? map_to_cta(at, r) : at;
-            const float4 a = ld_cluster4(from), b = ld_cluster4(from + 16);
-            x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
-            x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+        float4 a[kMaxSplit], b[kMaxSplit];                   // all parts on their way at once
+#pragma unroll
+        for (int r = 0; r < kMaxSplit; ++r) {
+            a[r] = b[r] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (r < p.split) {
+                const uint32_t from = map_to_cta(at, r);
+                a[r] = ld_cluster4(from);
+                b[r] = ld_cluster4(from + 16);
+            }
+        }
+        float x[8] = {};
+#pragma unroll
+        for (int r = 0; r < kMaxSplit; ++r) {
+            x[0] += a[r].x; x[1] += a[r].y; x[2] += a[r].z; x[3] += a[r].w;
+            x[4] += b[r].x; x[5] += b[r].y; x[6] += b[r].z; x[7] += b[r].w;
         }
         if (failed) {
 #pragma unroll

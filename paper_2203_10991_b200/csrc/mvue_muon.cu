@@ -383,6 +383,185 @@ struct Apply {
     }
 };
 
+// ---- all steps of a small matrix in one launch ---------------------------------------------------------------------------
+// A cluster of eight blocks per matrix goes through the products with a cluster barrier between them instead of a launch: fifteen dependent
+// launches of a product that takes two microseconds cost nine each.  Tiles of 128 x 64, a block's own; operands by TMA from L2, where the
+// last product's results are.
+//   warps 0-3 epilogue      warp 4 TMA producer      warp 5 tensor-memory allocation, MMA issue
+constexpr int kSmallBlocks = 8, kSmallThreads = 192, kSmallStages = 4;
+constexpr int kSmallBox = 64 * 128, kSmallStage = 3 * kSmallBox;        // 128 rows of the first operand, 64 of the second
+constexpr int kSmallBars = kSmallStages * kSmallStage, kSmallSmem = kSmallBars + 256 + 1024;
+constexpr int kSmallM = 256;
+constexpr int64_t kSmallElements = 256 * 1024;
+
+struct SmallParams {
+    int m, n, steps;
+    int64_t n_pitch, m_pitch;
+    __half *X[2], *lo, *A, *B;
+    const float* xs;
+    float S;
+    int* dev_status;
+};
+struct SmallMaps {
+    CUtensorMap X[2], A, B;                  // boxes of 64 x 64
+};
+
+__device__ __forceinline__ void mma_half(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"(accumulate) : "memory");
+}
+// 32 halves of a row from global memory; pieces of eight that do not begin before `left` are zero, or not written
+__device__ __forceinline__ void load_row(const __half* from, int left, uint4 (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = 8 * i < left ? *reinterpret_cast<const uint4*>(from + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+}
+__device__ __forceinline__ void store_row(__half* to, int left, const uint4 (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (8 * i < left) *reinterpret_cast<uint4*>(to + 8 * i) = w[i];
+}
+
+__global__ void __cluster_dims__(kSmallBlocks, 1, 1) __launch_bounds__(kSmallThreads, 2)
+small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ SmallParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+    const uint32_t bar_base = smem_base + kSmallBars;
+    const auto full_bar = [&](int s) { return bar_base + 8u * s; };
+    const auto empty_bar = [&](int s) { return bar_base + 8u * (kSmallStages + s); };
+    const auto acc_bar = [&](int b) { return bar_base + 8u * (2 * kSmallStages + b); };
+    const auto free_bar = [&](int b) { return bar_base + 8u * (2 * kSmallStages + 2 + b); };
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + kSmallBars + 8 * (2 * kSmallStages + 4));
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)cluster_ctarank(), z = blockIdx.x / kSmallBlocks;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kSmallStages; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_bar(b), 1);
+            mbar_init(free_bar(b), 4);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 5) {
+        tmem_alloc(smem_u32(tmem_slot), 128);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    grid_dependency_wait();
+
+    const int64_t x0 = (int64_t)z * p.m * p.n_pitch, a0 = (int64_t)z * p.m * p.m_pitch;
+    const float xs = p.xs[z];
+    int s = 0, done = 0;                                     // stage, tiles of this block so far: each role counts for itself
+    uint32_t parity = warp == 4 ? 1u : 0u;
+    for (int phase = 0; phase < 3 * p.steps; ++phase) {
+        const int k = phase / 3, what = phase - 3 * k;       // 0: A = X X^T, 1: B = b A + c A A, 2: X' = a X + B X
+        const int N = what == 2 ? p.n : p.m, K = what == 0 ? p.n : p.m;
+        const int tiles_n = (N + 63) / 64, tiles = (p.m + 127) / 128 * tiles_n, steps = (K + 63) / 64;
+        if (warp == 4 && lane == 0) {
+            asm volatile("fence.proxy.async.global;" ::: "memory");
+            const CUtensorMap* first = what == 0 ? &maps.X[k & 1] : what == 1 ? &maps.A : &maps.B;
+            const CUtensorMap* second = what == 1 ? &maps.A : &maps.X[k & 1];
+            bool ok = true;
+            for (int t = rank; t < tiles && ok; t += kSmallBlocks) {
+                const int m0 = t / tiles_n * 128, n0 = t % tiles_n * 64;
+                for (int i = 0; i < steps; ++i) {
+                    if (!(ok = mbar_wait(empty_bar(s), parity, abort_flag))) break;
+                    const uint32_t to = smem_base + s * kSmallStage;
+                    mbar_expect_tx(full_bar(s), kSmallStage);
+                    dense::tma_load_3d(to, first, 64 * i, m0, z, full_bar(s));
+                    dense::tma_load_3d(to + kSmallBox, first, 64 * i, m0 + 64, z, full_bar(s));
+                    dense::tma_load_3d(to + 2 * kSmallBox, second, what == 2 ? n0 : 64 * i, what == 2 ? 64 * i : n0, z, full_bar(s));
+                    if (++s == kSmallStages) { s = 0; parity ^= 1u; }
+                }
+            }
+        } else if (warp == 5 && lane == 0) {
+            const uint32_t instr = (1u << 4) | (what == 2 ? 1u << 16 : 0u) | (64u >> 3 << 17) | (128u >> 4 << 24);
+            const uint64_t da = make_smem_desc(smem_base, 16, 1024, kSwizzle128B), db = make_smem_desc(smem_base + 2 * kSmallBox, kSmallBox, 1024, kSwizzle128B);
+            const int b_step = what == 2 ? 16 * 128 / 16 : 2;
+            bool ok = true;
+            for (int t = rank; t < tiles && ok; t += kSmallBlocks, ++done) {
+                if (done > 1) {
+                    if (!(ok = mbar_wait(free_bar(done & 1), ((done >> 1) - 1) & 1u, abort_flag))) break;
+                    tc_fence_after();
+                }
+                for (int i = 0; i < steps; ++i) {
+                    if (!(ok = mbar_wait(full_bar(s), parity, abort_flag))) break;
+                    tc_fence_after();
+                    const uint64_t stage = (uint64_t)(s * (kSmallStage >> 4));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        mma_half(tmem_base + 64u * (done & 1), da + stage + 2 * j, db + stage + j * b_step, instr, (i > 0 || j > 0) ? 1u : 0u);
+                    tc_commit(empty_bar(s));
+                    if (++s == kSmallStages) { s = 0; parity ^= 1u; }
+                }
+                if (!ok) break;
+                tc_commit(acc_bar(done & 1));
+            }
+        } else if (warp < 4) {
+            const __half* hi = p.X[k & 1];
+            const bool read_lo = what == 2 && k < p.steps - 2, write_lo = what == 2 && k + 1 < p.steps - 2;
+            const float alpha = what == 0 ? p.S / xs / xs : what == 1 ? kC / p.S : 1.0f / p.S;
+            for (int t = rank; t < tiles; t += kSmallBlocks, ++done) {
+                const int row = t / tiles_n * 128 + 32 * warp + lane, n0 = t % tiles_n * 64;
+                const int64_t at = what == 2 ? x0 + row * p.n_pitch + n0 : a0 + row * p.m_pitch + n0;
+                const bool there = row < p.m;
+                // (read where other blocks wrote: from L2)
+                uint4 x[2][2][4];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int left = there ? N - n0 - 32 * c : 0;
+                    if (what == 1) load_row(p.A + at + 32 * c, left, x[c][0]);
+                    if (what == 2) load_row(hi + at + 32 * c, left, x[c][0]);
+                    if (read_lo) load_row(p.lo + at + 32 * c, left, x[c][1]);
+                }
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(done & 1), (done >> 1) & 1u, abort_flag))) break;
+                tc_fence_after();
+                uint32_t v[2][32];
+                tmem_ld_32x32b_x32(tmem_base + ((uint32_t)(32 * warp) << 16) + 64u * (done & 1), v[0]);
+                tmem_ld_32x32b_x32(tmem_base + ((uint32_t)(32 * warp) << 16) + 64u * (done & 1) + 32u, v[1]);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) dense::mbar_arrive(free_bar(done & 1));
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int left = there ? N - n0 - 32 * c : 0;
+                    if (what == 0) Symmetric<false>{nullptr, 0.0f}.compute(alpha, v[c], x[c]);
+                    else if (what == 1) Symmetric<true>{nullptr, 0.0f}.compute(alpha, v[c], x[c]);
+                    else if (read_lo) Apply<true>{0.0f, 0}.compute(alpha, v[c], x[c]);
+                    else Apply<false>{0.0f, 0}.compute(alpha, v[c], x[c]);
+                    store_row((what == 0 ? p.A : what == 1 ? p.B : p.X[(k + 1) & 1]) + at + 32 * c, left, x[c][0]);
+                    if (write_lo) store_row(p.lo + at + 32 * c, left, x[c][1]);
+                }
+            }
+            asm volatile("fence.proxy.async.global;" ::: "memory");
+        }
+        __syncwarp();
+        cluster_sync();                      // the product is complete and seen by the cluster's copies
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag && threadIdx.x == 0) {
+        for (int i = 0; i < kSmallStages; ++i)
+            for (uint32_t spin = 0; spin < 4096 && !mbar_try_wait(full_bar(i), 0) && !mbar_try_wait(full_bar(i), 1); ++spin) __nanosleep(64);
+        if (p.dev_status) *p.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
+    }
+    __syncthreads();
+    if (warp == 5) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, 128);
+    }
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------------
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 int64_t pitch_of(int64_t n) { return (n + 7) / 8 * 8; }
@@ -417,6 +596,21 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
     const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 8 * sm_count / q.count));
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
+    if (e == cudaSuccess && m <= kSmallM && m * n <= kSmallElements) {
+        static PerDeviceOnce once;
+        e = once_per_device(once, [](int) { return cudaFuncSetAttribute(small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem); });
+        const auto map = [&](CUtensorMap* to, const __half* base, int64_t rows, int64_t cols, int64_t pitch) {
+            return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, rows, q.count, pitch * 2, rows * pitch * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+        };
+        SmallMaps maps;
+        if (!map(&maps.X[0], X[0], m, n, q.n_pitch) || !map(&maps.X[1], X[1], m, n, q.n_pitch) || !map(&maps.A, A, m, m, mp) || !map(&maps.B, B, m, m, mp))
+            return cudaErrorInvalidValue;
+        const SmallParams p = {q.m, q.n, steps, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
+        if (e == cudaSuccess) e = launch_dependent(&small_kernel, dim3(kSmallBlocks * q.count), dim3(kSmallThreads), kSmallSmem, st, maps, p);
+        q.hi = X[steps & 1];
+        if (e == cudaSuccess) e = launch_dependent(&finish_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
+        return e;
+    }
     using KMajor = dense::Shape<false, false, 256, 4, true>;
     using NMajor = dense::Shape<false, true, 256, 4, true>;
     const dense::Operand oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2}, olo = {q.lo, q.n_pitch * 2, m * q.n_pitch * 2};
