@@ -388,9 +388,10 @@ struct Apply {
 // launches of a product that takes two microseconds cost nine each.  Tiles of 128 x 64, a block's own; operands by TMA from L2, where the
 // last product's results are.
 //   warps 0-3 epilogue      warp 4 TMA producer      warp 5 tensor-memory allocation, MMA issue
-constexpr int kSmallBlocks = 8, kSmallThreads = 192, kSmallStages = 4;
+// A block has eight stages and an SM to itself where the clusters leave room for that, else four.
+constexpr int kSmallBlocks = 8, kSmallThreads = 192;
 constexpr int kSmallBox = 64 * 128, kSmallStage = 3 * kSmallBox;        // 128 rows of the first operand, 64 of the second
-constexpr int kSmallBars = kSmallStages * kSmallStage, kSmallSmem = kSmallBars + 256 + 1024;
+constexpr int small_smem(int stages) { return stages * kSmallStage + 256 + 1024; }
 constexpr int kSmallM = 256;
 constexpr int64_t kSmallElements = 256 * 1024;
 
@@ -421,9 +422,11 @@ __device__ __forceinline__ void store_row(__half* to, int left, const uint4 (&w)
         if (8 * i < left) *reinterpret_cast<uint4*>(to + 8 * i) = w[i];
 }
 
-__global__ void __cluster_dims__(kSmallBlocks, 1, 1) __launch_bounds__(kSmallThreads, 2)
+template <int kSmallStages>
+__global__ void __cluster_dims__(kSmallBlocks, 1, 1) __launch_bounds__(kSmallThreads, kSmallStages == 4 ? 2 : 1)
 small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ SmallParams p) {
     extern __shared__ uint8_t smem_raw[];
+    constexpr int kSmallBars = kSmallStages * kSmallStage;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
     const uint32_t bar_base = smem_base + kSmallBars;
@@ -598,7 +601,10 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     if (e == cudaSuccess && m <= kSmallM && m * n <= kSmallElements) {
         static PerDeviceOnce once;
-        e = once_per_device(once, [](int) { return cudaFuncSetAttribute(small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem); });
+        e = once_per_device(once, [](int) {
+            const cudaError_t err = cudaFuncSetAttribute(small_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(4));
+            return err != cudaSuccess ? err : cudaFuncSetAttribute(small_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8));
+        });
         const auto map = [&](CUtensorMap* to, const __half* base, int64_t rows, int64_t cols, int64_t pitch) {
             return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, rows, q.count, pitch * 2, rows * pitch * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
         };
@@ -606,7 +612,9 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
         if (!map(&maps.X[0], X[0], m, n, q.n_pitch) || !map(&maps.X[1], X[1], m, n, q.n_pitch) || !map(&maps.A, A, m, m, mp) || !map(&maps.B, B, m, m, mp))
             return cudaErrorInvalidValue;
         const SmallParams p = {q.m, q.n, steps, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
-        if (e == cudaSuccess) e = launch_dependent(&small_kernel, dim3(kSmallBlocks * q.count), dim3(kSmallThreads), kSmallSmem, st, maps, p);
+        const int stages = kSmallBlocks * q.count <= sm_count ? 8 : 4;
+        if (e == cudaSuccess)
+            e = launch_dependent(stages == 8 ? &small_kernel<8> : &small_kernel<4>, dim3(kSmallBlocks * q.count), dim3(kSmallThreads), small_smem(stages), st, maps, p);
         q.hi = X[steps & 1];
         if (e == cudaSuccess) e = launch_dependent(&finish_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
         return e;
