@@ -594,7 +594,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     q.S = (float)std::ldexp(1.0, (int)std::lround(0.5 * std::log2((double)n)));
     q.growth = (float)std::pow((double)kA, (double)steps);
     const int64_t pieces = (m * n + 8 * kThreads - 1) / (8 * kThreads);
-    q.n_parts = (int)std::max<int64_t>(1, std::min<int64_t>({pieces, (int64_t)kMaxParts, 8 * (int64_t)sm_count / q.count}));
+    q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);          // whatever goes beside it: a matrix's bits are its own
     cudaError_t e = launch_dependent(&momentum_kernel, dim3(q.n_parts, q.count), dim3(kThreads), 0, st, q);
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
     const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 8 * sm_count / q.count));

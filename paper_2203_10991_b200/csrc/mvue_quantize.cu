@@ -128,8 +128,11 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
 // NaN codes for elements that have none other.
 template <typename T> __device__ __forceinline__ void put_nan(const Eight<T>& x, uint2& v) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if ((__float_as_uint(x.at(i)) & 0x7FFFFFFFu) >= kInf) (i < 4 ? v.x : v.y) |= 0x7Fu << (8 * (i & 3));
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = __float_as_uint(x.at(i)), at = 8 * (i & 3);
+        uint32_t& w = i < 4 ? v.x : v.y;
+        if ((bits & 0x7FFFFFFFu) >= kInf) w = (w & ~(0xFFu << at)) | ((0x7Fu | bits >> 24 & 0x80u) << at);
+    }
 }
 
 // Four codes rounded at random: y = the elements over their scale, times 2^-120.  The code fills the highest byte of the bits four
