@@ -632,47 +632,59 @@ def mvue_quantize_e4m3(x: torch.Tensor, block_rows: int = 1, *, seed: int | None
     blocks = -(-cols // SCALE_BLOCK)
     shape = (blocks, rows) if block_rows == 1 else (-(-rows // SCALE_BLOCK), blocks)
     if codes is None:
-        codes = x.new_empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn)[:, :cols]
+        pitch = -(-cols // 16) * 16
+        codes = x.new_empty((rows, pitch), dtype=torch.float8_e4m3fn)
+        if pitch != cols:
+            codes = codes[:, :cols]
     elif codes.shape != x.shape:
         raise ValueError("codes have the shape of x")
+    else:
+        pitch = _code_pitch(codes)
     if scales is None:
         scales = x.new_empty(shape, dtype=torch.uint8)
     else:
         _scale_bytes(scales, shape)
     _check(lib().mvue_quantize_e4m3(x.data_ptr(), _dtype_code(x), rows, cols, x.stride(0) if rows > 1 else cols, block_rows,
                                     MVUE_OPT_NONE if seed is None else MVUE_OPT_STOCHASTIC_ROUNDING, (seed or 0) & (2**64 - 1),
-                                    codes.data_ptr(), _code_pitch(codes), scales.data_ptr(), _stream_ptr()), "mvue_quantize_e4m3")
+                                    codes.data_ptr(), pitch, scales.data_ptr(), _stream_ptr()), "mvue_quantize_e4m3")
     return codes, scales
+
+
+_CODE_DTYPES = (torch.float8_e4m3fn, torch.uint8)
 
 
 def _code_pitch(codes: torch.Tensor) -> int:
     """Bytes from row to row of a matrix of e4m3 codes."""
-    if codes.dim() != 2 or codes.dtype not in (torch.float8_e4m3fn, torch.uint8) or (codes.stride(1) != 1 and codes.shape[1] != 1):
+    if codes.dim() != 2 or codes.dtype not in _CODE_DTYPES or (codes.stride(1) != 1 and codes.size(1) != 1):
         raise ValueError("codes are a float8_e4m3fn matrix with unit column stride")
-    return codes.stride(0) if codes.shape[0] > 1 else -(-codes.shape[1] // 16) * 16
+    return codes.stride(0) if codes.size(0) > 1 else -(-codes.size(1) // 16) * 16
 
 
 def _scale_bytes(scales: torch.Tensor, shape: tuple[int, int]) -> None:
-    if scales.dtype is not torch.uint8 or tuple(scales.shape) != shape or not scales.is_contiguous():
+    if scales.dtype is not torch.uint8 or scales.shape != shape or not scales.is_contiguous():
         raise ValueError(f"wants contiguous uint8 scales {list(shape)}")
 
 
-def _scaled_gemm(name, a, a_scales, W, W_scales, n, k, w_k, out, out_dtype, dev_status):
+def _scaled_gemm(name, forward, a, a_scales, W, W_scales, out, out_dtype, dev_status):
     _operands(a, a_scales, W, W_scales, out, dev_status=dev_status)
     lda, ldw = _code_pitch(a), _code_pitch(W)
-    if k != w_k:
+    rows, k = a.shape
+    outs, ins = W.shape
+    n = outs if forward else ins
+    if k != (ins if forward else outs):
         raise ValueError("the operands differ along the reduction axis")
-    rows = a.shape[0]
     _scale_bytes(a_scales, (-(-k // SCALE_BLOCK), rows))
-    _scale_bytes(W_scales, tuple(-(-d // SCALE_BLOCK) for d in W.shape))
+    _scale_bytes(W_scales, (-(-outs // SCALE_BLOCK), -(-ins // SCALE_BLOCK)))
     if out is None:
         out = a.new_empty((rows, n), dtype=out_dtype)
         ldc = n
     else:
         assert out.shape == (rows, n) and (out.stride(1) == 1 or n == 1)
         ldc = out.stride(0) if rows > 1 else n
-    _check(getattr(lib(), name)(a.data_ptr(), a_scales.data_ptr(), rows, k, lda, W.data_ptr(), W_scales.data_ptr(), n, ldw, out.data_ptr(),
-                                _dtype_code(out), ldc, _ptr(dev_status), _stream_ptr()), name)
+    status = getattr(lib(), name)(a.data_ptr(), a_scales.data_ptr(), rows, k, lda, W.data_ptr(), W_scales.data_ptr(), n, ldw, out.data_ptr(),
+                                  _dtype_code(out), ldc, None if dev_status is None else dev_status.data_ptr(), _stream_ptr())
+    if status != 0:
+        _check(status, name)
     return out
 
 
@@ -680,13 +692,13 @@ def mvue_scaled_forward_gemm(x: torch.Tensor, x_scales: torch.Tensor, W: torch.T
                              out: torch.Tensor | None = None, out_dtype=torch.bfloat16, dev_status: torch.Tensor | None = None) -> torch.Tensor:
     """x . W^T from e4m3 codes: x [tokens, in] with scales [ceil(in / 128), tokens], W [out, in] with scales
     [ceil(out / 128), ceil(in / 128)] (what mvue_quantize_e4m3 returns for block_rows = 1 and 128).  bf16 or fp32 out."""
-    return _scaled_gemm("mvue_scaled_forward_gemm", x, x_scales, W, W_scales, W.shape[0], x.shape[-1], W.shape[-1], out, out_dtype, dev_status)
+    return _scaled_gemm("mvue_scaled_forward_gemm", True, x, x_scales, W, W_scales, out, out_dtype, dev_status)
 
 
 def mvue_scaled_backward_gemm(g: torch.Tensor, g_scales: torch.Tensor, W: torch.Tensor, W_scales: torch.Tensor, *,
                               out: torch.Tensor | None = None, out_dtype=torch.bfloat16, dev_status: torch.Tensor | None = None) -> torch.Tensor:
     """g . W from e4m3 codes: g [tokens, out] with scales [ceil(out / 128), tokens]; W and its scales as in the forward product."""
-    return _scaled_gemm("mvue_scaled_backward_gemm", g, g_scales, W, W_scales, W.shape[-1], g.shape[-1], W.shape[0], out, out_dtype, dev_status)
+    return _scaled_gemm("mvue_scaled_backward_gemm", False, g, g_scales, W, W_scales, out, out_dtype, dev_status)
 
 
 def _matrices(t: torch.Tensor):
