@@ -205,6 +205,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
     cluster_sync();                          // the peer's barriers exist before anyone signals them
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    grid_launch_dependents();
     grid_dependency_wait();                  // nothing above touches global memory
 
     if (warp == 0) {

@@ -21,6 +21,11 @@ namespace mvue {
 __device__ __forceinline__ void grid_dependency_wait() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
+// Lets the next kernel of the stream be set up from now on (once all of this grid's blocks have come here): for kernels whose
+// successors wait as above before they touch memory, which every kernel of the library does.
+__device__ __forceinline__ void grid_launch_dependents() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 // ---------------------------------------------------------------------------
 // Philox4x32 with ten rounds (Salmon et al., SC'11).  The ten round keys depend

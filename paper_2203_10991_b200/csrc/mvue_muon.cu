@@ -383,20 +383,25 @@ struct Apply {
     }
 };
 
-// ---- all steps of a small matrix in one launch ---------------------------------------------------------------------------
-// A cluster of eight blocks per matrix goes through the products with a cluster barrier between them instead of a launch: fifteen dependent
-// launches of a product that takes two microseconds cost nine each.  Tiles of 128 x 64, a block's own; operands by TMA from L2, where the
-// last product's results are.
+// ---- small matrices --------------------------------------------------------------------------------------------------------
+// Tiles of 128 x 64, one thread block each; operands by TMA from L2, where the last product's results are.
+// kCluster: a cluster of eight blocks per matrix goes through all products with a cluster barrier between them instead of a launch
+// (fifteen dependent launches of a product that takes two microseconds cost nine each).  Else one product a launch, a block per tile:
+// for matrices that pair tiles would leave most SMs without.
 //   warps 0-3 epilogue      warp 4 TMA producer      warp 5 tensor-memory allocation, MMA issue
-// A block has eight stages and an SM to itself where the clusters leave room for that, else four.
+// A block has eight stages and an SM to itself where the blocks leave room for that, else four.
 constexpr int kSmallBlocks = 8, kSmallThreads = 192;
 constexpr int kSmallBox = 64 * 128, kSmallStage = 3 * kSmallBox;        // 128 rows of the first operand, 64 of the second
 constexpr int small_smem(int stages) { return stages * kSmallStage + 256 + 1024; }
 constexpr int kSmallM = 256;
 constexpr int64_t kSmallElements = 256 * 1024;
+// One product a launch while X has no more than this many tiles of 256 x 256 in all matrices: 512 x 512 94 us (pair tiles 165 us),
+// 1024 x 1024 133 us (200 us); 1024 x 4096, 64 tiles, 290 us either way.
+constexpr int64_t kSmallPairTiles = 40;
 
 struct SmallParams {
     int m, n, steps;
+    int blocks, first, last;                 // blocks of a matrix; phases (three a step)
     int64_t n_pitch, m_pitch;
     __half *X[2], *lo, *A, *B;
     const float* xs;
@@ -422,8 +427,8 @@ __device__ __forceinline__ void store_row(__half* to, int left, const uint4 (&w)
         if (8 * i < left) *reinterpret_cast<uint4*>(to + 8 * i) = w[i];
 }
 
-template <int kSmallStages>
-__global__ void __cluster_dims__(kSmallBlocks, 1, 1) __launch_bounds__(kSmallThreads, kSmallStages == 4 ? 2 : 1)
+template <int kSmallStages, bool kCluster>
+__global__ void __launch_bounds__(kSmallThreads, kSmallStages == 4 ? 2 : 1)
 small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ SmallParams p) {
     extern __shared__ uint8_t smem_raw[];
     constexpr int kSmallBars = kSmallStages * kSmallStage;
@@ -436,7 +441,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
     const auto free_bar = [&](int b) { return bar_base + 8u * (2 * kSmallStages + 2 + b); };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + kSmallBars + 8 * (2 * kSmallStages + 4));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = (int)cluster_ctarank(), z = blockIdx.x / kSmallBlocks;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, z = blockIdx.x / p.blocks, rank = blockIdx.x - z * p.blocks;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSmallStages; ++s) {
@@ -458,13 +463,14 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    grid_launch_dependents();
     grid_dependency_wait();
 
     const int64_t x0 = (int64_t)z * p.m * p.n_pitch, a0 = (int64_t)z * p.m * p.m_pitch;
     const float xs = p.xs[z];
     int s = 0, done = 0;                                     // stage, tiles of this block so far: each role counts for itself
     uint32_t parity = warp == 4 ? 1u : 0u;
-    for (int phase = 0; phase < 3 * p.steps; ++phase) {
+    for (int phase = p.first; phase < p.last; ++phase) {
         const int k = phase / 3, what = phase - 3 * k;       // 0: A = X X^T, 1: B = b A + c A A, 2: X' = a X + B X
         const int N = what == 2 ? p.n : p.m, K = what == 0 ? p.n : p.m;
         const int tiles_n = (N + 63) / 64, tiles = (p.m + 127) / 128 * tiles_n, steps = (K + 63) / 64;
@@ -473,7 +479,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
             const CUtensorMap* first = what == 0 ? &maps.X[k & 1] : what == 1 ? &maps.A : &maps.B;
             const CUtensorMap* second = what == 1 ? &maps.A : &maps.X[k & 1];
             bool ok = true;
-            for (int t = rank; t < tiles && ok; t += kSmallBlocks) {
+            for (int t = rank; t < tiles && ok; t += p.blocks) {
                 const int m0 = t / tiles_n * 128, n0 = t % tiles_n * 64;
                 for (int i = 0; i < steps; ++i) {
                     if (!(ok = mbar_wait(empty_bar(s), parity, abort_flag))) break;
@@ -490,7 +496,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
             const uint64_t da = make_smem_desc(smem_base, 16, 1024, kSwizzle128B), db = make_smem_desc(smem_base + 2 * kSmallBox, kSmallBox, 1024, kSwizzle128B);
             const int b_step = what == 2 ? 16 * 128 / 16 : 2;
             bool ok = true;
-            for (int t = rank; t < tiles && ok; t += kSmallBlocks, ++done) {
+            for (int t = rank; t < tiles && ok; t += p.blocks, ++done) {
                 if (done > 1) {
                     if (!(ok = mbar_wait(free_bar(done & 1), ((done >> 1) - 1) & 1u, abort_flag))) break;
                     tc_fence_after();
@@ -512,7 +518,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
             const __half* hi = p.X[k & 1];
             const bool read_lo = what == 2 && k < p.steps - 2, write_lo = what == 2 && k + 1 < p.steps - 2;
             const float alpha = what == 0 ? p.S / xs / xs : what == 1 ? kC / p.S : 1.0f / p.S;
-            for (int t = rank; t < tiles; t += kSmallBlocks, ++done) {
+            for (int t = rank; t < tiles; t += p.blocks, ++done) {
                 const int row = t / tiles_n * 128 + 32 * warp + lane, n0 = t % tiles_n * 64;
                 const int64_t at = what == 2 ? x0 + row * p.n_pitch + n0 : a0 + row * p.m_pitch + n0;
                 const bool there = row < p.m;
@@ -548,7 +554,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
             asm volatile("fence.proxy.async.global;" ::: "memory");
         }
         __syncwarp();
-        cluster_sync();                      // the product is complete and seen by the cluster's copies
+        if (kCluster) cluster_sync();        // the product is complete and seen by the cluster's copies
     }
 
     tc_fence_before();
@@ -580,6 +586,31 @@ bool extents_ok(int64_t rows, int64_t cols) {
            std::min(rows, cols) <= (1 << 20);
 }
 
+template <bool kCluster> cudaError_t launch_small(const SmallMaps& maps, const SmallParams& p, int count, int sm_count, cudaStream_t stream) {
+    static PerDeviceOnce once;
+    cudaError_t e = once_per_device(once, [](int) {
+        const cudaError_t err = cudaFuncSetAttribute(small_kernel<4, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(4));
+        return err != cudaSuccess ? err : cudaFuncSetAttribute(small_kernel<8, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8));
+    });
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = (int64_t)p.blocks * count;
+    const int stages = blocks <= sm_count ? 8 : 4;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = (size_t)small_smem(stages);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kSmallBlocks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kCluster ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, stages == 8 ? &small_kernel<8, kCluster> : &small_kernel<4, kCluster>, maps, p);
+}
+
 // The whole step of the q.count matrices of q, which have the extents q.m <= q.n.
 cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_count, cudaStream_t st) {
     const int64_t m = q.m, n = q.n, mp = pitch_of(m);
@@ -599,22 +630,26 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
     const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 8 * sm_count / q.count));
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
-    if (e == cudaSuccess && m <= kSmallM && m * n <= kSmallElements) {
-        static PerDeviceOnce once;
-        e = once_per_device(once, [](int) {
-            const cudaError_t err = cudaFuncSetAttribute(small_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(4));
-            return err != cudaSuccess ? err : cudaFuncSetAttribute(small_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8));
-        });
+    const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256) * q.count;
+    const bool cluster = m <= kSmallM && m * n <= kSmallElements;
+    if (e == cudaSuccess && (cluster || pair_tiles <= kSmallPairTiles)) {
         const auto map = [&](CUtensorMap* to, const __half* base, int64_t rows, int64_t cols, int64_t pitch) {
             return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, rows, q.count, pitch * 2, rows * pitch * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
         };
         SmallMaps maps;
         if (!map(&maps.X[0], X[0], m, n, q.n_pitch) || !map(&maps.X[1], X[1], m, n, q.n_pitch) || !map(&maps.A, A, m, m, mp) || !map(&maps.B, B, m, m, mp))
             return cudaErrorInvalidValue;
-        const SmallParams p = {q.m, q.n, steps, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
-        const int stages = kSmallBlocks * q.count <= sm_count ? 8 : 4;
-        if (e == cudaSuccess)
-            e = launch_dependent(stages == 8 ? &small_kernel<8> : &small_kernel<4>, dim3(kSmallBlocks * q.count), dim3(kSmallThreads), small_smem(stages), st, maps, p);
+        SmallParams p = {q.m, q.n, steps, kSmallBlocks, 0, 3 * steps, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
+        if (cluster) {
+            e = launch_small<true>(maps, p, q.count, sm_count, st);
+        } else {
+            for (int phase = 0; phase < 3 * steps && e == cudaSuccess; ++phase) {
+                p.first = phase;
+                p.last = phase + 1;
+                p.blocks = (int)((m + 127) / 128 * (((phase % 3 == 2 ? n : m) + 63) / 64));
+                e = launch_small<false>(maps, p, q.count, sm_count, st);
+            }
+        }
         q.hi = X[steps & 1];
         if (e == cudaSuccess) e = launch_dependent(&finish_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
         return e;
