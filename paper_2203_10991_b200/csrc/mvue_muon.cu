@@ -628,7 +628,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);          // whatever goes beside it: a matrix's bits are its own
     cudaError_t e = launch_dependent(&momentum_kernel, dim3(q.n_parts, q.count), dim3(kThreads), 0, st, q);
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
-    const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 8 * sm_count / q.count));
+    const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 32 * sm_count / q.count));
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256) * q.count;
     const bool cluster = m <= kSmallM && m * n <= kSmallElements;
