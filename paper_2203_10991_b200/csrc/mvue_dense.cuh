@@ -117,9 +117,9 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int 
 }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 
-// The matrices of a slab epilogue: up to two read, two written (the second may be the mirror image of the first).
+// The matrices of a slab epilogue: one read, two written (the second may be the mirror image of the first).
 struct SlabMaps {
-    CUtensorMap in[2], out[2];
+    CUtensorMap in, out[2];
 };
 struct NoMaps {};
 
@@ -325,7 +325,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         if constexpr (Epilogue::kSlabs) {
             if (lane == 0) {
                 constexpr int kPer = S::kBN / 64;                // slabs of a tile
-                // reads run two slabs ahead of writes; a buffer is free when the write before the last has been taken from it
+                // reads run a ring less one slab ahead of writes; a buffer is free when the write before the last has been taken from it
                 int64_t w_in = first, w_out = first;
                 int at_in = 0, at_out = 0, buf_in = 0, buf_out = 0;
                 uint32_t parity = 0u;
@@ -334,18 +334,15 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                     if (Epilogue::kIn > 0) {
                         const Tile t = tile_at(p, w_in, S::kBN);
                         const uint32_t to = smem_base + kSlabs + buf_in * 2 * kSlabBytes;
-                        mbar_expect_tx(slab_in_bar(buf_in), Epilogue::kIn * kSlabBytes);
-                        tma_load_3d(to, &maps.in[0], t.n + 64 * at_in, t.m + (int)rank * kRowsA, t.z, slab_in_bar(buf_in));
-                        if (Epilogue::kIn > 1)
-                            tma_load_3d(to + kSlabBytes, &maps.in[1], t.n + 64 * at_in, t.m + (int)rank * kRowsA, t.z, slab_in_bar(buf_in));
+                        mbar_expect_tx(slab_in_bar(buf_in), kSlabBytes);
+                        tma_load_3d(to, &maps.in, t.n + 64 * at_in, t.m + (int)rank * kRowsA, t.z, slab_in_bar(buf_in));
                     } else {
                         mbar_arrive(slab_in_bar(buf_in));
                     }
                     if (++buf_in == kSlabBufs) buf_in = 0;
                     if (++at_in == kPer) { at_in = 0; w_in += n_pairs; }
                 };
-                read();
-                read();
+                for (int i = 1; i < kSlabBufs; ++i) read();
                 while (w_out < p.n_work) {
                     if (!mbar_wait(slab_out_bar(buf_out), parity, abort_flag)) break;
                     const Tile t = tile_at(p, w_out, S::kBN);
@@ -394,7 +391,6 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (Epilogue::kIn > 0) x[0][i] = *piece(i);
-                        if (Epilogue::kIn > 1) x[1][i] = *(piece(i) + kSlabBytes / 16);
                     }
                     tmem_ld_wait();
                     if (c == S::kBN / 64 - 1) {                  // the accumulator is in registers: it may be overwritten
@@ -403,11 +399,11 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         if (lane == 0)
                             asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_free[par]) : "memory");
                     }
-                    epi.compute(values, v, x);
+                    epi.compute(values, v, x, t.m + (int)rank * kRowsA + 32 * q == t.n + 64 * c + 32 * half ? lane : -1);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         *piece(i) = x[0][i];
-                        if (!Epilogue::kMirror) *(piece(i) + kSlabBytes / 16) = x[1][i];
+                        if (!Epilogue::kMirror && epi.two_out()) *(piece(i) + kSlabBytes / 16) = x[1][i];
                     }
                     if (Epilogue::kMirror && t.m != t.n) {       // [64 columns][128 rows]
                         unsigned short* to = reinterpret_cast<unsigned short*>(slab + kSlabBytes) + 32 * half * kRowsA + row;

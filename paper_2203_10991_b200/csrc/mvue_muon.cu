@@ -1,12 +1,12 @@
 // The Muon step: momentum, the update's orthogonalisation by Newton-Schulz products, the param.
 //
 // With X the update over its norm, transposed where it has more rows than columns ([m x n], m <= n), a step of the iteration is
-//   A = X X^T;  B = b A + c A A;  X' = a X + B X
+//   A = X X^T;  B = a I + b A + c A A;  X' = B X
 // Products are binary16 on the tensor cores with fp32 accumulators: binary16 and not bf16, since the polynomial's slope of a = 3.4
 // at zero multiplies what a rounding adds to small singular values by up to 485 in five steps (an update of sixteen large
-// directions and noise a tenth as strong comes out 9 % off with bf16, 1 % with binary16).  The same update is 0.08 % off if, in all
-// steps but the last two, the term a X is taken from a second binary16 beside the first (x = hi + lo 2^-11): the error of B X lies in
-// few directions, that of a X in all.
+// directions and noise a tenth as strong comes out 9 % off with bf16, 1 % with binary16).  The same update is 0.1 % off if, in all
+// steps but the last two, a second binary16 beside the first (x = hi + lo 2^-11) adds a lo to B hi: what the roundings of B do lies in
+// few directions, what that of X does in all.
 // A and B are symmetric: only tiles on and above the diagonal are computed, and stored twice.
 // X is stored times xs, A and B times S, powers of two near the root of n, so that entries of 1 / sqrt(n) stay normal numbers; xs is larger for
 // an update far below eps.
@@ -318,7 +318,8 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-// A S = acc S / xs^2 (kPoly false), B S = b (A S) + c acc / S (true); symmetric, the tile's mirror image is stored too.
+// A S = acc S / xs^2 (kPoly false), B S = a S on the diagonal + b (A S) + c acc / S (true); symmetric, the tile's mirror image is stored
+// too.  diag: the column of these 32 that is the row's own, or -1.
 template <bool kPoly>
 struct Symmetric {
     using Maps = dense::SlabMaps;
@@ -328,7 +329,7 @@ struct Symmetric {
     float S;
     __device__ __forceinline__ bool two_out() const { return true; }
     __device__ __forceinline__ float values(int z) const { return kPoly ? kC / S : S / xs[z] / xs[z]; }
-    __device__ __forceinline__ void compute(float alpha, const uint32_t (&v)[32], uint4 (&x)[2][4]) const {
+    __device__ __forceinline__ void compute(float alpha, const uint32_t (&v)[32], uint4 (&x)[2][4], int diag) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t w[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w};
@@ -339,6 +340,10 @@ struct Symmetric {
                     const float2 a = halves(w[j]);
                     lo = fmaf(kB, a.x, lo);
                     hi = fmaf(kB, a.y, hi);
+                    if (diag >= 0) {                         // (a whole warp)
+                        if (8 * i + 2 * j == diag) lo = fmaf(kA, S, lo);
+                        if (8 * i + 2 * j + 1 == diag) hi = fmaf(kA, S, hi);
+                    }
                 }
                 w[j] = half_pair(lo, hi);
             }
@@ -347,30 +352,29 @@ struct Symmetric {
     }
 };
 
-// X' xs = a (X xs) + acc / S, with (kLo) or without the second half of X.
+// X' xs = acc / S, and with kWithLo a times the second half of X, which comes in x[0].
 template <bool kWithLo>
 struct Apply {
     using Maps = dense::SlabMaps;
     static constexpr bool kSlabs = true, kMirror = false;
-    static constexpr int kIn = kWithLo ? 2 : 1;
+    static constexpr int kIn = kWithLo ? 1 : 0;
     float inv_S;
     int write_lo;
     __device__ __forceinline__ bool two_out() const { return kWithLo && write_lo; }
     __device__ __forceinline__ float values(int) const { return inv_S; }
-    __device__ __forceinline__ void compute(float scale, const uint32_t (&v)[32], uint4 (&x)[2][4]) const {
+    __device__ __forceinline__ void compute(float scale, const uint32_t (&v)[32], uint4 (&x)[2][4], int) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint32_t h[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w}, l[4] = {};
-            if (kWithLo) { l[0] = x[1][i].x; l[1] = x[1][i].y; l[2] = x[1][i].z; l[3] = x[1][i].w; }
+            uint32_t h[4], l[4] = {};
+            if (kWithLo) { l[0] = x[0][i].x; l[1] = x[0][i].y; l[2] = x[0][i].z; l[3] = x[0][i].w; }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float2 f = halves(h[j]);
+                float a = __uint_as_float(v[8 * i + 2 * j]) * scale, b = __uint_as_float(v[8 * i + 2 * j + 1]) * scale;
                 if (kWithLo) {
                     const float2 y = halves(l[j]);
-                    f.x = fmaf(y.x, 1.0f / kLo, f.x);
-                    f.y = fmaf(y.y, 1.0f / kLo, f.y);
+                    a = fmaf(kA / kLo, y.x, a);
+                    b = fmaf(kA / kLo, y.y, b);
                 }
-                const float a = fmaf(kA, f.x, __uint_as_float(v[8 * i + 2 * j]) * scale), b = fmaf(kA, f.y, __uint_as_float(v[8 * i + 2 * j + 1]) * scale);
                 h[j] = half_pair(a, b);
                 if (kWithLo) {
                     const float2 r = halves(h[j]);
@@ -378,7 +382,7 @@ struct Apply {
                 }
             }
             x[0][i] = make_uint4(h[0], h[1], h[2], h[3]);
-            x[1][i] = make_uint4(l[0], l[1], l[2], l[3]);
+            if (kWithLo) x[1][i] = make_uint4(l[0], l[1], l[2], l[3]);
         }
     }
 };
@@ -471,7 +475,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
     int s = 0, done = 0;                                     // stage, tiles of this block so far: each role counts for itself
     uint32_t parity = warp == 4 ? 1u : 0u;
     for (int phase = p.first; phase < p.last; ++phase) {
-        const int k = phase / 3, what = phase - 3 * k;       // 0: A = X X^T, 1: B = b A + c A A, 2: X' = a X + B X
+        const int k = phase / 3, what = phase - 3 * k;       // 0: A = X X^T, 1: B = a I + b A + c A A, 2: X' = B X
         const int N = what == 2 ? p.n : p.m, K = what == 0 ? p.n : p.m;
         const int tiles_n = (N + 63) / 64, tiles = (p.m + 127) / 128 * tiles_n, steps = (K + 63) / 64;
         if (warp == 4 && lane == 0) {
@@ -515,7 +519,6 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
                 tc_commit(acc_bar(done & 1));
             }
         } else if (warp < 4) {
-            const __half* hi = p.X[k & 1];
             const bool read_lo = what == 2 && k < p.steps - 2, write_lo = what == 2 && k + 1 < p.steps - 2;
             const float alpha = what == 0 ? p.S / xs / xs : what == 1 ? kC / p.S : 1.0f / p.S;
             for (int t = rank; t < tiles; t += p.blocks, ++done) {
@@ -528,8 +531,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
                 for (int c = 0; c < 2; ++c) {
                     const int left = there ? N - n0 - 32 * c : 0;
                     if (what == 1) load_row(p.A + at + 32 * c, left, x[c][0]);
-                    if (what == 2) load_row(hi + at + 32 * c, left, x[c][0]);
-                    if (read_lo) load_row(p.lo + at + 32 * c, left, x[c][1]);
+                    if (read_lo) load_row(p.lo + at + 32 * c, left, x[c][0]);
                 }
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(done & 1), (done >> 1) & 1u, abort_flag))) break;
                 tc_fence_after();
@@ -543,10 +545,10 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const int left = there ? N - n0 - 32 * c : 0;
-                    if (what == 0) Symmetric<false>{nullptr, 0.0f}.compute(alpha, v[c], x[c]);
-                    else if (what == 1) Symmetric<true>{nullptr, 0.0f}.compute(alpha, v[c], x[c]);
-                    else if (read_lo) Apply<true>{0.0f, 0}.compute(alpha, v[c], x[c]);
-                    else Apply<false>{0.0f, 0}.compute(alpha, v[c], x[c]);
+                    if (what == 0) Symmetric<false>{nullptr, p.S}.compute(alpha, v[c], x[c], -1);
+                    else if (what == 1) Symmetric<true>{nullptr, p.S}.compute(alpha, v[c], x[c], row - lane == n0 + 32 * c ? lane : -1);
+                    else if (read_lo) Apply<true>{0.0f, 0}.compute(alpha, v[c], x[c], -1);
+                    else Apply<false>{0.0f, 0}.compute(alpha, v[c], x[c], -1);
                     store_row((what == 0 ? p.A : what == 1 ? p.B : p.X[(k + 1) & 1]) + at + 32 * c, left, x[c][0]);
                     if (write_lo) store_row(p.lo + at + 32 * c, left, x[c][1]);
                 }
@@ -663,11 +665,10 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
         dense::SlabMaps gram, poly, apply;
         if (!dense::make_slab_map(&gram.out[0], oa, m, m, q.count, false) || !dense::make_slab_map(&gram.out[1], oa, m, m, q.count, true) ||
             !dense::make_slab_map(&poly.out[0], ob, m, m, q.count, false) || !dense::make_slab_map(&poly.out[1], ob, m, m, q.count, true) ||
-            !dense::make_slab_map(&apply.in[0], ox, m, n, q.count, false) || !dense::make_slab_map(&apply.out[0], oy, m, n, q.count, false) ||
-            !dense::make_slab_map(&apply.in[1], olo, m, n, q.count, false))
+            !dense::make_slab_map(&apply.out[0], oy, m, n, q.count, false) || !dense::make_slab_map(&apply.out[1], olo, m, n, q.count, false))
             return cudaErrorInvalidValue;
-        gram.in[0] = gram.in[1] = poly.in[0] = poly.in[1] = gram.out[0];
-        apply.out[1] = apply.in[1];
+        gram.in = poly.in = gram.out[0];
+        apply.in = apply.out[1];
         dense::Params p = {};
         p.batch = q.count;
         p.dev_status = dev_status;

@@ -120,7 +120,8 @@ def orthogonalize(x, steps=5):
 
 def orthogonalize_rounded(x, steps=5):
     """The same with the binary16 roundings of the operands (in the power-of-two scale S of the entries, S = 2^round(log2(n) / 2)), sums
-    in 64 bits: X, A and B rounded once each step; the term a X unrounded (22 bits) in all steps but the last two."""
+    in 64 bits: X, A and a I + b A + c A A rounded once each step; what X loses is added to the product, a times it, in all steps but
+    the last two."""
     x = x.double()
     flip = x.shape[-2] > x.shape[-1]
     x = x.mT if flip else x
@@ -130,6 +131,6 @@ def orthogonalize_rounded(x, steps=5):
     for k in range(steps):
         r = h(x)
         s = h(r @ r.mT)
-        b = h(B * s + C * (s @ s))
-        x = A * (x if k < steps - 2 else r) + b @ r
+        b = h(A * torch.eye(s.shape[-1], dtype=s.dtype, device=s.device) + B * s + C * (s @ s))
+        x = b @ r + (A * (x - r) if k < steps - 2 else 0)
     return h(x).mT if flip else h(x)
