@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kMaxTeam = 512;                    // threads; eight columns each in the kernels for any alignment
 constexpr int kWideThreads = 1024;
+constexpr int kWideSlabs = 3;                    // wide rows of so many slabs of 8192 columns have their column sums in shared memory
 constexpr int kColumnRows = 8;                   // wide: teams of a warp in a column block
 
 struct Params {
@@ -42,6 +43,11 @@ template <int kVec> __device__ __forceinline__ void load_affine(const Cols<kVec>
     if (!from) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = none;
+        return;
+    }
+    if (kVec == 8 && c.count == 8 && (reinterpret_cast<uintptr_t>(from) & 31u) == 0) {
+        if (bf16) load8(static_cast<const __nv_bfloat16*>(from) + c.first, true, 8, v);
+        else load8(static_cast<const float*>(from) + c.first, true, 8, v);
         return;
     }
 #pragma unroll
@@ -448,16 +454,27 @@ __global__ void __launch_bounds__(kMaxTeam) forward_kernel(const __grid_constant
     const T* x = static_cast<const T*>(p.x);
     T* y = static_cast<T*>(p.y);
     const bool mine = c.count > 0;
-    for (int64_t row = ((int64_t)blockIdx.x * blockDim.y + team) * kR; row < p.rows; row += (int64_t)gridDim.x * blockDim.y * kR) {
-        float v[kR][8], s[kR];
+    const int64_t stride = (int64_t)gridDim.x * blockDim.y * kR;
+    int64_t row = ((int64_t)blockIdx.x * blockDim.y + team) * kR;
+    float next[kR][8];                                       // the rows to come, on their way while these are worked on
+    const auto fetch = [&](int64_t from) {
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
-            if (mine && row + r < p.rows) c.load(x + (row + r) * p.ldx, v[r]);
+            if (mine && from + r < p.rows) c.load(x + (from + r) * p.ldx, next[r]);
             else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[r][j] = 0.0f;
+                for (int j = 0; j < 8; ++j) next[r][j] = 0.0f;
             }
         }
+    };
+    fetch(row);
+    for (; row < p.rows; row += stride) {
+        float v[kR][8], s[kR];
+#pragma unroll
+        for (int r = 0; r < kR; ++r)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[r][j] = next[r][j];
+        fetch(row + stride);
 #pragma unroll
         for (int r = 0; r < kR; ++r) s[r] = ((v[r][0] + v[r][1]) + (v[r][2] + v[r][3])) + ((v[r][4] + v[r][5]) + (v[r][6] + v[r][7]));
         team_sum<kR>(s, sums0, team, threads, warp, lane);
@@ -505,25 +522,43 @@ __global__ void __launch_bounds__(kMaxTeam) backward_kernel(const __grid_constan
     const T *x = static_cast<const T*>(p.x), *dy = static_cast<const T*>(p.dy);
     T* dx = static_cast<T*>(p.dx);
     const bool mine = c.count > 0;
+    const int64_t stride = (int64_t)gridDim.x * blockDim.y * 2;
+    int64_t row = ((int64_t)blockIdx.x * blockDim.y + team) * 2;
+    float next_x[2][8], next_g[2][8], next_mean[2], next_rstd[2];
+    const auto fetch = [&](int64_t from) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const bool there = from + r < p.rows;
+            next_mean[r] = there ? p.mean_in[from + r] : 0.0f;
+            next_rstd[r] = there ? p.rstd_in[from + r] : 0.0f;
+            if (mine && there) {
+                c.load(x + (from + r) * p.ldx, next_x[r]);
+                c.load(dy + (from + r) * p.lddy, next_g[r]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) next_x[r][j] = next_g[r][j] = 0.0f;
+            }
+        }
+    };
+    fetch(row);
     int turn = 0;
-    for (int64_t row = ((int64_t)blockIdx.x * blockDim.y + team) * 2; row < p.rows; row += (int64_t)gridDim.x * blockDim.y * 2, turn ^= 1) {
+    for (; row < p.rows; row += stride, turn ^= 1) {
         float xh[2][8], g[2][8], s[4], rstd[2];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const bool there = row + r < p.rows;
-            if (mine && there) {
-                c.load(x + (row + r) * p.ldx, xh[r]);
-                c.load(dy + (row + r) * p.lddy, g[r]);
-            } else {
+            rstd[r] = next_rstd[r];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) xh[r][j] = g[r][j] = 0.0f;
+            for (int j = 0; j < 8; ++j) {
+                xh[r][j] = j < c.count ? (next_x[r][j] - next_mean[r]) * rstd[r] : 0.0f;
+                g[r][j] = next_g[r][j];
             }
-            const float mean = there ? p.mean_in[row + r] : 0.0f;
-            rstd[r] = there ? p.rstd_in[row + r] : 0.0f;
+        }
+        fetch(row + stride);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
             s[2 * r] = s[2 * r + 1] = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                xh[r][j] = j < c.count ? (xh[r][j] - mean) * rstd[r] : 0.0f;
                 if (kSums) {
                     dgamma[j] = fmaf(g[r][j], xh[r][j], dgamma[j]);
                     dbeta[j] += g[r][j];
@@ -637,29 +672,45 @@ __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const __grid
     }
 }
 
-template <typename T, int kVec>
+// kSums: the column sums too, in shared memory, a thread's sixteen of each slab of 8192 columns as four quarters that lie a block's
+// threads apart.
+template <typename T, int kVec, bool kSums>
 __global__ void __launch_bounds__(kWideThreads) wide_backward_kernel(const __grid_constant__ Params p) {
     __shared__ float slots[32];
+    extern __shared__ float4 wide_sums[];
     grid_dependency_wait();
+    if (kSums) {
+        for (int64_t c0 = 0, q = 0; c0 < p.cols; c0 += 8 * kWideThreads)
+            for (int i = 0; i < 4; ++i, ++q) wide_sums[q * kWideThreads + threadIdx.x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const T *x = static_cast<const T*>(p.x) + row * p.ldx, *dy = static_cast<const T*>(p.dy) + row * p.lddy;
         T* dx = static_cast<T*>(p.dx) + row * p.ldy;
         const float mean = p.mean_in[row], rstd = p.rstd_in[row];
         float s0 = 0.0f, s1 = 0.0f, v[8], g[8], gamma[8];
-        const auto take = [&](const Cols<kVec>& c) {
+        const auto take = [&](const Cols<kVec>& c, float4* sums) {
             c.load(x, v);
             c.load(dy, g);
             load_affine(c, p.gamma, p.affine_bf16, 1.0f, gamma);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = j < c.count ? (v[j] - mean) * rstd : 0.0f;
-                g[j] *= gamma[j];
+            for (int j = 0; j < 8; ++j) v[j] = j < c.count ? (v[j] - mean) * rstd : 0.0f;
+            if (kSums && sums) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float4 &a = sums[h * kWideThreads], &b = sums[(2 + h) * kWideThreads];
+                    a = make_float4(fmaf(g[4 * h], v[4 * h], a.x), fmaf(g[4 * h + 1], v[4 * h + 1], a.y), fmaf(g[4 * h + 2], v[4 * h + 2], a.z),
+                                    fmaf(g[4 * h + 3], v[4 * h + 3], a.w));
+                    b = make_float4(b.x + g[4 * h], b.y + g[4 * h + 1], b.z + g[4 * h + 2], b.w + g[4 * h + 3]);
+                }
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] *= gamma[j];
         };
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads) {
+        int64_t slab = 0;
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads, ++slab) {
             const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
             if (c.count == 0) break;
-            take(c);
+            take(c, wide_sums + slab * 4 * kWideThreads + threadIdx.x);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (j < c.count) {
@@ -671,10 +722,30 @@ __global__ void __launch_bounds__(kWideThreads) wide_backward_kernel(const __gri
         for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads) {
             const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
             if (c.count == 0) break;
-            take(c);
+            take(c, nullptr);
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[j] = rstd * (g[j] - fmaf(v[j], m1, m0));
             c.store(dx, g);
+        }
+    }
+    if (kSums) {
+        float* out = p.partial + (int64_t)blockIdx.x * 2 * p.cols;
+        int64_t slab = 0;
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads, ++slab) {
+            const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
+            if (c.count == 0) break;
+            const float4* sums = wide_sums + slab * 4 * kWideThreads + threadIdx.x;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 a = sums[h * kWideThreads], b = sums[(2 + h) * kWideThreads];
+                const float x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (4 * h + j < c.count) {
+                        out[c.at(4 * h + j)] = x[j];
+                        out[p.cols + c.at(4 * h + j)] = y[j];
+                    }
+            }
         }
     }
 }
@@ -770,6 +841,10 @@ Plan plan(bool backward, int64_t rows, int64_t cols, int dtype, int vec, int sm_
     if (cols > 8 * kMaxTeam) {
         q.kind = Plan::kWide;
         q.blocks = (int)std::min<int64_t>(rows, 2 * (int64_t)sm_count);
+        if (backward && cols <= 8 * kWideThreads * kWideSlabs) {
+            q.blocks = q.parts = (int)std::min<int64_t>(rows, sm_count);
+            return q;
+        }
         const int64_t slabs = (cols + 255) / 256;
         q.parts = (int)std::max<int64_t>(1, std::min<int64_t>((rows + 4 * kColumnRows - 1) / (4 * kColumnRows), 8 * (int64_t)sm_count / slabs));
         q.columns = dim3((unsigned)slabs, (unsigned)q.parts);
@@ -827,10 +902,19 @@ template <typename T, int kVec, bool kSums> cudaError_t backward(const Plan& q, 
         }
     }
     if (q.kind == Plan::kWide) {
+        const int slabs = (int)((p.cols + 8 * kWideThreads - 1) / (8 * kWideThreads));
+        if (kSums && slabs <= kWideSlabs) {
+            static PerDeviceOnce once;
+            const cudaError_t e = once_per_device(once, [](int) {
+                return cudaFuncSetAttribute(&wide_backward_kernel<T, kVec, kSums>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSlabs * 64 * kWideThreads);
+            });
+            if (e != cudaSuccess) return e;
+            return launch_dependent(&wide_backward_kernel<T, kVec, kSums>, dim3(q.blocks), dim3(kWideThreads), (size_t)slabs * 64 * kWideThreads, st, p);
+        }
         cudaError_t e = cudaSuccess;
         if (kSums) e = launch_dependent(&wide_column_kernel<T, kVec>, q.columns, dim3(32, kColumnRows), 0, st, p);
         if (e != cudaSuccess) return e;
-        return launch_dependent(&wide_backward_kernel<T, kVec>, dim3(q.blocks), dim3(kWideThreads), 0, st, p);
+        return launch_dependent(&wide_backward_kernel<T, kVec, false>, dim3(q.blocks), dim3(kWideThreads), 0, st, p);
     }
     return launch_dependent(&backward_kernel<T, kVec, kSums>, dim3(q.blocks), dim3(q.team, q.teams), kSums && q.teams > 1 ? q.team * 64 : 0, st, p);
 }

@@ -43,7 +43,7 @@ def check(x, w, b, dy, eps=1e-5, **kw):
 # every route: few and many rows, one and several teams of a block, rows that a team covers exactly and not, pieces of eight, two
 # and one, rows wider than a block's threads
 SHAPES = [(1, 1), (1, 8), (3, 17), (2, 256), (7, 1000), (300, 30), (5000, 64), (4099, 256), (2500, 768), (3001, 1024), (1300, 1111), (1025, 2048),
-          (601, 4096), (1200, 4104), (640, 4864), (150, 8192), (161, 8200), (5, 12288), (333, 16384), (160, 14336), (37, 9001)]
+          (601, 4096), (1200, 4104), (640, 4864), (150, 8192), (161, 8200), (5, 12288), (333, 16384), (160, 14336), (37, 9001), (400, 9000), (21, 30000), (3, 24577)]
 
 
 @pytest.mark.parametrize("dtype,affine", [(BF16, F32), (F32, BF16), (BF16, None), (F32, F32)])
