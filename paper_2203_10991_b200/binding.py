@@ -7,6 +7,7 @@ fallback: if the library is missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 from pathlib import Path
 
 import torch
@@ -583,6 +584,11 @@ def mvue_layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: t
     return out, mean, rstd
 
 
+@functools.lru_cache(maxsize=1024)
+def _layer_norm_workspace(rows: int, cols: int, device: int) -> int:
+    return mvue_layer_norm_workspace_bytes(rows, cols)
+
+
 def mvue_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
     b = ctypes.c_size_t()
     _check(lib().mvue_layer_norm_workspace_bytes(rows, cols, ctypes.byref(b)), "mvue_layer_norm_workspace_bytes")
@@ -604,8 +610,9 @@ def mvue_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tens
     else:
         assert out.shape == x.shape and out.dtype == x.dtype
         lddx = _rows(out)[2]
-    dweight, dbias = x.new_empty(cols, dtype=torch.float32), x.new_empty(cols, dtype=torch.float32)
-    need = mvue_layer_norm_workspace_bytes(rows, cols)
+    dweight = x.new_empty(cols, dtype=torch.float32)
+    dbias = torch.empty_like(dweight)
+    need = _layer_norm_workspace(rows, cols, x.get_device())
     if need and (workspace is None or workspace.numel() * workspace.element_size() < need):
         workspace = x.new_empty(need, dtype=torch.uint8)
     _check(lib().mvue_layer_norm_backward(dy.data_ptr(), _rows(dy)[2], x.data_ptr(), ldx, _dtype_code(x), rows, cols, mean.data_ptr(),

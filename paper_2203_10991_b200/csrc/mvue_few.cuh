@@ -51,6 +51,11 @@ __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, u
 __device__ __forceinline__ void scales_to_tmem(uint32_t tmem, uint32_t smem) {
     asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(make_smem_desc(smem, 16, 128, kSwizzleNone)) : "memory");
 }
+__device__ __forceinline__ float ld_cluster1(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
@@ -207,8 +212,29 @@ few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     }
     if (p.split > 1) cluster_sync();         // every part is in shared memory
 
-    // this block's share of the tokens, eight outs a thread
+    // this block's share of the tokens, eight outs a thread: neighbours, or where rows do not allow wide accesses every sixteenth
     const int share = S::kTN / p.split, first = (int)rank * share;           // (split divides kTN)
+    if (p.vec < 16) {
+        for (int i = threadIdx.x; i < share * 16; i += kFewThreads) {
+            const int token = first + (i >> 4), o = i & 15;
+            if (token0 + token >= p.tokens) continue;
+            const uint32_t at = smem_base + (uint32_t)(token * 128 + o) * 4;
+            float x[8] = {};
+            for (int r = 0; r < p.split; ++r) {
+                const uint32_t from = map_to_cta(at, r);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] += ld_cluster1(from + 64 * j);
+            }
+            const int64_t to = (int64_t)(token0 + token) * p.ldc + out0 + o;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (failed) x[j] = __uint_as_float(0x7FFFFFFFu);
+                if (out0 + o + 16 * j >= p.outs) break;
+                if (p.bf16) static_cast<__nv_bfloat16*>(p.C)[to + 16 * j] = __float2bfloat16_rn(x[j]);
+                else static_cast<float*>(p.C)[to + 16 * j] = x[j];
+            }
+        }
+    } else
     for (int i = threadIdx.x; i < share * 16; i += kFewThreads) {
         const int token = first + (i >> 4), o = (i & 15) * 8;
         if (token0 + token >= p.tokens || out0 + o >= p.outs) continue;

@@ -24,7 +24,7 @@ namespace {
 
 constexpr int kMaxTeam = 512;                    // threads; eight columns each in the kernels for any alignment
 constexpr int kWideThreads = 1024;
-constexpr int kWideSlabs = 3;                    // wide rows of so many slabs of 8192 columns have their column sums in shared memory
+constexpr int64_t kWideSums = 24576;             // columns whose sums an SM's shared memory holds, eight bytes each
 constexpr int kColumnRows = 8;                   // wide: teams of a warp in a column block
 
 struct Params {
@@ -621,7 +621,7 @@ __device__ __forceinline__ float block_sum(float v, float* slots) {
     const int lane = threadIdx.x & 31;
     if (lane == 0) slots[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = slots[lane];
+    v = lane < (int)(blockDim.x >> 5) ? slots[lane] : 0.0f;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     __syncthreads();
@@ -631,13 +631,14 @@ __device__ __forceinline__ float block_sum(float v, float* slots) {
 template <typename T, int kVec>
 __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const __grid_constant__ Params p) {
     __shared__ float slots[32];
+    const int threads = blockDim.x;
     grid_dependency_wait();
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const T* x = static_cast<const T*>(p.x) + row * p.ldx;
         T* y = static_cast<T*>(p.y) + row * p.ldy;
         float s = 0.0f, v[8];
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads) {
-            const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * threads) {
+            const Cols<kVec> c(c0, p.cols, threadIdx.x, threads);
             if (c.count == 0) break;
             c.load(x, v);
 #pragma unroll
@@ -645,8 +646,8 @@ __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const __grid
         }
         const float mean = block_sum(s, slots) * p.inv_cols;
         s = 0.0f;
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads) {
-            const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * threads) {
+            const Cols<kVec> c(c0, p.cols, threadIdx.x, threads);
             if (c.count == 0) break;
             c.load(x, v);
 #pragma unroll
@@ -654,8 +655,8 @@ __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const __grid
                 if (j < c.count) s = fmaf(v[j] - mean, v[j] - mean, s);
         }
         const float rstd = rsqrtf(fmaf(block_sum(s, slots), p.inv_cols, p.eps));
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads) {
-            const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * threads) {
+            const Cols<kVec> c(c0, p.cols, threadIdx.x, threads);
             if (c.count == 0) break;
             float gamma[8], beta[8];
             c.load(x, v);
@@ -672,16 +673,17 @@ __global__ void __launch_bounds__(kWideThreads) wide_forward_kernel(const __grid
     }
 }
 
-// kSums: the column sums too, in shared memory, a thread's sixteen of each slab of 8192 columns as four quarters that lie a block's
-// threads apart.
+// kSums: the column sums too, in shared memory, a thread's sixteen of each slab (eight columns a thread) as four quarters that lie a
+// block's threads apart.
 template <typename T, int kVec, bool kSums>
 __global__ void __launch_bounds__(kWideThreads) wide_backward_kernel(const __grid_constant__ Params p) {
     __shared__ float slots[32];
     extern __shared__ float4 wide_sums[];
+    const int threads = blockDim.x;
     grid_dependency_wait();
     if (kSums) {
-        for (int64_t c0 = 0, q = 0; c0 < p.cols; c0 += 8 * kWideThreads)
-            for (int i = 0; i < 4; ++i, ++q) wide_sums[q * kWideThreads + threadIdx.x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int64_t c0 = 0, q = 0; c0 < p.cols; c0 += 8 * threads)
+            for (int i = 0; i < 4; ++i, ++q) wide_sums[q * threads + threadIdx.x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const T *x = static_cast<const T*>(p.x) + row * p.ldx, *dy = static_cast<const T*>(p.dy) + row * p.lddy;
@@ -697,7 +699,7 @@ __global__ void __launch_bounds__(kWideThreads) wide_backward_kernel(const __gri
             if (kSums && sums) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float4 &a = sums[h * kWideThreads], &b = sums[(2 + h) * kWideThreads];
+                    float4 &a = sums[h * threads], &b = sums[(2 + h) * threads];
                     a = make_float4(fmaf(g[4 * h], v[4 * h], a.x), fmaf(g[4 * h + 1], v[4 * h + 1], a.y), fmaf(g[4 * h + 2], v[4 * h + 2], a.z),
                                     fmaf(g[4 * h + 3], v[4 * h + 3], a.w));
                     b = make_float4(b.x + g[4 * h], b.y + g[4 * h + 1], b.z + g[4 * h + 2], b.w + g[4 * h + 3]);
@@ -707,10 +709,10 @@ __global__ void __launch_bounds__(kWideThreads) wide_backward_kernel(const __gri
             for (int j = 0; j < 8; ++j) g[j] *= gamma[j];
         };
         int64_t slab = 0;
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads, ++slab) {
-            const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * threads, ++slab) {
+            const Cols<kVec> c(c0, p.cols, threadIdx.x, threads);
             if (c.count == 0) break;
-            take(c, wide_sums + slab * 4 * kWideThreads + threadIdx.x);
+            take(c, wide_sums + slab * 4 * threads + threadIdx.x);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (j < c.count) {
@@ -719,8 +721,8 @@ __global__ void __launch_bounds__(kWideThreads) wide_backward_kernel(const __gri
                 }
         }
         const float m0 = block_sum(s0, slots) * p.inv_cols, m1 = block_sum(s1, slots) * p.inv_cols;
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads) {
-            const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * threads) {
+            const Cols<kVec> c(c0, p.cols, threadIdx.x, threads);
             if (c.count == 0) break;
             take(c, nullptr);
 #pragma unroll
@@ -731,13 +733,13 @@ __global__ void __launch_bounds__(kWideThreads) wide_backward_kernel(const __gri
     if (kSums) {
         float* out = p.partial + (int64_t)blockIdx.x * 2 * p.cols;
         int64_t slab = 0;
-        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * kWideThreads, ++slab) {
-            const Cols<kVec> c(c0, p.cols, threadIdx.x, kWideThreads);
+        for (int64_t c0 = 0; c0 < p.cols; c0 += 8 * threads, ++slab) {
+            const Cols<kVec> c(c0, p.cols, threadIdx.x, threads);
             if (c.count == 0) break;
-            const float4* sums = wide_sums + slab * 4 * kWideThreads + threadIdx.x;
+            const float4* sums = wide_sums + slab * 4 * threads + threadIdx.x;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float4 a = sums[h * kWideThreads], b = sums[(2 + h) * kWideThreads];
+                const float4 a = sums[h * threads], b = sums[(2 + h) * threads];
                 const float x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -840,9 +842,14 @@ Plan plan(bool backward, int64_t rows, int64_t cols, int dtype, int vec, int sm_
     }
     if (cols > 8 * kMaxTeam) {
         q.kind = Plan::kWide;
-        q.blocks = (int)std::min<int64_t>(rows, 2 * (int64_t)sm_count);
-        if (backward && cols <= 8 * kWideThreads * kWideSlabs) {
-            q.blocks = q.parts = (int)std::min<int64_t>(rows, sm_count);
+        // blocks of 256 threads, eight an SM: several rows on their way at once (3387 x 4984 bf16 forward: 55 us with two of 1024)
+        q.team = 256;
+        q.blocks = (int)std::min<int64_t>(rows, 8 * (int64_t)sm_count);
+        if (backward && cols <= kWideSums) {
+            // as many blocks as have room for their sums
+            const int fit = std::min(8, (int)(kWideSums / round_up(cols, 2048)));
+            q.team = fit >= 4 ? 256 : fit >= 2 ? 512 : 1024;
+            q.blocks = q.parts = (int)std::min<int64_t>(rows, (int64_t)fit * sm_count);
             return q;
         }
         const int64_t slabs = (cols + 255) / 256;
@@ -888,7 +895,7 @@ template <typename T, int kVec> cudaError_t forward(const Plan& q, const Params&
             return q.team * q.teams <= 256 ? go(std::integral_constant<int, 256>()) : go(std::integral_constant<int, kEightThreads>());
         }
     }
-    if (q.kind == Plan::kWide) return launch_dependent(&wide_forward_kernel<T, kVec>, dim3(q.blocks), dim3(kWideThreads), 0, st, p);
+    if (q.kind == Plan::kWide) return launch_dependent(&wide_forward_kernel<T, kVec>, dim3(q.blocks), dim3(q.team), 0, st, p);
     const dim3 block(q.team, q.teams);
     if (q.at_once == 4) return launch_dependent(&forward_kernel<T, kVec, 4>, dim3(q.blocks), block, 0, st, p);
     return launch_dependent(&forward_kernel<T, kVec, 1>, dim3(q.blocks), block, 0, st, p);
@@ -902,19 +909,18 @@ template <typename T, int kVec, bool kSums> cudaError_t backward(const Plan& q, 
         }
     }
     if (q.kind == Plan::kWide) {
-        const int slabs = (int)((p.cols + 8 * kWideThreads - 1) / (8 * kWideThreads));
-        if (kSums && slabs <= kWideSlabs) {
+        if (kSums && p.cols <= kWideSums) {
             static PerDeviceOnce once;
             const cudaError_t e = once_per_device(once, [](int) {
-                return cudaFuncSetAttribute(&wide_backward_kernel<T, kVec, kSums>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSlabs * 64 * kWideThreads);
+                return cudaFuncSetAttribute(&wide_backward_kernel<T, kVec, kSums>, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kWideSums);
             });
             if (e != cudaSuccess) return e;
-            return launch_dependent(&wide_backward_kernel<T, kVec, kSums>, dim3(q.blocks), dim3(kWideThreads), (size_t)slabs * 64 * kWideThreads, st, p);
+            return launch_dependent(&wide_backward_kernel<T, kVec, kSums>, dim3(q.blocks), dim3(q.team), (size_t)round_up(p.cols, 8 * q.team) * 8, st, p);
         }
         cudaError_t e = cudaSuccess;
         if (kSums) e = launch_dependent(&wide_column_kernel<T, kVec>, q.columns, dim3(32, kColumnRows), 0, st, p);
         if (e != cudaSuccess) return e;
-        return launch_dependent(&wide_backward_kernel<T, kVec, false>, dim3(q.blocks), dim3(kWideThreads), 0, st, p);
+        return launch_dependent(&wide_backward_kernel<T, kVec, false>, dim3(q.blocks), dim3(q.team), 0, st, p);
     }
     return launch_dependent(&backward_kernel<T, kVec, kSums>, dim3(q.blocks), dim3(q.team, q.teams), kSums && q.teams > 1 ? q.team * 64 : 0, st, p);
 }

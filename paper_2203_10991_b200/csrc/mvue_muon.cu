@@ -588,28 +588,44 @@ bool extents_ok(int64_t rows, int64_t cols) {
            std::min(rows, cols) <= (1 << 20);
 }
 
-template <bool kCluster> cudaError_t launch_small(const SmallMaps& maps, const SmallParams& p, int count, int sm_count, cudaStream_t stream) {
-    static PerDeviceOnce once;
-    cudaError_t e = once_per_device(once, [](int) {
-        const cudaError_t err = cudaFuncSetAttribute(small_kernel<4, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(4));
-        return err != cudaSuccess ? err : cudaFuncSetAttribute(small_kernel<8, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8));
-    });
-    if (e != cudaSuccess) return e;
-    const int64_t blocks = (int64_t)p.blocks * count;
-    const int stages = blocks <= sm_count ? 8 : 4;
+cudaLaunchConfig_t small_config(int64_t blocks, int stages, cudaLaunchAttribute (&attr)[2], bool cluster, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kSmallThreads);
     cfg.dynamicSmemBytes = (size_t)small_smem(stages);
     cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
     attr[1].val.clusterDim.x = kSmallBlocks;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = kCluster ? 2 : 1;
+    cfg.numAttrs = cluster ? 2 : 1;
+    return cfg;
+}
+
+template <bool kCluster> cudaError_t launch_small(const SmallMaps& maps, const SmallParams& p, int count, int sm_count, cudaStream_t stream) {
+    static PerDeviceOnce once;
+    static int clusters[kMaxDevices];                        // of blocks with eight stages that run at once
+    cudaLaunchAttribute attr[2];
+    cudaError_t e = once_per_device(once, [&](int dev) {
+        cudaError_t err = cudaFuncSetAttribute(small_kernel<4, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(4));
+        if (err == cudaSuccess) err = cudaFuncSetAttribute(small_kernel<8, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8));
+        if (err == cudaSuccess && kCluster) {
+            cudaLaunchConfig_t cfg = small_config(kSmallBlocks, 8, attr, true, nullptr);
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, small_kernel<8, kCluster>, &cfg) == cudaSuccess) clusters[dev] = n;
+            (void)cudaGetLastError();
+        }
+        return err;
+    });
+    int dev = 0;
+    if (e == cudaSuccess) e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = (int64_t)p.blocks * count;
+    // (18 matrices of 136 x 141: a cluster takes eight SMs of one part of the chip, and 16 of them fit)
+    const int stages = (kCluster ? count <= clusters[dev] : blocks <= sm_count) ? 8 : 4;
+    const cudaLaunchConfig_t cfg = small_config(blocks, stages, attr, kCluster, stream);
     return cudaLaunchKernelEx(&cfg, stages == 8 ? &small_kernel<8, kCluster> : &small_kernel<4, kCluster>, maps, p);
 }
 

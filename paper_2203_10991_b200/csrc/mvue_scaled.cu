@@ -11,7 +11,22 @@
 namespace mvue {
 namespace {
 
-// 32 consecutive results of a row.
+// A 32 x 32 block of words turned over among the lanes: word i of lane l becomes word l of lane i.
+__device__ __forceinline__ void turn_over(uint32_t (&v)[32], int lane) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const bool up = (lane & d) != 0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            if (i & d) continue;
+            const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, up ? v[i] : v[i + d], d);
+            if (up) v[i] = got;
+            else v[i + d] = got;
+        }
+    }
+}
+
+// 32 consecutive results of a row; rows that do not allow wide accesses are turned over first, so that a warp's stores are neighbours.
 template <bool kBf16>
 struct Store {
     void* C;
@@ -21,37 +36,41 @@ struct Store {
     static constexpr bool kSlabs = false, kMirror = false;
     static constexpr int kIn = 0;
     __device__ __forceinline__ void store(const dense::Params& p, int row, int col, const uint32_t (&v)[32]) const {
-        if (row >= p.M || col >= p.N) return;
+        if (col >= p.N) return;                              // (a whole warp)
         const int left = p.N - col;
+        if (vec < 16 || left < 32) {
+            const int lane = threadIdx.x & 31, rows = p.M - (row - lane);
+            uint32_t w[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i] = v[i];
+            turn_over(w, lane);
+            if (lane >= left) return;
+            const int64_t at = (int64_t)(row - lane) * ldc + col + lane;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                if (i >= rows) break;
+                if constexpr (kBf16) static_cast<__nv_bfloat16*>(C)[at + i * ldc] = __float2bfloat16_rn(__uint_as_float(w[i]));
+                else static_cast<float*>(C)[at + i * ldc] = __uint_as_float(w[i]);
+            }
+            return;
+        }
+        if (row >= p.M) return;
         if constexpr (kBf16) {
             __nv_bfloat16* to = static_cast<__nv_bfloat16*>(C) + (int64_t)row * ldc + col;
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) w[i] = pack_bf16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-            if (left >= 32 && vec >= 16) {
-                if (vec == 32) {
-                    store8_b32(to, w);
-                    store8_b32(to + 16, w + 8);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(to)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-                }
+            if (vec == 32) {
+                store8_b32(to, w);
+                store8_b32(to + 16, w + 8);
             } else {
-                unsigned short* q = reinterpret_cast<unsigned short*>(to);
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i < left) q[i] = (unsigned short)(w[i >> 1] >> (16 * (i & 1)));
+                for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(to)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
             }
         } else {
             float* to = static_cast<float*>(C) + (int64_t)row * ldc + col;
-            if (left >= 32 && vec >= 16) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) store8_b32(to + i, v + i);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i < left) to[i] = __uint_as_float(v[i]);
-            }
+            for (int i = 0; i < 32; i += 8) store8_b32(to + i, v + i);
         }
     }
 };
