@@ -21,6 +21,7 @@
 
 #include "../../include/mvue_layer.h"
 #include "mvue_dense.cuh"
+#include "mvue_few.cuh"
 #include "mvue_train.cuh"
 
 namespace mvue {
@@ -397,15 +398,15 @@ struct Apply {
 constexpr int kSmallBlocks = 8, kSmallThreads = 192;
 constexpr int kSmallBox = 64 * 128, kSmallStage = 3 * kSmallBox;        // 128 rows of the first operand, 64 of the second
 constexpr int small_smem(int stages) { return stages * kSmallStage + 256 + 1024; }
-constexpr int kSmallM = 256;
-constexpr int64_t kSmallElements = 256 * 1024;
+constexpr int kSmallM = 256, kSmallN = 1024;         // extents of what a cluster takes
 // One product a launch while X has no more than this many tiles of 256 x 256 in all matrices: 512 x 512 94 us (pair tiles 165 us),
 // 1024 x 1024 133 us (200 us); 1024 x 4096, 64 tiles, 290 us either way.
 constexpr int64_t kSmallPairTiles = 40;
 
 struct SmallParams {
     int m, n, steps;
-    int blocks, first, last;                 // blocks of a matrix; phases (three a step)
+    int blocks, first, last;                 // blocks (tiles, where the sum is split) of a matrix; phases (three a step)
+    int split;                               // !kCluster, A = X X^T: blocks of a cluster that share the sum of a tile
     int64_t n_pitch, m_pitch;
     __half *X[2], *lo, *A, *B;
     const float* xs;
@@ -445,7 +446,8 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
     const auto free_bar = [&](int b) { return bar_base + 8u * (2 * kSmallStages + 2 + b); };
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_gen + kSmallBars + 8 * (2 * kSmallStages + 4));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, z = blockIdx.x / p.blocks, rank = blockIdx.x - z * p.blocks;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, unit = blockIdx.x / p.split;
+    const int part = blockIdx.x - unit * p.split, z = unit / p.blocks, rank = unit - z * p.blocks;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSmallStages; ++s) {
@@ -477,7 +479,9 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
     for (int phase = p.first; phase < p.last; ++phase) {
         const int k = phase / 3, what = phase - 3 * k;       // 0: A = X X^T, 1: B = a I + b A + c A A, 2: X' = B X
         const int N = what == 2 ? p.n : p.m, K = what == 0 ? p.n : p.m;
-        const int tiles_n = (N + 63) / 64, tiles = (p.m + 127) / 128 * tiles_n, steps = (K + 63) / 64;
+        const int tiles_n = (N + 63) / 64, tiles = (p.m + 127) / 128 * tiles_n;
+        // this block's share of the sum
+        const int all = (K + 63) / 64, share = (all + p.split - 1) / p.split, begin = part * share, steps = max(0, min(all - begin, share));
         if (warp == 4 && lane == 0) {
             asm volatile("fence.proxy.async.global;" ::: "memory");
             const CUtensorMap* first = what == 0 ? &maps.X[k & 1] : what == 1 ? &maps.A : &maps.B;
@@ -489,9 +493,10 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
                     if (!(ok = mbar_wait(empty_bar(s), parity, abort_flag))) break;
                     const uint32_t to = smem_base + s * kSmallStage;
                     mbar_expect_tx(full_bar(s), kSmallStage);
-                    dense::tma_load_3d(to, first, 64 * i, m0, z, full_bar(s));
-                    dense::tma_load_3d(to + kSmallBox, first, 64 * i, m0 + 64, z, full_bar(s));
-                    dense::tma_load_3d(to + 2 * kSmallBox, second, what == 2 ? n0 : 64 * i, what == 2 ? 64 * i : n0, z, full_bar(s));
+                    const int at = 64 * (begin + i);
+                    dense::tma_load_3d(to, first, at, m0, z, full_bar(s));
+                    dense::tma_load_3d(to + kSmallBox, first, at, m0 + 64, z, full_bar(s));
+                    dense::tma_load_3d(to + 2 * kSmallBox, second, what == 2 ? n0 : at, what == 2 ? at : n0, z, full_bar(s));
                     if (++s == kSmallStages) { s = 0; parity ^= 1u; }
                 }
             }
@@ -516,7 +521,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
                     if (++s == kSmallStages) { s = 0; parity ^= 1u; }
                 }
                 if (!ok) break;
-                tc_commit(acc_bar(done & 1));
+                tc_commit(acc_bar(done & 1));                // (a share of nothing: at once)
             }
         } else if (warp < 4) {
             const bool read_lo = what == 2 && k < p.steps - 2, write_lo = what == 2 && k + 1 < p.steps - 2;
@@ -535,6 +540,18 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
                 }
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(done & 1), (done >> 1) & 1u, abort_flag))) break;
                 tc_fence_after();
+                if (!kCluster && p.split > 1) {              // the sum of this block's share, [64 columns][128 rows]: the stages are done with
+                    float* to = reinterpret_cast<float*>(smem_gen) + 32 * warp + lane;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t v[32];
+                        tmem_ld_32x32b_x32(tmem_base + ((uint32_t)(32 * warp) << 16) + 64u * (done & 1) + 32u * c, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) to[(32 * c + i) * 128] = steps > 0 ? __uint_as_float(v[i]) : 0.0f;
+                    }
+                    continue;
+                }
                 uint32_t v[2][32];
                 tmem_ld_32x32b_x32(tmem_base + ((uint32_t)(32 * warp) << 16) + 64u * (done & 1), v[0]);
                 tmem_ld_32x32b_x32(tmem_base + ((uint32_t)(32 * warp) << 16) + 64u * (done & 1) + 32u, v[1]);
@@ -557,6 +574,34 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
         }
         __syncwarp();
         if (kCluster) cluster_sync();        // the product is complete and seen by the cluster's copies
+    }
+    if (!kCluster && p.split > 1) {
+        // Each block adds up a share of the tile's columns, in order of rank, and stores them where the tile's mirror image lies: A is
+        // symmetric, and there the rows of a column are neighbours.
+        const int tiles_n = (p.m + 63) / 64, m0 = rank / tiles_n * 128, n0 = rank % tiles_n * 64;
+        tc_fence_before();
+        __syncthreads();
+        const bool failed = *abort_flag != 0;
+        cluster_sync();
+        const int share = 64 / p.split;
+        const float alpha = p.S / xs / xs;
+        for (int i = threadIdx.x; i < share * 16; i += kSmallThreads) {
+            const int c = part * share + (i >> 4), r = (i & 15) * 8;
+            if (n0 + c >= p.m || m0 + r >= p.m) continue;
+            float x[8] = {};
+            for (int q = 0; q < p.split; ++q) {
+                const uint32_t from = map_to_cta(smem_base + (uint32_t)(c * 128 + r) * 4, q);
+                const float4 a = dense::ld_cluster4(from), b = dense::ld_cluster4(from + 16);
+                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
+                x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+            }
+            if (failed) x[0] = __uint_as_float(0x7FFFFFFFu);
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = half_pair(x[2 * j] * alpha, x[2 * j + 1] * alpha);
+            *reinterpret_cast<uint4*>(p.A + a0 + (int64_t)(n0 + c) * p.m_pitch + m0 + r) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        cluster_sync();                      // no block leaves while another reads its sums
     }
 
     tc_fence_before();
@@ -588,7 +633,7 @@ bool extents_ok(int64_t rows, int64_t cols) {
            std::min(rows, cols) <= (1 << 20);
 }
 
-cudaLaunchConfig_t small_config(int64_t blocks, int stages, cudaLaunchAttribute (&attr)[2], bool cluster, cudaStream_t stream) {
+cudaLaunchConfig_t small_config(int64_t blocks, int stages, cudaLaunchAttribute (&attr)[2], int cluster, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kSmallThreads);
@@ -597,10 +642,10 @@ cudaLaunchConfig_t small_config(int64_t blocks, int stages, cudaLaunchAttribute 
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = kSmallBlocks;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster ? 2 : 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cfg;
 }
 
@@ -612,7 +657,7 @@ template <bool kCluster> cudaError_t launch_small(const SmallMaps& maps, const S
         cudaError_t err = cudaFuncSetAttribute(small_kernel<4, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(4));
         if (err == cudaSuccess) err = cudaFuncSetAttribute(small_kernel<8, kCluster>, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8));
         if (err == cudaSuccess && kCluster) {
-            cudaLaunchConfig_t cfg = small_config(kSmallBlocks, 8, attr, true, nullptr);
+            cudaLaunchConfig_t cfg = small_config(kSmallBlocks, 8, attr, kSmallBlocks, nullptr);
             int n = 0;
             if (cudaOccupancyMaxActiveClusters(&n, small_kernel<8, kCluster>, &cfg) == cudaSuccess) clusters[dev] = n;
             (void)cudaGetLastError();
@@ -622,10 +667,10 @@ template <bool kCluster> cudaError_t launch_small(const SmallMaps& maps, const S
     int dev = 0;
     if (e == cudaSuccess) e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    const int64_t blocks = (int64_t)p.blocks * count;
+    const int64_t blocks = (int64_t)p.blocks * p.split * count;
     // (18 matrices of 136 x 141: a cluster takes eight SMs of one part of the chip, and 16 of them fit)
     const int stages = (kCluster ? count <= clusters[dev] : blocks <= sm_count) ? 8 : 4;
-    const cudaLaunchConfig_t cfg = small_config(blocks, stages, attr, kCluster, stream);
+    const cudaLaunchConfig_t cfg = small_config(blocks, stages, attr, kCluster ? kSmallBlocks : p.split, stream);
     return cudaLaunchKernelEx(&cfg, stages == 8 ? &small_kernel<8, kCluster> : &small_kernel<4, kCluster>, maps, p);
 }
 
@@ -649,15 +694,15 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 32 * sm_count / q.count));
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256) * q.count;
-    const bool cluster = m <= kSmallM && m * n <= kSmallElements;
-    if (e == cudaSuccess && (cluster || pair_tiles <= kSmallPairTiles)) {
+    const bool cluster = m <= kSmallM && n <= kSmallN;
+    if (e == cudaSuccess && (cluster || pair_tiles <= (m <= kSmallM ? 4 : 1) * kSmallPairTiles)) {
         const auto map = [&](CUtensorMap* to, const __half* base, int64_t rows, int64_t cols, int64_t pitch) {
             return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, rows, q.count, pitch * 2, rows * pitch * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
         };
         SmallMaps maps;
         if (!map(&maps.X[0], X[0], m, n, q.n_pitch) || !map(&maps.X[1], X[1], m, n, q.n_pitch) || !map(&maps.A, A, m, m, mp) || !map(&maps.B, B, m, m, mp))
             return cudaErrorInvalidValue;
-        SmallParams p = {q.m, q.n, steps, kSmallBlocks, 0, 3 * steps, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
+        SmallParams p = {q.m, q.n, steps, kSmallBlocks, 0, 3 * steps, 1, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
         if (cluster) {
             e = launch_small<true>(maps, p, q.count, sm_count, st);
         } else {
@@ -665,6 +710,9 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
                 p.first = phase;
                 p.last = phase + 1;
                 p.blocks = (int)((m + 127) / 128 * (((phase % 3 == 2 ? n : m) + 63) / 64));
+                // as many shares as there are SMs for, of eight steps of 64 at least
+                p.split = 1;
+                while (phase % 3 == 0 && p.split < 8 && 2 * p.split * p.blocks * (int64_t)q.count <= sm_count && n >= 1024 * p.split) p.split *= 2;
                 e = launch_small<false>(maps, p, q.count, sm_count, st);
             }
         }
