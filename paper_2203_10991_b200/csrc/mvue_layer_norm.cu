@@ -215,7 +215,7 @@ constexpr int kEightThreads = 512;
 template <typename T, int kC, int kR, int kThreads>
 __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 1) forward8_kernel(const __grid_constant__ Params p) {
     __shared__ float2 slots[2][kThreads / 32][kR];
-    extern __shared__ float affine[];
+    extern __shared__ __align__(16) float affine[];
     const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cols = (int)p.cols, pieces = cols >> 3, step = threads * 8;
     const int64_t first = ((int64_t)blockIdx.x * blockDim.y + team) * kR, stride = (int64_t)gridDim.x * blockDim.y * kR;
@@ -321,7 +321,7 @@ __device__ __forceinline__ bool join_teams(float (&dgamma)[kN], float (&dbeta)[k
 template <typename T, int kC, int kR, bool kSums, bool kFull>
 __global__ void __launch_bounds__(kEightThreads, 1) backward8_kernel(const __grid_constant__ Params p) {
     __shared__ float slots[2][32][4];
-    extern __shared__ float affine[];                        // the weight; at the end the teams' sums
+    extern __shared__ __align__(16) float affine[];          // the weight; at the end the teams' sums
     const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cols = (int)p.cols, pieces = cols >> 3, c0 = threadIdx.x * 8, step = threads * 8;
     const T *x = static_cast<const T*>(p.x), *dy = static_cast<const T*>(p.dy);
@@ -428,13 +428,12 @@ __global__ void __launch_bounds__(kEightThreads, 1) backward8_kernel(const __gri
 #pragma unroll
         for (int c = 0; c < kC; ++c) {
             if (c0 + c * step >= cols) break;
-            float o[8];
+            float4 *to_a = reinterpret_cast<float4*>(out + c0 + c * step), *to_b = reinterpret_cast<float4*>(out + p.cols + c0 + c * step);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = a[8 * c + j];
-            store8(out + c0 + c * step, true, 8, o);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = b[8 * c + j];
-            store8(out + p.cols + c0 + c * step, true, 8, o);
+            for (int h = 0; h < 2; ++h) {                    // (the workspace is aligned to 16 bytes)
+                to_a[h] = make_float4(a[8 * c + 4 * h], a[8 * c + 4 * h + 1], a[8 * c + 4 * h + 2], a[8 * c + 4 * h + 3]);
+                to_b[h] = make_float4(b[8 * c + 4 * h], b[8 * c + 4 * h + 1], b[8 * c + 4 * h + 2], b[8 * c + 4 * h + 3]);
+            }
         }
     }
 }

@@ -198,3 +198,16 @@ def test_offsets_beyond_32_bits():
     assert not bool(y[:-300].any()) and torch.allclose(rstd[-300:], want[2], rtol=1e-5)
     del x, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(3000, 1024, BF16), (3000, 1024, F32), (2000, 4864, BF16), (500, 9000, F32), (300, 1000, BF16), (9, 25000, F32)])
+def test_workspace_of_any_allowed_alignment(rows, cols, dtype):
+    x, w, b, dy = inputs(rows, cols, dtype, F32)
+    _, mean, rstd = binding.mvue_layer_norm(x, w, b)
+    want = binding.mvue_layer_norm_backward(dy, x, mean, rstd, w)
+    room = torch.empty(binding.mvue_layer_norm_workspace_bytes(rows, cols) + 16, dtype=torch.uint8, device="cuda")
+    got = binding.mvue_layer_norm_backward(dy, x, mean, rstd, w, workspace=room[16:])
+    assert all(torch.equal(a, v) for a, v in zip(got, want))
+    with pytest.raises(binding.MvueError) as e:
+        binding.mvue_layer_norm_backward(dy, x, mean, rstd, w, workspace=room[8:-8])
+    assert e.value.status == -7
