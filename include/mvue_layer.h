@@ -94,7 +94,7 @@ MVUE_API int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int6
  * 1e-3 to 3e-3 of the result's norm, whatever the spectrum, and up to 5e-3 for a few dozen elements.
  * A matrix with an element that is not finite, or whose sum of squares overflows binary32 in eight neighbours, becomes NaN throughout.
  *  x          [batch, rows, cols], MVUE_F32 or MVUE_BF16, ldx >= cols, x_stride elements between matrices.
- *  out        the same, MVUE_F32 or MVUE_BF16; it may be x.
+ *  out        the same, MVUE_F32 or MVUE_BF16; matrices do not overlap.  It may be x, with x's type, ldx and x_stride.
  *  workspace  mvue_orthogonalize_workspace_bytes(batch, rows, cols) bytes, 256-byte aligned; contents scratch.
  *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires; otherwise left untouched.
  * min(rows, cols) <= 2^20.  An empty extent: nothing.  Equal inputs give equal bits. */

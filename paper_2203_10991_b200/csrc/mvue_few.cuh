@@ -209,6 +209,8 @@ few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
             if (p.dev_status) *p.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
         }
         __syncthreads();
+        for (int i = threadIdx.x; i < S::kTN * 128; i += kFewThreads) part[i] = __uint_as_float(0x7FFFFFFFu);       // for all that add it
+        __syncthreads();
     }
     if (p.split > 1) cluster_sync();         // every part is in shared memory
 
@@ -228,7 +230,6 @@ few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
             const int64_t to = (int64_t)(token0 + token) * p.ldc + out0 + o;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (failed) x[j] = __uint_as_float(0x7FFFFFFFu);
                 if (out0 + o + 16 * j >= p.outs) break;
                 if (p.bf16) static_cast<__nv_bfloat16*>(p.C)[to + 16 * j] = __float2bfloat16_rn(x[j]);
                 else static_cast<float*>(p.C)[to + 16 * j] = x[j];
@@ -254,10 +255,6 @@ few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
         for (int r = 0; r < kMaxSplit; ++r) {
             x[0] += a[r].x; x[1] += a[r].y; x[2] += a[r].z; x[3] += a[r].w;
             x[4] += b[r].x; x[5] += b[r].y; x[6] += b[r].z; x[7] += b[r].w;
-        }
-        if (failed) {
-#pragma unroll
-            for (float& y : x) y = __uint_as_float(0x7FFFFFFFu);
         }
         const int left = p.outs - out0 - o;
         const int64_t to = (int64_t)(token0 + token) * p.ldc + out0 + o;

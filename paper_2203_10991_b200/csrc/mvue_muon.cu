@@ -583,7 +583,9 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
         const int tiles_n = (p.m + 63) / 64, m0 = rank / tiles_n * 128, n0 = rank % tiles_n * 64;
         tc_fence_before();
         __syncthreads();
-        const bool failed = *abort_flag != 0;
+        if (*abort_flag) {                   // its sum is a NaN for all that add it
+            for (int i = threadIdx.x; i < 64 * 128; i += kSmallThreads) reinterpret_cast<float*>(smem_gen)[i] = __uint_as_float(0x7FFFFFFFu);
+        }
         cluster_sync();
         const int share = 64 / p.split;
         const float alpha = p.S / xs / xs;
@@ -597,7 +599,6 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
                 x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
                 x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
             }
-            if (failed) x[0] = __uint_as_float(0x7FFFFFFFu);
             uint32_t w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = half_pair(x[2 * j] * alpha, x[2 * j + 1] * alpha);
@@ -631,7 +632,7 @@ int64_t group_bytes(int64_t count, int64_t m, int64_t n) {
 int64_t batch_of(int64_t m, int64_t n) { return std::max<int64_t>(1, std::min<int64_t>(kBatch, kBatchElements / (m * n))); }
 
 bool extents_ok(int64_t rows, int64_t cols) {
-    return rows >= 0 && cols >= 0 && rows <= 0x7FFFFF00 && cols <= 0x7FFFFF00 && (rows == 0 || cols <= ((int64_t)1 << 40) / rows) &&
+    return rows >= 0 && cols >= 0 && rows <= 0x7FFFFF00 && cols <= 0x7FFFFF00 && (rows == 0 || cols <= ((int64_t)1 << 38) / rows) &&
            std::min(rows, cols) <= (1 << 20);
 }
 
@@ -861,6 +862,8 @@ extern "C" int mvue_orthogonalize(const void* x, int dtype, int64_t batch, int64
     if (ns_steps < 1 || ns_steps > 16 || ldx < cols || ldo < cols || x_stride < 0 || out_stride < 0) return MVUE_ERR_SHAPE;
     size_t need = 0;
     if (int s = mvue_orthogonalize_workspace_bytes(batch, rows, cols, &need)) return s;
+    // results one behind the other, or the rows of all matrices side by side
+    if (batch > 1 && need > 0 && (rows - 1) * ldo + cols > out_stride && (out_stride < cols || (batch - 1) * out_stride + cols > ldo)) return MVUE_ERR_SHAPE;
     if (need == 0) return MVUE_OK;
     if (!x || !out) return MVUE_ERR_NULL;
     if (off(x, size_of(dtype)) || off(out, size_of(out_dtype))) return MVUE_ERR_ALIGN;

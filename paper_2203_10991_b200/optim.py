@@ -186,9 +186,13 @@ class MuonPlan:
         self.params, self.momentums, self.masters = list(params), list(momentums), list(masters)
         self._memory = [t.detach() for ts in (params, masters, momentums) for t in ts if t is not None]
         self._addresses = _addresses(self.params)
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self._memory if t.numel())
+        if any(end > start for (_, end), (start, _) in zip(spans, spans[1:])):
+            raise ValueError("two of the plan's tensors share memory")
         self._config = binding.MuonConfig()
         need = binding.mvue_muon_workspace_bytes(self._array, n)
         self._workspace = torch.empty(need, dtype=torch.uint8, device=self._device) if need else None
+        self._stream = torch.cuda.current_stream(self._device) if need else None        # the workspace's own
         self._grads = self._grad_addresses = None
         if grads is not None:
             self._point(grads)
@@ -222,7 +226,8 @@ class MuonPlan:
         """One step on the current stream of the params' device.  grads: this step's gradients (they stay the plan's until others are
         given); None reads the buffers the plan has.  scale: "rms" multiplies the orthogonal update by 0.2 sqrt(max(rows, cols)), which makes
         it as large as AdamW's; "shape" by sqrt(max(1, rows / cols)).  stochastic_rounding (bf16 params without a float copy)
-        wants a seed, another one each step.  Steps of one plan share its workspace: they run in the order of one stream."""
+        wants a seed, another one each step.  Steps of one plan share its workspace: they run in the order of one stream, and a graph
+        that has captured one needs the plan alive."""
         if grads is not None:
             self._point(grads)
         elif self._grads is None and len(self._array):
@@ -238,6 +243,10 @@ class MuonPlan:
             raise ValueError("stochastic rounding wants a seed, another one each step")
         if scale not in binding.MVUE_MUON_SCALES:
             raise ValueError(f"scale is one of {', '.join(binding.MVUE_MUON_SCALES)}")
+        if self._workspace is not None and not torch.cuda.is_current_stream_capturing():
+            stream = torch.cuda.current_stream(self._device)
+            if stream != self._stream:
+                self._workspace.record_stream(stream)        # it outlives the plan until this step is done
         c = self._config
         c.lr, c.momentum, c.weight_decay, c.grad_scale = lr, momentum, weight_decay, grad_scale
         c.dev_grad_scale = None if dev_grad_scale is None else dev_grad_scale.data_ptr()

@@ -259,3 +259,44 @@ def test_plan_refuses():
         with pytest.raises(ValueError):
             bad()
     assert binding.mvue_orthogonalize(torch.zeros(3, 0, 5, device="cuda")).shape == (3, 0, 5)
+
+
+def test_results_side_by_side_and_results_that_overlap():
+    x = torch.randn(3, 40, 24, generator=torch.Generator(device="cuda").manual_seed(9), device="cuda")
+    beside = torch.full((40, 3, 24), 7.0, device="cuda")
+    binding.mvue_orthogonalize(x, out=beside.transpose(0, 1))
+    assert torch.equal(beside.transpose(0, 1), binding.mvue_orthogonalize(x))
+    same = torch.randn(40, 24, generator=torch.Generator(device="cuda").manual_seed(10), device="cuda").expand(3, 40, 24)
+    assert torch.equal(binding.mvue_orthogonalize(same)[2], binding.mvue_orthogonalize(same[0]))        # read three times
+    for out in (torch.zeros(40, 24, device="cuda").expand(3, 40, 24), torch.zeros(4000, device="cuda").as_strided((3, 40, 24), (900, 24, 1)),
+                torch.zeros(4000, device="cuda").as_strided((3, 40, 24), (20, 72, 1))):
+        with pytest.raises(binding.MvueError) as e:
+            binding.mvue_orthogonalize(x, out=out)
+        assert e.value.status == -3
+
+
+def test_a_plan_refuses_tensors_that_share_memory():
+    a, b, c = (torch.zeros(8, 16, device="cuda") for _ in range(3))
+    for params, momentums in (([a, a], [b, c]), ([a, b], [c, c]), ([a], [a]), ([a[:4], a[3:7]], [b[:4], c[:4]])):
+        with pytest.raises(ValueError):
+            optim.MuonPlan(params, momentums)
+    optim.MuonPlan([a[:4], a[4:]], [b[:4], b[4:]])
+
+
+def test_a_plan_dropped_after_a_step_on_another_stream():
+    p, _, m, g = problem([(300, 260), (40, 500)], "f32", F32)
+    want = [t.clone() for t in p]
+    again = optim.MuonPlan(want, [t.clone() for t in m], grads=g)
+    again.step(lr=0.02)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    plan = optim.MuonPlan(p, m, grads=g)
+    need = plan._workspace.numel()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        plan.step(lr=0.02)
+    del plan
+    junk = [torch.full((need,), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]      # would be the plan's workspace
+    torch.cuda.synchronize()
+    assert len(junk) == 3 and all(torch.equal(a, b) for a, b in zip(p, want))
