@@ -38,21 +38,149 @@ struct Params {
     int affine_bf16;
 };
 
+// bf16 rows that are not whole pieces of eight, or do not begin at one, still have aligned pieces inside.  A thread's eight neighbours begin
+// at 8 lane - shift, where the row begins `shift` elements behind an aligned address: all pieces but the first and the last are accesses
+// of eight.  Rows eight apart have the same shift, so a block that takes such rows has the same columns in a thread all along.
+// 16384 x 1111: forward 29 us, backward 40 us (with accesses of single elements 55 and 78, of pairs for 1110 columns 47 and 54).  fp32 in
+// single elements and pairs is as fast (16384 x 1110: 33 and 42 us; shifted 35 and 49).
+constexpr int kShifted = 16;
+template <int kVec> struct Place : Cols<kVec> {
+    __device__ __forceinline__ Place(int64_t cols, int lane, int team, int) : Cols<kVec>(0, cols, lane, team) {}
+    __device__ __forceinline__ bool has(int j) const { return j < this->count; }
+};
+template <> struct Place<kShifted> {
+    int64_t first, second;                       // the second thread's first, of a whole piece
+    int from, count;                             // of the eight, those in [from, count) exist
+    __device__ __forceinline__ Place(int64_t cols, int lane, int, int shift) {
+        first = 8 * (int64_t)lane - shift;
+        second = 8 - shift;
+        from = first < 0 ? (int)-first : 0;
+        count = (int)min((int64_t)8, cols - first);
+    }
+    __device__ __forceinline__ bool whole() const { return from == 0 && count == 8; }
+    __device__ __forceinline__ bool has(int j) const { return j >= from && j < count; }
+    __device__ __forceinline__ int64_t at(int j) const { return first + j; }
+    __device__ __forceinline__ void store(__nv_bfloat16* row, const float (&x)[8]) const {
+        if (whole()) {
+            Cols<8> c(0, 8, 0, 1);
+            c.store(row + first, x);
+        } else {
+            const uint32_t own = bits();
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (own >> j & 1u) row[first + j] = __float2bfloat16_rn(x[j]);
+        }
+    }
+    __device__ __forceinline__ uint32_t bits() const { return count <= 0 ? 0u : (0xFFu << from) & (0xFFu >> (8 - count)); }
+};
+// A thread's eight elements as they were read, so that nothing waits for them before they are used.
+template <typename T, int kVec> struct Held {
+    static constexpr bool kPairs = sizeof(T) == 2 && kVec != 1;
+    uint32_t w[kPairs ? 4 : 8];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (uint32_t& x : w) x = 0u;
+    }
+    __device__ __forceinline__ void wide(const T* p) {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            ld256(p, w);
+        }
+    }
+    // Row `row` of the `rows` at `base`; one that does not exist leaves what there is.  kShifted: without a choice between accesses, which would
+    // wait for the elements.  A piece that is not all of its row's takes elements of the rows beside it too, or where there are none gives
+    // way to the second piece (whole in sixteen columns).  All of a block's rows have its shift: an access begins at 8 elements.
+    __device__ __forceinline__ void load(const Place<kVec>& c, const T* base, int64_t ld, int64_t row, int64_t rows) {
+        if constexpr (kVec == kShifted) {
+            if (row < rows) wide(base + row * ld + (c.whole() || (c.count > 0 && beside(row, rows)) ? c.first : c.second));
+        } else {
+            if (row >= rows || c.count <= 0) {
+                clear();
+                return;
+            }
+            const T* from = base + row * ld;
+            if constexpr (kVec == 8) {
+                wide(from + c.first);
+            } else if constexpr (kVec == 2) {
+                clear();
+#pragma unroll
+                for (int j = 0; j < 8; j += 2)
+                    if (c.has(j)) {
+                        if constexpr (sizeof(T) == 2) {
+                            w[j / 2] = *reinterpret_cast<const uint32_t*>(from + c.at(j));
+                        } else {
+                            const uint2 v = *reinterpret_cast<const uint2*>(from + c.at(j));
+                            w[j] = v.x;
+                            w[j + 1] = v.y;
+                        }
+                    }
+            } else {
+                clear();
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c.has(j)) {
+                        if constexpr (sizeof(T) == 2) w[j] = *reinterpret_cast<const unsigned short*>(from + c.at(j));
+                        else w[j] = __float_as_uint(from[c.at(j)]);
+                    }
+            }
+        }
+    }
+    static __device__ __forceinline__ bool beside(int64_t row, int64_t rows) { return row > 0 && row + 1 < rows; }
+    // What a piece has of its own, without a comparison for each element of each row: a mask for the words, and one or zero for the mean.
+    struct Own {
+        uint32_t words[4];
+        float one[8];
+        __device__ __forceinline__ Own(const Place<kVec>& c) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) one[j] = c.has(j) ? 1.0f : 0.0f;
+            if constexpr (kVec == kShifted) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) words[i] = (c.has(2 * i) ? 0xFFFFu : 0u) | (c.has(2 * i + 1) ? 0xFFFF0000u : 0u);
+            }
+        }
+    };
+    __device__ __forceinline__ void floats(const Place<kVec>& c, const Own& own, const T* base, int64_t ld, int64_t row, int64_t rows, float (&x)[8]) const {
+        constexpr bool kShift = kVec == kShifted;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (kPairs) {
+                const uint32_t v = kShift ? w[j / 2] & own.words[j / 2] : w[j / 2];
+                x[j] = j & 1 ? bf16_hi(v) : bf16_lo(v);
+            } else {
+                x[j] = __uint_as_float(sizeof(T) == 2 ? w[j] << 16 : w[j]);
+            }
+        }
+        if constexpr (kShift) {
+            if (!beside(row, rows)) {                        // (the first row, the last, and those that do not exist)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (row >= rows) x[j] = 0.0f;
+                    else if (!c.whole() && c.has(j)) x[j] = __bfloat162float(base[row * ld + c.at(j)]);
+            }
+        }
+    }
+};
+
+template <int kVec> __device__ __forceinline__ bool there(const Cols<kVec>& c, int j) { return j < c.count; }
+__device__ __forceinline__ bool there(const Place<kShifted>& c, int j) { return c.has(j); }
 // Eight columns of weight or bias; `none` where there is no such tensor.
-template <int kVec> __device__ __forceinline__ void load_affine(const Cols<kVec>& c, const void* from, int bf16, float none, float (&v)[8]) {
+template <typename C> __device__ __forceinline__ void load_affine(const C& c, const void* from, int bf16, float none, float (&v)[8]) {
     if (!from) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = none;
         return;
     }
-    if (kVec == 8 && c.count == 8 && (reinterpret_cast<uintptr_t>(from) & 31u) == 0) {
+    constexpr bool kEight = std::is_base_of<Cols<8>, C>::value;
+    if (kEight && c.count == 8 && (reinterpret_cast<uintptr_t>(from) & 31u) == 0) {
         if (bf16) load8(static_cast<const __nv_bfloat16*>(from) + c.first, true, 8, v);
         else load8(static_cast<const float*>(from) + c.first, true, 8, v);
         return;
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        v[j] = j >= c.count ? 0.0f : bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(from)[c.at(j)]) : static_cast<const float*>(from)[c.at(j)];
+        v[j] = !there(c, j) ? 0.0f : bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(from)[c.at(j)]) : static_cast<const float*>(from)[c.at(j)];
 }
 
 __device__ __forceinline__ void team_barrier(int team, int threads) {
@@ -438,7 +566,20 @@ __global__ void __launch_bounds__(kEightThreads, 1) backward8_kernel(const __gri
     }
 }
 
-// Block: blockDim.x threads a team, blockDim.y teams.  kR rows at a time: 4, or 1 where there are few.
+// Block: blockDim.x threads a team, blockDim.y teams.  kR rows at a time: 4, or 1 where there are few.  kShifted: a block's rows lie eight
+// apart, and there are a multiple of eight blocks.
+template <typename T, int kVec>
+struct Rows {
+    static constexpr int kGap = kVec == kShifted ? 8 : 1;
+    int shift;
+    int64_t first, stride;
+    __device__ __forceinline__ Rows(const void* base, int64_t ld, int at_once) {
+        const int64_t block = kGap == 8 ? blockIdx.x >> 3 : blockIdx.x, rest = kGap == 8 ? blockIdx.x & 7 : 0;
+        shift = (int)((reinterpret_cast<uintptr_t>(base) / sizeof(T) + (uint64_t)(rest * ld)) & 7u);
+        first = rest + kGap * ((block * blockDim.y + threadIdx.y) * at_once);
+        stride = (int64_t)gridDim.x * blockDim.y * at_once;
+    }
+};
 template <typename T, int kVec, int kR>
 __global__ void __launch_bounds__(kMaxTeam) forward_kernel(const __grid_constant__ Params p) {
     __shared__ float slots[2][32][4];
@@ -446,33 +587,30 @@ __global__ void __launch_bounds__(kMaxTeam) forward_kernel(const __grid_constant
     const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     float(*sums0)[4] = slots[0] + team * (threads >> 5);
     float(*sums1)[4] = slots[1] + team * (threads >> 5);
-    const Cols<kVec> c(0, p.cols, threadIdx.x, threads);
+    const Rows<T, kVec> rows(p.x, p.ldx, kR);
+    constexpr int kGap = Rows<T, kVec>::kGap;
+    const Place<kVec> c(p.cols, threadIdx.x, threads, rows.shift);
     float gamma[8], beta[8];
     load_affine(c, p.gamma, p.affine_bf16, 1.0f, gamma);
     load_affine(c, p.beta, p.affine_bf16, 0.0f, beta);
     const T* x = static_cast<const T*>(p.x);
     T* y = static_cast<T*>(p.y);
     const bool mine = c.count > 0;
-    const int64_t stride = (int64_t)gridDim.x * blockDim.y * kR;
-    int64_t row = ((int64_t)blockIdx.x * blockDim.y + team) * kR;
-    float next[kR][8];                                       // the rows to come, on their way while these are worked on
+    const typename Held<T, kVec>::Own own(c);
+    const int64_t stride = rows.stride;
+    int64_t row = rows.first;
+    Held<T, kVec> next[kR];                                  // the rows to come, on their way while these are worked on
+#pragma unroll
+    for (Held<T, kVec>& h : next) h.clear();
     const auto fetch = [&](int64_t from) {
 #pragma unroll
-        for (int r = 0; r < kR; ++r) {
-            if (mine && from + r < p.rows) c.load(x + (from + r) * p.ldx, next[r]);
-            else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) next[r][j] = 0.0f;
-            }
-        }
+        for (int r = 0; r < kR; ++r) next[r].load(c, x, p.ldx, from + r * kGap, p.rows);
     };
     fetch(row);
     for (; row < p.rows; row += stride) {
         float v[kR][8], s[kR];
 #pragma unroll
-        for (int r = 0; r < kR; ++r)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[r][j] = next[r][j];
+        for (int r = 0; r < kR; ++r) next[r].floats(c, own, x, p.ldx, row + r * kGap, p.rows, v[r]);
         fetch(row + stride);
 #pragma unroll
         for (int r = 0; r < kR; ++r) s[r] = ((v[r][0] + v[r][1]) + (v[r][2] + v[r][3])) + ((v[r][4] + v[r][5]) + (v[r][6] + v[r][7]));
@@ -484,23 +622,24 @@ __global__ void __launch_bounds__(kMaxTeam) forward_kernel(const __grid_constant
             s[r] = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[r][j] = j < c.count ? v[r][j] - mean[r] : 0.0f;
+                v[r][j] = fmaf(-mean[r], own.one[j], v[r][j]);
                 s[r] = fmaf(v[r][j], v[r][j], s[r]);
             }
         }
         team_sum<kR>(s, sums1, team, threads, warp, lane);
 #pragma unroll
         for (int r = 0; r < kR; ++r) {
-            if (row + r >= p.rows) break;
+            const int64_t at = row + r * kGap;
+            if (at >= p.rows) break;
             const float rstd = rsqrtf(fmaf(s[r], p.inv_cols, p.eps));
             if (threadIdx.x == 0) {
-                if (p.mean) p.mean[row + r] = mean[r];
-                if (p.rstd) p.rstd[row + r] = rstd;
+                if (p.mean) p.mean[at] = mean[r];
+                if (p.rstd) p.rstd[at] = rstd;
             }
             if (mine) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[r][j] = fmaf(v[r][j] * rstd, gamma[j], beta[j]);
-                c.store(y + (row + r) * p.ldy, v[r]);
+                c.store(y + at * p.ldy, v[r]);
             }
         }
     }
@@ -513,7 +652,9 @@ __global__ void __launch_bounds__(kMaxTeam) backward_kernel(const __grid_constan
     extern __shared__ float joined[];                       // [2][blockDim.x * 8] where there are several teams
     grid_dependency_wait();
     const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Cols<kVec> c(0, p.cols, threadIdx.x, threads);
+    const Rows<T, kVec> rows(p.x, p.ldx, 2);
+    constexpr int kGap = Rows<T, kVec>::kGap;
+    const Place<kVec> c(p.cols, threadIdx.x, threads, rows.shift);
     float gamma[8], dgamma[8], dbeta[8];
     load_affine(c, p.gamma, p.affine_bf16, 1.0f, gamma);
 #pragma unroll
@@ -521,22 +662,25 @@ __global__ void __launch_bounds__(kMaxTeam) backward_kernel(const __grid_constan
     const T *x = static_cast<const T*>(p.x), *dy = static_cast<const T*>(p.dy);
     T* dx = static_cast<T*>(p.dx);
     const bool mine = c.count > 0;
-    const int64_t stride = (int64_t)gridDim.x * blockDim.y * 2;
-    int64_t row = ((int64_t)blockIdx.x * blockDim.y + team) * 2;
-    float next_x[2][8], next_g[2][8], next_mean[2], next_rstd[2];
+    const typename Held<T, kVec>::Own own(c);
+    const int64_t stride = rows.stride;
+    int64_t row = rows.first;
+    Held<T, kVec> next_x[2], next_g[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        next_x[r].clear();
+        next_g[r].clear();
+    }
+    float next_mean[2], next_rstd[2];
     const auto fetch = [&](int64_t from) {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const bool there = from + r < p.rows;
-            next_mean[r] = there ? p.mean_in[from + r] : 0.0f;
-            next_rstd[r] = there ? p.rstd_in[from + r] : 0.0f;
-            if (mine && there) {
-                c.load(x + (from + r) * p.ldx, next_x[r]);
-                c.load(dy + (from + r) * p.lddy, next_g[r]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) next_x[r][j] = next_g[r][j] = 0.0f;
-            }
+            const int64_t at = from + r * kGap;
+            const bool there = at < p.rows;
+            next_mean[r] = there ? p.mean_in[at] : 0.0f;
+            next_rstd[r] = there ? p.rstd_in[at] : 0.0f;
+            next_x[r].load(c, x, p.ldx, at, p.rows);
+            next_g[r].load(c, dy, p.lddy, at, p.rows);
         }
     };
     fetch(row);
@@ -546,11 +690,10 @@ __global__ void __launch_bounds__(kMaxTeam) backward_kernel(const __grid_constan
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             rstd[r] = next_rstd[r];
+            next_x[r].floats(c, own, x, p.ldx, row + r * kGap, p.rows, xh[r]);
+            next_g[r].floats(c, own, dy, p.lddy, row + r * kGap, p.rows, g[r]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                xh[r][j] = j < c.count ? (next_x[r][j] - next_mean[r]) * rstd[r] : 0.0f;
-                g[r][j] = next_g[r][j];
-            }
+            for (int j = 0; j < 8; ++j) xh[r][j] = fmaf(-next_mean[r], own.one[j], xh[r][j]) * rstd[r];
         }
         fetch(row + stride);
 #pragma unroll
@@ -570,11 +713,11 @@ __global__ void __launch_bounds__(kMaxTeam) backward_kernel(const __grid_constan
         team_sum<4>(s, slots[turn] + team * (threads >> 5), team, threads, warp, lane);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            if (row + r >= p.rows || !mine) break;
+            if (row + r * kGap >= p.rows || !mine) break;
             const float m0 = s[2 * r] * p.inv_cols, m1 = s[2 * r + 1] * p.inv_cols;
 #pragma unroll
             for (int j = 0; j < 8; ++j) g[r][j] = rstd[r] * (g[r][j] - fmaf(xh[r][j], m1, m0));
-            c.store(dx + (row + r) * p.ldy, g[r]);
+            c.store(dx + (row + r * kGap) * p.ldy, g[r]);
         }
     }
     if constexpr (kSums) {
@@ -582,7 +725,7 @@ __global__ void __launch_bounds__(kMaxTeam) backward_kernel(const __grid_constan
         if (!join_teams(dgamma, dbeta, joined, team, threads)) return;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j < c.count) {
+            if (c.has(j)) {
                 out[c.at(j)] = dgamma[j];
                 out[p.cols + c.at(j)] = dbeta[j];
             }
@@ -857,12 +1000,15 @@ Plan plan(bool backward, int64_t rows, int64_t cols, int dtype, int vec, int sm_
         return q;
     }
     q.kind = Plan::kAny;
-    q.team = round_up((cols + 7) / 8, 32);
+    q.team = round_up((cols + (vec == kShifted ? 14 : 7)) / 8, 32);
     q.teams = std::max(1, 512 / q.team);
     q.at_once = backward ? 2 : rows >= (int64_t)4 * q.teams * sm_count ? 4 : 1;
     if (q.at_once == 1) q.teams = 1;
     const int64_t per_block = (int64_t)q.teams * q.at_once;
-    q.blocks = q.parts = (int)std::min<int64_t>((rows + per_block - 1) / per_block, (int64_t)sm_count * std::max(1, (backward ? 512 : 1024) / (q.team * q.teams)));
+    const int64_t most = (int64_t)sm_count * std::max(1, (backward ? 512 : 1024) / (q.team * q.teams));
+    if (vec == kShifted) q.blocks = (int)(8 * std::min<int64_t>((rows + 8 * per_block - 1) / (8 * per_block), std::max<int64_t>(1, most / 8)));
+    else q.blocks = (int)std::min<int64_t>((rows + per_block - 1) / per_block, most);
+    q.parts = q.blocks;
     return q;
 }
 
@@ -894,7 +1040,8 @@ template <typename T, int kVec> cudaError_t forward(const Plan& q, const Params&
             return q.team * q.teams <= 256 ? go(std::integral_constant<int, 256>()) : go(std::integral_constant<int, kEightThreads>());
         }
     }
-    if (q.kind == Plan::kWide) return launch_dependent(&wide_forward_kernel<T, kVec>, dim3(q.blocks), dim3(q.team), 0, st, p);
+    if constexpr (kVec != kShifted)
+        if (q.kind == Plan::kWide) return launch_dependent(&wide_forward_kernel<T, kVec>, dim3(q.blocks), dim3(q.team), 0, st, p);
     const dim3 block(q.team, q.teams);
     if (q.at_once == 4) return launch_dependent(&forward_kernel<T, kVec, 4>, dim3(q.blocks), block, 0, st, p);
     return launch_dependent(&forward_kernel<T, kVec, 1>, dim3(q.blocks), block, 0, st, p);
@@ -907,6 +1054,7 @@ template <typename T, int kVec, bool kSums> cudaError_t backward(const Plan& q, 
             return q.pieces == 1 ? backward8<T, 1, kRoom, kSums, false>(q, p, st) : backward8<T, 2, 1, kSums, false>(q, p, st);
         }
     }
+    if constexpr (kVec != kShifted) {
     if (q.kind == Plan::kWide) {
         if (kSums && p.cols <= kWideSums) {
             static PerDeviceOnce once;
@@ -921,15 +1069,23 @@ template <typename T, int kVec, bool kSums> cudaError_t backward(const Plan& q, 
         if (e != cudaSuccess) return e;
         return launch_dependent(&wide_backward_kernel<T, kVec, false>, dim3(q.blocks), dim3(q.team), 0, st, p);
     }
+    }
     return launch_dependent(&backward_kernel<T, kVec, kSums>, dim3(q.blocks), dim3(q.team, q.teams), kSums && q.teams > 1 ? q.team * 64 : 0, st, p);
 }
+// whether the rows of all tensors begin at the same distance from an aligned address, and the pieces fit a block's threads
+bool shifts_alike(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t rows, int dtype) {
+    const uint64_t size = (uint64_t)size_of(dtype), pa = reinterpret_cast<uintptr_t>(a) / size, pb = reinterpret_cast<uintptr_t>(b) / size;
+    return (pa - pb) % 8 == 0 && (rows == 1 || (lda - ldb) % 8 == 0);
+}
+bool shifted_fits(int64_t cols, int dtype) { return dtype == MVUE_BF16 && cols >= 16 && (cols + 14) / 8 <= kMaxTeam; }
 int widest(int v, const void* p, int64_t ld, int64_t cols, int64_t rows, int dtype) { return std::min(v, row_vector(p, rows > 1 ? ld : cols, cols, dtype)); }
 
 // enough for any alignment and type
 size_t workspace_bytes_of(int64_t rows, int64_t cols, int sm_count) {
     int parts = 0;
     for (const int dtype : {MVUE_F32, MVUE_BF16})
-        for (const int vec : {8, 1}) parts = std::max(parts, plan(true, rows, cols, dtype, vec, sm_count).parts);
+        for (const int vec : {8, 1, kShifted})
+            if (vec != kShifted || shifted_fits(cols, dtype)) parts = std::max(parts, plan(true, rows, cols, dtype, vec, sm_count).parts);
     return (size_t)parts * 2 * (size_t)cols * sizeof(float);
 }
 
@@ -960,11 +1116,14 @@ extern "C" int mvue_layer_norm(const void* x, int dtype, int64_t rows, int64_t c
     p.x = x; p.y = y; p.gamma = gamma; p.beta = beta; p.mean = mean; p.rstd = rstd;
     p.rows = rows; p.cols = cols; p.ldx = ldx; p.ldy = ldy;
     p.eps = eps; p.inv_cols = (float)(1.0 / (double)cols); p.affine_bf16 = affine_dtype == MVUE_BF16;
-    const int v = widest(widest(8, x, ldx, cols, rows, dtype), y, ldy, cols, rows, dtype);
+    int v = widest(widest(8, x, ldx, cols, rows, dtype), y, ldy, cols, rows, dtype);
+    if (v < 8 && shifted_fits(cols, dtype) && shifts_alike(x, ldx, y, ldy, rows, dtype)) v = kShifted;
     const Plan q = plan(false, rows, cols, dtype, v, dev.sm_count);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const auto pick = [&](auto t) {
         using T = decltype(t);
+        if constexpr (std::is_same<T, __nv_bfloat16>::value)
+            if (v == kShifted) return forward<T, kShifted>(q, p, st);
         return v == 8 ? forward<T, 8>(q, p, st) : v == 2 ? forward<T, 2>(q, p, st) : forward<T, 1>(q, p, st);
     };
     const cudaError_t e = dtype == MVUE_BF16 ? pick(__nv_bfloat16()) : pick(float());
@@ -994,12 +1153,15 @@ extern "C" int mvue_layer_norm_backward(const void* dy, int64_t lddy, const void
     p.x = x; p.dy = dy; p.dx = dx; p.gamma = gamma; p.mean_in = mean; p.rstd_in = rstd; p.partial = static_cast<float*>(workspace);
     p.rows = rows; p.cols = cols; p.ldx = ldx; p.lddy = lddy; p.ldy = lddx;
     p.inv_cols = (float)(1.0 / (double)cols); p.affine_bf16 = affine_dtype == MVUE_BF16;
-    const int v = widest(widest(widest(8, x, ldx, cols, rows, dtype), dy, lddy, cols, rows, dtype), dx, lddx, cols, rows, dtype);
+    int v = widest(widest(widest(8, x, ldx, cols, rows, dtype), dy, lddy, cols, rows, dtype), dx, lddx, cols, rows, dtype);
+    if (v < 8 && shifted_fits(cols, dtype) && shifts_alike(x, ldx, dy, lddy, rows, dtype) && shifts_alike(x, ldx, dx, lddx, rows, dtype)) v = kShifted;
     const Plan q = plan(true, rows, cols, dtype, v, dev.sm_count);
     const auto pick = [&](auto t) {
         using T = decltype(t);
         const auto go = [&](auto s) {
             constexpr bool kSums = decltype(s)::value;
+            if constexpr (std::is_same<T, __nv_bfloat16>::value)
+                if (v == kShifted) return backward<T, kShifted, kSums>(q, p, st);
             return v == 8 ? backward<T, 8, kSums>(q, p, st) : v == 2 ? backward<T, 2, kSums>(q, p, st) : backward<T, 1, kSums>(q, p, st);
         };
         return sums ? go(std::true_type()) : go(std::false_type());

@@ -211,3 +211,35 @@ def test_workspace_of_any_allowed_alignment(rows, cols, dtype):
     with pytest.raises(binding.MvueError) as e:
         binding.mvue_layer_norm_backward(dy, x, mean, rstd, w, workspace=room[8:-8])
     assert e.value.status == -7
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 16), (2, 17), (3, 23), (9, 31), (17, 40), (100, 77), (4001, 250), (2005, 1001), (40, 4081)])
+@pytest.mark.parametrize("first,pad", [(0, 0), (1, 0), (3, 2), (0, 5), (8, 8)])
+def test_what_lies_beside_a_row_does_not_count(rows, cols, first, pad):
+    # rows at any distance from an aligned address in a matrix of NaN, alone and in place; and a row of NaN among others
+    x, w, b, dy = inputs(rows, cols, BF16, F32, seed=rows)
+    big_x, big_dy, big_y = (torch.full((rows, first + cols + pad), float("nan"), dtype=BF16, device="cuda") for _ in range(3))
+    cut = slice(first, first + cols)
+    big_x[:, cut], big_dy[:, cut] = x, dy
+    y, mean, rstd = binding.mvue_layer_norm(big_x[:, cut], w, b, out=big_y[:, cut])
+    want, bounds = ref.layer_norm(x, w, b, 1e-5)
+    for g, v, e, t in zip((y, mean, rstd), want, bounds, (BF16, F32, F32)):
+        within(g, v, e, t)
+    assert int(big_y.isnan().sum()) == rows * (first + pad)
+    dx, dw, db = binding.mvue_layer_norm_backward(big_dy[:, cut], big_x[:, cut], mean, rstd, w)
+    want, bounds = ref.layer_norm_backward(dy, x, mean, rstd, w)
+    for g, v, e, t in zip((dx, dw, db), want, bounds, (BF16, F32, F32)):
+        within(g, v, e, t)
+    again = binding.mvue_layer_norm_backward(big_dy[:, cut], big_x[:, cut], mean, rstd, w, out=big_dy[:, cut])
+    if first == 0 and pad == 0:                       # (dx apart has another layout, and its sums another order, where there are gaps)
+        assert all(torch.equal(a, v) for a, v in zip(again, (dx, dw, db)))
+    within(again[0], want[0], bounds[0], BF16)
+    assert int(big_dy.isnan().sum()) == rows * (first + pad)
+    same, _, _ = binding.mvue_layer_norm(big_x[:, cut], w, b, out=big_x[:, cut])
+    assert torch.equal(same, y)
+    if rows > 2:
+        bad = x.clone()
+        bad[rows // 2] = float("nan")
+        y_bad = binding.mvue_layer_norm(bad, w, b)[0]
+        keep = torch.arange(rows, device="cuda") != rows // 2
+        assert bool(y_bad[rows // 2].isnan().all()) and torch.equal(y_bad[keep], binding.mvue_layer_norm(x, w, b)[0][keep])
