@@ -1,4 +1,4 @@
-"""Python binding of the C ABI in include/mvue.h: argument marshalling only.
+"""Python binding of the C ABI in include/mvue.h, mvue_train.h and mvue_layer.h: argument marshalling only.
 
 Tensors are torch CUDA tensors used purely as device memory; every function passes
 raw pointers, sizes and the current CUDA stream to the library.  There is no

@@ -84,7 +84,7 @@ using namespace mvue;
 
 extern "C" {
 
-int mvue_version(void) { return 150; }   // 1.5: AdamW, embedding, group norm (mvue_train.h)
+int mvue_version(void) { return 160; }   // 1.6: layer norm, e4m3 codes and their products, Muon (mvue_layer.h)
 
 const char* mvue_status_string(int status) {
     switch (status) {

@@ -6,7 +6,7 @@
 // partial sums go to the blocks' own shared memory, and each block adds up a share of the tokens over the cluster in order of rank.
 //   warps 0-3   warp 0: scales to shared memory in tensor-core order during the loop; then all: results
 //   warp 4      TMA producer        warp 5   tensor-memory allocation, MMA issue
-// Two blocks fit an SM.  8 x 14336 x 4096: 10 us of HBM time for the weights.
+// Two blocks fit an SM.  8 x 14336 x 4096: 10.9 us, of which the weights' 58.7 MB take 9.1 us at the rate of a copy.
 #pragma once
 #include "mvue_dense.cuh"
 #include "mvue_train.cuh"

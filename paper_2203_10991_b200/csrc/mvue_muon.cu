@@ -12,6 +12,12 @@
 // an update far below eps.
 //
 // Matrices of equal extents go through the products together.
+//
+// 24 of 4096 x 1024, binary32 gradients, bf16 params and binary32 copies, five steps: 2.32 ms.  momentum 0.19, start 0.20 and param 0.17 ms
+// run at 5.3 to 6.2 TB/s.  The products' 1.7 TFLOP take 1.7 ms: B X 0.17 to 0.21 ms a step (1.0 to 1.2 PFLOP/s; a library product sustains
+// 1.4 under the power limit), X X^T 0.12 ms, of which a fifth is what 240 tiles leave of four rounds of 74 pairs, B 0.04 ms, where 16
+// steps of 64 are too short for a tile's epilogue.
+// 256 x 256: 64 us, fifteen dependent products in one launch, 4 us each, of which the tensor cores have work for a tenth.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -211,68 +217,87 @@ __global__ void __launch_bounds__(kThreads) start_kernel(const __grid_constant__
     }
 }
 
-// What comes of the last X (hi / xs): the output, or the param's step.  Tiles as above.
-__global__ void __launch_bounds__(kThreads) finish_kernel(const __grid_constant__ Group q) {
-    __shared__ float tile[kTile][kTile + 1];
-    grid_dependency_wait();
-    const int z = blockIdx.y;
-    const Matrix& t = q.matrix[z];
+// What comes of the last X (hi / xs): the output, or the param's step.  Tiles as above.  What a thread reads of a tile is on its way at
+// once: of 24 matrices of 4096 x 1024 bf16 params, rounded at random, 165 us (222 us with each piece loaded before it is used).
+enum { kOutput, kBf16Param, kFloatParam };
+template <int kKind, bool kTurn>
+__device__ __forceinline__ void finish_tiles(const Group& q, const Matrix& t, int z, float (*tile)[kTile + 1]) {
+    constexpr int kWords = kKind == kOutput ? 1 : kKind == kBf16Param ? 4 : 8;
     const int rows = q.rows(t), cols = q.cols(t);
     const float inv = 1.0f / q.xs[z];
     const int tiles_x = (cols + kTile - 1) / kTile, tiles = tiles_x * ((rows + kTile - 1) / kTile);
     const __half* hi = q.hi + (int64_t)z * q.m * q.n_pitch;
-    const auto take = [&](int row, int col, float (&x)[8]) {          // eight neighbours in a row of X
-        const uint4 v = *reinterpret_cast<const uint4*>(hi + (int64_t)row * q.n_pitch + col);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-            x[2 * i] = f.x * inv;
-            x[2 * i + 1] = f.y * inv;
-        }
-    };
+    const float* from32 = t.master ? t.master : static_cast<const float*>(t.param);
+    const __nv_bfloat16* from16 = static_cast<const __nv_bfloat16*>(t.param);
+    const bool rounds = kKind == kBf16Param && q.random;
+    const int c = (threadIdx.x & 7) * 8;
     for (int w = blockIdx.x; w < tiles; w += gridDim.x) {
         const int row0 = w / tiles_x * kTile, col0 = w % tiles_x * kTile;
-        const int c = (threadIdx.x & 7) * 8;
-        if (t.flags & kTransposed) {
-            __syncthreads();
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const int r = (threadIdx.x >> 3) + 32 * it, row = col0 + r, col = row0 + c;       // of X
-                if (row < q.m && col < q.n) {
-                    float x[8];
-                    take(row, col, x);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) tile[c + i][r] = x[i];
-                }
-            }
-            __syncthreads();
-        }
+        uint4 v[2];
+        uint32_t held[2][kWords];
+        int count[2];
+        bool wide[2];
 #pragma unroll
         for (int it = 0; it < 2; ++it) {
             const int r = (threadIdx.x >> 3) + 32 * it, row = row0 + r, col = col0 + c;
-            const int count = row < rows ? max(0, min(8, cols - col)) : 0;
-            if (count == 0) continue;
-            const bool wide = (t.flags & kWideOut) && count == 8;
-            float x[8];
-            if (t.flags & kTransposed) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = tile[r][c + i];
-            } else {
-                take(row, col, x);
+            count[it] = row < rows ? max(0, min(8, cols - col)) : 0;
+            wide[it] = (t.flags & kWideOut) && count[it] == 8;
+            const int x_row = kTurn ? col0 + r : row, x_col = kTurn ? row0 + c : col;
+            v[it] = make_uint4(0u, 0u, 0u, 0u);
+            if (x_row < q.m && x_col < q.n) v[it] = *reinterpret_cast<const uint4*>(hi + (int64_t)x_row * q.n_pitch + x_col);
+            if (kKind != kOutput && wide[it]) {
+                const int64_t at = (int64_t)row * q.ld_param + col;
+                if constexpr (kKind == kBf16Param) {
+                    const uint4 p = *reinterpret_cast<const uint4*>(from16 + at);
+                    held[it][0] = p.x; held[it][1] = p.y; held[it][2] = p.z; held[it][3] = p.w;
+                } else if constexpr (kKind == kFloatParam) {
+                    ld256(from32 + at, held[it]);
+                }
             }
-            const int64_t at = (int64_t)row * q.ld_param + col;
-            uint32_t random[4];
-            bool rounds = false;
-            if (t.momentum) {
-                float p[8];
-                if (t.master) load8(t.master + at, wide, count, p);
-                else if (t.flags & kParamBf16) load8(static_cast<const __nv_bfloat16*>(t.param) + at, wide, count, p);
-                else load8(static_cast<const float*>(t.param) + at, wide, count, p);
+        }
+        float x[2][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = fmaf(p[i], q.decay, -q.size * x[i]);
-                if (t.master) store8(t.master + at, wide, count, x);
-                rounds = q.random && (t.flags & kParamBf16) && !t.master;
+        for (int it = 0; it < 2; ++it) {
+            const uint32_t words[4] = {v[it].x, v[it].y, v[it].z, v[it].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&words[i]));
+                x[it][2 * i] = f.x * inv;
+                x[it][2 * i + 1] = f.y * inv;
+            }
+        }
+        if (kTurn) {
+            const int r = threadIdx.x >> 3;
+            __syncthreads();                       // the last tile has been read
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) tile[c + i][r + 32 * it] = x[it][i];
+            __syncthreads();
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[it][i] = tile[r + 32 * it][c + i];
+        }
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+            if (count[it] == 0) continue;
+            const int64_t at = (int64_t)(row0 + (threadIdx.x >> 3) + 32 * it) * q.ld_param + col0 + c;
+            uint32_t random[4];
+            if constexpr (kKind != kOutput) {
+                float p[8];
+                if (wide[it]) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        p[i] = kKind == kFloatParam ? __uint_as_float(held[it][i]) : i & 1 ? bf16_hi(held[it][i / 2]) : bf16_lo(held[it][i / 2]);
+                } else if constexpr (kKind == kBf16Param) {
+                    load8(from16 + at, false, count[it], p);
+                } else {
+                    load8(from32 + at, false, count[it], p);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[it][i] = fmaf(p[i], q.decay, -q.size * x[it][i]);
+                if (t.master) store8(t.master + at, wide[it], count[it], x[it]);
                 if (rounds) {
                     // elements 8u .. 8u + 7 of the padded list share a call; a piece that starts inside one takes two
                     const uint64_t first = (uint64_t)t.first_block * 256u + (uint64_t)at;
@@ -298,19 +323,29 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const __grid_constant_
                 for (int i = 0; i < 4; ++i) {
                     if (rounds) {
                         // (a NaN whose lower half is zero: random bits do not carry into its sign)
-                        const float lo = x[2 * i] == x[2 * i] ? x[2 * i] : __uint_as_float(0x7FC00000u);
-                        const float hi2 = x[2 * i + 1] == x[2 * i + 1] ? x[2 * i + 1] : __uint_as_float(0x7FC00000u);
+                        const float lo = x[it][2 * i] == x[it][2 * i] ? x[it][2 * i] : __uint_as_float(0x7FC00000u);
+                        const float hi2 = x[it][2 * i + 1] == x[it][2 * i + 1] ? x[it][2 * i + 1] : __uint_as_float(0x7FC00000u);
                         o[i] = pack_out<true>(lo, hi2, random[i]);
                     } else {
-                        o[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                        o[i] = pack_bf16x2(x[it][2 * i], x[it][2 * i + 1]);
                     }
                 }
-                store8_words(static_cast<__nv_bfloat16*>(t.param) + at, wide, count, o);
+                store8_words(static_cast<__nv_bfloat16*>(t.param) + at, wide[it], count[it], o);
             } else {
-                store8(static_cast<float*>(t.param) + at, wide, count, x);
+                store8(static_cast<float*>(t.param) + at, wide[it], count[it], x[it]);
             }
         }
     }
+}
+__global__ void __launch_bounds__(kThreads, 4) finish_kernel(const __grid_constant__ Group q) {
+    __shared__ float tile[kTile][kTile + 1];
+    grid_dependency_wait();
+    const int z = blockIdx.y;
+    const Matrix& t = q.matrix[z];
+    const bool turn = t.flags & kTransposed;
+    if (!t.momentum) turn ? finish_tiles<kOutput, true>(q, t, z, tile) : finish_tiles<kOutput, false>(q, t, z, tile);
+    else if ((t.flags & kParamBf16) && !t.master) turn ? finish_tiles<kBf16Param, true>(q, t, z, tile) : finish_tiles<kBf16Param, false>(q, t, z, tile);
+    else turn ? finish_tiles<kFloatParam, true>(q, t, z, tile) : finish_tiles<kFloatParam, false>(q, t, z, tile);
 }
 
 // ---- epilogues of the products -----------------------------------------------------------------------------------------
@@ -694,7 +729,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);          // whatever goes beside it: a matrix's bits are its own
     cudaError_t e = launch_dependent(&momentum_kernel, dim3(q.n_parts, q.count), dim3(kThreads), 0, st, q);
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
-    const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 32 * sm_count / q.count));
+    const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 64 * sm_count / q.count));
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256) * q.count;
     const bool cluster = m <= kSmallM && n <= kSmallN && (n <= kSmallN / 2 || m <= 128 || q.count >= 16);
