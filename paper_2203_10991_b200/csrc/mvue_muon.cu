@@ -437,7 +437,9 @@ constexpr int small_smem(int stages) { return stages * kSmallStage + 256 + 1024;
 // there are few rows or many matrices (24 of 256 x 1024: 178 us, 193 us; one 112 us, 90 us).
 constexpr int kSmallM = 256, kSmallN = 1024;
 // One product a launch while X has no more than this many tiles of 256 x 256 in all matrices: 512 x 512 94 us (pair tiles 165 us),
-// 1024 x 1024 133 us (200 us); 1024 x 4096, 64 tiles, 290 us either way.
+// 1024 x 1024 133 us (200 us); 1024 x 4096, 64 tiles, 290 us either way.  Up to 256 rows four times as many (24 of 256 x 4096, 384 tiles,
+// 460 us, 573 us with these; 14 of 197 x 3708, 210 tiles, 318 us, 373 us), and up to 128, where half of a pair tile would be empty, any
+// number (24 of 128 x 4096 296 us, 353 us; 24 of 64 x 4096 200 us, 318 us).
 constexpr int64_t kSmallPairTiles = 40;
 
 struct SmallParams {
@@ -733,7 +735,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256) * q.count;
     const bool cluster = m <= kSmallM && n <= kSmallN && (n <= kSmallN / 2 || m <= 128 || q.count >= 16);
-    if (e == cudaSuccess && (cluster || pair_tiles <= (m <= kSmallM ? 4 : 1) * kSmallPairTiles)) {
+    if (e == cudaSuccess && (cluster || m <= 128 || pair_tiles <= (m <= kSmallM ? 4 : 1) * kSmallPairTiles)) {
         const auto map = [&](CUtensorMap* to, const __half* base, int64_t rows, int64_t cols, int64_t pitch) {
             return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, rows, q.count, pitch * 2, rows * pitch * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
         };
