@@ -436,11 +436,12 @@ constexpr int small_smem(int stages) { return stages * kSmallStage + 256 + 1024;
 // What a cluster takes: up to 256 x 512 (256 x 256: 64 us, a launch a product 73 us; 24 of 256 x 512 117 us, 137 us), twice as long where
 // there are few rows or many matrices (24 of 256 x 1024: 178 us, 193 us; one 112 us, 90 us).
 constexpr int kSmallM = 256, kSmallN = 1024;
-// One product a launch while X has no more than this many tiles of 256 x 256 in all matrices: 512 x 512 94 us (pair tiles 165 us),
-// 1024 x 1024 133 us (200 us); 1024 x 4096, 64 tiles, 290 us either way.  Up to 256 rows four times as many (24 of 256 x 4096, 384 tiles,
-// 460 us, 573 us with these; 14 of 197 x 3708, 210 tiles, 318 us, 373 us), and up to 128, where half of a pair tile would be empty, any
-// number (24 of 128 x 4096 296 us, 353 us; 24 of 64 x 4096 200 us, 318 us).
-constexpr int64_t kSmallPairTiles = 40;
+// One product a launch, in tiles of 128 x 64, while a product has no more than this many tiles of 256 x 256 in all matrices.
+// B X: 512 x 512 94 us (pair tiles 165 us), 1024 x 1024 133 us (200 us).  X X^T and A A, of which pair tiles cover the upper half alone:
+// 1024 x 4096, 10 tiles, 240 us (286 us), two of 321 x 3274 181 us (222 us), 12 of 308 x 2389, 36 tiles, 343 us (332 us).
+// Up to 256 rows four times as many (14 of 197 x 3708 281 us, 318 us, but all in small tiles 373 us), and up to 128, where half of a pair
+// tile would be empty, any number (24 of 128 x 4096 296 us, 353 us; 24 of 64 x 4096 200 us, 318 us).
+constexpr int64_t kSmallPairTiles = 40, kSmallSquareTiles = 24;
 
 struct SmallParams {
     int m, n, steps;
@@ -728,67 +729,64 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     q.S = (float)std::ldexp(1.0, (int)std::lround(0.5 * std::log2((double)n)));
     q.growth = (float)std::pow((double)kA, (double)steps);
     const int64_t pieces = (m * n + 8 * kThreads - 1) / (8 * kThreads);
-    q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);          // whatever goes beside it: a matrix's bits are its own
+    q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);          // whatever goes beside it
     cudaError_t e = launch_dependent(&momentum_kernel, dim3(q.n_parts, q.count), dim3(kThreads), 0, st, q);
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
     const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 64 * sm_count / q.count));
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
-    const int64_t pair_tiles = (m + 255) / 256 * ((n + 255) / 256) * q.count;
+    const int64_t t = (m + 255) / 256, square_tiles = t * (t + 1) / 2 * q.count, rect_tiles = t * ((n + 255) / 256) * q.count;
     const bool cluster = m <= kSmallM && n <= kSmallN && (n <= kSmallN / 2 || m <= 128 || q.count >= 16);
-    if (e == cudaSuccess && (cluster || m <= 128 || pair_tiles <= (m <= kSmallM ? 4 : 1) * kSmallPairTiles)) {
-        const auto map = [&](CUtensorMap* to, const __half* base, int64_t rows, int64_t cols, int64_t pitch) {
-            return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, base, cols, rows, q.count, pitch * 2, rows * pitch * 2, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
+    const bool small_square = m <= 128 || square_tiles <= (m <= kSmallM ? 4 : 1) * kSmallSquareTiles;
+    const bool small_rect = m <= 128 || rect_tiles <= (m <= kSmallM ? 4 : 1) * kSmallPairTiles;
+    const dense::Operand oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2}, olo = {q.lo, q.n_pitch * 2, m * q.n_pitch * 2};
+    const dense::Operand ox[2] = {{X[0], olo.pitch, olo.matrix}, {X[1], olo.pitch, olo.matrix}};
+    SmallMaps maps;
+    SmallParams small = {q.m, q.n, steps, kSmallBlocks, 0, 3 * steps, 1, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
+    if (cluster || small_square || small_rect) {
+        const auto map = [&](CUtensorMap* to, const dense::Operand& from, int64_t cols) {
+            return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, from.base, cols, m, q.count, from.pitch, from.matrix, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
         };
-        SmallMaps maps;
-        if (!map(&maps.X[0], X[0], m, n, q.n_pitch) || !map(&maps.X[1], X[1], m, n, q.n_pitch) || !map(&maps.A, A, m, m, mp) || !map(&maps.B, B, m, m, mp))
+        if (!map(&maps.X[0], ox[0], n) || !map(&maps.X[1], ox[1], n) || !map(&maps.A, oa, m) || !map(&maps.B, ob, m)) return cudaErrorInvalidValue;
+    }
+    dense::SlabMaps gram, poly, apply[2];
+    if (!cluster && !(small_square && small_rect)) {
+        if (!dense::make_slab_map(&gram.out[0], oa, m, m, q.count, false) || !dense::make_slab_map(&gram.out[1], oa, m, m, q.count, true) ||
+            !dense::make_slab_map(&poly.out[0], ob, m, m, q.count, false) || !dense::make_slab_map(&poly.out[1], ob, m, m, q.count, true) ||
+            !dense::make_slab_map(&apply[0].out[0], ox[1], m, n, q.count, false) || !dense::make_slab_map(&apply[1].out[0], ox[0], m, n, q.count, false) ||
+            !dense::make_slab_map(&apply[0].out[1], olo, m, n, q.count, false))
             return cudaErrorInvalidValue;
-        SmallParams p = {q.m, q.n, steps, kSmallBlocks, 0, 3 * steps, 1, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
-        if (cluster) {
-            e = launch_small<true>(maps, p, q.count, sm_count, st);
-        } else {
-            for (int phase = 0; phase < 3 * steps && e == cudaSuccess; ++phase) {
-                p.first = phase;
-                p.last = phase + 1;
-                p.blocks = (int)((m + 127) / 128 * (((phase % 3 == 2 ? n : m) + 63) / 64));
-                // as many shares as there are SMs for, of eight steps of 64 at least
-                p.split = 1;
-                while (phase % 3 == 0 && p.split < 8 && 2 * p.split * p.blocks * (int64_t)q.count <= sm_count && n >= 1024 * p.split) p.split *= 2;
-                e = launch_small<false>(maps, p, q.count, sm_count, st);
-            }
-        }
-        q.hi = X[steps & 1];
-        if (e == cudaSuccess) e = launch_dependent(&finish_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
-        return e;
+        gram.in = poly.in = gram.out[0];
+        apply[0].in = apply[1].in = apply[1].out[1] = apply[0].out[1];
     }
     using KMajor = dense::Shape<false, false, 256, 4, true>;
     using NMajor = dense::Shape<false, true, 256, 4, true>;
-    const dense::Operand oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2}, olo = {q.lo, q.n_pitch * 2, m * q.n_pitch * 2};
-    for (int k = 0; k < steps && e == cudaSuccess; ++k) {
-        const dense::Operand ox = {X[k & 1], q.n_pitch * 2, m * q.n_pitch * 2}, oy = {X[(k + 1) & 1], ox.pitch, ox.matrix};
-        const bool read_lo = k < steps - 2, write_lo = k + 1 < steps - 2;
-        dense::SlabMaps gram, poly, apply;
-        if (!dense::make_slab_map(&gram.out[0], oa, m, m, q.count, false) || !dense::make_slab_map(&gram.out[1], oa, m, m, q.count, true) ||
-            !dense::make_slab_map(&poly.out[0], ob, m, m, q.count, false) || !dense::make_slab_map(&poly.out[1], ob, m, m, q.count, true) ||
-            !dense::make_slab_map(&apply.out[0], oy, m, n, q.count, false) || !dense::make_slab_map(&apply.out[1], olo, m, n, q.count, false))
-            return cudaErrorInvalidValue;
-        gram.in = poly.in = gram.out[0];
-        apply.in = apply.out[1];
+    if (e == cudaSuccess && cluster) e = launch_small<true>(maps, small, q.count, sm_count, st);
+    for (int phase = 0; phase < 3 * steps && e == cudaSuccess && !cluster; ++phase) {
+        const int k = phase / 3, what = phase - 3 * k;
+        if (what == 2 ? small_rect : small_square) {
+            small.first = phase;
+            small.last = phase + 1;
+            small.blocks = (int)((m + 127) / 128 * (((what == 2 ? n : m) + 63) / 64));
+            // as many shares as there are SMs for, of eight steps of 64 at least
+            small.split = 1;
+            while (what == 0 && small.split < 8 && 2 * small.split * small.blocks * (int64_t)q.count <= sm_count && n >= 1024 * small.split) small.split *= 2;
+            e = launch_small<false>(maps, small, q.count, sm_count, st);
+            continue;
+        }
         dense::Params p = {};
         p.batch = q.count;
         p.dev_status = dev_status;
-        p.M = p.N = (int)m;
-        p.K = (int)n;
-        p.symmetric = 1;
-        e = dense::launch_pair<KMajor>(p, ox, ox, gram, Symmetric<false>{q.xs, q.S}, st);
-        p.K = (int)m;
-        if (e == cudaSuccess) e = dense::launch_pair<KMajor>(p, oa, oa, poly, Symmetric<true>{q.xs, q.S}, st);
-        p.symmetric = 0;
-        p.N = (int)n;
-        if (e == cudaSuccess)
-            e = read_lo ? dense::launch_pair<NMajor>(p, ob, ox, apply, Apply<true>{1.0f / q.S, write_lo}, st)
-                        : dense::launch_pair<NMajor>(p, ob, ox, apply, Apply<false>{1.0f / q.S, 0}, st);
-        q.hi = X[(k + 1) & 1];
+        p.M = q.m;
+        p.N = what == 2 ? q.n : q.m;
+        p.K = what == 0 ? q.n : q.m;
+        p.symmetric = what != 2;
+        const bool read_lo = k < steps - 2, write_lo = k + 1 < steps - 2;
+        if (what == 0) e = dense::launch_pair<KMajor>(p, ox[k & 1], ox[k & 1], gram, Symmetric<false>{q.xs, q.S}, st);
+        else if (what == 1) e = dense::launch_pair<KMajor>(p, oa, oa, poly, Symmetric<true>{q.xs, q.S}, st);
+        else e = read_lo ? dense::launch_pair<NMajor>(p, ob, ox[k & 1], apply[k & 1], Apply<true>{1.0f / q.S, write_lo}, st)
+                         : dense::launch_pair<NMajor>(p, ob, ox[k & 1], apply[k & 1], Apply<false>{1.0f / q.S, 0}, st);
     }
+    q.hi = X[steps & 1];
     if (e == cudaSuccess) e = launch_dependent(&finish_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     return e;
 }

@@ -300,3 +300,20 @@ def test_a_plan_dropped_after_a_step_on_another_stream():
     junk = [torch.full((need,), 255, dtype=torch.uint8, device="cuda") for _ in range(3)]      # would be the plan's workspace
     torch.cuda.synchronize()
     assert len(junk) == 3 and all(torch.equal(a, b) for a, b in zip(p, want))
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 5])
+@pytest.mark.parametrize("batch,rows,cols", [(2, 321, 3274), (30, 300, 520), (12, 520, 300), (5, 1030, 512), (3, 600, 2000), (7, 197, 3708), (2, 2100, 1050), (40, 100, 2500)])
+def test_products_of_every_tile_in_batches(batch, rows, cols, steps):
+    # X X^T, A A and B X each go through the tiles that suit their own number: all small, all of pairs, or some of each
+    gen = torch.Generator(device="cuda").manual_seed(batch + rows)
+    x = torch.randn(batch, rows, cols, generator=gen, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = binding.mvue_orthogonalize(x, steps=steps, dev_status=status)
+    assert torch.equal(got, binding.mvue_orthogonalize(x, steps=steps)) and int(status) == 0
+    for i in {0, batch // 2, batch - 1}:
+        want = ref.orthogonalize(x[i], steps)
+        # 3^0.5 roundings of 2^-12 / 3^0.5 a step, by the slopes of later steps: 3.4 each from small values, 12 for the last two together
+        assert rel(got[i], want) < 6e-3, (i, rel(got[i], want))
+        if steps <= 2:                               # (sums of 4096 instead of 1024: twice as many roundings flip, 2^0.5 of 4.5e-5 and 2.5e-4)
+            assert rel(got[i], ref.orthogonalize_rounded(x[i], steps)) < (1e-4, 5e-4)[steps - 1]
