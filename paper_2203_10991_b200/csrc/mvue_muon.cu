@@ -13,10 +13,10 @@
 //
 // Matrices of equal extents go through the products together.
 //
-// 24 of 4096 x 1024, binary32 gradients, bf16 params and binary32 copies, five steps: 2.32 ms.  momentum 0.19, start 0.20 and param 0.17 ms
-// run at 5.3 to 6.2 TB/s.  The products' 1.7 TFLOP take 1.7 ms: B X 0.17 to 0.21 ms a step (1.0 to 1.2 PFLOP/s; a library product sustains
-// 1.4 under the power limit), X X^T 0.12 ms, of which a fifth is what 240 tiles leave of four rounds of 74 pairs, B 0.04 ms, where 16
-// steps of 64 are too short for a tile's epilogue.
+// 24 of 4096 x 1024, binary32 gradients, bf16 params rounded at random, five steps: 2.3 ms, 2.5 ms in a long run under the power limit.
+// Momentum 0.19, start 0.20 and param 0.17 ms run at 3.7 (param: the random numbers, and a matrix that is turned over) to 6.2 TB/s.
+// The products' 1.7 TFLOP take 1.7 ms: B X 0.17 to 0.21 ms a step (1.0 to 1.2 PFLOP/s; a library product sustains 1.4), X X^T 0.12 ms, of
+// which a fifth is what 240 tiles leave of four rounds of 74 pairs, B 0.04 ms, where 16 steps of 64 are too short for a tile's epilogue.
 // 256 x 256: 64 us, fifteen dependent products in one launch, 4 us each, of which the tensor cores have work for a tenth.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -1,9 +1,10 @@
 // Dense products in 8-bit floating point with block scales: the forward product of a layer, C = x W^T, and its backward
 // product, C = g W.
 //
-// 16384 x 14336 x 4096 bf16 out: 0.80 ms, 2.4 PFLOP/s, 1.44 times the rate of a large bf16 library product (16-bit operands); the tensor pipe
-// is active 63 % of the time, at 1.6 GHz under the power limit, and waits for operands from L2: a pair's 256 x 256 tile wants 9 TB/s of
-// them.  Stores take 6 %, the hand-over between tiles 1 %.  32768 x 1024 from 4096 outs, backward: 0.12 ms, 2.3 PFLOP/s.
+// 16384 x 14336 x 4096 bf16 out: 0.80 ms in a short run, 2.4 PFLOP/s, and 0.92 ms, 2.1 PFLOP/s, in a long one, where the power limit holds: 1.44
+// and 1.48 times the rate of a large bf16 library product in the same state.  The tensor pipe is active 63 % of the time and waits for
+// operands from L2: a pair's 256 x 256 tiles want 9 TB/s of them.  Stores take 6 %, the hand-over between tiles 1 %.
+// 32768 x 1024 from 4096 outs, backward: 0.12 and 0.14 ms, 2.3 and 2.0 PFLOP/s.
 // 8 x 14336 x 4096: 11 us, the weights at 5.4 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
