@@ -9,7 +9,8 @@
 // few directions, what that of X does in all.
 // A and B are symmetric: only tiles on and above the diagonal are computed, and stored twice.
 // X is stored times xs, A and B times S, powers of two near the root of n, so that entries of 1 / sqrt(n) stay normal numbers; xs is larger for
-// an update far below eps.
+// an update far below eps.  The norm counts every update that binary32 can hold: an update of 5e-24 whose squares all came out as zero had X scaled
+// as if it were nothing, and grew beyond binary16.
 //
 // Matrices of equal extents go through the products together.
 //
@@ -40,6 +41,7 @@ constexpr int64_t kBatchElements = 1 << 27;         // unless they have more ele
 constexpr int kMaxParts = 128;                      // blocks that share a matrix's norm
 constexpr int kThreads = 256, kTile = 64;
 constexpr float kLo = 2048.0f;                      // 2^11: lo holds what hi lost, times this
+constexpr float kSquaresFrom = 7.88860905e-31f;     // 2^-100: what eight squares lose below 2^-149 is nothing beside such a sum
 
 enum : uint32_t { kTransposed = 1, kGradBf16 = 2, kParamBf16 = 4, kWideIn = 8, kWideOut = 16 };
 
@@ -115,7 +117,12 @@ __global__ void __launch_bounds__(kThreads) momentum_kernel(const __grid_constan
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s = fmaf(u[i], u[i], s);
-        sum += (double)s;
+        if (s >= kSquaresFrom && s <= 3.402823466e38f) {
+            sum += (double)s;
+        } else {                                   // squares that binary32 loses or has no room for, and what is not finite
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (double)u[i] * (double)u[i];
+        }
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
@@ -146,7 +153,7 @@ __device__ __forceinline__ void split8(const float (&x)[8], uint4* hi, uint4* lo
 // Eight neighbours a thread; n_pitch is a multiple of eight, so what is written in X's rows is whole pieces of it.
 __global__ void __launch_bounds__(kThreads) start_kernel(const __grid_constant__ Group q) {
     __shared__ float tile[kTile][kTile + 1];
-    __shared__ float factor;
+    __shared__ float factor[2];
     grid_dependency_wait();
     const int z = blockIdx.y;
     const Matrix& t = q.matrix[z];
@@ -158,15 +165,21 @@ __global__ void __launch_bounds__(kThreads) start_kernel(const __grid_constant__
         for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
         if (threadIdx.x == 0) {
             const double norm = sqrt(s);
-            // xs: S, or more where even the last X stays below one (eps outweighs the update): S 2^k, k at most 60
+            // xs: S, or more where even the last X stays below one (eps outweighs the update): S 2^k, k at most 100, which brings the last X's
+            // norm to 2^13 or above, so that the first, smaller by 3.4445^steps, is not lost
             const float last = fminf((float)(norm / (norm + kEps)) * q.growth, 1.25f);
-            const float xs = last < 1.25f ? q.S * exp2f(fminf(floorf(log2f(1.25f / fmaxf(last, 1e-37f))), 60.0f)) : q.S;
-            factor = isfinite(norm) ? (float)((double)xs / (norm + kEps)) : __uint_as_float(0x7FFFFFFFu);
+            const float xs = last < 1.25f ? q.S * exp2f(fminf(floorf(log2f(16384.0f / (q.S * fmaxf(last, 1e-37f)))), 100.0f)) : q.S;
+            // xs / (norm + eps) in two factors near its root, the first a power of two: the whole is beyond binary32 for the least updates and
+            // subnormal for the largest
+            const double whole = (double)xs / (norm + kEps);
+            const double first = isfinite(norm) ? exp2((double)(ilogb(whole) / 2)) : 1.0;
+            factor[0] = (float)first;
+            factor[1] = isfinite(norm) ? (float)(whole / first) : __uint_as_float(0x7FFFFFFFu);
             if (blockIdx.x == 0) q.xs[z] = xs;
         }
     }
     __syncthreads();
-    const float gs = q.scale(), f = factor;
+    const float gs = q.scale(), f0 = factor[0], f1 = factor[1];
     const int tiles_x = (cols + kTile - 1) / kTile, tiles = tiles_x * ((rows + kTile - 1) / kTile);
     __half *hi = q.hi + (int64_t)z * q.m * q.n_pitch, *lo = q.lo + (int64_t)z * q.m * q.n_pitch;
     for (int w = blockIdx.x; w < tiles; w += gridDim.x) {
@@ -189,7 +202,7 @@ __global__ void __launch_bounds__(kThreads) start_kernel(const __grid_constant__
                     for (int i = 0; i < 8; ++i) x[i] = q.nesterov ? fmaf(q.mu, u[i], q.one_mu * x[i]) : u[i];
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] *= f;
+                for (int i = 0; i < 8; ++i) x[i] = x[i] * f0 * f1;
             }
             if (t.flags & kTransposed) {
 #pragma unroll
