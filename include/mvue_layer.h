@@ -97,7 +97,8 @@ MVUE_API int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int6
  *  out        the same, MVUE_F32 or MVUE_BF16; matrices do not overlap.  It may be x, with x's type, ldx and x_stride.
  *  workspace  mvue_orthogonalize_workspace_bytes(batch, rows, cols) bytes, 256-byte aligned; contents scratch.
  *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires; otherwise left untouched.
- * min(rows, cols) <= 2^20.  An empty extent: nothing.  Equal inputs give equal bits. */
+ * min(rows, cols) <= 2^17, max(rows, cols) <= 2^20 (MVUE_ERR_SHAPE): sums of more terms would be further off than that.  An empty extent:
+ * nothing.  Equal inputs give equal bits. */
 MVUE_API int mvue_orthogonalize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ldx, int64_t x_stride, int ns_steps,
                                 void* out, int out_dtype, int64_t ldo, int64_t out_stride, void* workspace, size_t workspace_bytes,
                                 int* dev_status, void* stream);
@@ -143,7 +144,7 @@ typedef struct {
 } mvue_muon_config;
 
 /* tensors: HOST array of `count` entries (0, and empty matrices, are accepted); it may be freed on return.  Matrices of equal extents go
- * through the products together, up to 64 and 2^27 elements at a time.  workspace: mvue_muon_workspace_bytes(tensors, count) bytes (only the
+ * through the products together, up to 64 and 2^27 elements at a time; extents as in mvue_orthogonalize.  workspace: mvue_muon_workspace_bytes(tensors, count) bytes (only the
  * extents are looked at), 256-byte aligned; contents scratch.  Errors as mvue_adamw_step's, MVUE_ERR_WORKSPACE beside them. */
 MVUE_API int mvue_muon_step(const mvue_muon_tensor* tensors, int64_t count, const mvue_muon_config* config, void* workspace,
                             size_t workspace_bytes, int* dev_status, void* stream);

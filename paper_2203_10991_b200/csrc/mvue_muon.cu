@@ -455,6 +455,10 @@ constexpr int kSmallM = 256, kSmallN = 1024;
 // Up to 256 rows four times as many (14 of 197 x 3708 281 us, 318 us, but all in small tiles 373 us), and up to 128, where half of a pair
 // tile would be empty, any number (24 of 128 x 4096 296 us, 353 us; 24 of 64 x 4096 200 us, 318 us).
 constexpr int64_t kSmallPairTiles = 40, kSmallSquareTiles = 24;
+// Terms that an accumulator adds up: what an addition has below the sum's last place is cut off, always downwards, so A shrinks with their
+// number.  2 x n, five steps, at the worst of some: 1.5e-3 off at 2^15 terms, 1.8e-3 at 2^17, 6.3e-3 at 2^18, 2.3e-2 at 2^20, 1.2e-1 at 2^23.  X X^T of longer
+// rows is split over a cluster.
+constexpr int64_t kSumTerms = 1 << 17, kMostTerms = 8 * kSumTerms;
 
 struct SmallParams {
     int m, n, steps;
@@ -683,8 +687,7 @@ int64_t group_bytes(int64_t count, int64_t m, int64_t n) {
 int64_t batch_of(int64_t m, int64_t n) { return std::max<int64_t>(1, std::min<int64_t>(kBatch, kBatchElements / (m * n))); }
 
 bool extents_ok(int64_t rows, int64_t cols) {
-    return rows >= 0 && cols >= 0 && rows <= 0x7FFFFF00 && cols <= 0x7FFFFF00 && (rows == 0 || cols <= ((int64_t)1 << 38) / rows) &&
-           std::min(rows, cols) <= (1 << 20);
+    return rows >= 0 && cols >= 0 && std::min(rows, cols) <= kSumTerms && std::max(rows, cols) <= kMostTerms;
 }
 
 cudaLaunchConfig_t small_config(int64_t blocks, int stages, cudaLaunchAttribute (&attr)[2], int cluster, cudaStream_t stream) {
@@ -739,7 +742,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     q.parts = reinterpret_cast<double*>(ws + 3 * x_bytes + 2 * a_bytes);
     q.xs = reinterpret_cast<float*>(ws + 3 * x_bytes + 2 * a_bytes + padded((int64_t)q.count * kMaxParts * 8));
     q.hi = X[0];
-    q.S = (float)std::ldexp(1.0, (int)std::lround(0.5 * std::log2((double)n)));
+    q.S = (float)std::ldexp(1.0, (int)std::lround(0.5 * std::log2((double)n)));       // up to 2^10: 3.4445 S, B's largest entry, is a binary16
     q.growth = (float)std::pow((double)kA, (double)steps);
     const int64_t pieces = (m * n + 8 * kThreads - 1) / (8 * kThreads);
     q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);          // whatever goes beside it
@@ -749,13 +752,14 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     const int64_t t = (m + 255) / 256, square_tiles = t * (t + 1) / 2 * q.count, rect_tiles = t * ((n + 255) / 256) * q.count;
     const bool cluster = m <= kSmallM && n <= kSmallN && (n <= kSmallN / 2 || m <= 128 || q.count >= 16);
+    const bool long_sum = n > kSumTerms;
     const bool small_square = m <= 128 || square_tiles <= (m <= kSmallM ? 4 : 1) * kSmallSquareTiles;
     const bool small_rect = m <= 128 || rect_tiles <= (m <= kSmallM ? 4 : 1) * kSmallPairTiles;
     const dense::Operand oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2}, olo = {q.lo, q.n_pitch * 2, m * q.n_pitch * 2};
     const dense::Operand ox[2] = {{X[0], olo.pitch, olo.matrix}, {X[1], olo.pitch, olo.matrix}};
     SmallMaps maps;
     SmallParams small = {q.m, q.n, steps, kSmallBlocks, 0, 3 * steps, 1, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
-    if (cluster || small_square || small_rect) {
+    if (cluster || small_square || small_rect || long_sum) {
         const auto map = [&](CUtensorMap* to, const dense::Operand& from, int64_t cols) {
             return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, from.base, cols, m, q.count, from.pitch, from.matrix, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
         };
@@ -776,13 +780,15 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     if (e == cudaSuccess && cluster) e = launch_small<true>(maps, small, q.count, sm_count, st);
     for (int phase = 0; phase < 3 * steps && e == cudaSuccess && !cluster; ++phase) {
         const int k = phase / 3, what = phase - 3 * k;
-        if (what == 2 ? small_rect : small_square) {
+        if (what == 2 ? small_rect : small_square || (what == 0 && long_sum)) {
             small.first = phase;
             small.last = phase + 1;
             small.blocks = (int)((m + 127) / 128 * (((what == 2 ? n : m) + 63) / 64));
-            // as many shares as there are SMs for, of eight steps of 64 at least
+            // as many shares as there are SMs for, of eight steps of 64 at least, or as a long sum needs
             small.split = 1;
-            while (what == 0 && small.split < 8 && 2 * small.split * small.blocks * (int64_t)q.count <= sm_count && n >= 1024 * small.split) small.split *= 2;
+            while (what == 0 && small.split < 8 &&
+                   (n > kSumTerms * small.split || (2 * small.split * small.blocks * (int64_t)q.count <= sm_count && n >= 1024 * small.split)))
+                small.split *= 2;
             e = launch_small<false>(maps, small, q.count, sm_count, st);
             continue;
         }
