@@ -98,7 +98,8 @@ MVUE_API int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int6
  *  workspace  mvue_orthogonalize_workspace_bytes(batch, rows, cols) bytes, 256-byte aligned; contents scratch.
  *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires; otherwise left untouched.
  * min(rows, cols) <= 2^17, max(rows, cols) <= 2^20 (MVUE_ERR_SHAPE): sums of more terms would be further off than that.  An empty extent:
- * nothing.  Equal inputs give equal bits. */
+ * nothing.  Equal calls give equal bits; how the sums of X X^T are split depends on how many matrices of the same extents a call has, so a
+ * matrix of 1024 columns or more (rows, where it has more) may differ by roundings between a call of its own and one with others. */
 MVUE_API int mvue_orthogonalize(const void* x, int dtype, int64_t batch, int64_t rows, int64_t cols, int64_t ldx, int64_t x_stride, int ns_steps,
                                 void* out, int out_dtype, int64_t ldo, int64_t out_stride, void* workspace, size_t workspace_bytes,
                                 int* dev_status, void* stream);
@@ -144,8 +145,8 @@ typedef struct {
 } mvue_muon_config;
 
 /* tensors: HOST array of `count` entries (0, and empty matrices, are accepted); it may be freed on return.  Matrices of equal extents go
- * through the products together, up to 64 and 2^27 elements at a time; extents as in mvue_orthogonalize.  workspace: mvue_muon_workspace_bytes(tensors, count) bytes (only the
- * extents are looked at), 256-byte aligned; contents scratch.  Errors as mvue_adamw_step's, MVUE_ERR_WORKSPACE beside them. */
+ * through the products together, up to 64 and 2^27 elements at a time; extents and bits as in mvue_orthogonalize.  workspace:
+ * mvue_muon_workspace_bytes(tensors, count) bytes (only the extents are looked at), 256-byte aligned; contents scratch.  Errors as mvue_adamw_step's, MVUE_ERR_WORKSPACE beside them. */
 MVUE_API int mvue_muon_step(const mvue_muon_tensor* tensors, int64_t count, const mvue_muon_config* config, void* workspace,
                             size_t workspace_bytes, int* dev_status, void* stream);
 MVUE_API int mvue_muon_workspace_bytes(const mvue_muon_tensor* tensors, int64_t count, size_t* bytes);   /* bytes: HOST */

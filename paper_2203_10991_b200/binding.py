@@ -738,7 +738,8 @@ def mvue_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
 def mvue_orthogonalize(x: torch.Tensor, *, steps: int = 5, out: torch.Tensor | None = None, out_dtype=None,
                        workspace: torch.Tensor | None = None, dev_status: torch.Tensor | None = None) -> torch.Tensor:
     """Each matrix of x [..., rows, cols] (fp32 or bf16) with its singular values brought towards one by `steps` Newton-Schulz steps, its
-    singular vectors kept.  Returns a tensor of out_dtype (x's own unless given); out may be x."""
+    singular vectors kept.  Returns a tensor of out_dtype (x's own unless given); out may be x.  From 1024 columns (or rows) on, how many matrices
+    a call has decides in what order a matrix's sums are added: alone and among others it may differ by roundings."""
     _operands(x, out, workspace=workspace, dev_status=dev_status)
     batch, rows, cols, ldx, stride = _matrices(x)
     if out is None:

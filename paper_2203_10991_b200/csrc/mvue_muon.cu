@@ -745,7 +745,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     q.S = (float)std::ldexp(1.0, (int)std::lround(0.5 * std::log2((double)n)));       // up to 2^10: 3.4445 S, B's largest entry, is a binary16
     q.growth = (float)std::pow((double)kA, (double)steps);
     const int64_t pieces = (m * n + 8 * kThreads - 1) / (8 * kThreads);
-    q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);          // whatever goes beside it
+    q.n_parts = (int)std::min<int64_t>(pieces, kMaxParts);
     cudaError_t e = launch_dependent(&momentum_kernel, dim3(q.n_parts, q.count), dim3(kThreads), 0, st, q);
     const int64_t tiles = ((m + kTile - 1) / kTile) * ((n + kTile - 1) / kTile);
     const unsigned tile_blocks = (unsigned)std::min<int64_t>(tiles, std::max(1, 64 * sm_count / q.count));
@@ -784,7 +784,9 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
             small.first = phase;
             small.last = phase + 1;
             small.blocks = (int)((m + 127) / 128 * (((what == 2 ? n : m) + 63) / 64));
-            // as many shares as there are SMs for, of eight steps of 64 at least, or as a long sum needs
+            // as many shares as there are SMs for, of eight steps of 64 at least, or as a long sum needs.  So what goes beside a matrix decides in
+            // what order its sums are added.  Shares that do not depend on it cost one side or the other: 512 x 14336 in one share 489 us instead of
+            // 265, 24 of 512 x 4096 in two 1186 us instead of 776.
             small.split = 1;
             while (what == 0 && small.split < 8 &&
                    (n > kSumTerms * small.split || (2 * small.split * small.blocks * (int64_t)q.count <= sm_count && n >= 1024 * small.split)))
