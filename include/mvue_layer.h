@@ -72,7 +72,8 @@ MVUE_API int mvue_quantize_e4m3(const void* x, int dtype, int64_t rows, int64_t 
  *  x, g, W    e4m3 codes, 16-byte aligned, leading dimensions multiples of 16 bytes (MVUE_ERR_ALIGN); any extents.
  *  scales     as mvue_quantize_e4m3 leaves them; the byte 255 stands for NaN.
  *  C          MVUE_F32 or MVUE_BF16, ldc >= its columns; 32-byte aligned rows take the wide stores.
- *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires; otherwise left untouched.
+ *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires (the tiles of C that it was for are NaN then);
+ *             otherwise left untouched.
  * tokens = 0: nothing.  Equal inputs give equal bits. */
 MVUE_API int mvue_scaled_forward_gemm(const void* x, const void* x_scales, int64_t tokens, int64_t in, int64_t ldx, const void* W,
                                       const void* W_scales, int64_t out, int64_t ldW, void* C, int c_dtype, int64_t ldc, int* dev_status,
@@ -96,7 +97,8 @@ MVUE_API int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int6
  *  x          [batch, rows, cols], MVUE_F32 or MVUE_BF16, ldx >= cols, x_stride elements between matrices.
  *  out        the same, MVUE_F32 or MVUE_BF16; matrices do not overlap.  It may be x, with x's type, ldx and x_stride.
  *  workspace  mvue_orthogonalize_workspace_bytes(batch, rows, cols) bytes, 256-byte aligned; contents scratch.
- *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires; otherwise left untouched.
+ *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires (matrices it was for are NaN then); otherwise
+ *             left untouched.
  * min(rows, cols) <= 2^17, max(rows, cols) <= 2^20 (MVUE_ERR_SHAPE): sums of more terms would be further off than that.  An empty extent:
  * nothing.  Equal calls give equal bits; how the sums of X X^T are split depends on how many matrices of the same extents a call has, so a
  * matrix of 1024 columns or more (rows, where it has more) may differ by roundings between a call of its own and one with others. */

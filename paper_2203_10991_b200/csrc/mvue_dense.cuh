@@ -132,6 +132,7 @@ struct Params {
     const uint8_t* a_scales;                 // Scaled: exponent bytes [ceil(K / 128), M]
     const uint8_t* b_scales;                 // exponent bytes of the 128 x 128 blocks
     int64_t b_scales_n, b_scales_k;          // bytes from one block to the next along N, along K
+    float* lost;                             // a number of each matrix that becomes NaN if a wait runs out: the caller hands it on to the results
     int* dev_status;
 };
 
@@ -438,7 +439,17 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         for (int64_t w = first; w < p.n_work; w += n_pairs, ++done) {
             const Tile t = tile_at(p, w, S::kBN);
             const int row = t.m + (int)rank * kRowsA + 32 * q + lane, par = done & 1;
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(par), (done >> 1) & 1u, abort_flag))) break;
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(par), (done >> 1) & 1u, abort_flag))) {
+                // a wait ran out: this tile and the ones to come are NaN, not what the output held before
+                uint32_t nan[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) nan[i] = 0x7FFFFFFFu;
+                for (; w < p.n_work; w += n_pairs) {
+                    const Tile rest = tile_at(p, w, S::kBN);
+                    for (int c = half * kChunks; c < (half + 1) * kChunks; ++c) epi.store(p, rest.m + (int)rank * kRowsA + 32 * q + lane, rest.n + 32 * c, nan);
+                }
+                break;
+            }
             tc_fence_after();
             // the columns that this accumulator shares with the other one are among this half's first two chunks
             const bool shares = S::kOverlap && half != par;
@@ -475,6 +486,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             for (uint32_t spin = 0; spin < 4096 && !mbar_try_wait(full_bar(s), 0) && !mbar_try_wait(full_bar(s), 1); ++spin) __nanosleep(64);
         for (int b = 0; b < (Epilogue::kSlabs ? kSlabBufs : 0); ++b)
             for (uint32_t spin = 0; spin < 4096 && !mbar_try_wait(slab_in_bar(b), 0) && !mbar_try_wait(slab_in_bar(b), 1); ++spin) __nanosleep(64);
+        if (p.lost)
+            for (int z = 0; z < p.batch; ++z) p.lost[z] = __uint_as_float(0x7FFFFFFFu);
         if (p.dev_status) *p.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
     }
     cluster_sync();                          // neither block leaves while the other may still touch it

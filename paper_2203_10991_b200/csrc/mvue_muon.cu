@@ -466,7 +466,7 @@ struct SmallParams {
     int split;                               // !kCluster, A = X X^T: blocks of a cluster that share the sum of a tile
     int64_t n_pitch, m_pitch;
     __half *X[2], *lo, *A, *B;
-    const float* xs;
+    float* xs;                               // [matrices]; NaN where a wait ran out, which finish_kernel hands on to the results
     float S;
     int* dev_status;
 };
@@ -667,6 +667,7 @@ small_kernel(const __grid_constant__ SmallMaps maps, const __grid_constant__ Sma
     if (*abort_flag && threadIdx.x == 0) {
         for (int i = 0; i < kSmallStages; ++i)
             for (uint32_t spin = 0; spin < 4096 && !mbar_try_wait(full_bar(i), 0) && !mbar_try_wait(full_bar(i), 1); ++spin) __nanosleep(64);
+        p.xs[z] = __uint_as_float(0x7FFFFFFFu);
         if (p.dev_status) *p.dev_status = MVUE_ERR_DEVICE_TIMEOUT;
     }
     __syncthreads();
@@ -796,6 +797,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
         }
         dense::Params p = {};
         p.batch = q.count;
+        p.lost = q.xs;
         p.dev_status = dev_status;
         p.M = q.m;
         p.N = what == 2 ? q.n : q.m;
