@@ -46,18 +46,24 @@ class PrunedNet:
         params = [self.embedding, *norms] if optimizer == "muon" else [self.embedding, *self.weights, *norms]
         self.plan = optim.AdamWPlan.zeros(params, state_bits=state_bits, master=True)
         self.muon = optim.MuonPlan.zeros(self.weights, master=True) if optimizer == "muon" else None
+        self.dev_status = torch.zeros(1, dtype=torch.int32, device="cuda")       # of all calls of all steps
         self.steps = 0
+
+    def check(self) -> None:
+        """Raises if a call of a step so far met an id outside the vocabulary or a wait that ran out (waits for the device)."""
+        binding._check(int(self.dev_status), "a call of a training step")
 
     def forward(self, ids: torch.Tensor):
         """(prediction, what the backward pass needs) for ids [n, s]."""
-        h = binding.mvue_embedding(ids, self.embedding, scale=self.scale)
+        status = self.dev_status
+        h = binding.mvue_embedding(ids, self.embedding, scale=self.scale, dev_status=status)
         kept = []
         for i, w in enumerate(self.weights):
             codes = None
             if self.products == "e4m3":
                 n, s = h.shape[:2]
                 codes = binding.mvue_quantize_e4m3(w, 128)
-                z = binding.mvue_scaled_forward_gemm(*binding.mvue_quantize_e4m3(h.reshape(n * s, -1), 1), *codes).reshape(n, s, -1)
+                z = binding.mvue_scaled_forward_gemm(*binding.mvue_quantize_e4m3(h.reshape(n * s, -1), 1), *codes, dev_status=status).reshape(n, s, -1)
             else:
                 z = h @ w.T
             if i + 1 == len(self.weights):
@@ -68,23 +74,23 @@ class PrunedNet:
                 kept.append((h, (z, mean, rstd), codes))
                 h = y.clamp_(min=0)
                 continue
-            y, mean, rstd = binding.mvue_group_norm_act(z, self.groups, *self.norms[i], act="silu")
+            y, mean, rstd = binding.mvue_group_norm_act(z, self.groups, *self.norms[i], act="silu", dev_status=status)
             kept.append((h, (z, mean, rstd), codes))
             h = y
 
     def backward(self, ids: torch.Tensor, g: torch.Tensor, kept, base_seed: int):
         """Gradients of all tensors (embedding, weights, norms in turn) for the neural gradient g of the prediction."""
         n, s = ids.shape
-        norm_grads = []
+        status, norm_grads = self.dev_status, []
         for i in reversed(range(len(self.weights))):
             flat, s_upd_bwd = g.reshape(n * s, -1), layer_seeds(base_seed, i)
             values, meta = binding.mvue_prune(flat, 2, 4, 0, s_upd_bwd[0], layout=TC, joint=self.joint)
-            binding.mvue_sparse_update_gemm(values, meta, kept[i][0].reshape(n * s, -1), out=self.d_weights[i])
+            binding.mvue_sparse_update_gemm(values, meta, kept[i][0].reshape(n * s, -1), out=self.d_weights[i], dev_status=status)
             if self.products == "e4m3":
-                dh = binding.mvue_scaled_backward_gemm(*binding.mvue_quantize_e4m3(flat, 1, seed=s_upd_bwd[1]), *kept[i][2])
+                dh = binding.mvue_scaled_backward_gemm(*binding.mvue_quantize_e4m3(flat, 1, seed=s_upd_bwd[1]), *kept[i][2], dev_status=status)
             else:
                 values, meta = binding.mvue_prune(flat, 2, 4, 1, s_upd_bwd[1], layout=TC, joint=self.joint)
-                dh = binding.mvue_sparse_backward_gemm(values, meta, self.weights[i])
+                dh = binding.mvue_sparse_backward_gemm(values, meta, self.weights[i], dev_status=status)
             dh = dh.reshape(n, s, -1)
             if i > 0 and self.norm == "layer":
                 z, mean, rstd = kept[i - 1][1]
@@ -93,9 +99,10 @@ class PrunedNet:
                 norm_grads = [dweight, dbias] + norm_grads
             elif i > 0:
                 z, mean, rstd = kept[i - 1][1]
-                g, dweight, dbias = binding.mvue_group_norm_act_backward(dh, z, mean, rstd, self.groups, *self.norms[i - 1], act="silu")
+                g, dweight, dbias = binding.mvue_group_norm_act_backward(dh, z, mean, rstd, self.groups, *self.norms[i - 1], act="silu",
+                                                                         dev_status=status)
                 norm_grads = [dweight, dbias] + norm_grads
-        binding.mvue_embedding_grad(ids, dh, self.vocab, scale=self.scale, out=self.d_embedding)
+        binding.mvue_embedding_grad(ids, dh, self.vocab, scale=self.scale, out=self.d_embedding, dev_status=status)
         return [self.d_embedding, *self.d_weights, *norm_grads]
 
     def step(self, ids: torch.Tensor, target: torch.Tensor, lr: float = 1e-3) -> torch.Tensor:
@@ -107,7 +114,7 @@ class PrunedNet:
         self.steps += 1
         if self.muon is not None:
             n = len(self.weights)
-            self.muon.step(grads[1:1 + n], lr=lr, weight_decay=0.01, grad_scale=1.0 / diff.numel())
+            self.muon.step(grads[1:1 + n], lr=lr, weight_decay=0.01, grad_scale=1.0 / diff.numel(), dev_status=self.dev_status)
             grads = [grads[0], *grads[1 + n:]]
         self.plan.step(grads, step=self.steps, lr=lr, weight_decay=0.01, grad_scale=1.0 / diff.numel(), seed=self.seed + self.steps)
         return 0.5 * diff.square().mean()
@@ -131,6 +138,7 @@ def main(argv=None) -> float:
         value = net.step(ids, table[ids], lr=2e-3)
         if i % 20 == 0 or i + 1 == a.steps:
             loss = float(value)
+            net.check()
             print(f"step {i:4d}  loss {loss:.4f}")
     return loss
 
