@@ -5,7 +5,7 @@
 //            along K of one instruction; four instructions take the same one), so no partial sum leaves the accumulator early
 // A is K-major; B is K-major ([N x K] in memory) or N-major ([K x N]).
 //
-// Pair kernel: a cluster of two thread blocks computes one 256 x kBN tile with cta_group::2; block r loads its own 128 rows
+// Pair kernel: a cluster of two thread blocks computes one 256 x 256 tile with cta_group::2; block r loads its own 128 rows
 // of A and its own half of B's columns, 128 bytes along K per stage.  Persistent: a pair walks the tiles.
 //   warp 0      TMA producer (both blocks)          warp 1   MMA issue (leader)
 //   warps 2, 3  tensor-memory allocation; Scaled: the scales from global to shared memory in tensor-core order
@@ -29,6 +29,7 @@ namespace mvue {
 namespace dense {
 
 constexpr int kRowsA = 128;                  // rows of A per thread block
+constexpr int kBN = 256;                     // columns of a pair's tile
 constexpr int kLine = 128;                   // bytes along K per stage: 64 binary16 or 128 e4m3
 constexpr int kPairThreads = 384;
 constexpr int kEpiWarps = 8;
@@ -40,48 +41,43 @@ constexpr int kBand = 8;                     // row tiles per band of the tile o
 constexpr int kSlabBufs = 3;
 constexpr int kSlabBytes = kRowsA * 64 * 2;  // 16 KiB; two matrices in a buffer
 
-// How a product's operands lie and how large its tiles are.
-template <bool kScaledT, bool kNMajorT, int kBNT, int kStagesT, bool kSlabsT = false>
+// How a product's operands lie and what its stages hold.  Scaled products have direct epilogues, the others slabs.
+template <bool kScaledT, bool kNMajorT, int kStagesT>
 struct Shape {
     static constexpr bool kScaled = kScaledT, kNMajor = kNMajorT;
-    static constexpr int kBN = kBNT;
     static constexpr int kBK = kScaled ? 128 : 64;                       // elements along K per stage
     static constexpr int kMmaK = kScaled ? 32 : 16;                      // elements along K per instruction: 32 bytes
     static constexpr int kABytes = kRowsA * kLine;                       // 16 KiB
     static constexpr int kHalfN = kBN / 2;                               // columns that one block of the pair loads
     static constexpr int kBBytes = kHalfN * kLine;                       // either order
-    static constexpr int kColsBox = kScaled ? (kHalfN < 128 ? kHalfN : 128) : 64;     // columns of an N-major box
+    static constexpr int kColsBox = kScaled ? 128 : 64;                  // columns of an N-major box: a line of 128 bytes
     static constexpr int kBoxes = kNMajor ? kHalfN / kColsBox : 1;
     static constexpr int kBoxBytes = kBBytes / kBoxes;
-    static constexpr int kBoxLine = kNMajor ? kColsBox * (kScaled ? 1 : 2) : kLine;   // bytes of a shared-memory line: 128, or 64
-    static constexpr int kBStep = (kNMajor ? kMmaK * kBoxLine : 32) / 16;             // from one instruction's B to the next, in 16 bytes
+    static constexpr int kBStep = (kNMajor ? kMmaK * kLine : 32) / 16;   // from one instruction's B to the next, in 16 bytes
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = kStagesT;
-    static constexpr int kSlabBase = kSlabsT ? kSlabBufs * 2 * kSlabBytes : 0;        // bytes of that ring
+    static constexpr int kSlabBase = kScaled ? 0 : kSlabBufs * 2 * kSlabBytes;        // bytes of that ring
     // Scales of kGroup stages travel together, four bytes of a row in a word, through rings of kGroups in shared and tensor memory.
     static constexpr int kGroup = 4, kGroups = kScaled ? 3 : 0;
     static constexpr int kScaleParts = 1 + kBN / 128;                                 // 128 rows of A, the columns of B
     static constexpr int kGroupBytes = 512 * kScaleParts;
     static constexpr int kScaleCols = 4 * kScaleParts;                                // tensor-memory columns of a group
     static constexpr int kTmemScale = 512 - kGroups * kScaleCols;
-    static constexpr bool kOverlap = kScaled && kBN == 256;
-    static constexpr int kAcc1 = kOverlap ? kTmemScale - kBN : kBN;                   // first column of the second accumulator
-    static constexpr int kShared = kOverlap ? kBN - kAcc1 : 0;                        // columns that the accumulators share
+    static constexpr int kAcc1 = kScaled ? kTmemScale - kBN : kBN;                    // first column of the second accumulator
+    static constexpr int kShared = kBN - kAcc1;                                       // columns that the accumulators share
     static constexpr int kSmem = kStages * kStageBytes + kGroups * kGroupBytes + kSlabBase + 1024 /*alignment*/ + 256 /*barriers*/;
     static constexpr uint32_t kInstr = (kScaled ? (1u << 23) /*scales: powers of two*/ : (1u << 4) /*D = f32*/) |
                                        ((kNMajor ? 1u : 0u) << 16) | ((uint32_t)(kBN >> 3) << 17);      // + M >> 4 at bit 24
     static_assert(kSmem <= 227 * 1024 && kStageBytes % 1024 == 0 && kAcc1 + kBN <= kTmemScale && kShared <= 64, "does not fit");
 };
 
-constexpr uint32_t kSwizzle64B = 4;
-
 // Descriptors of a stage's operands; an address in one counts 16 bytes, so a stage's or an instruction's are sums.
 constexpr int kAStep = 2;                    // 32 bytes along K per instruction
 __device__ __forceinline__ uint64_t a_desc(uint32_t addr) { return make_smem_desc(addr, 16, 1024, kSwizzle128B); }
 template <class S> __device__ __forceinline__ uint64_t b_desc(uint32_t addr) {
     if (!S::kNMajor) return make_smem_desc(addr, 16, 1024, kSwizzle128B);
-    // groups of eight lines 8 kBoxLine apart, columns beyond a line in the next box
-    return make_smem_desc(addr, S::kBoxBytes, 8 * S::kBoxLine, S::kBoxLine == 128 ? kSwizzle128B : kSwizzle64B);
+    // groups of eight lines 1024 bytes apart, columns beyond a line in the next box
+    return make_smem_desc(addr, S::kBoxBytes, 8 * kLine, kSwizzle128B);
 }
 
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t leader_bar) {
@@ -156,6 +152,7 @@ template <class S, class Epilogue>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Params p,
             const __grid_constant__ typename Epilogue::Maps maps, const __grid_constant__ Epilogue epi) {
+    static_assert(S::kScaled != Epilogue::kSlabs, "scaled products store directly, the others through slabs");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -216,7 +213,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             uint32_t parity = 1u;                            // of the stage's last release (a fresh barrier passes at parity 1)
             bool ok = true;
             for (int64_t w = first; w < p.n_work && ok; w += n_pairs) {
-                const Tile t = tile_at(p, w, S::kBN);
+                const Tile t = tile_at(p, w, kBN);
                 const int m = t.m + (int)rank * kRowsA, n = t.n + (int)rank * S::kHalfN;
                 for (int i = 0; i < steps; ++i) {
                     if (!(ok = mbar_wait(empty_bar(s), parity, abort_flag))) break;
@@ -246,8 +243,8 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             bool ok = true;
             for (int64_t w = first; w < p.n_work && ok; w += n_pairs, ++done) {
                 // Half: this accumulator's last tile is drained.  Scaled: the last tile's shared columns are.
-                if (S::kOverlap ? done > 0 : done > 1) {
-                    ok = S::kOverlap ? mbar_wait_cluster(free_bar(0), (done - 1) & 1u, abort_flag)
+                if (S::kScaled ? done > 0 : done > 1) {
+                    ok = S::kScaled ? mbar_wait_cluster(free_bar(0), (done - 1) & 1u, abort_flag)
                                      : mbar_wait_cluster(free_bar(done & 1), ((done >> 1) - 1) & 1u, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
@@ -292,28 +289,28 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         bool ok = true;
         const int blocks_n = (p.N + 127) >> 7;
         for (int64_t w = first; w < p.n_work && ok; w += n_pairs) {
-            const Tile t = tile_at(p, w, S::kBN);
+            const Tile t = tile_at(p, w, kBN);
             const int row0 = t.m + (int)rank * kRowsA + lane;
             const uint8_t* a_at[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) a_at[j] = p.a_scales + min(row0 + 32 * j, p.M - 1);        // rows that do not exist are zeros: any scale
             for (int i0 = 0; i0 < steps; i0 += S::kGroup, ++group) {
                 if (((group ^ warp) & 1u) == 0u) {
-                    uint32_t a[4] = {}, b[S::kBN / 128] = {};
+                    uint32_t a[4] = {}, b[kBN / 128] = {};
 #pragma unroll
                     for (int u = 0; u < S::kGroup; ++u) {                          // all loads before the wait
                         const int64_t i = min(i0 + u, steps - 1);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) a[j] |= (uint32_t)__ldg(a_at[j] + i * p.M) << (8 * u);
 #pragma unroll
-                        for (int j = 0; j < S::kBN / 128; ++j)
+                        for (int j = 0; j < kBN / 128; ++j)
                             b[j] |= (uint32_t)__ldg(p.b_scales + min((t.n >> 7) + j, blocks_n - 1) * p.b_scales_n + i * p.b_scales_k) << (8 * u);
                     }
                     if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(scale_empty_bar(slot), parity, abort_flag)))) break;
                     uint4* to = reinterpret_cast<uint4*>(smem_gen + kScaleBase + slot * S::kGroupBytes) + lane;
                     to[0] = make_uint4(a[0], a[1], a[2], a[3]);
 #pragma unroll
-                    for (int j = 0; j < S::kBN / 128; ++j) to[32 * (1 + j)] = make_uint4(b[j], b[j], b[j], b[j]);
+                    for (int j = 0; j < kBN / 128; ++j) to[32 * (1 + j)] = make_uint4(b[j], b[j], b[j], b[j]);
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor cores read what the lanes wrote
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(map_to_cta(scale_full_bar(slot), 0));
@@ -325,7 +322,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         // ------------------------------------------------------------ slabs of the epilogue (both blocks, own rows)
         if constexpr (Epilogue::kSlabs) {
             if (lane == 0) {
-                constexpr int kPer = S::kBN / 64;                // slabs of a tile
+                constexpr int kPer = kBN / 64;                // slabs of a tile
                 // reads run a ring less one slab ahead of writes; a buffer is free when the write before the last has been taken from it
                 int64_t w_in = first, w_out = first;
                 int at_in = 0, at_out = 0, buf_in = 0, buf_out = 0;
@@ -333,7 +330,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 const auto read = [&] {
                     if (w_in >= p.n_work) return;
                     if (Epilogue::kIn > 0) {
-                        const Tile t = tile_at(p, w_in, S::kBN);
+                        const Tile t = tile_at(p, w_in, kBN);
                         const uint32_t to = smem_base + kSlabs + buf_in * 2 * kSlabBytes;
                         mbar_expect_tx(slab_in_bar(buf_in), kSlabBytes);
                         tma_load_3d(to, &maps.in, t.n + 64 * at_in, t.m + (int)rank * kRowsA, t.z, slab_in_bar(buf_in));
@@ -346,7 +343,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                 for (int i = 1; i < kSlabBufs; ++i) read();
                 while (w_out < p.n_work) {
                     if (!mbar_wait(slab_out_bar(buf_out), parity, abort_flag)) break;
-                    const Tile t = tile_at(p, w_out, S::kBN);
+                    const Tile t = tile_at(p, w_out, kBN);
                     const int m = t.m + (int)rank * kRowsA, n = t.n + 64 * at_out;
                     const uint32_t from = smem_base + kSlabs + buf_out * 2 * kSlabBytes;
                     if (m < p.M && n < p.N) {
@@ -376,13 +373,13 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
             int buf = 0;
             bool ok = true;
             for (int64_t w = first; w < p.n_work && ok; w += n_pairs, ++done) {
-                const Tile t = tile_at(p, w, S::kBN);
+                const Tile t = tile_at(p, w, kBN);
                 const auto values = epi.values(t.z);
                 const int par = done & 1;
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(par), (done >> 1) & 1u, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t acc = tmem_base + rows_at + (par ? S::kAcc1 : 0) + 32 * half;
-                for (int c = 0; c < S::kBN / 64; ++c) {
+                for (int c = 0; c < kBN / 64; ++c) {
                     uint32_t v[32];
                     tmem_ld_32x32b_x32(acc + 64 * c, v);
                     if (!(ok = __all_sync(0xFFFFFFFFu, mbar_wait(slab_in_bar(buf), parity, abort_flag)))) break;
@@ -394,7 +391,7 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
                         if (Epilogue::kIn > 0) x[0][i] = *piece(i);
                     }
                     tmem_ld_wait();
-                    if (c == S::kBN / 64 - 1) {                  // the accumulator is in registers: it may be overwritten
+                    if (c == kBN / 64 - 1) {                  // the accumulator is in registers: it may be overwritten
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0)
@@ -427,17 +424,17 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
         // ------------------------------------------------------------ epilogue (both blocks, own rows)
         const int q = warp & 3, half = (warp - 4) >> 2;          // a quarter of the lanes, half of the columns
         const uint32_t rows_at = (uint32_t)(32 * q) << 16;
-        const uint32_t leader_free[2] = {map_to_cta(free_bar(0), 0), map_to_cta(free_bar(1), 0)};
-        constexpr int kChunks = S::kBN / 64, kFirst = kChunks / 2;
+        const uint32_t leader_free = map_to_cta(free_bar(0), 0);
+        constexpr int kChunks = kBN / 64, kFirst = kChunks / 2;
         // (relaxed: what is handed back was read by tcgen05.wait::ld; a release would wait for earlier stores to global memory)
-        const auto arrive = [&](int b) {
+        const auto arrive = [&] {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_free[b]) : "memory");
+            if (lane == 0) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leader_free) : "memory");
         };
         uint32_t done = 0;
         for (int64_t w = first; w < p.n_work; w += n_pairs, ++done) {
-            const Tile t = tile_at(p, w, S::kBN);
+            const Tile t = tile_at(p, w, kBN);
             const int row = t.m + (int)rank * kRowsA + 32 * q + lane, par = done & 1;
             if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_bar(par), (done >> 1) & 1u, abort_flag))) {
                 // a wait ran out: this tile and the ones to come are NaN, not what the output held before
@@ -445,23 +442,23 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 #pragma unroll
                 for (int i = 0; i < 32; ++i) nan[i] = 0x7FFFFFFFu;
                 for (; w < p.n_work; w += n_pairs) {
-                    const Tile rest = tile_at(p, w, S::kBN);
+                    const Tile rest = tile_at(p, w, kBN);
                     for (int c = half * kChunks; c < (half + 1) * kChunks; ++c) epi.store(p, rest.m + (int)rank * kRowsA + 32 * q + lane, rest.n + 32 * c, nan);
                 }
                 break;
             }
             tc_fence_after();
             // the columns that this accumulator shares with the other one are among this half's first two chunks
-            const bool shares = S::kOverlap && half != par;
-            if (S::kOverlap && !shares) arrive(0);
+            const bool shares = half != par;
+            if (!shares) arrive();
             const uint32_t acc = tmem_base + rows_at + (par ? S::kAcc1 : 0);
-            const auto chunk_at = [&](int c) { return half ? S::kBN - 32 * (c + 1) : 32 * c; };       // upper half: from the end
+            const auto chunk_at = [&](int c) { return half ? kBN - 32 * (c + 1) : 32 * c; };       // upper half: from the end
             {
                 uint32_t v[kFirst][32];
 #pragma unroll
                 for (int c = 0; c < kFirst; ++c) tmem_ld_32x32b_x32(acc + chunk_at(c), v[c]);
                 tmem_ld_wait();
-                if (shares) arrive(0);
+                if (shares) arrive();
 #pragma unroll
                 for (int c = 0; c < kFirst; ++c) epi.store(p, row, t.n + chunk_at(c), v[c]);
             }
@@ -470,7 +467,6 @@ pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ C
 #pragma unroll
                 for (int c = 0; c < kFirst; ++c) tmem_ld_32x32b_x32(acc + chunk_at(kFirst + c), v[c]);
                 tmem_ld_wait();
-                if (!S::kOverlap) arrive(par);
 #pragma unroll
                 for (int c = 0; c < kFirst; ++c) epi.store(p, row, t.n + chunk_at(kFirst + c), v[c]);
             }
@@ -547,15 +543,14 @@ cudaError_t launch_pair(Params p, const Operand& a, const Operand& b, const type
     int dev = 0;
     if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
     p.tiles_m = (p.M + 2 * kRowsA - 1) / (2 * kRowsA);
-    p.tiles_n = (p.N + S::kBN - 1) / S::kBN;
+    p.tiles_n = (p.N + kBN - 1) / kBN;
     p.tiles = p.symmetric ? p.tiles_n * (p.tiles_n + 1) / 2 : p.tiles_m * p.tiles_n;
     p.n_work = (int64_t)p.tiles * p.batch;
     const CUtensorMapDataType dt = S::kScaled ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     CUtensorMap map_a, map_b;
-    const CUtensorMapSwizzle sb = S::kBoxLine == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
     if (!make_map_3d(&map_a, dt, a.base, p.K, p.M, p.batch, a.pitch, a.matrix, S::kBK, kRowsA, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !(S::kNMajor ? make_map_3d(&map_b, dt, b.base, p.N, p.K, p.batch, b.pitch, b.matrix, S::kColsBox, S::kBK, sb)
-                     : make_map_3d(&map_b, dt, b.base, p.K, p.N, p.batch, b.pitch, b.matrix, S::kBK, S::kHalfN, sb)))
+        !(S::kNMajor ? make_map_3d(&map_b, dt, b.base, p.N, p.K, p.batch, b.pitch, b.matrix, S::kColsBox, S::kBK, CU_TENSOR_MAP_SWIZZLE_128B)
+                     : make_map_3d(&map_b, dt, b.base, p.K, p.N, p.batch, b.pitch, b.matrix, S::kBK, S::kHalfN, CU_TENSOR_MAP_SWIZZLE_128B)))
         return cudaErrorInvalidValue;
     int64_t pairs = st.max_pairs[dev] > 0 ? st.max_pairs[dev] : 1;
     if (pairs > p.n_work) pairs = p.n_work;

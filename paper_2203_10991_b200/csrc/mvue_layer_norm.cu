@@ -345,9 +345,9 @@ __device__ __forceinline__ void team_moments(float (&mean)[kR], float (&m2)[kR],
 // takes mean and squares about it of its own elements.
 // 16384 x 4096 bf16: a row at a time, with the weight's pieces in their own order (bank conflicts), took 71 us.
 constexpr int kEightThreads = 512;
-template <typename T, int kC, int kR, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 3 : 1) forward8_kernel(const __grid_constant__ Params p) {
-    __shared__ float2 slots[2][kThreads / 32][kR];
+template <typename T, int kC, int kR>
+__global__ void __launch_bounds__(kEightThreads, 1) forward8_kernel(const __grid_constant__ Params p) {
+    __shared__ float2 slots[2][kEightThreads / 32][kR];
     extern __shared__ __align__(16) float affine[];
     const int threads = blockDim.x, team = threadIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cols = (int)p.cols, pieces = cols >> 3, step = threads * 8;
@@ -1020,10 +1020,10 @@ Plan plan(bool backward, int64_t rows, int64_t cols, int dtype, int vec, int sm_
 template <typename K> cudaError_t roomy(PerDeviceOnce& once, K kernel) {
     return once_per_device(once, [&](int) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kEightThreads * 4 * 8); });
 }
-template <typename T, int kC, int kR, int kThreads> cudaError_t forward8(const Plan& q, const Params& p, cudaStream_t st) {
+template <typename T, int kC, int kR> cudaError_t forward8(const Plan& q, const Params& p, cudaStream_t st) {
     static PerDeviceOnce once;
-    if (cudaError_t e = roomy(once, &forward8_kernel<T, kC, kR, kThreads>)) return e;
-    return launch_dependent(&forward8_kernel<T, kC, kR, kThreads>, dim3(q.blocks), dim3(q.team, q.teams), (size_t)p.cols * 8, st, p);
+    if (cudaError_t e = roomy(once, &forward8_kernel<T, kC, kR>)) return e;
+    return launch_dependent(&forward8_kernel<T, kC, kR>, dim3(q.blocks), dim3(q.team, q.teams), (size_t)p.cols * 8, st, p);
 }
 template <typename T, int kC, int kR, bool kSums, bool kFull> cudaError_t backward8(const Plan& q, const Params& p, cudaStream_t st) {
     static PerDeviceOnce once;
@@ -1035,14 +1035,10 @@ template <typename T, int kC, int kR, bool kSums, bool kFull> cudaError_t backwa
 template <typename T, int kVec> cudaError_t forward(const Plan& q, const Params& p, cudaStream_t st) {
     if constexpr (kVec == 8) {
         if (q.kind == Plan::kEight) {
-            const auto go = [&](auto threads) {
-                constexpr int kThreads = decltype(threads)::value;
-                constexpr int kRoom = sizeof(T) == 2 ? 4 : 2;
-                return q.pieces == 1   ? forward8<T, 1, kRoom, kThreads>(q, p, st)
-                       : q.pieces == 2 ? forward8<T, 2, kRoom / 2, kThreads>(q, p, st)
-                                       : forward8<T, 4, 1, kThreads>(q, p, st);
-            };
-            return q.team * q.teams <= 256 ? go(std::integral_constant<int, 256>()) : go(std::integral_constant<int, kEightThreads>());
+            constexpr int kRoom = sizeof(T) == 2 ? 4 : 2;
+            return q.pieces == 1   ? forward8<T, 1, kRoom>(q, p, st)
+                   : q.pieces == 2 ? forward8<T, 2, kRoom / 2>(q, p, st)
+                                   : forward8<T, 4, 1>(q, p, st);
         }
     }
     if constexpr (kVec != kShifted)

@@ -776,8 +776,8 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
         gram.in = poly.in = gram.out[0];
         apply[0].in = apply[1].in = apply[1].out[1] = apply[0].out[1];
     }
-    using KMajor = dense::Shape<false, false, 256, 4, true>;
-    using NMajor = dense::Shape<false, true, 256, 4, true>;
+    using KMajor = dense::Shape<false, false, 4>;
+    using NMajor = dense::Shape<false, true, 4>;
     if (e == cudaSuccess && cluster) e = launch_small<true>(maps, small, q.count, sm_count, st);
     for (int phase = 0; phase < 3 * steps && e == cudaSuccess && !cluster; ++phase) {
         const int k = phase / 3, what = phase - 3 * k;

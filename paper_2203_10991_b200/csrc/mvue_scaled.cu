@@ -82,8 +82,8 @@ struct Store {
 
 template <bool kBf16>
 cudaError_t launch(const dense::Params& p, const dense::Operand& a, const dense::Operand& b, bool n_major, const Store<kBf16>& out, cudaStream_t stream) {
-    if (n_major) return dense::launch_pair<dense::Shape<true, true, 256, 6>>(p, a, b, {}, out, stream);
-    return dense::launch_pair<dense::Shape<true, false, 256, 6>>(p, a, b, {}, out, stream);
+    if (n_major) return dense::launch_pair<dense::Shape<true, true, 6>>(p, a, b, {}, out, stream);
+    return dense::launch_pair<dense::Shape<true, false, 6>>(p, a, b, {}, out, stream);
 }
 
 template <int kTN> cudaError_t launch_few(const dense::FewParams& p, const dense::Operand& t, const dense::Operand& w, bool n_major, cudaStream_t stream) {
