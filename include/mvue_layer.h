@@ -26,7 +26,9 @@ extern "C" {
  *  x, y       MVUE_F32 or MVUE_BF16 (the same); ldx, ldy >= cols.  y may be x.
  *  gamma, beta   [cols], MVUE_F32 or MVUE_BF16 (affine_dtype), either may be NULL (ones, zeros).
  *  mean, rstd [rows] float outputs for the backward pass, either may be NULL.
- * Arithmetic in binary32; the output is rounded once.  rows = 0: nothing.  cols >= 1. */
+ * Arithmetic in binary32; the output is rounded once.  Its range is the row's, too: where the sum of squares about the mean overflows (elements
+ * about 2^64 / sqrt(cols) from it) rstd is 0 and y beta, where the sum of the elements does y may be NaN; squares below 2^-149 count as nothing
+ * beside eps.  rows = 0: nothing.  cols >= 1. */
 MVUE_API int mvue_layer_norm(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, const void* gamma, const void* beta,
                              int affine_dtype, float eps, void* y, int64_t ldy, float* mean, float* rstd, void* stream);
 
