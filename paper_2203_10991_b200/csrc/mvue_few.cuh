@@ -6,7 +6,7 @@
 // partial sums go to the blocks' own shared memory, and each block adds up a share of the tokens over the cluster in order of rank.
 //   warps 0-3   warp 0: scales to shared memory in tensor-core order during the loop; then all: results
 //   warp 4      TMA producer        warp 5   tensor-memory allocation, MMA issue
-// Two blocks fit an SM.  8 x 14336 x 4096: 13.4 us, of which the weights' 58.7 MB take 9.1 us at the rate of a copy (10.9 us where they are
+// Two blocks fit an SM.  8 x 14336 x 4096: 13.3 us in a graph, of which the weights' 58.7 MB take 9.1 us at the rate of a copy (9.3 us where they are
 // in L2).
 #pragma once
 #include "mvue_dense.cuh"
@@ -215,8 +215,8 @@ few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CU
     }
     if (p.split > 1) cluster_sync();         // every part is in shared memory
 
-    // The next kernel is set up while this one adds up (8 x 14336 x 4096 one behind the other: 14.6 us without, 13.4 us; from the start on, its
-    // blocks took shared memory that this kernel's own wait for).
+    // The next kernel is set up while this one adds up (8 x 14336 x 4096 one behind the other in a graph: 14.5 us without, 13.3 us; by calls from
+    // Python 14.6 and 14.0; from the start on, its blocks took shared memory that this kernel's own wait for).
     grid_launch_dependents();
     // this block's share of the tokens, eight outs a thread: neighbours, or where rows do not allow wide accesses every sixteenth
     const int share = S::kTN / p.split, first = (int)rank * share;           // (split divides kTN)

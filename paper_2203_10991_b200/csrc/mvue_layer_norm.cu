@@ -8,11 +8,12 @@
 // blocks leave one partial sum each, and a second launch adds those in order: equal inputs give equal bits.
 //   forward8, backward8   accesses of eight elements and rows for all SMs; the weight in shared memory, packed pairs of binary32.
 //                         16384 x 4096 bf16 forward 53 us (5.0 of 6.46 TB/s copy), 32768 x 1024 bf16 backward 43 us (4.7 TB/s):
-//                         half of the issue slots are taken, and a barrier in three phases keeps 16 warps an SM from more
+//                         half of the issue slots are taken, and a barrier in three phases keeps 16 warps an SM from more.  4096 x 14336
+//                         bf16 forward 59 to 70 us, by where the buffers lie
 //   forward, backward     any alignment, up to 4096 columns, and few rows; the weight in registers (4097 x 1111 fp32 backward 17 us
-//                         with the join, 8 x 4096 bf16 forward 2.5 us)
+//                         with the join, 8 x 4096 bf16 forward 2.1 us)
 //   wide                  rows that do not fit a block's threads are gone over again, from L2; column sums in shared memory
-//                         (4096 x 14336 bf16 forward 59 us, backward 157 us: two and three times over the row, not bandwidth)
+//                         (4096 x 14344 bf16 forward 89 us, 4096 x 14336 backward 160 us: three and two times over the row, not bandwidth)
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

@@ -6,7 +6,7 @@
 // Rounding at random: the element over its scale, times 2^-120, has its binary32 subnormals where e4m3 has its own, so the
 // code is the upper bits of the bit pattern for subnormal, normal and zero alike; adding a random number to the 16 bits below
 // them carries into them as often as the element is nearer to its upper neighbour.
-// 16384 x 14336 bf16: to the nearest 116 us (6.1 of 6.46 TB/s copy), at random 197 to 202 us: the generator's ten rounds for every eight elements
+// 16384 x 14336 bf16: to the nearest 117 us (6.0 of 6.46 TB/s copy), at random 197 to 202 us: the generator's ten rounds for every eight elements
 // (74 us alone) and the rounding fill the issue slots (71 %), not memory.  14336 x 4096 in blocks of 128 x 128: 29 us (6.0 TB/s).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
