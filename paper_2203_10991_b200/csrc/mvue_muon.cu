@@ -370,13 +370,13 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 __device__ __forceinline__ float2 halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
-// A S = acc S / xs^2 (kPoly false), B S = a S on the diagonal + b (A S) + c acc / S (true); symmetric, the tile's mirror image is stored
-// too.  diag: the column of these 32 that is the row's own, or -1.
-template <bool kPoly>
+// A S = acc S / xs^2 (kPoly false; kAdd: added to what there is of a long sum), B S = a S on the diagonal + b (A S) + c acc / S (true); symmetric,
+// the tile's mirror image is stored too.  diag: the column of these 32 that is the row's own, or -1.
+template <bool kPoly, bool kAdd = false>
 struct Symmetric {
     using Maps = dense::SlabMaps;
     static constexpr bool kSlabs = true, kMirror = true;
-    static constexpr int kIn = kPoly ? 1 : 0;
+    static constexpr int kIn = kPoly || kAdd ? 1 : 0;
     const float* xs;
     float S;
     __device__ __forceinline__ bool two_out() const { return true; }
@@ -396,6 +396,11 @@ struct Symmetric {
                         if (8 * i + 2 * j == diag) lo = fmaf(kA, S, lo);
                         if (8 * i + 2 * j + 1 == diag) hi = fmaf(kA, S, hi);
                     }
+                }
+                if (kAdd) {
+                    const float2 a = halves(w[j]);
+                    lo += a.x;
+                    hi += a.y;
                 }
                 w[j] = half_pair(lo, hi);
             }
@@ -460,7 +465,7 @@ constexpr int kSmallM = 256, kSmallN = 1024;
 constexpr int64_t kSmallPairTiles = 40, kSmallSquareTiles = 24;
 // Terms that an accumulator adds up: what an addition has below the sum's last place is cut off, always downwards, so A shrinks with their
 // number.  2 x n, five steps, at the worst of some: 1.5e-3 off at 2^15 terms, 1.8e-3 at 2^17, 6.3e-3 at 2^18, 2.3e-2 at 2^20, 1.2e-1 at 2^23.  X X^T of longer
-// rows is split over a cluster.
+// rows is split over a cluster, or in pair tiles summed up by several launches (A is rounded to binary16 in between).
 constexpr int64_t kSumTerms = 1 << 17, kMostTerms = 8 * kSumTerms;
 
 struct SmallParams {
@@ -756,14 +761,13 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     if (e == cudaSuccess) e = launch_dependent(&start_kernel, dim3(tile_blocks, q.count), dim3(kThreads), 0, st, q);
     const int64_t t = (m + 255) / 256, square_tiles = t * (t + 1) / 2 * q.count, rect_tiles = t * ((n + 255) / 256) * q.count;
     const bool cluster = m <= kSmallM && n <= kSmallN && (n <= kSmallN / 2 || m <= 128 || q.count >= 16);
-    const bool long_sum = n > kSumTerms;
     const bool small_square = m <= 128 || square_tiles <= (m <= kSmallM ? 4 : 1) * kSmallSquareTiles;
     const bool small_rect = m <= 128 || rect_tiles <= (m <= kSmallM ? 4 : 1) * kSmallPairTiles;
     const dense::Operand oa = {A, mp * 2, m * mp * 2}, ob = {B, mp * 2, m * mp * 2}, olo = {q.lo, q.n_pitch * 2, m * q.n_pitch * 2};
     const dense::Operand ox[2] = {{X[0], olo.pitch, olo.matrix}, {X[1], olo.pitch, olo.matrix}};
     SmallMaps maps;
     SmallParams small = {q.m, q.n, steps, kSmallBlocks, 0, 3 * steps, 1, q.n_pitch, mp, {X[0], X[1]}, q.lo, A, B, q.xs, q.S, dev_status};
-    if (cluster || small_square || small_rect || long_sum) {
+    if (cluster || small_square || small_rect) {
         const auto map = [&](CUtensorMap* to, const dense::Operand& from, int64_t cols) {
             return dense::make_map_3d(to, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, from.base, cols, m, q.count, from.pitch, from.matrix, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B);
         };
@@ -784,7 +788,7 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
     if (e == cudaSuccess && cluster) e = launch_small<true>(maps, small, q.count, sm_count, st);
     for (int phase = 0; phase < 3 * steps && e == cudaSuccess && !cluster; ++phase) {
         const int k = phase / 3, what = phase - 3 * k;
-        if (what == 2 ? small_rect : small_square || (what == 0 && long_sum)) {
+        if (what == 2 ? small_rect : small_square) {
             small.first = phase;
             small.last = phase + 1;
             small.blocks = (int)((m + 127) / 128 * (((what == 2 ? n : m) + 63) / 64));
@@ -807,8 +811,14 @@ cudaError_t run_group(Group& q, int steps, uint8_t* ws, int* dev_status, int sm_
         p.K = what == 0 ? q.n : q.m;
         p.symmetric = what != 2;
         const bool read_lo = k < steps - 2, write_lo = k + 1 < steps - 2;
-        if (what == 0) e = dense::launch_pair<KMajor>(p, ox[k & 1], ox[k & 1], gram, Symmetric<false>{q.xs, q.S}, st);
-        else if (what == 1) e = dense::launch_pair<KMajor>(p, oa, oa, poly, Symmetric<true>{q.xs, q.S}, st);
+        if (what == 0) {
+            for (int64_t k0 = 0; k0 < n && e == cudaSuccess; k0 += kSumTerms) {
+                p.K = (int)std::min(kSumTerms, n - k0);
+                const dense::Operand part = {X[k & 1] + k0, olo.pitch, olo.matrix};
+                e = k0 == 0 ? dense::launch_pair<KMajor>(p, part, part, gram, Symmetric<false>{q.xs, q.S}, st)
+                            : dense::launch_pair<KMajor>(p, part, part, gram, Symmetric<false, true>{q.xs, q.S}, st);
+            }
+        } else if (what == 1) e = dense::launch_pair<KMajor>(p, oa, oa, poly, Symmetric<true>{q.xs, q.S}, st);
         else e = read_lo ? dense::launch_pair<NMajor>(p, ob, ox[k & 1], apply[k & 1], Apply<true>{1.0f / q.S, write_lo}, st)
                          : dense::launch_pair<NMajor>(p, ob, ox[k & 1], apply[k & 1], Apply<false>{1.0f / q.S, 0}, st);
     }

@@ -1,6 +1,7 @@
 """Newton-Schulz orthogonalisation of long rows: a tensor core's sum cuts off what lies below its last place, so one accumulator takes
 2^17 terms at most.  2^13 additions (of sixteen terms) that lose half of 2^-23 of the sum each: A is off by 2^-11, a step by as much at most, less
-than what the roundings of the operands do in five steps.  Rows longer than eight such sums are refused."""
+than what the roundings of the operands do in five steps.  Rows longer than eight such sums are refused.  Sums of pair tiles
+go through a rounding of A to binary16 for each 2^17 terms: 2^-12 of A, eight times at most, as the one that there is anyway."""
 import ctypes
 
 import pytest
@@ -40,7 +41,8 @@ def off(got, x, steps):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("batch,rows,cols", [(1, 2, 2**20), (1, 16, 2**20 - 7), (24, 16, 2**20), (40, 2, 2**19 + 1), (1, 1030, 2**20), (3, 300, 2**18 + 8), (1, 700, 2**19),
-                                             (1, 128, 2**18), (64, 2, 2**18)])
+                                             (1, 128, 2**18), (64, 2, 2**18),
+                                             (1, 1800, 2**17 + 8), (1, 2000, 2**19), (1, 1793, 2**18 - 1)])
 def test_long_rows(batch, rows, cols):
     if torch.cuda.mem_get_info()[0] < 40e9:
         pytest.skip("needs 40 GB of device memory")
