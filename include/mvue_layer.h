@@ -76,7 +76,8 @@ MVUE_API int mvue_quantize_e4m3(const void* x, int dtype, int64_t rows, int64_t 
  *  C          MVUE_F32 or MVUE_BF16, ldc >= its columns; 32-byte aligned rows take the wide stores.
  *  dev_status optional device int, receives MVUE_ERR_DEVICE_TIMEOUT if a bounded wait expires (the tiles of C that it was for are NaN then);
  *             otherwise left untouched.
- * tokens = 0: nothing.  Equal inputs give equal bits. */
+ * tokens = 0: nothing.  Equal inputs give equal bits.  The tensor core cuts off what an addition has below the sum's last place: sums of one
+ * sign over 150,000 terms come out 5e-5 too small, over 2^20 terms 1.5e-3; up to 65,000 nothing is seen. */
 MVUE_API int mvue_scaled_forward_gemm(const void* x, const void* x_scales, int64_t tokens, int64_t in, int64_t ldx, const void* W,
                                       const void* W_scales, int64_t out, int64_t ldW, void* C, int c_dtype, int64_t ldc, int* dev_status,
                                       void* stream);
