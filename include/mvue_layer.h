@@ -95,7 +95,8 @@ MVUE_API int mvue_scaled_backward_gemm(const void* g, const void* g_scales, int6
  *   X = x / (||x|| + 1e-7);  ns_steps times:  A = X X^T,  X = 3.4445 X + (-4.7750 A + 2.0315 A A) X
  * (X^T X where rows > cols).  Products of binary16 values with binary32 sums, the first term with the others (3.4445 I - 4.7750 A + 2.0315 A A
  * is one matrix); in all steps but the last two the first term is taken from 22 bits of X.  Against exact arithmetic, five steps:
- * 1e-3 to 3e-3 of the result's norm, whatever the spectrum, and up to 5e-3 for a few dozen elements.
+ * 1e-3 to 3e-3 of the result's norm from sixteen rows and columns on, whatever the spectrum.  Below, the result hangs on a few singular values, and
+ * one may lie where the polynomials are steep: 2e-3 to 3e-3 as a rule, but up to 7e-3 with eight rows or columns, 1e-2 with four, 2e-2 with two.
  * A matrix with an element that is not finite becomes NaN throughout.
  *  x          [batch, rows, cols], MVUE_F32 or MVUE_BF16, ldx >= cols, x_stride elements between matrices.
  *  out        the same, MVUE_F32 or MVUE_BF16; matrices do not overlap.  It may be x, with x's type, ldx and x_stride.
