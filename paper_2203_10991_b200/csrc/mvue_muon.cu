@@ -175,9 +175,9 @@ __global__ void __launch_bounds__(kThreads) start_kernel(const __grid_constant__
             // xs / (norm + eps) in two factors near its root, the first a power of two: the whole is beyond binary32 for the least updates and
             // subnormal for the largest
             const double whole = (double)xs / (norm + kEps);
-            const double first = isfinite(norm) ? exp2((double)(ilogb(whole) / 2)) : 1.0;
-            factor[0] = (float)first;
-            factor[1] = isfinite(norm) ? (float)(whole / first) : __uint_as_float(0x7FFFFFFFu);
+            const int e = isfinite(norm) ? ((__double2hiint(whole) >> 20) - 1023) / 2 : 0;       // (whole is a normal number from 2^-148 to 2^134)
+            factor[0] = __int_as_float((127 + e) << 23);
+            factor[1] = isfinite(norm) ? (float)(whole * (double)__int_as_float((127 - e) << 23)) : __uint_as_float(0x7FFFFFFFu);
             if (blockIdx.x == 0) q.xs[z] = xs;
         }
     }
